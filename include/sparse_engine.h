@@ -71,6 +71,7 @@ extern "C" {
 #define SE_DEV_BAD_PAGE_ID          1u  /* page_table entry >= num_phys_pages              */
 #define SE_DEV_BAD_SELECTION        2u  /* sel_idx entry outside the request / sel_cnt > k_max */
 #define SE_DEV_WAIT_TIMEOUT         4u  /* a bounded wait (200 ms) on an asynchronous copy gave up */
+#define SE_DEV_BAD_LENGTH           8u  /* prompt calls: cu_seqlens / seq_lens / pair_axis entry out of range */
 
 typedef struct se_params {
     int32_t B;               /* requests in the batch, 1..8192                              */
@@ -374,6 +375,90 @@ int se_h2o_retain(const se_params *p, const float *score_accum, const int32_t *p
 int se_h2o_compact(const se_params *p, void *k_cache, void *v_cache, float *score_accum,
                    const int32_t *page_table, const int32_t *keep_idx, const int32_t *keep_cnt,
                    int32_t budget_tokens, int32_t *new_seq_lens, void *workspace, void *stream);
+
+/*
+ * Prompt side: a packed batch of new tokens (whole prompts, or the next chunk of each request) on its way into
+ * the cache and through the layer's attention, up to the point where decode steps take over.
+ *
+ * Rules shared by the four calls below
+ *  - The new tokens of all requests lie one after the other in token-major arrays of total_tokens rows;
+ *    request r owns rows cu_seqlens[r] .. cu_seqlens[r+1]-1 ([B+1] int32, device, not decreasing).  Rows from
+ *    cu_seqlens[B] on are spare: never written, and never read into a result.
+ *  - n_r = cu_seqlens[r+1] - cu_seqlens[r] may be 0 (the request takes no part) and differs freely between
+ *    requests: single decode tokens and long chunks may share a call.
+ *  - seq_lens[r] counts the request's tokens INCLUDING its n_r new ones: row cu_seqlens[r]+i is the token at
+ *    logical position seq_lens[r] - n_r + i.
+ *  - A request with cu_seqlens outside the rows, n_r > seq_lens[r] or seq_lens[r] > 16*max_pages is left out and
+ *    reported (SE_DEV_BAD_LENGTH).
+ *  - q, k, v rows [H, D] are contiguous; the *_stride arguments give the elements from one token to the next
+ *    (>= H*D, a multiple of 8), so that the calls read views of one [T, H_q + 2*H_kv, D] projection output.
+ *  - Of se_params they use B, H_q, H_kv, D, max_pages, num_phys_pages and sm_scale; the other fields only
+ *    have to be valid.
+ *  - They take a workspace of their own kind: se_prompt_workspace_bytes bytes (256-byte aligned), initialised
+ *    once by se_prompt_workspace_init, then good for any number of calls with the same se_params that are ordered
+ *    on the device.  se_last_device_status reads its status word.  After a call that reported
+ *    SE_DEV_WAIT_TIMEOUT it has to be initialised again.
+ */
+size_t se_prompt_workspace_bytes(const se_params *p);
+int se_prompt_workspace_init(const se_params *p, void *workspace, void *stream);
+
+/*
+ * New tokens enter the cache: rotary positions with n_axes axes (1..4; text has one, images and video time,
+ * height, width), K and V written into the requests' pages, Quest summaries of the touched pages.
+ *   positions  [n_axes, total_tokens] int32   position of every token on every axis
+ *   inv_freq   [rot_dim/2] fp64               angle of channel pair c = positions[pair_axis[c]][t] * inv_freq[c]
+ *   pair_axis  [rot_dim/2] int32              axis of every channel pair (0..n_axes-1)
+ * The first rot_dim channels (a multiple of 16, <= D) of every q and k head are rotated, the others copied.
+ * interleaved = 0: pair c is channels (c, c + rot_dim/2); 1: channels (2c, 2c+1).  Angles are reduced in fp64, the
+ * rotation is fp32, the result is rounded once to bf16.
+ *   q_out  [total_tokens, H_q, D]  bf16       may be q itself when q_stride == H_q*D
+ *   k_out  [total_tokens, H_kv, D] bf16 or NULL: rotated K also in token order (for se_prompt_attend)
+ * k_cache / v_cache slots of the new tokens are written; a token whose page is absent or out of range is
+ * left out of the cache and reported (SE_DEV_BAD_PAGE_ID).  With meta != NULL the summaries of the touched pages
+ * become those of se_meta_update over the page's tokens below seq_lens[r] (bit for bit).  Pages that receive tokens
+ * must not be shared between requests.
+ */
+int se_rope_append(const se_params *p, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                   const void *v, int64_t v_stride, int32_t total_tokens, const int32_t *cu_seqlens,
+                   const int32_t *seq_lens, const int32_t *page_table, const int32_t *positions, int32_t n_axes,
+                   const double *inv_freq, const int32_t *pair_axis, int32_t rot_dim, int32_t interleaved,
+                   void *q_out, void *k_out, void *k_cache, void *v_cache, void *meta, void *workspace,
+                   void *stream);
+
+/*
+ * Causal attention of the new tokens over the cache (Appendix A, the attention equations of "MHA, MQA, and GQA"
+ * with the positions of "Logical Positions and Physical Blocks"): the token at position i attends every position
+ * j <= i of its request whose page is present,
+ *     z_j = sm_scale * q.k_j,   out = sum_j softmax(z)_j v_j,   lse = ln sum_j exp(z_j).
+ * The new tokens' own K and V are in the cache already (se_rope_append).  No visible position: out = 0, lse = -inf.
+ *   out  [total_tokens, H_q, D] bf16 (the next operation of a layer is a bf16 product)
+ *   lse  [total_tokens, H_q] fp32, or NULL
+ * Cache slots past a request's length may hold anything, NaN included.  n_r = 1 is a dense decode step.
+ */
+int se_chunk_attend(const se_params *p, const void *q, int64_t q_stride, int32_t total_tokens,
+                    const int32_t *cu_seqlens, const void *k_cache, const void *v_cache,
+                    const int32_t *page_table, const int32_t *seq_lens, void *out, float *lse, void *workspace,
+                    void *stream);
+
+/*
+ * The same for whole prompts whose K and V are still contiguous [total_tokens, H_kv, D] (a method that prunes the
+ * prompt before it caches anything, an encoder pass without a cache): token i of a request attends its tokens 0..i.
+ */
+int se_prompt_attend(const se_params *p, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                     const void *v, int64_t v_stride, int32_t total_tokens, const int32_t *cu_seqlens, void *out,
+                     float *lse, void *workspace, void *stream);
+
+/*
+ * Accumulated attention weight of a chunk (Appendix A, H2O accumulated score equation, over the queries of a chunk
+ * instead of one decode step): for every present position j of request r and kv-head h, with lse as
+ * se_chunk_attend left it for the same q and cache,
+ *     score_accum[pid(j),h,j%16] += sum over the new tokens i >= j and the heads a of group h of exp(z_ij^a - lse_i^a).
+ * After the last chunk of a prompt this is the statistic that se_h2o_retain ranks and the decode steps go on with.
+ * The physical pages of different requests must be distinct.  The sum's order is fixed: equal inputs give equal bits.
+ */
+int se_h2o_accumulate(const se_params *p, const void *q, int64_t q_stride, int32_t total_tokens,
+                      const int32_t *cu_seqlens, const void *k_cache, const int32_t *page_table,
+                      const int32_t *seq_lens, const float *lse, float *score_accum, void *workspace, void *stream);
 
 /*
  * Measurement aid (no counterpart in the paper): a read-only gather with the access pattern and

@@ -19,13 +19,16 @@ SE_OK = 0
 SE_DEV_BAD_PAGE_ID = 1
 SE_DEV_BAD_SELECTION = 2
 SE_DEV_WAIT_TIMEOUT = 4
+SE_DEV_BAD_LENGTH = 8
 
 EXPORTS = ("se_version", "se_strerror", "se_workspace_bytes", "se_decode_num_splits", "se_workspace_init",
            "se_meta_update",
            "se_page_select", "se_page_select_scores", "se_page_select_topk", "se_page_select_fused", "se_sparse_decode", "se_sparse_decode_splits", "se_combine",
            "se_last_device_status", "se_h2o_retain", "se_h2o_compact", "se_observe_decode", "se_token_select",
            "se_token_decode",
-           "se_page_select_static", "se_decode_step", "se_decode_step_launches", "se_probe_gather")
+           "se_page_select_static", "se_decode_step", "se_decode_step_launches", "se_probe_gather",
+           "se_prompt_workspace_bytes", "se_prompt_workspace_init", "se_rope_append", "se_chunk_attend",
+           "se_prompt_attend", "se_h2o_accumulate")
 SE_STATIC_SCRATCH_BYTES = 4 * 1024 * 1024
 
 
@@ -87,11 +90,21 @@ def load(build_if_missing: bool = True):
     lib.se_probe_gather.argtypes = [vp, vp, i32p, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                     ctypes.c_int32, ctypes.c_int32, vp]
     lib.se_probe_gather.restype = ctypes.c_int
+    i32, i64 = ctypes.c_int32, ctypes.c_int64
+    lib.se_prompt_workspace_bytes.restype = ctypes.c_size_t
+    lib.se_prompt_workspace_bytes.argtypes = [pp]
+    lib.se_prompt_workspace_init.argtypes = [pp, vp, vp]
+    lib.se_rope_append.argtypes = [pp, vp, i64, vp, i64, vp, i64, i32, i32p, i32p, i32p, i32p, i32, vp, i32p, i32, i32,
+                                   vp, vp, vp, vp, vp, vp, vp]
+    lib.se_chunk_attend.argtypes = [pp, vp, i64, i32, i32p, vp, vp, i32p, i32p, vp, fp, vp, vp]
+    lib.se_prompt_attend.argtypes = [pp, vp, i64, vp, i64, vp, i64, i32, i32p, vp, fp, vp, vp]
+    lib.se_h2o_accumulate.argtypes = [pp, vp, i64, i32, i32p, vp, i32p, i32p, fp, fp, vp, vp]
     for name in ("se_workspace_init", "se_meta_update", "se_page_select", "se_page_select_fused",
                  "se_sparse_decode", "se_sparse_decode_splits", "se_combine", "se_last_device_status",
                  "se_h2o_retain", "se_h2o_compact", "se_decode_num_splits", "se_page_select_static",
                  "se_observe_decode", "se_token_select", "se_token_decode", "se_page_select_scores",
-                 "se_page_select_topk", "se_decode_step", "se_decode_step_launches"):
+                 "se_page_select_topk", "se_decode_step", "se_decode_step_launches", "se_prompt_workspace_init",
+                 "se_rope_append", "se_chunk_attend", "se_prompt_attend", "se_h2o_accumulate"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -325,6 +338,143 @@ def se_h2o_compact(p, k_cache, v_cache, score_accum, page_table, keep_idx, keep_
                                  _ptr(keep_idx, torch.int32, "keep_idx"), _ptr(keep_cnt, torch.int32, "keep_cnt"),
                                  int(keep_idx.shape[-1]), _ptr(new_seq_lens, torch.int32, "new_seq_lens"),
                                  _ptr(workspace, torch.uint8, "workspace"), _stream()), "se_h2o_compact")
+
+
+# ---- prompt side: a packed batch of new tokens -------------------------------------------------------
+
+def se_prompt_workspace_bytes(p: SeParams) -> int:
+    return int(load().se_prompt_workspace_bytes(ctypes.byref(p)))
+
+
+def se_prompt_workspace_init(p: SeParams, workspace: torch.Tensor) -> None:
+    with torch.cuda.device(workspace.device):
+        _check(load().se_prompt_workspace_init(ctypes.byref(p), _ptr(workspace, torch.uint8, "workspace"), _stream()),
+               "se_prompt_workspace_init")
+
+
+def alloc_prompt_workspace(p: SeParams, device="cuda") -> torch.Tensor:
+    """Allocates (through torch) and initialises a workspace of the prompt calls for ``p``."""
+    n = se_prompt_workspace_bytes(p)
+    if n == 0:
+        raise SparseEngineError("invalid se_params")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    se_prompt_workspace_init(p, ws)
+    return ws
+
+
+def _rows(t: torch.Tensor, heads: int, D: int, name: str):
+    """Pointer and token stride of a [T, heads, D] bf16 tensor whose rows are contiguous (a view of a wider
+    projection output counts)."""
+    if not t.is_cuda:
+        raise SparseEngineError("%s must be a CUDA tensor" % name)
+    if t.dtype != torch.bfloat16:
+        raise SparseEngineError("%s must have dtype torch.bfloat16, got %s" % (name, t.dtype))
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != D:
+        raise SparseEngineError("%s must have shape [T, %d, %d], got %s" % (name, heads, D, tuple(t.shape)))
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != D):
+        raise SparseEngineError("the rows [H, D] of %s must be contiguous" % name)
+    # a dimension of one row has no stride to speak of
+    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else heads * D)
+
+
+def _shape(t: Optional[torch.Tensor], shape, name: str) -> None:
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise SparseEngineError("%s must have shape %s, got %s" % (name, list(shape), list(t.shape)))
+
+
+def _one_device(workspace: torch.Tensor, tensors) -> torch.device:
+    """The workspace's device, after a check that every other tensor is there too."""
+    for t in tensors:
+        if t is not None and t.device != workspace.device:
+            raise SparseEngineError("all tensors must be on %s, got one on %s" % (workspace.device, t.device))
+    return workspace.device
+
+
+def _prompt_common(p: SeParams, workspace: torch.Tensor, cu_seqlens, page_table=None, seq_lens=None, k_cache=None, v_cache=None):
+    _shape(cu_seqlens, [p.B + 1], "cu_seqlens")
+    _shape(page_table, [p.B, p.max_pages], "page_table")
+    _shape(seq_lens, [p.B], "seq_lens")
+    _shape(k_cache, [p.num_phys_pages, p.H_kv, 16, p.D], "k_cache")
+    _shape(v_cache, [p.num_phys_pages, p.H_kv, 16, p.D], "v_cache")
+    if workspace.numel() < se_prompt_workspace_bytes(p):
+        raise SparseEngineError("workspace is smaller than se_prompt_workspace_bytes")
+
+
+def se_rope_append(p, q, k, v, cu_seqlens, seq_lens, page_table, positions, inv_freq, pair_axis, q_out, k_cache,
+                   v_cache, workspace, meta=None, k_out=None, interleaved=False) -> None:
+    """``q``, ``k``, ``v`` may be views of one [T, H_q + 2*H_kv, D] projection output; rot_dim is twice the length of
+    ``inv_freq``; ``positions`` is [n_axes, T]."""
+    T = q.shape[0]
+    _prompt_common(p, workspace, cu_seqlens, page_table, seq_lens, k_cache, v_cache)
+    _shape(positions, [positions.shape[0], T], "positions")
+    _shape(k, [T, p.H_kv, p.D], "k")
+    _shape(v, [T, p.H_kv, p.D], "v")
+    _shape(q_out, [T, p.H_q, p.D], "q_out")
+    _shape(k_out, [T, p.H_kv, p.D], "k_out")
+    _shape(meta, [p.num_phys_pages, p.H_kv, 2, p.D], "meta")
+    _shape(pair_axis, inv_freq.shape, "pair_axis")
+    (qp, qs), (kp, ks), (vp_, vs) = _rows(q, p.H_q, p.D, "q"), _rows(k, p.H_kv, p.D, "k"), _rows(v, p.H_kv, p.D, "v")
+    if T == 0:           # an empty tensor has no address
+        return
+    with torch.cuda.device(_one_device(workspace, (q, k, v, cu_seqlens, seq_lens, page_table, positions, inv_freq, pair_axis,
+                                                   q_out, k_cache, v_cache, meta, k_out))):
+        _check(load().se_rope_append(ctypes.byref(p), qp, qs, kp, ks, vp_, vs, T, _ptr(cu_seqlens, torch.int32, "cu_seqlens"),
+                                     _ptr(seq_lens, torch.int32, "seq_lens"), _ptr(page_table, torch.int32, "page_table"),
+                                     _ptr(positions, torch.int32, "positions"), positions.shape[0],
+                                     _ptr(inv_freq, torch.float64, "inv_freq"), _ptr(pair_axis, torch.int32, "pair_axis"),
+                                     2 * inv_freq.numel(), int(bool(interleaved)), _ptr(q_out, torch.bfloat16, "q_out"),
+                                     _ptr(k_out, torch.bfloat16, "k_out"), _ptr(k_cache, torch.bfloat16, "k_cache"),
+                                     _ptr(v_cache, torch.bfloat16, "v_cache"), _ptr(meta, torch.bfloat16, "meta"),
+                                     _ptr(workspace, torch.uint8, "workspace"), _stream()), "se_rope_append")
+
+
+def se_chunk_attend(p, q, cu_seqlens, k_cache, v_cache, page_table, seq_lens, out, workspace, lse=None) -> None:
+    T = q.shape[0]
+    _prompt_common(p, workspace, cu_seqlens, page_table, seq_lens, k_cache, v_cache)
+    _shape(out, [T, p.H_q, p.D], "out")
+    _shape(lse, [T, p.H_q], "lse")
+    qp, qs = _rows(q, p.H_q, p.D, "q")
+    if T == 0:           # an empty tensor has no address
+        return
+    with torch.cuda.device(_one_device(workspace, (q, cu_seqlens, k_cache, v_cache, page_table, seq_lens, out, lse))):
+        _check(load().se_chunk_attend(ctypes.byref(p), qp, qs, T, _ptr(cu_seqlens, torch.int32, "cu_seqlens"),
+                                      _ptr(k_cache, torch.bfloat16, "k_cache"), _ptr(v_cache, torch.bfloat16, "v_cache"),
+                                      _ptr(page_table, torch.int32, "page_table"), _ptr(seq_lens, torch.int32, "seq_lens"),
+                                      _ptr(out, torch.bfloat16, "out"), _ptr(lse, torch.float32, "lse"),
+                                      _ptr(workspace, torch.uint8, "workspace"), _stream()), "se_chunk_attend")
+
+
+def se_prompt_attend(p, q, k, v, cu_seqlens, out, workspace, lse=None) -> None:
+    T = q.shape[0]
+    _prompt_common(p, workspace, cu_seqlens)
+    _shape(k, [T, p.H_kv, p.D], "k")
+    _shape(v, [T, p.H_kv, p.D], "v")
+    _shape(out, [T, p.H_q, p.D], "out")
+    _shape(lse, [T, p.H_q], "lse")
+    (qp, qs), (kp, ks), (vp_, vs) = _rows(q, p.H_q, p.D, "q"), _rows(k, p.H_kv, p.D, "k"), _rows(v, p.H_kv, p.D, "v")
+    if T == 0:           # an empty tensor has no address
+        return
+    with torch.cuda.device(_one_device(workspace, (q, k, v, cu_seqlens, out, lse))):
+        _check(load().se_prompt_attend(ctypes.byref(p), qp, qs, kp, ks, vp_, vs, T,
+                                       _ptr(cu_seqlens, torch.int32, "cu_seqlens"), _ptr(out, torch.bfloat16, "out"),
+                                       _ptr(lse, torch.float32, "lse"), _ptr(workspace, torch.uint8, "workspace"), _stream()),
+               "se_prompt_attend")
+
+
+def se_h2o_accumulate(p, q, cu_seqlens, k_cache, page_table, seq_lens, lse, score_accum, workspace) -> None:
+    T = q.shape[0]
+    _prompt_common(p, workspace, cu_seqlens, page_table, seq_lens, k_cache)
+    _shape(lse, [T, p.H_q], "lse")
+    _shape(score_accum, [p.num_phys_pages, p.H_kv, 16], "score_accum")
+    qp, qs = _rows(q, p.H_q, p.D, "q")
+    if T == 0:           # an empty tensor has no address
+        return
+    with torch.cuda.device(_one_device(workspace, (q, cu_seqlens, k_cache, page_table, seq_lens, lse, score_accum))):
+        _check(load().se_h2o_accumulate(ctypes.byref(p), qp, qs, T, _ptr(cu_seqlens, torch.int32, "cu_seqlens"),
+                                        _ptr(k_cache, torch.bfloat16, "k_cache"), _ptr(page_table, torch.int32, "page_table"),
+                                        _ptr(seq_lens, torch.int32, "seq_lens"), _ptr(lse, torch.float32, "lse"),
+                                        _ptr(score_accum, torch.float32, "score_accum"),
+                                        _ptr(workspace, torch.uint8, "workspace"), _stream()), "se_h2o_accumulate")
 
 
 def se_last_device_status(workspace) -> int:

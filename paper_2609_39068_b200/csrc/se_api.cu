@@ -430,6 +430,120 @@ int se_h2o_compact(const se_params *p, void *k_cache, void *v_cache, float *scor
     return e == cudaSuccess ? SE_OK : SE_ERR_CUDA;
 }
 
+// ---- prompt side ----
+static bool bad_stride(int64_t stride, int heads, int D) {
+    // one tensor copy addresses the rows, so the stride in bytes stays below 2^40
+    return stride < (int64_t)heads * D || stride % 8 != 0 || stride > (1ll << 38);
+}
+
+size_t se_prompt_workspace_bytes(const se_params *p) {
+    if (validate(p) != SE_OK) return 0;
+    return prompt_workspace_bytes(*p);
+}
+
+int se_prompt_workspace_init(const se_params *p, void *workspace, void *stream) {
+    int rc = validate(p);
+    if (rc != SE_OK) return rc;
+    if (!workspace) return SE_ERR_NULL_POINTER;
+    if (!aligned16(workspace)) return SE_ERR_MISALIGNED;
+    cudaError_t e = cudaMemsetAsync(workspace, 0, prompt_workspace_control_bytes(), static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? SE_OK : SE_ERR_CUDA;
+}
+
+int se_rope_append(const se_params *p, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                   const void *v, int64_t v_stride, int32_t total_tokens, const int32_t *cu_seqlens,
+                   const int32_t *seq_lens, const int32_t *page_table, const int32_t *positions, int32_t n_axes,
+                   const double *inv_freq, const int32_t *pair_axis, int32_t rot_dim, int32_t interleaved,
+                   void *q_out, void *k_out, void *k_cache, void *v_cache, void *meta, void *workspace,
+                   void *stream) {
+    int rc = validate(p);
+    if (rc != SE_OK) return rc;
+    if (!q || !k || !v || !cu_seqlens || !seq_lens || !page_table || !positions || !inv_freq || !pair_axis || !q_out ||
+        !k_cache || !v_cache || !workspace)
+        return SE_ERR_NULL_POINTER;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(cu_seqlens) || !aligned16(seq_lens) ||
+        !aligned16(page_table) || !aligned16(positions) || !aligned16(inv_freq) || !aligned16(pair_axis) ||
+        !aligned16(q_out) || !aligned16(k_out) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(meta) ||
+        !aligned16(workspace))
+        return SE_ERR_MISALIGNED;
+    if (total_tokens < 0 || bad_stride(q_stride, p->H_q, p->D) || bad_stride(k_stride, p->H_kv, p->D) ||
+        bad_stride(v_stride, p->H_kv, p->D) || n_axes < 1 || n_axes > 4 || rot_dim < 16 || rot_dim > p->D ||
+        rot_dim % 16 != 0 || (interleaved != 0 && interleaved != 1) || (q_out == q && q_stride != (int64_t)p->H_q * p->D))
+        return SE_ERR_INVALID_ARG;
+    if (total_tokens == 0) return SE_OK;
+    RopeCall c = {};
+    c.q = q, c.k = k, c.v = v, c.q_stride = q_stride, c.k_stride = k_stride, c.v_stride = v_stride;
+    c.total_tokens = total_tokens, c.n_axes = n_axes, c.rot_dim = rot_dim, c.interleaved = interleaved != 0;
+    c.cu_seqlens = cu_seqlens, c.seq_lens = seq_lens, c.page_table = page_table, c.positions = positions;
+    c.pair_axis = pair_axis, c.inv_freq = inv_freq;
+    c.q_out = q_out, c.k_out = k_out, c.k_cache = k_cache, c.v_cache = v_cache, c.meta = meta;
+    c.status = static_cast<uint32_t *>(workspace);
+    cudaError_t e = launch_rope_append(*p, c, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? SE_OK : SE_ERR_CUDA;
+}
+
+int se_chunk_attend(const se_params *p, const void *q, int64_t q_stride, int32_t total_tokens,
+                    const int32_t *cu_seqlens, const void *k_cache, const void *v_cache,
+                    const int32_t *page_table, const int32_t *seq_lens, void *out, float *lse, void *workspace,
+                    void *stream) {
+    int rc = validate(p);
+    if (rc != SE_OK) return rc;
+    if (!q || !cu_seqlens || !k_cache || !v_cache || !page_table || !seq_lens || !out || !workspace)
+        return SE_ERR_NULL_POINTER;
+    if (!aligned16(q) || !aligned16(cu_seqlens) || !aligned16(k_cache) || !aligned16(v_cache) ||
+        !aligned16(page_table) || !aligned16(seq_lens) || !aligned16(out) || !aligned16(lse) || !aligned16(workspace))
+        return SE_ERR_MISALIGNED;
+    if (total_tokens < 0 || bad_stride(q_stride, p->H_q, p->D)) return SE_ERR_INVALID_ARG;
+    if (total_tokens == 0) return SE_OK;
+    AttendCall c = {};
+    c.q = q, c.k = k_cache, c.v = v_cache, c.q_stride = q_stride, c.total_tokens = total_tokens;
+    c.cu_seqlens = cu_seqlens, c.seq_lens = seq_lens, c.page_table = page_table;
+    c.out = out, c.lse = lse, c.workspace = static_cast<uint8_t *>(workspace);
+    cudaError_t e = launch_prompt_attend(*p, c, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? SE_OK : SE_ERR_CUDA;
+}
+
+int se_prompt_attend(const se_params *p, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                     const void *v, int64_t v_stride, int32_t total_tokens, const int32_t *cu_seqlens, void *out,
+                     float *lse, void *workspace, void *stream) {
+    int rc = validate(p);
+    if (rc != SE_OK) return rc;
+    if (!q || !k || !v || !cu_seqlens || !out || !workspace) return SE_ERR_NULL_POINTER;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(cu_seqlens) || !aligned16(out) ||
+        !aligned16(lse) || !aligned16(workspace))
+        return SE_ERR_MISALIGNED;
+    if (total_tokens < 0 || bad_stride(q_stride, p->H_q, p->D) || bad_stride(k_stride, p->H_kv, p->D) ||
+        bad_stride(v_stride, p->H_kv, p->D))
+        return SE_ERR_INVALID_ARG;
+    if (total_tokens == 0) return SE_OK;
+    AttendCall c = {};
+    c.q = q, c.k = k, c.v = v, c.q_stride = q_stride, c.k_stride = k_stride, c.v_stride = v_stride;
+    c.total_tokens = total_tokens, c.cu_seqlens = cu_seqlens;
+    c.out = out, c.lse = lse, c.workspace = static_cast<uint8_t *>(workspace);
+    cudaError_t e = launch_prompt_attend(*p, c, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? SE_OK : SE_ERR_CUDA;
+}
+
+int se_h2o_accumulate(const se_params *p, const void *q, int64_t q_stride, int32_t total_tokens,
+                      const int32_t *cu_seqlens, const void *k_cache, const int32_t *page_table,
+                      const int32_t *seq_lens, const float *lse, float *score_accum, void *workspace, void *stream) {
+    int rc = validate(p);
+    if (rc != SE_OK) return rc;
+    if (!q || !cu_seqlens || !k_cache || !page_table || !seq_lens || !lse || !score_accum || !workspace)
+        return SE_ERR_NULL_POINTER;
+    if (!aligned16(q) || !aligned16(cu_seqlens) || !aligned16(k_cache) || !aligned16(page_table) ||
+        !aligned16(seq_lens) || !aligned16(lse) || !aligned16(score_accum) || !aligned16(workspace))
+        return SE_ERR_MISALIGNED;
+    if (total_tokens < 0 || bad_stride(q_stride, p->H_q, p->D)) return SE_ERR_INVALID_ARG;
+    if (total_tokens == 0) return SE_OK;
+    AttendCall c = {};
+    c.q = q, c.k = k_cache, c.q_stride = q_stride, c.total_tokens = total_tokens;
+    c.cu_seqlens = cu_seqlens, c.seq_lens = seq_lens, c.page_table = page_table;
+    c.lse = const_cast<float *>(lse), c.workspace = static_cast<uint8_t *>(workspace);
+    cudaError_t e = launch_h2o_accumulate(*p, c, score_accum, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? SE_OK : SE_ERR_CUDA;
+}
+
 int se_last_device_status(void *workspace, void *stream, int32_t *host_out) {
     if (!workspace || !host_out) return SE_ERR_NULL_POINTER;
     cudaStream_t s = static_cast<cudaStream_t>(stream);

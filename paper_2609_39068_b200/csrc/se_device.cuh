@@ -147,6 +147,27 @@ __device__ __forceinline__ int cta_excl_scan(int v, int *tot, int lane, int warp
     return __shfl_sync(kFull, winc - wt, warp) + inc - v;
 }
 
+// New tokens of request r in a packed batch: rows [start, start + n) of the token-major arrays, positions
+// past .. past + n - 1 of the request.  seq_lens == nullptr: whole prompts (past = 0).  A request whose
+// offsets or length make no sense (outside the T rows, more new tokens than the length, more tokens than the
+// page table's row holds) has valid = false and no tokens.
+struct TokenRange {
+    int start, n, past;
+    bool valid;
+};
+__device__ __forceinline__ TokenRange token_range(const int32_t *cu, const int32_t *seq_lens, int r, int T,
+                                                  int max_tokens) {
+    const int start = cu[r], end = cu[r + 1];
+    const int n = end - start;
+    const int len = seq_lens ? seq_lens[r] : n;
+    TokenRange t;
+    t.valid = start >= 0 && end >= start && end <= T && (n == 0 || (len >= n && len <= max_tokens));
+    t.start = t.valid ? start : 0;
+    t.n = t.valid ? n : 0;
+    t.past = t.valid && n ? len - n : 0;
+    return t;
+}
+
 // ---------------------------------------------------------------------------------
 // warp-level matrix helpers (bf16 inputs, fp32 accumulation)
 // ---------------------------------------------------------------------------------

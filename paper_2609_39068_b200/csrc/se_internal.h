@@ -82,4 +82,33 @@ cudaError_t launch_token_decode(const se_params &p, const void *q, const void *k
                                 const WorkspaceLayout &L, cudaStream_t stream);
 // stages: 1 = split attention kernel, 2 = combine kernel (merge + H2O epilogue), 3 = both
 
+// ---- prompt side: calls over a packed batch of new tokens ----
+struct RopeCall {
+    const void *q, *k, *v;
+    long long q_stride, k_stride, v_stride;      // elements between tokens
+    int total_tokens, n_axes, rot_dim;
+    bool interleaved;
+    const int32_t *cu_seqlens, *seq_lens, *page_table, *positions, *pair_axis;
+    const double *inv_freq;
+    void *q_out, *k_out, *k_cache, *v_cache, *meta;
+    uint32_t *status;
+};
+cudaError_t launch_rope_append(const se_params &p, const RopeCall &c, cudaStream_t stream);
+
+// attention of the new tokens over the cache (page_table != nullptr: k, v are the caches) or over contiguous K and V
+struct AttendCall {
+    const void *q, *k, *v;
+    long long q_stride, k_stride, v_stride;
+    int total_tokens;
+    const int32_t *cu_seqlens, *seq_lens, *page_table;   // seq_lens, page_table nullptr: whole prompts, contiguous K and V
+    void *out;
+    float *lse;
+    uint8_t *workspace;
+};
+cudaError_t launch_prompt_attend(const se_params &p, const AttendCall &c, cudaStream_t stream);
+// score_accum += the queries' weights on every cached token (k, lse of `c` are read, v and out are not used)
+cudaError_t launch_h2o_accumulate(const se_params &p, const AttendCall &c, float *score_accum, cudaStream_t stream);
+size_t prompt_workspace_bytes(const se_params &p);
+size_t prompt_workspace_control_bytes();
+
 }  // namespace se
