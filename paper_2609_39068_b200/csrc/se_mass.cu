@@ -44,52 +44,6 @@ __device__ __forceinline__ float dot(const float (&x)[D / 32], const float (&y)[
     return s;
 }
 
-__device__ __forceinline__ int max_tokens(const SimpleArgs &a) { return a.page_table ? a.max_pages * kPage : a.T; }
-
-template <int D>
-__global__ void attend_kernel(const SimpleArgs a) {
-    const int lane = threadIdx.x & 31;
-    const long long w = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-    const int t = (int)(w / a.H_q), hq = (int)(w % a.H_q), h = hq / (a.H_q / a.H_kv);
-    if (t >= a.T) return;
-    for (int r = 0; r < a.B; ++r) {
-        const TokenRange tr = token_range(a.cu, a.seq_lens, r, a.T, max_tokens(a));
-        if (!tr.valid && lane == 0) atomicOr(a.status, SE_DEV_BAD_LENGTH);
-        if (t < tr.start || t >= tr.start + tr.n) continue;
-        float q[D / 32], o[D / 32] = {}, m = -INFINITY, l = 0.f;
-        load_row<D>(q, a.q + t * a.q_stride + hq * D, lane);
-        for (int j = 0; j <= tr.past + t - tr.start; ++j) {
-            const uint16_t *kr, *vr;
-            if (a.page_table) {
-                const int pid = a.page_table[(size_t)r * a.max_pages + j / kPage];
-                if (pid >= a.P_phys && lane == 0) atomicOr(a.status, SE_DEV_BAD_PAGE_ID);
-                if (pid < 0 || pid >= a.P_phys) continue;
-                const size_t at = (((size_t)pid * a.H_kv + h) * kPage + j % kPage) * D;
-                kr = a.k + at, vr = a.v + at;
-            } else {
-                kr = a.k + (tr.start + j) * a.k_stride + h * D, vr = a.v + (tr.start + j) * a.v_stride + h * D;
-            }
-            float x[D / 32];
-            load_row<D>(x, kr, lane);
-            const float z = dot<D>(q, x) * a.scale_log2, mn = fmaxf(m, z);
-            const float f = exp2f(m - mn), e = exp2f(z - mn);
-            load_row<D>(x, vr, lane);
-            l = l * f + e, m = mn;
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) o[i] = o[i] * f + e * x[i];
-        }
-        const float inv = l > 0.f ? 1.f / l : 0.f;
-        uint32_t *dst = reinterpret_cast<uint32_t *>(a.out + ((size_t)t * a.H_q + hq) * D);
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-            const __nv_bfloat162 b = __float22bfloat162_rn(make_float2(o[2 * i] * inv, o[2 * i + 1] * inv));
-            dst[i * 32 + lane] = *reinterpret_cast<const uint32_t *>(&b);
-        }
-        if (a.lse && lane == 0) a.lse[(size_t)t * a.H_q + hq] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
-        return;
-    }
-}
-
 template <int D>
 __global__ void accumulate_kernel(const SimpleArgs a) {
     const int lane = threadIdx.x & 31, G = a.H_q / a.H_kv;
@@ -128,17 +82,6 @@ SimpleArgs simple_args(const se_params &p, const AttendCall &c) {
 }
 
 }  // namespace
-
-size_t prompt_workspace_control_bytes() { return 256; }
-size_t prompt_workspace_bytes(const se_params &) { return prompt_workspace_control_bytes(); }
-
-cudaError_t launch_prompt_attend(const se_params &p, const AttendCall &c, cudaStream_t stream) {
-    const SimpleArgs a = simple_args(p, c);
-    const unsigned grid = (unsigned)(((long long)c.total_tokens * p.H_q + 7) / 8);
-    if (p.D == 128) attend_kernel<128><<<grid, 256, 0, stream>>>(a);
-    else attend_kernel<64><<<grid, 256, 0, stream>>>(a);
-    return cudaGetLastError();
-}
 
 cudaError_t launch_h2o_accumulate(const se_params &p, const AttendCall &c, float *score_accum, cudaStream_t stream) {
     SimpleArgs a = simple_args(p, c);
