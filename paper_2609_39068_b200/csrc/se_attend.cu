@@ -23,20 +23,17 @@
 #include <math.h>
 
 #include "se_internal.h"
+#include "se_pieces.cuh"
 #include "se_tc.cuh"
 
 namespace se {
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLn2 = 0.69314718055994530942f;
-
-constexpr int kThreads = 384;          // 2 softmax warpgroups, copy warp, product warp, 2 idle warps
+constexpr int kThreads = kPromptThreads;   // 2 softmax warpgroups, copy warp, product warp, 2 idle warps
 constexpr int kCopyWarp = 8, kMmaWarp = 9;
 constexpr int kRegsSoftmax = 208, kRegsOther = 88;   // 256 * 208 + 128 * 88 = 384 * 168
 constexpr int kTile = 128;             // query rows of a tile, tokens of a KV tile
-constexpr int kMaxCtas = 148;
 constexpr int kControlBytes = 2048;    // status word, tickets
 constexpr int kItemCost = 128;         // cost of starting a query tile, in tokens
 constexpr int kMinCost = 4 * kTile;    // a CTA takes at least two shared KV tiles
@@ -70,34 +67,41 @@ enum Bar { kQFull, kQEmpty, kSFull, kPReady = kSFull + 2, kODone = kPReady + 2, 
 template <int D>
 struct Control {
     uint64_t bars[kRing + 2 * Cfg<D>::kSlots];
-    int bound_item[kMaxCtas + 2], bound_tile[kMaxCtas + 2];
+    Pieces pieces;
     uint32_t mask[Cfg<D>::kMasks];     // present 16-token groups of the tiles in flight
-    int begin[3];                      // request, head, item of this CTA's first piece (request B: none)
     int last[2];
     int gave_up;
     uint32_t tmem;
 };
 
 // ---- the work list -----------------------------------------------------------------
-// cost of the first i query tile pairs of a request (all of them full)
-__device__ __forceinline__ long long pairs_cost(long long past, int c, long long i) {
-    return 2 * (i * (past + kItemCost) + (long long)c * (i * (i + 1) / 2));
-}
-__device__ __forceinline__ long long request_cost(const TokenRange &t, int tpt, int &items) {
-    const int c = 2 * tpt, m = t.n / c, rem = t.n - m * c;
-    items = m + (rem > 0);
-    long long w = pairs_cost(t.past, c, m);
-    if (rem > 0) w += (long long)(rem > tpt ? 2 : 1) * (t.past + t.n + kItemCost);
-    return w;
-}
-__device__ __forceinline__ TokenRange tokens_of(const AttendArgs &a, int r) {
-    return token_range(a.cu, a.seq_lens, r, a.T, a.page_table ? a.max_pages * kPage : a.T);
-}
+// item = two query tiles (the last one of a request may be a single tile), unit = KV tile.  Cost in tokens seen, twice
+// for two tiles.
+struct AttendWork {
+    const int32_t *cu, *seq_lens;
+    int T, max_tokens, tpt;            // tpt: new tokens of a query tile
 
-struct Cursor {
-    int r, h, i, tile, item;
-    TokenRange t;
+    __device__ __forceinline__ explicit AttendWork(const AttendArgs &a)
+        : cu(a.cu), seq_lens(a.seq_lens), T(a.T), max_tokens(a.page_table ? a.max_pages * kPage : a.T), tpt(kTile / a.G) {}
+    __device__ __forceinline__ TokenRange tokens(int r) const { return token_range(cu, seq_lens, r, T, max_tokens); }
+    __device__ __forceinline__ int items(const TokenRange &t) const { return (t.n + 2 * tpt - 1) / (2 * tpt); }
+    __device__ __forceinline__ int new_tokens(const TokenRange &t, int i) const { return min(2 * tpt, t.n - i * 2 * tpt); }
+    __device__ __forceinline__ long long cost(const TokenRange &t, long long i) const {
+        const int full = t.n / (2 * tpt);
+        const long long m = min(i, (long long)full);
+        long long c = 2 * (m * (t.past + kItemCost) + 2 * tpt * (m * (m + 1) / 2));
+        if (i > full) c += (long long)(t.n - full * 2 * tpt > tpt ? 2 : 1) * (t.past + t.n + kItemCost);
+        return c;
+    }
+    __device__ __forceinline__ int units(const TokenRange &t, int i) const {
+        return (t.past + i * 2 * tpt + new_tokens(t, i) + kTile - 1) / kTile;
+    }
+    __device__ __forceinline__ int unit_at(const TokenRange &t, int i, long long z) const {
+        return (int)(z / (kTile * (new_tokens(t, i) > tpt ? 2 : 1)));
+    }
+    __device__ __forceinline__ long long min_cost() const { return kMinCost; }
 };
+
 struct Segment {
     int r, h, item;
     TokenRange t;
@@ -109,145 +113,25 @@ struct Segment {
 };
 
 // This CTA's next piece; every role walks the same list.
-template <int D>
-__device__ __forceinline__ bool next_segment(const AttendArgs &a, const Control<D> *ctl, Cursor &c, Segment &s) {
-    const int e_item = ctl->bound_item[blockIdx.x + 1], e_tile = ctl->bound_tile[blockIdx.x + 1];
-    if (c.r >= a.B || c.item > e_item || (c.item == e_item && c.tile >= e_tile)) return false;
-    const int tpt = kTile / a.G;
+__device__ __forceinline__ bool next_segment(const AttendArgs &a, const AttendWork &w, const Pieces &p, Cursor &c, Segment &s) {
+    if (piece_done(c, a.B, p)) return false;
     s.r = c.r, s.h = c.h, s.item = c.item, s.t = c.t;
-    s.tok0 = c.i * 2 * tpt;
-    s.ntok = min(2 * tpt, c.t.n - s.tok0);
-    s.alt = s.ntok <= tpt;
-    s.nkv = (c.t.past + s.tok0 + s.ntok + kTile - 1) / kTile;
-    s.a = c.tile;
-    s.b = c.item == e_item ? min(e_tile, s.nkv) : s.nkv;
+    s.tok0 = c.i * 2 * w.tpt;
+    s.ntok = w.new_tokens(c.t, c.i);
+    s.alt = s.ntok <= w.tpt;
+    s.nkv = w.units(c.t, c.i);
+    s.a = c.unit;
+    s.b = piece_end(c, p, s.nkv);
     if (s.alt) {
         s.steps0 = (s.b - s.a + 1) / 2;
         s.steps1 = (s.b - s.a) / 2;
     } else {
-        const int n0 = (c.t.past + s.tok0 + tpt + kTile - 1) / kTile;      // the first tile's tokens see no more than this
+        const int n0 = (c.t.past + s.tok0 + w.tpt + kTile - 1) / kTile;    // the first tile's tokens see no more than this
         s.steps0 = max(min(s.b, n0) - s.a, 0);
         s.steps1 = s.b - s.a;
     }
-    c.tile = 0;
-    ++c.item;
-    if (s.tok0 + s.ntok < c.t.n) {
-        ++c.i;
-    } else {
-        c.i = 0;
-        if (++c.h == a.H_kv) {
-            c.h = 0;
-            do {
-                if (++c.r < a.B) c.t = tokens_of(a, c.r);
-            } while (c.r < a.B && c.t.n == 0);
-        }
-    }
+    next_item(w, a.B, a.H_kv, c);
     return true;
-}
-
-// Cuts the work into gridDim.x pieces: bounds of all CTAs into the control block.  scratch: the ring (160 KB), of which
-// 12 * (B + 1) <= 98316 bytes hold the requests' prefix sums.
-template <int D>
-__device__ __forceinline__ void cut_work(const AttendArgs &a, Control<D> *ctl, uint8_t *scratch) {
-    long long *cost = reinterpret_cast<long long *>(scratch);              // [B + 1] prefix sums
-    int *first = reinterpret_cast<int *>(cost + a.B + 1);                  // [B + 1]
-    long long *s_cost = reinterpret_cast<long long *>(scratch + 131072);   // per-warp sums
-    int *s_items = reinterpret_cast<int *>(s_cost + kThreads / 32);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int tpt = kTile / a.G;
-    const int per = (a.B + kThreads - 1) / kThreads;
-    long long w = 0;
-    int n = 0;
-    for (int k = 0; k < per; ++k) {
-        const int r = tid * per + k;
-        if (r >= a.B) break;
-        const TokenRange t = tokens_of(a, r);
-        if (!t.valid && blockIdx.x == 0) atomicOr(a.status, SE_DEV_BAD_LENGTH);
-        int items;
-        const long long wr = request_cost(t, tpt, items);
-        cost[r] = wr, first[r] = items;
-        w += wr * a.H_kv, n += items * a.H_kv;
-    }
-    long long wi = w;
-    int ni = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long x = __shfl_up_sync(kFull, wi, o);
-        const int y = __shfl_up_sync(kFull, ni, o);
-        if (lane >= o) wi += x, ni += y;
-    }
-    if (lane == 31) s_cost[warp] = wi, s_items[warp] = ni;
-    __syncthreads();
-    long long wb = wi - w;
-    int nb = ni - n;
-    for (int k = 0; k < warp; ++k) wb += s_cost[k], nb += s_items[k];
-    for (int k = 0; k < per; ++k) {
-        const int r = tid * per + k;
-        if (r >= a.B) break;
-        const long long wr = cost[r];
-        const int items = first[r];
-        cost[r] = wb, first[r] = nb;
-        wb += wr * a.H_kv, nb += items * a.H_kv;
-    }
-    if (tid == kThreads - 1) cost[a.B] = wb, first[a.B] = nb;
-    __syncthreads();
-    const long long total = cost[a.B];
-    long long piece = (total + gridDim.x - 1) / gridDim.x;
-    if (piece < kMinCost) piece = kMinCost;
-    if (tid <= (int)gridDim.x) {
-        const long long at = piece * tid;
-        int item = first[a.B], tile = 0;
-        if (at < total) {
-            int lo = 0, hi = a.B;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (cost[mid] <= at) lo = mid; else hi = mid;
-            }
-            const TokenRange t = tokens_of(a, lo);
-            int items;
-            const long long wr = request_cost(t, tpt, items);
-            const long long x = at - cost[lo];
-            const int h = (int)(x / wr);
-            const long long y = x - h * wr;
-            int i0 = 0, i1 = items;
-            while (i1 - i0 > 1) {
-                const int mid = (i0 + i1) >> 1;
-                if (pairs_cost(t.past, 2 * tpt, mid) <= y) i0 = mid; else i1 = mid;
-            }
-            const int tok0 = i0 * 2 * tpt, ntok = min(2 * tpt, t.n - tok0);
-            const int nkv = (t.past + tok0 + ntok + kTile - 1) / kTile;
-            const long long z = y - pairs_cost(t.past, 2 * tpt, i0);
-            tile = (int)(z / (kTile * (ntok > tpt ? 2 : 1)));
-            item = first[lo] + h * items + i0;
-            // no crumbs: a piece of a tile that is split has two KV tiles at least
-            if (tile < 2) tile = 0;
-            else if (tile > nkv - 2) tile = 0, ++item;
-            if (tid == (int)blockIdx.x) {
-                int r = lo, hh = h, i = i0;
-                if (item != first[lo] + h * items + i0 && ++i == items) {
-                    i = 0;
-                    if (++hh == a.H_kv) {
-                        hh = 0, ++r;
-                        while (r < a.B && first[r + 1] == first[r]) ++r;
-                    }
-                }
-                ctl->begin[0] = r, ctl->begin[1] = hh, ctl->begin[2] = i;
-            }
-        } else if (tid == (int)blockIdx.x) {
-            ctl->begin[0] = a.B, ctl->begin[1] = ctl->begin[2] = 0;
-        }
-        ctl->bound_item[tid] = item, ctl->bound_tile[tid] = tile;
-    }
-}
-
-template <int D>
-__device__ __forceinline__ Cursor first_piece(const AttendArgs &a, const Control<D> *ctl) {
-    Cursor c;
-    c.r = ctl->begin[0], c.h = ctl->begin[1], c.i = ctl->begin[2];
-    c.item = ctl->bound_item[blockIdx.x], c.tile = ctl->bound_tile[blockIdx.x];
-    c.t = TokenRange{0, 0, 0, false};
-    if (c.r < a.B) c.t = tokens_of(a, c.r);
-    return c;
 }
 
 // ---- copies ------------------------------------------------------------------------
@@ -314,11 +198,12 @@ __device__ __forceinline__ void copy_role(const AttendArgs &a, const CUtensorMap
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     const int tpt = kTile / a.G;
-    Cursor c = first_piece(a, ctl);
+    const AttendWork work(a);
+    Cursor c = first_piece(work, a.B, ctl->pieces);
     Segment s;
     uint32_t pos = 0, tiles = 0, pieces = 0;
     bool ok = true;
-    while (ok && next_segment(a, ctl, c, s)) {
+    while (ok && next_segment(a, work, ctl->pieces, c, s)) {
         const int stop = s.t.past + s.t.n;                                 // tokens the request has
         int pid = group_page(a, s, s.a, stop, lane);
         ok = warp_wait(bars + 8 * kQEmpty, (pieces & 1) ^ 1, gave_up, a.status);
@@ -362,11 +247,12 @@ __device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, u
     volatile int *gave_up = &ctl->gave_up;
     constexpr uint32_t kInstrS = mma_instr(kTile, false), kInstrO = mma_instr(D, true);
     const uint32_t tmem = ctl->tmem;
-    Cursor c = first_piece(a, ctl);
+    const AttendWork work(a);
+    Cursor c = first_piece(work, a.B, ctl->pieces);
     Segment s;
     uint32_t pos = 0, pieces = 0, p_seen = 0, o_used = 0;      // bit st: parity of the stream's next wait
     bool ok = true, any = false;
-    while (ok && next_segment(a, ctl, c, s)) {
+    while (ok && next_segment(a, work, ctl->pieces, c, s)) {
         const int steps = max(s.steps0, s.steps1);
         // ring position of the K tile of step i of stream st; its V tile follows
         auto place = [&](int st, int i) { return pos + 2u * (s.alt ? 2 * i + st : i); };
@@ -505,7 +391,8 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     const uint32_t t_s = ctl->tmem + lanes + st * kTile, t_o = ctl->tmem + lanes + C::kTmemO + st * D;
     const float sl = a.scale_log2;
-    Cursor c = first_piece(a, ctl);
+    const AttendWork work(a);
+    Cursor c = first_piece(work, a.B, ctl->pieces);
     Segment s;
     uint32_t step = 0, tiles = 0, verdicts = 0, swaps = 0;
     // both warpgroups have come here
@@ -514,7 +401,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
         if (lane == 0) mbar_arrive(bars + 8 * kSwap);
         return warp_wait(bars + 8 * kSwap, swaps++ & 1, gave_up, a.status);
     };
-    while (next_segment(a, ctl, c, s)) {
+    while (next_segment(a, work, ctl->pieces, c, s)) {
         const int tok = s.tok0 + (s.alt ? 0 : st * tpt);                   // the tile's first new token
         const int ntok = min(tpt, s.tok0 + s.ntok - tok);
         const int q = min(row / a.G, ntok - 1);
@@ -657,8 +544,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
         }
         if (steps == 0 && s.alt) continue;
         // the CTAs of the item: from the one that begins it to the one that ends it
-        int from = blockIdx.x;
-        while (ctl->bound_item[from] == s.item && ctl->bound_tile[from] > 0) --from;
+        const int from = first_cta(ctl->pieces, s.item);
         uint32_t *ticket = a.tickets + 2 * from + (s.alt ? 0 : st);
         __threadfence();
         __syncwarp();
@@ -680,19 +566,10 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
         if (ctl->last[st]) {
             __threadfence();
             auto each = [&](auto f) {
-                for (int y = from;; ++y) {
-                    const bool ends = !(ctl->bound_item[y + 1] == s.item && ctl->bound_tile[y + 1] > 0);
-                    const int ya = y == from ? 0 : ctl->bound_tile[y], yb = ends ? s.nkv : ctl->bound_tile[y + 1];
-                    if (yb > ya) {
-                        if (s.alt) {
-                            f((const float *)partial_slot<D>(a, y, ya == 0, 0));
-                            if (yb - ya > 1) f((const float *)partial_slot<D>(a, y, ya == 0, 1));
-                        } else {
-                            f((const float *)partial_slot<D>(a, y, ya == 0, st));
-                        }
-                    }
-                    if (ends) break;
-                }
+                each_cta(ctl->pieces, s.item, s.nkv, from, [&](int y, int ya, int yb) {
+                    f((const float *)partial_slot<D>(a, y, ya == 0, s.alt ? 0 : st));
+                    if (s.alt && yb - ya > 1) f((const float *)partial_slot<D>(a, y, ya == 0, 1));
+                });
             };
             merge_rows<D>(a, s, st, warp, 4, each, lane);
         }
@@ -732,7 +609,7 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
         ctl->gave_up = 0;
     }
     if (warp == kMmaWarp) tmem_alloc(smem_u32(&ctl->tmem), 512);
-    cut_work<D>(a, ctl, smem + 2 * C::kTileBytes);
+    cut_work(AttendWork(a), a.B, a.H_kv, a.status, &ctl->pieces, smem + 2 * C::kTileBytes);
     // query rows that no tensor copy fills (G does not divide 128) stay zero
     for (int i = threadIdx.x; i < 2 * C::kTileBytes / 16; i += kThreads)
         reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
@@ -759,37 +636,6 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
 }
 
 // ---- host side ---------------------------------------------------------------------
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
-                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                  CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-    static EncodeTiledFn fn = [] {
-        void *sym = nullptr;
-        cudaDriverEntryPointQueryResult qres;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &qres) != cudaSuccess ||
-            qres != cudaDriverEntryPointSuccess)
-            sym = nullptr;
-        return reinterpret_cast<EncodeTiledFn>(sym);
-    }();
-    return fn;
-}
-
-// bf16 tensor [rows][heads][D], boxes of 64 channels x box_heads x box_rows, 128-byte swizzle, zeros outside
-bool make_rows_map(CUtensorMap *map, const void *base, int D, long long heads, long long rows, long long stride, int box_heads,
-                   int box_rows) {
-    EncodeTiledFn fn = encode_fn();
-    if (!fn) return false;
-    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)rows};
-    const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2};
-    const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
-    const cuuint32_t estr[3] = {1, 1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int D>
 cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t stream) {
     using C = Cfg<D>;
@@ -821,7 +667,7 @@ cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t 
     const size_t smem = (2 + C::kSlots) * C::kTileBytes + sizeof(Control<D>);
     e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    kern<<<kMaxCtas, kThreads, smem, stream>>>(q_map, k_map, v_map, a);
+    kern<<<kPromptCtas, kThreads, smem, stream>>>(q_map, k_map, v_map, a);
     return cudaGetLastError();
 }
 
@@ -830,7 +676,7 @@ cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t 
 size_t prompt_workspace_control_bytes() { return kControlBytes; }
 size_t prompt_workspace_bytes(const se_params &p) {
     const size_t slot = ((size_t)kTile * p.D + 2 * kTile) * sizeof(float);
-    return kControlBytes + (size_t)kMaxCtas * 4 * slot;
+    return kControlBytes + (size_t)kPromptCtas * 4 * slot;
 }
 
 cudaError_t launch_prompt_attend(const se_params &p, const AttendCall &c, cudaStream_t stream) {

@@ -1,95 +1,423 @@
-// Attention of a packed batch of new tokens (Appendix A, attention equations of "MHA, MQA, and GQA"), over the paged
-// cache or over contiguous K and V, and the accumulated weights of a chunk (H2O accumulated score equation).
+// Accumulated attention weights of a chunk (Appendix A, H2O accumulated score equation, summed over the queries of a chunk):
+//     u[j,h] += sum over the new tokens i >= j and the heads a of group h of exp(z_ij^a - lse_i^a).
 //
-// First form: one warp per (token, query head) with an online softmax over the tokens it sees, and one warp per
-// (cached token, kv-head) for the weights.  Right for every case, bound by its shuffles.
+// The sum runs over queries, so the tile is laid the other way round than in the attention kernel: a tile of 128 cached
+// tokens is the M side (tensor-memory lanes), a query tile of 128/G tokens x G heads the N side (columns), S^T = K Q^T.
+// A thread owns one cached token and adds up 2^(S sl - lse log2 e) along its columns in a register: no reduction between
+// threads, no atomics, no second pass, and the result does not depend on timing.
+//
+// What bounds it: per 128 x 128 tile one product of 512 tensor cycles (D = 128) and 16384 exponentials = 1024 cycles of
+// the special-function units; K is read once per item, the queries come from L2.  A CTA works on two tiles of cached tokens
+// (one warpgroup each) that share every query tile.  Scores are double-buffered in tensor memory (4 x 128 columns), so the
+// products of the next query tile run under the exponentials of this one.
+//
+// Item = 256 cached tokens of one (request, kv-head), unit = query tile; pieces and merging as in se_pieces.cuh (a partial
+// result is one number per cached token).
 #include <math.h>
 
 #include "se_internal.h"
+#include "se_pieces.cuh"
+#include "se_tc.cuh"
 
 namespace se {
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLn2 = 0.69314718055994530942f;
+constexpr int kThreads = kPromptThreads;   // 2 summing warpgroups, copy warp, product warp, lse warp, idle warp
+constexpr int kCopyWarp = 8, kMmaWarp = 9, kLseWarp = 10;
+constexpr int kTile = 128;             // cached tokens of a tile, query rows of a tile
+constexpr int kLseSlots = 2;
+constexpr int kControlBytes = 2048;    // status word, tickets (layout shared with the attention kernel)
 
-struct SimpleArgs {
-    const uint16_t *q, *k, *v;
-    long long q_stride, k_stride, v_stride;
+template <int D>
+struct Cfg {
+    static constexpr int kHalves = D / 64;
+    static constexpr int kTileBytes = kTile * D * 2;
+    static constexpr int kPairs = 2;                              // K tile pairs in shared memory
+    static constexpr int kSlots = 3 * 128 / D;                    // ring of query tiles, 96 KB
+};
+
+struct MassArgs {
     const int32_t *cu, *seq_lens, *page_table;
-    uint16_t *out;
-    float *lse, *accum;
-    uint32_t *status;
-    int B, H_q, H_kv, T, max_pages, P_phys;
+    const float *lse;
+    float *accum, *partials;
+    uint32_t *status, *tickets;
+    int B, H_q, H_kv, G, T, max_pages, P_phys;
     float scale_log2;
 };
 
+enum Bar { kSFull, kSFree = kSFull + 4, kLseFull = kSFree + 4, kLseEmpty = kLseFull + kLseSlots, kKFull = kLseEmpty + kLseSlots,
+           kKEmpty = kKFull + 2, kAll = kKEmpty + 2, kVerdict = kAll + 2, kDrain = kVerdict + 2, kRing };
+
 template <int D>
-__device__ __forceinline__ void load_row(float (&x)[D / 32], const uint16_t *row, int lane) {
+struct Control {
+    uint64_t bars[kRing + 2 * Cfg<D>::kSlots];
+    alignas(16) float lse[kLseSlots][kTile];   // -lse log2 e of the query tiles' rows, -inf for rows that count for nothing
+    Pieces pieces;
+    int last[2];
+    int gave_up;
+    uint32_t tmem;
+};
+
+struct MassWork {
+    const int32_t *cu, *seq_lens;
+    int T, max_tokens, tpt;            // tpt: new tokens of a query tile
+
+    __device__ __forceinline__ explicit MassWork(const MassArgs &a)
+        : cu(a.cu), seq_lens(a.seq_lens), T(a.T), max_tokens(a.max_pages * kPage), tpt(kTile / a.G) {}
+    __device__ __forceinline__ TokenRange tokens(int r) const { return token_range(cu, seq_lens, r, T, max_tokens); }
+    __device__ __forceinline__ int items(const TokenRange &t) const { return (t.past + t.n + 2 * kTile - 1) / (2 * kTile); }
+    // new tokens that see nothing of a tile of cached tokens beginning at `pos`
+    __device__ __forceinline__ int blind(const TokenRange &t, int pos) const { return max(pos - t.past, 0); }
+    // cost: new tokens that see the item, and the start of an item as much as two query tiles
+    __device__ __forceinline__ long long cost(const TokenRange &t, long long i) const {
+        const long long all = t.past / (2 * kTile) + 1;           // items that every new token sees
+        long long c = i * (t.n + 2 * tpt);
+        if (i > all) c -= 2 * kTile * (i * (i - 1) / 2 - all * (all - 1) / 2) - (i - all) * t.past;
+        return c;
+    }
+    __device__ __forceinline__ int query_tiles(const TokenRange &t) const { return (t.n + tpt - 1) / tpt; }
+    __device__ __forceinline__ int units(const TokenRange &t, int i) const {
+        return query_tiles(t) - blind(t, i * 2 * kTile) / tpt;
+    }
+    __device__ __forceinline__ int unit_at(const TokenRange &, int, long long z) const { return (int)(z / tpt); }
+    __device__ __forceinline__ long long min_cost() const { return 4 * tpt; }
+};
+
+struct Segment {
+    int r, h, item;
+    TokenRange t;
+    int pos0;              // first cached token of the item
+    int units, a, b;       // query tiles: all of the item's, this CTA's
+    int q0;                // the item's first query tile within the request
+    int skip1;             // units before the second tile of cached tokens is seen
+};
+
+__device__ __forceinline__ bool next_segment(const MassArgs &a, const MassWork &w, const Pieces &p, Cursor &c, Segment &s) {
+    if (piece_done(c, a.B, p)) return false;
+    s.r = c.r, s.h = c.h, s.item = c.item, s.t = c.t;
+    s.pos0 = c.i * 2 * kTile;
+    s.units = w.units(c.t, c.i);
+    s.a = c.unit, s.b = piece_end(c, p, s.units);
+    s.q0 = w.blind(c.t, s.pos0) / w.tpt;
+    s.skip1 = s.pos0 + kTile >= c.t.past + c.t.n ? s.units : w.blind(c.t, s.pos0 + kTile) / w.tpt - s.q0;
+    next_item(w, a.B, a.H_kv, c);
+    return true;
+}
+
+// Page of 16-token group g of the request, -1 if absent, past the end or out of range.
+__device__ __forceinline__ int group_page(const MassArgs &a, const Segment &s, int g, bool report) {
+    if (g * kPage >= s.t.past + s.t.n) return -1;
+    const int pid = a.page_table[(size_t)s.r * a.max_pages + g];
+    if (pid >= a.P_phys) {
+        if (report) atomicOr(a.status, SE_DEV_BAD_PAGE_ID);
+        return -1;
+    }
+    return pid < 0 ? -1 : pid;
+}
+
+template <int D>
+__device__ __forceinline__ void copy_role(const MassArgs &a, const CUtensorMap *q_map, const CUtensorMap *k_map, Control<D> *ctl,
+                                          uint32_t k_smem, uint32_t ring, uint32_t bars, int lane) {
+    using C = Cfg<D>;
+    volatile int *gave_up = &ctl->gave_up;
+    const MassWork work(a);
+    Cursor c = first_piece(work, a.B, ctl->pieces);
+    Segment s;
+    uint32_t pos = 0, pairs = 0;
+    bool ok = true;
+    while (ok && next_segment(a, work, ctl->pieces, c, s)) {
+        // K: 16 groups of 16 tokens; a lane brings a group's 64 channels, D = 128 in two turns.  Absent groups come from behind
+        // the tensor's last row, which reads as zeros.
+        const int pid = group_page(a, s, s.pos0 / kPage + (lane & 15), lane < 16);
+        const uint32_t kb = pairs & 1, kbar = bars + 8 * (kKFull + kb);
+        ok = warp_wait(bars + 8 * (kKEmpty + kb), (pairs >> 1 & 1) ^ 1, gave_up, a.status);
+        if (!ok) break;
+        if (lane == 0) mbar_expect_tx(kbar, 2 * C::kTileBytes);
+        __syncwarp();
+        {
+            const int g = lane & 15, half = lane >> 4;
+            if (half < C::kHalves)
+                tma_load_3d(k_smem + (2 * kb + (g >> 3)) * C::kTileBytes + half * (kTile * 128) + (g & 7) * (kPage * 128), k_map,
+                            half * 64, 0, pid >= 0 ? (pid * a.H_kv + s.h) * kPage : a.P_phys * a.H_kv * kPage, kbar);
+        }
+        ++pairs;
+        for (int u = s.a; u < s.b; ++u, ++pos) {
+            const uint32_t slot = pos % C::kSlots, bar = bars + 8 * (kRing + slot);
+            ok = warp_wait(bar + 8 * C::kSlots, (pos / C::kSlots & 1) ^ 1, gave_up, a.status);
+            if (!ok) break;
+            if (lane == 0) mbar_expect_tx(bar, work.tpt * a.G * D * 2);
+            __syncwarp();
+            if (lane < C::kHalves)
+                tma_load_3d(ring + slot * C::kTileBytes + lane * (kTile * 128), q_map, lane * 64, s.h * a.G,
+                            s.t.start + (s.q0 + u) * work.tpt, bar);
+        }
+    }
+    // no copy may be in flight when the CTA's shared memory goes away
+    if (!ok) {
+        const uint32_t first = pos > C::kSlots ? pos - C::kSlots : 0;
+        for (uint32_t p = first; p < pos; ++p) mbar_wait(bars + 8 * (kRing + p % C::kSlots), p / C::kSlots & 1);
+        for (uint32_t p = pairs > 2 ? pairs - 2 : 0; p < pairs; ++p) mbar_wait(bars + 8 * (kKFull + (p & 1)), p >> 1 & 1);
+    }
+}
+
+// The query tiles' log-sum-exps, a tile ahead in registers.
+template <int D>
+__device__ __forceinline__ void lse_role(const MassArgs &a, Control<D> *ctl, uint32_t bars, int lane) {
+    volatile int *gave_up = &ctl->gave_up;
+    const MassWork work(a);
+    Cursor c = first_piece(work, a.B, ctl->pieces);
+    Segment s;
+    uint32_t tiles = 0;
+    const int live = work.tpt * a.G;
+    while (next_segment(a, work, ctl->pieces, c, s)) {
+        float x[4];
+        auto fetch = [&](int u) {
+            const int tok = (s.q0 + u) * work.tpt;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
-        const float2 f = bf16x2_to_f2(reinterpret_cast<const uint32_t *>(row)[i * 32 + lane]);
-        x[2 * i] = f.x, x[2 * i + 1] = f.y;
+            for (int k = 0; k < 4; ++k) {
+                const int row = lane + 32 * k, q = tok + row / a.G;
+                x[k] = row < live && q < s.t.n ? a.lse[(size_t)(s.t.start + q) * a.H_q + s.h * a.G + row % a.G] : INFINITY;
+            }
+        };
+        fetch(s.a);
+        for (int u = s.a; u < s.b; ++u, ++tiles) {
+            const uint32_t slot = tiles % kLseSlots;
+            if (!warp_wait(bars + 8 * (kLseEmpty + slot), (tiles / kLseSlots & 1) ^ 1, gave_up, a.status)) return;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) ctl->lse[slot][lane + 32 * k] = x[k] == -INFINITY ? -INFINITY : -x[k] * kLog2e;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bars + 8 * (kLseFull + slot));
+            if (u + 1 < s.b) fetch(u + 1);
+        }
     }
 }
 
 template <int D>
-__device__ __forceinline__ float dot(const float (&x)[D / 32], const float (&y)[D / 32]) {
-    float s = 0.f;
+__device__ __forceinline__ void mma_role(const MassArgs &a, Control<D> *ctl, uint32_t k_smem, uint32_t ring, uint32_t bars) {
+    using C = Cfg<D>;
+    volatile int *gave_up = &ctl->gave_up;
+    constexpr uint32_t kInstr = mma_instr(kTile, false);
+    const uint32_t tmem = ctl->tmem;
+    const MassWork work(a);
+    Cursor c = first_piece(work, a.B, ctl->pieces);
+    Segment s;
+    uint32_t pos = 0, pairs = 0, step0 = 0, step1 = 0;
+    bool ok = true, any = false;
+    while (ok && next_segment(a, work, ctl->pieces, c, s)) {
+        const uint32_t kb = pairs & 1;
+        ok = role_wait(bars + 8 * (kKFull + kb), pairs >> 1 & 1, gave_up, a.status);
+        ++pairs;
+        for (int u = s.a; u < s.b && ok; ++u, ++pos) {
+            const uint32_t slot = pos % C::kSlots;
+            ok = role_wait(bars + 8 * (kRing + slot), pos / C::kSlots & 1, gave_up, a.status);
+            const uint64_t qd = smem_operand(ring + slot * C::kTileBytes, 16, 1024);
+            for (int st = 0; st < 2 && ok; ++st) {
+                if (st == 1 && u < s.skip1) continue;
+                const uint32_t step = st ? step1++ : step0++, buf = 2 * st + (step & 1);
+                ok = role_wait(bars + 8 * (kSFree + buf), (step >> 1 & 1) ^ 1, gave_up, a.status);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t kd = smem_operand(k_smem + (2 * kb + st) * C::kTileBytes, 16, 1024);
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) s += x[i] * y[i];
-#pragma unroll
-    for (int m = 16; m; m >>= 1) s += __shfl_xor_sync(kFull, s, m);
-    return s;
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t off = (k / 4) * (kTile * 128 >> 4) + (k % 4) * 2;
+                    mma_ss(tmem + buf * kTile, kd + off, qd + off, kInstr, k > 0);
+                }
+                mma_commit(bars + 8 * (kSFull + buf));
+                any = true;
+            }
+            if (ok) mma_commit(bars + 8 * (kRing + C::kSlots + slot));
+        }
+        if (ok) mma_commit(bars + 8 * (kKEmpty + kb));
+    }
+    if (any) {                           // nothing may be running when tensor memory goes away
+        mma_commit(bars + 8 * kDrain);
+        mbar_wait(bars + 8 * kDrain, 0);
+    }
 }
 
 template <int D>
-__global__ void accumulate_kernel(const SimpleArgs a) {
-    const int lane = threadIdx.x & 31, G = a.H_q / a.H_kv;
-    const long long w = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-    const int h = (int)(w % a.H_kv), j = (int)(w / a.H_kv % (a.max_pages * kPage));
-    const int r = (int)(w / a.H_kv / (a.max_pages * kPage));
-    if (r >= a.B) return;
-    const TokenRange tr = token_range(a.cu, a.seq_lens, r, a.T, a.max_pages * kPage);
-    if (!tr.valid && lane == 0) atomicOr(a.status, SE_DEV_BAD_LENGTH);
-    if (j >= tr.past + tr.n || tr.n == 0) return;
-    const int pid = a.page_table[(size_t)r * a.max_pages + j / kPage];
-    if (pid >= a.P_phys && lane == 0) atomicOr(a.status, SE_DEV_BAD_PAGE_ID);
-    if (pid < 0 || pid >= a.P_phys) return;
-    const size_t slot = ((size_t)pid * a.H_kv + h) * kPage + j % kPage;
-    float k[D / 32], sum = 0.f;
-    load_row<D>(k, a.k + slot * D, lane);
-    for (int i = max(j - tr.past, 0); i < tr.n; ++i)
-        for (int g = 0; g < G; ++g) {
-            const size_t t = tr.start + i;
-            float x[D / 32];
-            load_row<D>(x, a.q + t * a.q_stride + (h * G + g) * D, lane);
-            sum += exp2f(dot<D>(k, x) * a.scale_log2 - a.lse[t * a.H_q + h * G + g] * kLog2e);
+__device__ __forceinline__ void sum_role(const MassArgs &a, Control<D> *ctl, uint32_t bars, int st) {
+    volatile int *gave_up = &ctl->gave_up;
+    const int row = threadIdx.x & 127, lane = threadIdx.x & 31, warp = row >> 5;
+    const uint32_t t_s = ctl->tmem + ((uint32_t)(warp * 32) << 16) + 2 * st * kTile;
+    const float2 sl = make_float2(a.scale_log2, a.scale_log2);
+    const MassWork work(a);
+    Cursor c = first_piece(work, a.B, ctl->pieces);
+    Segment s;
+    uint32_t step = 0, tiles = 0, verdicts = 0;
+    while (next_segment(a, work, ctl->pieces, c, s)) {
+        const int pos = s.pos0 + st * kTile + row;                         // the thread's cached token
+        const int pid = group_page(a, s, pos / kPage, false);
+        float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+        for (int u = s.a; u < s.b; ++u, ++tiles) {
+            const uint32_t slot = tiles % kLseSlots;
+            if (!warp_wait(bars + 8 * (kLseFull + slot), tiles / kLseSlots & 1, gave_up, a.status)) return;
+            if (st == 0 || u >= s.skip1) {
+                const int tok = (s.q0 + u) * work.tpt;                     // the tile's first new token
+                // columns [from, to) count: the queries at or behind the cached token, and of this request
+                const int from = min(max(pos - s.t.past - tok, 0), kTile) * a.G, to = (s.t.n - tok) * a.G;
+                const bool masked = __any_sync(kFull, from > 0) || to < work.tpt * a.G;
+                const uint32_t buf = step & 1;
+                if (!warp_wait(bars + 8 * (kSFull + 2 * st + buf), step >> 1 & 1, gave_up, a.status)) return;
+                ++step;
+                tc_fence_after();
+                const float4 *nl = reinterpret_cast<const float4 *>(ctl->lse[slot]);
+                float x[2][32];
+                tmem_ld32(t_s + buf * kTile, x[0]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    tmem_wait_ld();
+                    settle<32>(x[k & 1]);
+                    if (k < 3) tmem_ld32(t_s + buf * kTile + 32 * (k + 1), x[(k + 1) & 1]);
+                    if (k == 3) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bars + 8 * (kSFree + 2 * st + buf));
+                    }
+                    float *y = x[k & 1];
+                    if (masked) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (32 * k + e < from || 32 * k + e >= to) y[e] = -INFINITY;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        const float4 n = nl[8 * k + e / 4];
+                        const float2 z0 = ffma2(make_float2(y[e], y[e + 1]), sl, make_float2(n.x, n.y));
+                        const float2 z1 = ffma2(make_float2(y[e + 2], y[e + 3]), sl, make_float2(n.z, n.w));
+                        s0 = __fadd2_rn(s0, make_float2(ex2(z0.x), ex2(z0.y)));
+                        s1 = __fadd2_rn(s1, make_float2(ex2(z1.x), ex2(z1.y)));
+                    }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bars + 8 * (kLseEmpty + slot));
         }
-    if (lane == 0) a.accum[slot] += sum;
+        const float sum = (s0.x + s0.y) + (s1.x + s1.y);
+        const size_t at = ((size_t)max(pid, 0) * a.H_kv + s.h) * kPage + pos % kPage;
+        if (s.a == 0 && s.b == s.units) {
+            // the only addition to this token in this call
+            if (pid >= 0 && pos < s.t.past + s.t.n) a.accum[at] += sum;
+            continue;
+        }
+        auto part = [&](int cta, int kind) { return a.partials + (size_t)((cta * 2 + kind) * 2 + st) * kTile + row; };
+        __stcg(part(blockIdx.x, s.a == 0), sum);
+        const int from = first_cta(ctl->pieces, s.item);
+        __threadfence();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bars + 8 * (kAll + st));
+        if (warp == 0) {
+            if (!warp_wait(bars + 8 * (kAll + st), verdicts & 1, gave_up, a.status)) return;
+            if (lane == 0) {
+                __threadfence();
+                uint32_t *ticket = a.tickets + 2 * from + st;
+                const uint32_t add = s.b - s.a;
+                const bool last = atomicAdd(ticket, add) + add == (uint32_t)s.units;
+                if (last) atomicExch(ticket, 0u);
+                ctl->last[st] = last;
+                mbar_arrive(bars + 8 * (kVerdict + st));
+            }
+            __syncwarp();
+        }
+        if (!warp_wait(bars + 8 * (kVerdict + st), verdicts & 1, gave_up, a.status)) return;
+        ++verdicts;
+        if (ctl->last[st]) {
+            __threadfence();
+            float all = 0.f;
+            each_cta(ctl->pieces, s.item, s.units, from, [&](int y, int ya, int) { all += __ldcg(part(y, ya == 0)); });
+            if (pid >= 0 && pos < s.t.past + s.t.n) a.accum[at] += all;
+        }
+    }
 }
 
-SimpleArgs simple_args(const se_params &p, const AttendCall &c) {
-    SimpleArgs a = {};
-    a.q = (const uint16_t *)c.q, a.k = (const uint16_t *)c.k, a.v = (const uint16_t *)c.v;
-    a.q_stride = c.q_stride, a.k_stride = c.k_stride, a.v_stride = c.v_stride;
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+mass_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ MassArgs a) {
+    using C = Cfg<D>;
+    constexpr int kTiles = 2 * C::kPairs + C::kSlots;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const uint32_t base = smem_u32(smem);
+    Control<D> *ctl = reinterpret_cast<Control<D> *>(smem + kTiles * C::kTileBytes);
+    const uint32_t bars = smem_u32(ctl->bars), ring = base + 2 * C::kPairs * C::kTileBytes;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (base & 1023u) {                  // the swizzle pattern hangs on the address
+        if (threadIdx.x == 0) atomicOr(a.status, SE_DEV_WAIT_TIMEOUT);
+        return;
+    }
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(bars + 8 * (kSFull + i), 1);
+            mbar_init(bars + 8 * (kSFree + i), 4);
+        }
+        for (int i = 0; i < kLseSlots; ++i) {
+            mbar_init(bars + 8 * (kLseFull + i), 1);
+            mbar_init(bars + 8 * (kLseEmpty + i), 8);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bars + 8 * (kKFull + i), 1);
+            mbar_init(bars + 8 * (kKEmpty + i), 1);
+            mbar_init(bars + 8 * (kAll + i), 4);
+            mbar_init(bars + 8 * (kVerdict + i), 1);
+        }
+        mbar_init(bars + 8 * kDrain, 1);
+        for (int i = 0; i < 2 * C::kSlots; ++i) mbar_init(bars + 8 * (kRing + i), 1);
+        mbar_fence_init();
+        ctl->gave_up = 0;
+    }
+    if (warp == kMmaWarp) tmem_alloc(smem_u32(&ctl->tmem), 512);
+    static_assert(kPieceScratch <= kTiles * C::kTileBytes, "the tiles' memory holds the prefix sums first");
+    cut_work(MassWork(a), a.B, a.H_kv, a.status, &ctl->pieces, smem);
+    __syncthreads();
+    // query rows that no tensor copy fills (G does not divide 128) stay zero
+    for (int i = threadIdx.x; i < C::kSlots * C::kTileBytes / 16; i += kThreads)
+        reinterpret_cast<uint4 *>(smem + 2 * C::kPairs * C::kTileBytes)[i] = make_uint4(0, 0, 0, 0);
+    fence_async_proxy();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+
+    if (warp < 8) sum_role<D>(a, ctl, bars, warp >> 2);
+    else if (warp == kCopyWarp) copy_role<D>(a, &q_map, &k_map, ctl, base, ring, bars, lane);
+    else if (warp == kLseWarp) lse_role<D>(a, ctl, bars, lane);
+    else if (warp == kMmaWarp && lane == 0) mma_role<D>(a, ctl, base, ring, bars);
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        tmem_free(ctl->tmem, 512);
+    }
+}
+
+template <int D>
+cudaError_t launch_mass(const se_params &p, const AttendCall &c, float *score_accum, cudaStream_t stream) {
+    using C = Cfg<D>;
+    const int G = p.H_q / p.H_kv;
+    CUtensorMap q_map, k_map;
+    if (!make_rows_map(&q_map, c.q, D, p.H_q, c.total_tokens, c.q_stride, G, kTile / G) ||
+        !make_rows_map(&k_map, c.k, D, 1, (long long)p.num_phys_pages * p.H_kv * kPage, D, 1, kPage))
+        return cudaErrorInvalidValue;
+    MassArgs a = {};
     a.cu = c.cu_seqlens, a.seq_lens = c.seq_lens, a.page_table = c.page_table;
-    a.out = (uint16_t *)c.out, a.lse = c.lse, a.status = (uint32_t *)c.workspace;
-    a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.T = c.total_tokens, a.max_pages = p.max_pages;
+    a.lse = c.lse, a.accum = score_accum;
+    a.status = reinterpret_cast<uint32_t *>(c.workspace), a.tickets = reinterpret_cast<uint32_t *>(c.workspace + 256);
+    a.partials = reinterpret_cast<float *>(c.workspace + kControlBytes);
+    a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.G = G, a.T = c.total_tokens, a.max_pages = p.max_pages;
     a.P_phys = p.num_phys_pages, a.scale_log2 = effective_scale(p) * kLog2e;
-    return a;
+    const size_t smem = (2 * C::kPairs + C::kSlots) * C::kTileBytes + sizeof(Control<D>);
+    auto kern = mass_kernel<D>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    kern<<<kPromptCtas, kThreads, smem, stream>>>(q_map, k_map, a);
+    return cudaGetLastError();
 }
 
 }  // namespace
 
 cudaError_t launch_h2o_accumulate(const se_params &p, const AttendCall &c, float *score_accum, cudaStream_t stream) {
-    SimpleArgs a = simple_args(p, c);
-    a.accum = score_accum;
-    const unsigned grid = (unsigned)(((long long)p.B * p.max_pages * kPage * p.H_kv + 7) / 8);
-    if (p.D == 128) accumulate_kernel<128><<<grid, 256, 0, stream>>>(a);
-    else accumulate_kernel<64><<<grid, 256, 0, stream>>>(a);
-    return cudaGetLastError();
+    return p.D == 128 ? launch_mass<128>(p, c, score_accum, stream) : launch_mass<64>(p, c, score_accum, stream);
 }
 
 }  // namespace se
