@@ -61,6 +61,11 @@ struct AttendArgs {
     float scale_log2;
 };
 
+template <int ST>
+struct Stream {
+    static constexpr int value = ST;
+};
+
 enum Bar { kQFull, kQEmpty, kSFull, kPReady = kSFull + 2, kODone = kPReady + 2, kOFree = kODone + 2, kAll = kOFree + 2, kVerdict = kAll + 2, kSwap = kVerdict + 2,
            kDrain, kRing };
 
@@ -114,7 +119,7 @@ struct Segment {
 
 // This CTA's next piece; every role walks the same list.
 __device__ __forceinline__ bool next_segment(const AttendArgs &a, const AttendWork &w, const Pieces &p, Cursor &c, Segment &s) {
-    if (piece_done(c, a.B, p)) return false;
+    if (piece_done(w, a.B, p, c)) return false;
     s.r = c.r, s.h = c.h, s.item = c.item, s.t = c.t;
     s.tok0 = c.i * 2 * w.tpt;
     s.ntok = w.new_tokens(c.t, c.i);
@@ -139,8 +144,16 @@ __device__ __forceinline__ bool next_segment(const AttendArgs &a, const AttendWo
 // are absent or past the end come from behind the tensor's last row, which reads as zeros.  With `by_hand` (V) the group
 // that holds the end of the request is copied row by row, so that what lies behind the end, which may be anything, is zero.
 template <int D>
-__device__ __forceinline__ void load_tile(const AttendArgs &a, const CUtensorMap *map, const Segment &s, int tile, int pid, int end,
+__device__ __forceinline__ void load_tile(const AttendArgs &a, const CUtensorMap *map, const CUtensorMap *wide, const Segment &s, int tile, int pid, int end,
                                           bool by_hand, uint32_t slot, uint32_t bar, int lane) {
+    using C = Cfg<D>;
+    if (!a.page_table && (tile + 1) * kTile <= end) {
+        if (lane == 0) mbar_expect_tx(bar, C::kTileBytes);
+        __syncwarp();
+        if (lane < C::kHalves)
+            tma_load_3d(slot + lane * (kTile * 128), wide, lane * 64, s.h, s.t.start + tile * kTile, bar);
+        return;
+    }
     const int pg = lane & 7, half = lane >> 3;
     const int tok = tile * kTile + pg * kPage;                             // the group's first token
     const bool part = by_hand && pid >= 0 && tok < end && end - tok < kPage;
@@ -193,13 +206,14 @@ __device__ __forceinline__ int group_page(const AttendArgs &a, const Segment &s,
 
 template <int D>
 __device__ __forceinline__ void copy_role(const AttendArgs &a, const CUtensorMap *q_map, const CUtensorMap *k_map,
-                                          const CUtensorMap *v_map, Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars,
+                                          const CUtensorMap *v_map, const CUtensorMap *k_wide, const CUtensorMap *v_wide,
+                                          Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars,
                                           int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     const int tpt = kTile / a.G;
     const AttendWork work(a);
-    Cursor c = first_piece(work, a.B, ctl->pieces);
+    Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
     Segment s;
     uint32_t pos = 0, tiles = 0, pieces = 0;
     bool ok = true;
@@ -226,7 +240,7 @@ __device__ __forceinline__ void copy_role(const AttendArgs &a, const CUtensorMap
                 const uint32_t slot = pos % C::kSlots, bar = bars + 8 * (kRing + slot);
                 ok = warp_wait(bar + 8 * C::kSlots, (pos / C::kSlots & 1) ^ 1, gave_up, a.status);
                 if (!ok) break;
-                load_tile<D>(a, kv ? v_map : k_map, s, t, pid, stop, kv == 1, ring + slot * C::kTileBytes, bar, lane);
+                load_tile<D>(a, kv ? v_map : k_map, kv ? v_wide : k_wide, s, t, pid, stop, kv == 1, ring + slot * C::kTileBytes, bar, lane);
             }
             if (!ok) break;
             pid = next_pid;
@@ -241,72 +255,112 @@ __device__ __forceinline__ void copy_role(const AttendArgs &a, const CUtensorMap
 }
 
 // ---- products ----------------------------------------------------------------------
+// The whole warp walks the list, so that addresses stay in uniform registers; one elected lane issues (a role run by a
+// single lane took 82 cycles per instruction to issue, more than the 64 that it computes).
+template <int D, int ST>
+struct Products {
+    using C = Cfg<D>;
+    // S[ST] = Q K^T
+    static __device__ __forceinline__ void scores(uint32_t tmem, uint32_t q, uint32_t k, uint32_t bars, int release) {
+        const uint64_t qd = smem_operand(q, 16, 1024), kd = smem_operand(k, 16, 1024);
+        if (elect_one()) {
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                const uint32_t off = (i / 4) * (kTile * 128 >> 4) + (i % 4) * 2;
+                mma_ss(tmem + ST * kTile, qd + off, kd + off, mma_instr(kTile, false), i > 0);
+            }
+            mma_commit(bars + 8 * (kSFull + ST));
+            if (release >= 0) mma_commit(bars + 8 * release);
+        }
+    }
+    // O[ST] += P V
+    static __device__ __forceinline__ void values(uint32_t tmem, uint32_t v, bool accumulate, uint32_t bars, int release) {
+        const uint64_t vd = smem_operand(v, kTile * 128, 1024);
+        if (elect_one()) {
+#pragma unroll
+            for (int i = 0; i < kTile / 16; ++i)
+                mma_ts(tmem + C::kTmemO + ST * D, tmem + ST * kTile + i * 8, vd + i * (16 * 128 >> 4), mma_instr(D, true),
+                       accumulate || i > 0);
+            mma_commit(bars + 8 * (kODone + ST));
+            if (release >= 0) mma_commit(bars + 8 * release);
+        }
+    }
+};
+
 template <int D>
 __device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
-    constexpr uint32_t kInstrS = mma_instr(kTile, false), kInstrO = mma_instr(D, true);
     const uint32_t tmem = ctl->tmem;
     const AttendWork work(a);
-    Cursor c = first_piece(work, a.B, ctl->pieces);
+    Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
     Segment s;
-    uint32_t pos = 0, pieces = 0, p_seen = 0, o_used = 0;      // bit st: parity of the stream's next wait
-    bool ok = true, any = false;
-    while (ok && next_segment(a, work, ctl->pieces, c, s)) {
+    uint32_t pos = 0, pieces = 0, p_seen = 0, o_used = 0;                  // bit st: parity of the stream's next wait
+    bool any = false;
+    auto wait = [&](int bar, uint32_t parity) { return warp_wait(bars + 8 * bar, parity & 1, gave_up, a.status); };
+    // K and V tiles are waited for in order: `k_next`, `v_next` are the first ring positions not waited for yet
+    uint32_t k_next = 0, v_next = 1;
+    auto wait_k = [&](uint32_t at) {
+        for (; k_next <= at; k_next += 2)
+            if (!wait(kRing + k_next % C::kSlots, k_next / C::kSlots)) return false;
+        return true;
+    };
+    auto wait_v = [&](uint32_t at) {
+        for (; v_next <= at; v_next += 2)
+            if (!wait(kRing + v_next % C::kSlots, v_next / C::kSlots)) return false;
+        return true;
+    };
+    while (next_segment(a, work, ctl->pieces, c, s)) {
         const int steps = max(s.steps0, s.steps1);
+        const uint32_t q1 = q_smem + (s.alt ? 0 : C::kTileBytes);
         // ring position of the K tile of step i of stream st; its V tile follows
         auto place = [&](int st, int i) { return pos + 2u * (s.alt ? 2 * i + st : i); };
-        auto scores = [&](int st, int i) {
-            const uint32_t at = place(st, i), slot = at % C::kSlots;
-            if (!role_wait(bars + 8 * (kRing + slot), at / C::kSlots & 1, gave_up, a.status)) return false;
-            tc_fence_after();
-            const uint64_t qd = smem_operand(q_smem + (s.alt ? 0 : st) * C::kTileBytes, 16, 1024);
-            const uint64_t kd = smem_operand(ring + slot * C::kTileBytes, 16, 1024);
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                const uint32_t off = (k / 4) * (kTile * 128 >> 4) + (k % 4) * 2;
-                mma_ss(tmem + st * kTile, qd + off, kd + off, kInstrS, k > 0);
-            }
-            mma_commit(bars + 8 * (kSFull + st));
-            if (s.alt || st == 1) mma_commit(bars + 8 * (kRing + C::kSlots + slot));
-            any = true;
-            return true;
-        };
-        auto values = [&](int st, int i) {
-            const uint32_t at = place(st, i) + 1, slot = at % C::kSlots;
-            if (!role_wait(bars + 8 * (kRing + slot), at / C::kSlots & 1, gave_up, a.status)) return false;
+        auto slot = [&](uint32_t at) { return ring + at % C::kSlots * C::kTileBytes; };
+        auto release = [&](int st, uint32_t at) { return s.alt || st == 1 ? (int)(kRing + C::kSlots + at % C::kSlots) : -1; };
+        // a step: everything that can be waited for early comes before the wait for the weights
+        auto step = [&](auto stream, int i) {
+            constexpr int ST = decltype(stream)::value;
+            const int mine = ST ? s.steps1 : s.steps0;
+            if (i >= mine) return true;
+            const bool more = i + 1 < mine;
+            const uint32_t at = place(ST, i), next = place(ST, i + 1);
+            if (!wait_v(at + 1) || (more && !wait_k(next))) return false;
             if (i == 0) {                // the epilogue of the stream's last piece has read O
-                if (!role_wait(bars + 8 * (kOFree + st), (o_used >> st & 1) ^ 1, gave_up, a.status)) return false;
-                o_used ^= 1u << st;
+                if (!wait(kOFree + ST, (o_used >> ST & 1) ^ 1)) return false;
+                o_used ^= 1u << ST;
             }
-            if (!role_wait(bars + 8 * (kPReady + st), p_seen >> st & 1, gave_up, a.status)) return false;
-            p_seen ^= 1u << st;
+            if (!wait(kPReady + ST, p_seen >> ST)) return false;
+            p_seen ^= 1u << ST;
             tc_fence_after();
-            const uint64_t vd = smem_operand(ring + slot * C::kTileBytes, kTile * 128, 1024);
-#pragma unroll
-            for (int k = 0; k < kTile / 16; ++k)
-                mma_ts(tmem + C::kTmemO + st * D, tmem + st * kTile + k * 8, vd + k * (16 * 128 >> 4), kInstrO, i > 0 || k > 0);
-            mma_commit(bars + 8 * (kODone + st));
-            if (s.alt || st == 1) mma_commit(bars + 8 * (kRing + C::kSlots + slot));
+            Products<D, ST>::values(tmem, slot(at + 1), i > 0, bars, release(ST, at + 1));
+            if (more) Products<D, ST>::scores(tmem, ST ? q1 : q_smem, slot(next), bars, release(ST, next));
             return true;
         };
-        if (!role_wait(bars + 8 * kQFull, pieces & 1, gave_up, a.status)) break;
+        if (!wait(kQFull, pieces)) break;
         ++pieces;
-        for (int st = 0; st < 2 && ok; ++st)
-            if (s.steps(st) > 0) ok = scores(st, 0);
-        if (ok && steps == 1) mma_commit(bars + 8 * kQEmpty);
-        for (int i = 0; i < steps && ok; ++i) {
-            for (int st = 0; st < 2 && ok; ++st) {
-                if (i >= s.steps(st)) continue;
-                ok = values(st, i);
-                if (ok && i + 1 < s.steps(st)) ok = scores(st, i + 1);
-            }
-            if (ok && i + 2 == steps) mma_commit(bars + 8 * kQEmpty);       // the last product with Q is on its way
+        any = true;
+        if (s.steps0 > 0) {
+            if (!wait_k(place(0, 0))) break;
+            tc_fence_after();
+            Products<D, 0>::scores(tmem, q_smem, slot(place(0, 0)), bars, release(0, place(0, 0)));
         }
+        if (s.steps1 > 0) {
+            if (!wait_k(place(1, 0))) break;
+            tc_fence_after();
+            Products<D, 1>::scores(tmem, q1, slot(place(1, 0)), bars, release(1, place(1, 0)));
+        }
+        if (steps == 1 && elect_one()) mma_commit(bars + 8 * kQEmpty);
+        bool ok = true;
+        for (int i = 0; i < steps && ok; ++i) {
+            ok = step(Stream<0>{}, i) && step(Stream<1>{}, i);
+            if (i + 2 == steps && elect_one()) mma_commit(bars + 8 * kQEmpty);   // the last product with Q is on its way
+        }
+        if (!ok) break;
         pos += 2u * (s.b - s.a);
     }
     if (any) {                           // nothing may be running when tensor memory goes away
-        mma_commit(bars + 8 * kDrain);
+        if (elect_one()) mma_commit(bars + 8 * kDrain);
+        __syncwarp();
         mbar_wait(bars + 8 * kDrain, 0);
     }
 }
@@ -392,7 +446,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
     const uint32_t t_s = ctl->tmem + lanes + st * kTile, t_o = ctl->tmem + lanes + C::kTmemO + st * D;
     const float sl = a.scale_log2;
     const AttendWork work(a);
-    Cursor c = first_piece(work, a.B, ctl->pieces);
+    Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
     Segment s;
     uint32_t step = 0, tiles = 0, verdicts = 0, swaps = 0;
     // both warpgroups have come here
@@ -579,7 +633,8 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
-              const __grid_constant__ CUtensorMap v_map, const __grid_constant__ AttendArgs a) {
+              const __grid_constant__ CUtensorMap v_map, const __grid_constant__ CUtensorMap k_wide,
+              const __grid_constant__ CUtensorMap v_wide, const __grid_constant__ AttendArgs a) {
     using C = Cfg<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t base = smem_u32(smem);
@@ -623,8 +678,8 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
         softmax_role<D>(a, ctl, bars, warp >> 2);
     } else {
         regs_down<kRegsOther>();
-        if (warp == kCopyWarp) copy_role<D>(a, &q_map, &k_map, &v_map, ctl, base, base + 2 * C::kTileBytes, bars, lane);
-        else if (warp == kMmaWarp && lane == 0) mma_role<D>(a, ctl, base, base + 2 * C::kTileBytes, bars);
+        if (warp == kCopyWarp) copy_role<D>(a, &q_map, &k_map, &v_map, &k_wide, &v_wide, ctl, base, base + 2 * C::kTileBytes, bars, lane);
+        else if (warp == kMmaWarp) mma_role<D>(a, ctl, base, base + 2 * C::kTileBytes, bars);
         __syncwarp();
     }
     tc_fence_before();
@@ -640,14 +695,17 @@ template <int D>
 cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t stream) {
     using C = Cfg<D>;
     const int G = p.H_q / p.H_kv;
-    CUtensorMap q_map, k_map, v_map;
+    CUtensorMap q_map, k_map, v_map, k_wide, v_wide;
     bool ok = make_rows_map(&q_map, c.q, D, p.H_q, c.total_tokens, c.q_stride, G, kTile / G);
     if (c.page_table) {
         const long long rows = (long long)p.num_phys_pages * p.H_kv * kPage;
         ok = ok && make_rows_map(&k_map, c.k, D, 1, rows, D, 1, kPage) && make_rows_map(&v_map, c.v, D, 1, rows, D, 1, kPage);
+        k_wide = k_map, v_wide = v_map;                      // not used
     } else {
         ok = ok && make_rows_map(&k_map, c.k, D, p.H_kv, c.total_tokens, c.k_stride, 1, kPage) &&
-             make_rows_map(&v_map, c.v, D, p.H_kv, c.total_tokens, c.v_stride, 1, kPage);
+             make_rows_map(&v_map, c.v, D, p.H_kv, c.total_tokens, c.v_stride, 1, kPage) &&
+             make_rows_map(&k_wide, c.k, D, p.H_kv, c.total_tokens, c.k_stride, 1, kTile) &&
+             make_rows_map(&v_wide, c.v, D, p.H_kv, c.total_tokens, c.v_stride, 1, kTile);
     }
     if (!ok) return cudaErrorInvalidValue;
     AttendArgs a = {};
@@ -667,7 +725,7 @@ cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t 
     const size_t smem = (2 + C::kSlots) * C::kTileBytes + sizeof(Control<D>);
     e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    kern<<<kPromptCtas, kThreads, smem, stream>>>(q_map, k_map, v_map, a);
+    kern<<<kPromptCtas, kThreads, smem, stream>>>(q_map, k_map, v_map, k_wide, v_wide, a);
     return cudaGetLastError();
 }
 

@@ -94,7 +94,7 @@ struct Segment {
 };
 
 __device__ __forceinline__ bool next_segment(const MassArgs &a, const MassWork &w, const Pieces &p, Cursor &c, Segment &s) {
-    if (piece_done(c, a.B, p)) return false;
+    if (piece_done(w, a.B, p, c)) return false;
     s.r = c.r, s.h = c.h, s.item = c.item, s.t = c.t;
     s.pos0 = c.i * 2 * kTile;
     s.units = w.units(c.t, c.i);
@@ -122,7 +122,7 @@ __device__ __forceinline__ void copy_role(const MassArgs &a, const CUtensorMap *
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     const MassWork work(a);
-    Cursor c = first_piece(work, a.B, ctl->pieces);
+    Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
     Segment s;
     uint32_t pos = 0, pairs = 0;
     bool ok = true;
@@ -166,7 +166,7 @@ template <int D>
 __device__ __forceinline__ void lse_role(const MassArgs &a, Control<D> *ctl, uint32_t bars, int lane) {
     volatile int *gave_up = &ctl->gave_up;
     const MassWork work(a);
-    Cursor c = first_piece(work, a.B, ctl->pieces);
+    Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
     Segment s;
     uint32_t tiles = 0;
     const int live = work.tpt * a.G;
@@ -200,7 +200,7 @@ __device__ __forceinline__ void mma_role(const MassArgs &a, Control<D> *ctl, uin
     constexpr uint32_t kInstr = mma_instr(kTile, false);
     const uint32_t tmem = ctl->tmem;
     const MassWork work(a);
-    Cursor c = first_piece(work, a.B, ctl->pieces);
+    Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
     Segment s;
     uint32_t pos = 0, pairs = 0, step0 = 0, step1 = 0;
     bool ok = true, any = false;
@@ -244,7 +244,7 @@ __device__ __forceinline__ void sum_role(const MassArgs &a, Control<D> *ctl, uin
     const uint32_t t_s = ctl->tmem + ((uint32_t)(warp * 32) << 16) + 2 * st * kTile;
     const float2 sl = make_float2(a.scale_log2, a.scale_log2);
     const MassWork work(a);
-    Cursor c = first_piece(work, a.B, ctl->pieces);
+    Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
     Segment s;
     uint32_t step = 0, tiles = 0, verdicts = 0;
     while (next_segment(a, work, ctl->pieces, c, s)) {

@@ -28,10 +28,14 @@ struct Pieces {
     int begin[3];                                       // request, kv-head, index of this CTA's first item (request B: none)
 };
 
-// A walk over this CTA's items; every role of the CTA does it for itself.
+// A walk over this CTA's items; every role of the CTA does it for itself.  An item that an earlier CTA began comes last:
+// whole items and the item that a later CTA ends are walked from their first unit, and what is left of the first item then
+// falls on the units that the neighbours are at, so CTAs that share a head read the same tiles at about the same time
+// and all but one of them find the tile in L2.
 struct Cursor {
     int r, h, i, unit, item;
     TokenRange t;
+    int late;              // 0: no item to come back to, 1: still to come, 2: being done
 };
 
 // scratch: kPieceScratch bytes of shared memory (up to 8193 x 12 of prefix sums); all threads; ends without a barrier.
@@ -125,23 +129,18 @@ __device__ __forceinline__ void cut_work(const Work &w, int B, int H_kv, uint32_
     if (tid == (int)blockIdx.x) out->begin[0] = r, out->begin[1] = h, out->begin[2] = i;
 }
 
+// Where this CTA's part of the cursor's item ends.
+__device__ __forceinline__ int piece_end(const Cursor &c, const Pieces &p, int units) {
+    return c.item == p.item[blockIdx.x + 1] ? min(p.unit[blockIdx.x + 1], units) : units;
+}
 template <class Work>
-__device__ __forceinline__ Cursor first_piece(const Work &w, int B, const Pieces &p) {
+__device__ __forceinline__ Cursor piece_begin(const Work &w, int B, const Pieces &p) {
     Cursor c;
     c.r = p.begin[0], c.h = p.begin[1], c.i = p.begin[2];
     c.item = p.item[blockIdx.x], c.unit = p.unit[blockIdx.x];
     c.t = TokenRange{0, 0, 0, false};
     if (c.r < B) c.t = w.tokens(c.r);
     return c;
-}
-
-// Where this CTA's part of the cursor's item ends.
-__device__ __forceinline__ int piece_end(const Cursor &c, const Pieces &p, int units) {
-    return c.item == p.item[blockIdx.x + 1] ? min(p.unit[blockIdx.x + 1], units) : units;
-}
-__device__ __forceinline__ bool piece_done(const Cursor &c, int B, const Pieces &p) {
-    const int e_item = p.item[blockIdx.x + 1], e_unit = p.unit[blockIdx.x + 1];
-    return c.r >= B || c.item > e_item || (c.item == e_item && c.unit >= e_unit);
 }
 template <class Work>
 __device__ __forceinline__ void next_item(const Work &w, int B, int H_kv, Cursor &c) {
@@ -154,6 +153,23 @@ __device__ __forceinline__ void next_item(const Work &w, int B, int H_kv, Cursor
     do {
         if (++c.r < B) c.t = w.tokens(c.r);
     } while (c.r < B && c.t.n == 0);
+}
+template <class Work>
+__device__ __forceinline__ Cursor first_piece(const Work &w, int B, int H_kv, const Pieces &p) {
+    Cursor c = piece_begin(w, B, p);
+    c.late = c.r < B && c.unit > 0 && c.item < p.item[blockIdx.x + 1];
+    if (c.late) next_item(w, B, H_kv, c);
+    return c;
+}
+// Nothing left; moves on to the item that was left for the end.
+template <class Work>
+__device__ __forceinline__ bool piece_done(const Work &w, int B, const Pieces &p, Cursor &c) {
+    const int e_item = p.item[blockIdx.x + 1], e_unit = p.unit[blockIdx.x + 1];
+    if (c.late < 2 && c.r < B && (c.item < e_item || (c.item == e_item && c.unit < e_unit))) return false;
+    if (c.late != 1) return true;
+    c = piece_begin(w, B, p);
+    c.late = 2;
+    return false;
 }
 
 // The CTAs that share an item: the first one, and for each its units.
