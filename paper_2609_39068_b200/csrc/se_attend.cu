@@ -2,14 +2,14 @@
 // cache or over contiguous K and V.
 //
 // Mathematics.  A query tile is 128 rows = 128/G tokens x the G query heads of one kv-head, so the heads of a group share
-// every K and V tile.  Over the KV tiles j of 128 tokens:  S = Q K_j^T,  p = 2^(S sl - m)  with sl = sm_scale log2 e,
+// every K and V tile.  Over the KV tiles j of 64 tokens:  S = Q K_j^T,  p = 2^(S sl - m)  with sl = sm_scale log2 e,
 // O += P V_j, l += rowsum p;  out = O / l,  lse = (m + log2 l) ln 2.  m is a row maximum that is moved (and O, l
-// rescaled) only when the tile's maximum exceeds it by more than 8, so p <= 2^8 and most tiles leave O alone.
+// rescaled) only when the scores exceed it by more than 40, so nearly all steps leave O alone.
 //
 // What bounds it.  Per (128 rows x 128 tokens) at D = 128 the two products take 1024 cycles of the tensor cores and
 // the 16384 exponentials 1024 cycles of the special-function units: both have to run all the time.  So a CTA (one per
-// SM, persistent) works on two streams of tiles: two warpgroups do the softmax of one stream each, one thread issues all
-// products, one warp all copies.  S (fp32), P (bf16, in S's columns) and O (fp32) live in tensor memory: 2 x (128 + D)
+// SM, persistent) works on two streams of tiles: two warpgroups do the softmax of one stream each, two warps issue a
+// stream's products each, two warps copy.  S (fp32), P (bf16, in S's columns) and O (fp32) live in tensor memory: 2 x (128 + D)
 // of 512 columns.
 //   pair   more than 128 query rows left: the streams are two neighbouring query tiles, K and V tiles are shared
 //   alt    up to 128 rows (decode tokens, short chunks, ends of prompts): both streams are the same query tile, one
@@ -30,20 +30,23 @@ namespace se {
 
 namespace {
 
-constexpr int kThreads = kPromptThreads;   // 2 softmax warpgroups, copy warp, product warp, 2 idle warps
-constexpr int kCopyWarp = 8, kMmaWarp = 9;
-constexpr int kRegsSoftmax = 208, kRegsOther = 88;   // 256 * 208 + 128 * 88 = 384 * 168
-constexpr int kTile = 128;             // query rows of a tile, tokens of a KV tile
+constexpr int kThreads = kPromptThreads;   // 2 softmax warpgroups, K warp, 2 product warps, V warp
+constexpr int kKWarp = 8, kMmaWarp = 9, kVWarp = 11;
+constexpr int kTile = 128;             // query rows of a tile
+constexpr int kKv = 64;                // tokens of a KV tile
 constexpr int kControlBytes = 2048;    // status word, tickets
 constexpr int kItemCost = 128;         // cost of starting a query tile, in tokens
-constexpr int kMinCost = 4 * kTile;    // a CTA takes at least two shared KV tiles
-constexpr float kSlack = 8.f;          // the running maximum may lag by 2^8
+constexpr int kMinCost = 512;          // a CTA takes at least 256 tokens of a pair, 512 of a single tile
+// The running maximum may lag: weights up to 2^40 lose nothing (bf16 and fp32 keep their exponents, and 2^40 * 131072
+// tokens is far from the end of the range).
+constexpr float kSlack = 40.f;
 
 template <int D>
 struct Cfg {
     static constexpr int kHalves = D / 64;
-    static constexpr int kTileBytes = kTile * D * 2;
-    static constexpr int kSlots = 5 * 128 / D;                    // ring of K and V tiles, 160 KB
+    static constexpr int kTileBytes = kTile * D * 2;              // query tile
+    static constexpr int kKvBytes = kKv * D * 2;                  // K or V tile
+    static constexpr int kSlots = 10 * 128 / D;                   // ring of K and V tiles, 160 KB
     static constexpr int kMasks = 16;
     static constexpr int kSlotFloats = kTile * D + 2 * kTile;     // a partial result: O, m, l
     static constexpr int kTmemO = 256;                            // S0, S1 at columns 0, 128; O0, O1 behind
@@ -61,13 +64,8 @@ struct AttendArgs {
     float scale_log2;
 };
 
-template <int ST>
-struct Stream {
-    static constexpr int value = ST;
-};
-
-enum Bar { kQFull, kQEmpty, kSFull, kPReady = kSFull + 2, kODone = kPReady + 2, kOFree = kODone + 2, kAll = kOFree + 2, kVerdict = kAll + 2, kSwap = kVerdict + 2,
-           kDrain, kRing };
+enum Bar { kQFull, kQEmpty, kSFull, kPReady = kSFull + 4, kODone = kPReady + 4, kOLast = kODone + 2, kOFree = kOLast + 2, kAll = kOFree + 2, kVerdict = kAll + 2, kSwap = kVerdict + 2,
+           kDrain, kRing = kDrain + 2 };
 
 template <int D>
 struct Control {
@@ -99,12 +97,13 @@ struct AttendWork {
         return c;
     }
     __device__ __forceinline__ int units(const TokenRange &t, int i) const {
-        return (t.past + i * 2 * tpt + new_tokens(t, i) + kTile - 1) / kTile;
+        return (t.past + i * 2 * tpt + new_tokens(t, i) + kKv - 1) / kKv;
     }
     __device__ __forceinline__ int unit_at(const TokenRange &t, int i, long long z) const {
-        return (int)(z / (kTile * (new_tokens(t, i) > tpt ? 2 : 1)));
+        return (int)(z / (kKv * (new_tokens(t, i) > tpt ? 2 : 1)));
     }
     __device__ __forceinline__ long long min_cost() const { return kMinCost; }
+    static constexpr int kCrumb = 4;   // least units of a part of an item
 };
 
 struct Segment {
@@ -113,7 +112,7 @@ struct Segment {
     int tok0, ntok;        // new tokens of the item, relative to the request
     bool alt;
     int a, b, nkv;         // KV tiles of this piece, of the item
-    int steps0, steps1;    // per stream
+    int steps0, steps1;    // KV tiles per stream
     __device__ __forceinline__ int steps(int st) const { return st ? steps1 : steps0; }
 };
 
@@ -131,7 +130,7 @@ __device__ __forceinline__ bool next_segment(const AttendArgs &a, const AttendWo
         s.steps0 = (s.b - s.a + 1) / 2;
         s.steps1 = (s.b - s.a) / 2;
     } else {
-        const int n0 = (c.t.past + s.tok0 + w.tpt + kTile - 1) / kTile;    // the first tile's tokens see no more than this
+        const int n0 = (c.t.past + s.tok0 + w.tpt + kKv - 1) / kKv;        // the first tile's tokens see no more than this
         s.steps0 = max(min(s.b, n0) - s.a, 0);
         s.steps1 = s.b - s.a;
     }
@@ -140,228 +139,267 @@ __device__ __forceinline__ bool next_segment(const AttendArgs &a, const AttendWo
 }
 
 // ---- copies ------------------------------------------------------------------------
-// One K or V tile (128 tokens of one head) into a ring slot, by a warp.  A lane brings 16 tokens x 64 channels; groups that
-// are absent or past the end come from behind the tensor's last row, which reads as zeros.  With `by_hand` (V) the group
-// that holds the end of the request is copied row by row, so that what lies behind the end, which may be anything, is zero.
-template <int D>
-__device__ __forceinline__ void load_tile(const AttendArgs &a, const CUtensorMap *map, const CUtensorMap *wide, const Segment &s, int tile, int pid, int end,
-                                          bool by_hand, uint32_t slot, uint32_t bar, int lane) {
-    using C = Cfg<D>;
-    if (!a.page_table && (tile + 1) * kTile <= end) {
-        if (lane == 0) mbar_expect_tx(bar, C::kTileBytes);
-        __syncwarp();
-        if (lane < C::kHalves)
-            tma_load_3d(slot + lane * (kTile * 128), wide, lane * 64, s.h, s.t.start + tile * kTile, bar);
-        return;
-    }
-    const int pg = lane & 7, half = lane >> 3;
-    const int tok = tile * kTile + pg * kPage;                             // the group's first token
-    const bool part = by_hand && pid >= 0 && tok < end && end - tok < kPage;
-    const unsigned parts = __ballot_sync(kFull, part && half == 0);
-    if (parts) {
-        const int src = __ffs(parts) - 1;
-        const int ppid = __shfl_sync(kFull, pid, src), ptok = __shfl_sync(kFull, tok, src), rows = end - ptok;
-        const uint16_t *base = a.page_table ? a.v + ((size_t)ppid * a.H_kv + s.h) * (kPage * D)
-                                            : a.v + (long long)(s.t.start + ptok) * a.v_stride + s.h * D;
-        const long long pitch = a.page_table ? D : a.v_stride;
-        constexpr int kPieces = D / 8;
-#pragma unroll
-        for (int i = 0; i < kPage * kPieces / 32; ++i) {
-            const int e = i * 32 + lane, row = e / kPieces, c = e % kPieces, at = src * kPage + row;
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (row < rows) x = *reinterpret_cast<const uint4 *>(base + row * pitch + c * 8);
-            const uint32_t dst = slot + (c >> 3) * (kTile * 128) + at * 128 + (((c & 7) ^ (at & 7)) << 4);
-            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
-        }
-        fence_async_proxy();
-        __syncwarp();
-    }
-    const int groups = parts ? 7 : 8;
-    if (lane == 0) mbar_expect_tx(bar, groups * kPage * D * 2);
-    __syncwarp();
-    if (half < Cfg<D>::kHalves && !part) {
-        int y = 0, z;
-        if (a.page_table) {
-            z = pid >= 0 ? (pid * a.H_kv + s.h) * kPage : a.P_phys * a.H_kv * kPage;
-        } else {
-            y = s.h;
-            z = pid >= 0 ? s.t.start + tok : a.T;
-        }
-        tma_load_3d(slot + half * (kTile * 128) + pg * (kPage * 128), map, half * 64, y, z, bar);
-    }
-}
+// One warp brings K (and Q), one V: each has every second slot of the ring.  A tile is 64 tokens of one head.  K lies as
+// [D/64][64 tokens][64 channels]: a page is D/64 copies (one for all where K is contiguous).  V lies as
+// [4][D/64][16 tokens][64 channels], because a product takes 16 tokens at a time: a page is one copy.
+// Groups that are absent or past the end come from behind the tensor's last row, which reads as zeros.
 
-// Page of the lane's 16-token group of a tile: >= 0 present (contiguous K and V: 0), -1 absent or past the end.
-__device__ __forceinline__ int group_page(const AttendArgs &a, const Segment &s, int tile, int end, int lane) {
-    const int g = tile * (kTile / kPage) + (lane & 7);
-    if (g * kPage >= end) return -1;
-    if (!a.page_table) return 0;
-    const int pid = a.page_table[(size_t)s.r * a.max_pages + g];
-    if (pid >= a.P_phys) {
-        if (lane < 8) atomicOr(a.status, SE_DEV_BAD_PAGE_ID);
-        return -1;
+// Pages of 32 groups of 16 tokens at a time, a lane each, and of the next 32 ahead.  Contiguous K and V: 0 for "present".
+struct Pages {
+    int ids, next, block;
+
+    __device__ __forceinline__ int fetch(const AttendArgs &a, const Segment &s, int g, bool report) const {
+        if (g * kPage >= s.t.past + s.t.n) return -1;
+        if (!a.page_table) return 0;
+        const int pid = a.page_table[(size_t)s.r * a.max_pages + g];
+        if (pid >= a.P_phys) {
+            if (report) atomicOr(a.status, SE_DEV_BAD_PAGE_ID);
+            return -1;
+        }
+        return pid < 0 ? -1 : pid;
     }
-    return pid < 0 ? -1 : pid;
-}
+    __device__ __forceinline__ void begin(const AttendArgs &a, const Segment &s, int tile, bool report, int lane) {
+        block = tile / 8;
+        ids = fetch(a, s, block * 32 + lane, report);
+        next = fetch(a, s, block * 32 + 32 + lane, report);
+    }
+    // tiles come in ascending order
+    __device__ __forceinline__ void reach(const AttendArgs &a, const Segment &s, int tile, bool report, int lane) {
+        if (tile / 8 == block) return;
+        ++block;
+        ids = next;
+        next = fetch(a, s, block * 32 + 32 + lane, report);
+    }
+    __device__ __forceinline__ int of(int tile, int pg) const { return __shfl_sync(kFull, ids, (tile & 7) * 4 + pg); }
+};
 
 template <int D>
-__device__ __forceinline__ void copy_role(const AttendArgs &a, const CUtensorMap *q_map, const CUtensorMap *k_map,
-                                          const CUtensorMap *v_map, const CUtensorMap *k_wide, const CUtensorMap *v_wide,
-                                          Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars,
-                                          int lane) {
+__device__ __forceinline__ void k_role(const AttendArgs &a, const CUtensorMap *q_map, const CUtensorMap *k_map, const CUtensorMap *k_wide,
+                                       Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     const int tpt = kTile / a.G;
     const AttendWork work(a);
     Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
     Segment s;
+    Pages pages;
     uint32_t pos = 0, tiles = 0, pieces = 0;
+    const bool chosen = elect_one();
     bool ok = true;
     while (ok && next_segment(a, work, ctl->pieces, c, s)) {
-        const int stop = s.t.past + s.t.n;                                 // tokens the request has
-        int pid = group_page(a, s, s.a, stop, lane);
+        const int stop = s.t.past + s.t.n;                                 // tokens of the request
+        pages.begin(a, s, s.a, true, lane);
         ok = warp_wait(bars + 8 * kQEmpty, (pieces & 1) ^ 1, gave_up, a.status);
         if (!ok) break;
-        if (lane == 0) mbar_expect_tx(bars + 8 * kQFull, (s.alt ? 1 : 2) * tpt * a.G * D * 2);
-        __syncwarp();
-        if (lane < 2 * C::kHalves) {
-            const int st = lane / C::kHalves, half = lane % C::kHalves;
-            if (st == 0 || !s.alt)
-                tma_load_3d(q_smem + st * C::kTileBytes + half * (kTile * 128), q_map, half * 64, s.h * a.G,
-                            s.t.start + s.tok0 + st * tpt, bars + 8 * kQFull);
+        if (chosen) {
+            mbar_expect_tx(bars + 8 * kQFull, (s.alt ? 1 : 2) * tpt * a.G * D * 2);
+            for (int st = 0; st < (s.alt ? 1 : 2); ++st)
+                for (int half = 0; half < C::kHalves; ++half)
+                    tma_load_3d(q_smem + st * C::kTileBytes + half * (kTile * 128), q_map, half * 64, s.h * a.G,
+                                s.t.start + s.tok0 + st * tpt, bars + 8 * kQFull);
         }
         ++pieces;
-        for (int t = s.a; t < s.b; ++t) {
-            const int next_pid = t + 1 < s.b ? group_page(a, s, t + 1, stop, lane) : -1;
-            const unsigned mask = __ballot_sync(kFull, pid >= 0) & 0xffu;
-            if (lane == 0) ctl->mask[tiles % C::kMasks] = mask;
-            ++tiles;
-            for (int kv = 0; kv < 2 && ok; ++kv, ++pos) {
-                const uint32_t slot = pos % C::kSlots, bar = bars + 8 * (kRing + slot);
-                ok = warp_wait(bar + 8 * C::kSlots, (pos / C::kSlots & 1) ^ 1, gave_up, a.status);
-                if (!ok) break;
-                load_tile<D>(a, kv ? v_map : k_map, kv ? v_wide : k_wide, s, t, pid, stop, kv == 1, ring + slot * C::kTileBytes, bar, lane);
-            }
+        for (int t = s.a; t < s.b; ++t, ++tiles, pos += 2) {
+            const uint32_t slot = pos % C::kSlots, bar = bars + 8 * (kRing + slot), dst = ring + slot * C::kKvBytes;
+            pages.reach(a, s, t, true, lane);
+            const unsigned mask = __ballot_sync(kFull, pages.ids >= 0) >> (t & 7) * 4 & 0xfu;
+            int pid[4];
+#pragma unroll
+            for (int pg = 0; pg < 4; ++pg) pid[pg] = pages.of(t, pg);
+            ok = warp_wait(bar + 8 * C::kSlots, (pos / C::kSlots & 1) ^ 1, gave_up, a.status);
             if (!ok) break;
-            pid = next_pid;
+            if (chosen) {
+                ctl->mask[tiles % C::kMasks] = mask;
+                mbar_expect_tx(bar, C::kKvBytes);
+                if (!a.page_table && (t + 1) * kKv <= stop) {
+                    tma_load_4d(dst, k_wide, 0, s.h, s.t.start + t * kKv, 0, bar);
+                } else {
+#pragma unroll
+                    for (int pg = 0; pg < 4; ++pg) {
+                        const int y = a.page_table ? 0 : s.h;
+                        const int z = pid[pg] < 0 ? (a.page_table ? a.P_phys * a.H_kv * kPage : a.T)
+                                                  : a.page_table ? (pid[pg] * a.H_kv + s.h) * kPage : s.t.start + t * kKv + pg * kPage;
+#pragma unroll
+                        for (int half = 0; half < C::kHalves; ++half)
+                            tma_load_3d(dst + half * (kKv * 128) + pg * (kPage * 128), k_map, half * 64, y, z, bar);
+                    }
+                }
+            }
+            __syncwarp();
         }
     }
     // no copy may be in flight when the CTA's shared memory goes away
     if (!ok) {
-        const uint32_t first = pos > C::kSlots ? pos - C::kSlots : 0;
-        for (uint32_t p = first; p < pos; ++p) mbar_wait(bars + 8 * (kRing + p % C::kSlots), p / C::kSlots & 1);
+        for (uint32_t p = pos > C::kSlots ? pos - C::kSlots : 0; p < pos; p += 2)
+            mbar_wait(bars + 8 * (kRing + p % C::kSlots), p / C::kSlots & 1);
         if (pieces) mbar_wait(bars + 8 * kQFull, (pieces - 1) & 1);
     }
 }
 
-// ---- products ----------------------------------------------------------------------
-// The whole warp walks the list, so that addresses stay in uniform registers; one elected lane issues (a role run by a
-// single lane took 82 cycles per instruction to issue, more than the 64 that it computes).
-template <int D, int ST>
-struct Products {
-    using C = Cfg<D>;
-    // S[ST] = Q K^T
-    static __device__ __forceinline__ void scores(uint32_t tmem, uint32_t q, uint32_t k, uint32_t bars, int release) {
-        const uint64_t qd = smem_operand(q, 16, 1024), kd = smem_operand(k, 16, 1024);
-        if (elect_one()) {
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) {
-                const uint32_t off = (i / 4) * (kTile * 128 >> 4) + (i % 4) * 2;
-                mma_ss(tmem + ST * kTile, qd + off, kd + off, mma_instr(kTile, false), i > 0);
-            }
-            mma_commit(bars + 8 * (kSFull + ST));
-            if (release >= 0) mma_commit(bars + 8 * release);
-        }
-    }
-    // O[ST] += P V
-    static __device__ __forceinline__ void values(uint32_t tmem, uint32_t v, bool accumulate, uint32_t bars, int release) {
-        const uint64_t vd = smem_operand(v, kTile * 128, 1024);
-        if (elect_one()) {
-#pragma unroll
-            for (int i = 0; i < kTile / 16; ++i)
-                mma_ts(tmem + C::kTmemO + ST * D, tmem + ST * kTile + i * 8, vd + i * (16 * 128 >> 4), mma_instr(D, true),
-                       accumulate || i > 0);
-            mma_commit(bars + 8 * (kODone + ST));
-            if (release >= 0) mma_commit(bars + 8 * release);
-        }
-    }
-};
-
 template <int D>
-__device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars) {
+__device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v_map, Control<D> *ctl, uint32_t ring, uint32_t bars, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
-    const uint32_t tmem = ctl->tmem;
     const AttendWork work(a);
     Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
     Segment s;
-    uint32_t pos = 0, pieces = 0, p_seen = 0, o_used = 0;                  // bit st: parity of the stream's next wait
+    Pages pages;
+    uint32_t pos = 1;
+    const bool chosen = elect_one();
+    bool ok = true;
+    while (ok && next_segment(a, work, ctl->pieces, c, s)) {
+        const int stop = s.t.past + s.t.n;                                 // tokens of the request
+        pages.begin(a, s, s.a, false, lane);
+        for (int t = s.a; t < s.b; ++t, pos += 2) {
+            const uint32_t slot = pos % C::kSlots, bar = bars + 8 * (kRing + slot), dst = ring + slot * C::kKvBytes;
+            pages.reach(a, s, t, false, lane);
+            int pid[4];
+#pragma unroll
+            for (int pg = 0; pg < 4; ++pg) pid[pg] = pages.of(t, pg);
+            ok = warp_wait(bar + 8 * C::kSlots, (pos / C::kSlots & 1) ^ 1, gave_up, a.status);
+            if (!ok) break;
+            // The group that holds the end of the request is copied row by row: what lies behind the end may be anything, and
+            // a weight of zero would not hide a NaN.
+            const int part = stop % kPage && stop / kKv == t ? stop % kKv / kPage : -1;
+            bool by_hand = false;
+#pragma unroll
+            for (int pg = 0; pg < 4; ++pg) {
+                if (pg != part || pid[pg] < 0) continue;
+                by_hand = true;
+                const int tok = t * kKv + pg * kPage;
+                const uint16_t *base = a.page_table ? a.v + ((size_t)pid[pg] * a.H_kv + s.h) * (kPage * D)
+                                                    : a.v + (long long)(s.t.start + tok) * a.v_stride + s.h * D;
+                const long long pitch = a.page_table ? D : a.v_stride;
+                constexpr int kPieces = D / 8;
+#pragma unroll
+                for (int i = 0; i < kPage * kPieces / 32; ++i) {
+                    const int e = i * 32 + lane, row = e / kPieces, ch = e % kPieces;
+                    uint4 x = make_uint4(0, 0, 0, 0);
+                    if (row < stop - tok) x = *reinterpret_cast<const uint4 *>(base + row * pitch + ch * 8);
+                    const uint32_t at = dst + pg * (kPage * D * 2) + (ch >> 3) * (kPage * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4);
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+                }
+                fence_async_proxy();
+                __syncwarp();
+            }
+            if (chosen) {
+                mbar_expect_tx(bar, C::kKvBytes - (by_hand ? kPage * D * 2 : 0));
+#pragma unroll
+                for (int pg = 0; pg < 4; ++pg) {
+                    if (pg == part && by_hand) continue;
+                    const int y = a.page_table ? 0 : s.h;
+                    const int z = pid[pg] < 0 ? (a.page_table ? a.P_phys * a.H_kv * kPage : a.T)
+                                              : a.page_table ? (pid[pg] * a.H_kv + s.h) * kPage : s.t.start + t * kKv + pg * kPage;
+                    tma_load_4d(dst + pg * (kPage * D * 2), v_map, 0, y, z, 0, bar);
+                }
+            }
+            __syncwarp();
+        }
+    }
+    if (!ok)
+        for (uint32_t p = pos > C::kSlots ? pos - C::kSlots : 1; p < pos; p += 2)
+            mbar_wait(bars + 8 * (kRing + p % C::kSlots), p / C::kSlots & 1);
+}
+
+// ---- products ----------------------------------------------------------------------
+// The scores of a KV tile of 64 tokens take 64 columns, so every stream has two score buffers, and the next scores are there
+// when the softmax gets to them.  (Tiles of 128 tokens leave room for one buffer: products and softmax of a stream then
+// wait for one another, and the tensor cores stood idle for 40 % of the time.  A score product of 64 columns is bound by
+// shared memory, 49 cycles instead of 32: 20 % of both products, the smaller loss.)
+// One warp per stream issues its products: a wait queues up behind the products that its own warp has issued, so a single
+// warp for both streams let the tensor cores run dry at every wait.  The whole warp walks the list, so that addresses stay in
+// uniform registers; one elected lane issues.
+template <int D, int ST>
+__device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars) {
+    using C = Cfg<D>;
+    volatile int *gave_up = &ctl->gave_up;
+    const uint32_t tmem_s = ctl->tmem + ST * kTile, tmem_o = ctl->tmem + C::kTmemO + ST * D;
+    const AttendWork work(a);
+    Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
+    Segment s = {};
+    uint32_t pos = 0, pieces = 0, o_used = 0, n = 0;                       // n: steps so far
     bool any = false;
+    const bool chosen = elect_one();
     auto wait = [&](int bar, uint32_t parity) { return warp_wait(bars + 8 * bar, parity & 1, gave_up, a.status); };
-    // K and V tiles are waited for in order: `k_next`, `v_next` are the first ring positions not waited for yet
-    uint32_t k_next = 0, v_next = 1;
-    auto wait_k = [&](uint32_t at) {
-        for (; k_next <= at; k_next += 2)
-            if (!wait(kRing + k_next % C::kSlots, k_next / C::kSlots)) return false;
-        return true;
+    auto full = [&](uint32_t at) { return wait(kRing + at % C::kSlots, at / C::kSlots); };
+    auto slot = [&](uint32_t at) { return ring + at % C::kSlots * C::kKvBytes; };
+    // a ring slot is free when both streams have let it go; a tile of one stream alone is let go twice by it
+    auto let_go = [&](uint32_t at) {
+        const uint32_t bar = bars + 8 * (kRing + C::kSlots + at % C::kSlots);
+        mma_commit(bar);
+        if (s.alt) mma_commit(bar);
     };
-    auto wait_v = [&](uint32_t at) {
-        for (; v_next <= at; v_next += 2)
-            if (!wait(kRing + v_next % C::kSlots, v_next / C::kSlots)) return false;
-        return true;
+    // S = Q K^T of the n-th step
+    auto scores = [&](uint32_t at, uint32_t n) {
+        const uint64_t qd = smem_operand(q_smem + (s.alt ? 0 : ST * C::kTileBytes), 16, 1024), kd = smem_operand(slot(at), 16, 1024);
+        const uint32_t d = tmem_s + (n & 1) * kKv;
+        tc_fence_after();
+        if (chosen) {
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+                mma_ss(d, qd + (k / 4) * (kTile * 128 >> 4) + (k % 4) * 2, kd + (k / 4) * (kKv * 128 >> 4) + (k % 4) * 2, mma_instr(kKv, false),
+                       k > 0);
+            mma_commit(bars + 8 * (kSFull + 2 * ST + (n & 1)));
+            let_go(at);
+        }
+    };
+    // O += P V
+    auto values = [&](uint32_t at, uint32_t n, bool accumulate, bool last) {
+        const uint64_t vd = smem_operand(slot(at), kPage * 128, 1024);
+        const uint32_t p = tmem_s + (n & 1) * kKv;
+        tc_fence_after();
+        if (chosen) {
+#pragma unroll
+            for (int k = 0; k < kKv / 16; ++k) mma_ts(tmem_o, p + k * 8, vd + k * (kPage * D * 2 >> 4), mma_instr(D, true), accumulate || k > 0);
+            mma_commit(bars + 8 * (kODone + ST));
+            if (last) mma_commit(bars + 8 * (kOLast + ST));
+            let_go(at);
+        }
     };
     while (next_segment(a, work, ctl->pieces, c, s)) {
-        const int steps = max(s.steps0, s.steps1);
-        const uint32_t q1 = q_smem + (s.alt ? 0 : C::kTileBytes);
-        // ring position of the K tile of step i of stream st; its V tile follows
-        auto place = [&](int st, int i) { return pos + 2u * (s.alt ? 2 * i + st : i); };
-        auto slot = [&](uint32_t at) { return ring + at % C::kSlots * C::kTileBytes; };
-        auto release = [&](int st, uint32_t at) { return s.alt || st == 1 ? (int)(kRing + C::kSlots + at % C::kSlots) : -1; };
-        // a step: everything that can be waited for early comes before the wait for the weights
-        auto step = [&](auto stream, int i) {
-            constexpr int ST = decltype(stream)::value;
-            const int mine = ST ? s.steps1 : s.steps0;
-            if (i >= mine) return true;
-            const bool more = i + 1 < mine;
-            const uint32_t at = place(ST, i), next = place(ST, i + 1);
-            if (!wait_v(at + 1) || (more && !wait_k(next))) return false;
-            if (i == 0) {                // the epilogue of the stream's last piece has read O
-                if (!wait(kOFree + ST, (o_used >> ST & 1) ^ 1)) return false;
-                o_used ^= 1u << ST;
-            }
-            if (!wait(kPReady + ST, p_seen >> ST)) return false;
-            p_seen ^= 1u << ST;
-            tc_fence_after();
-            Products<D, ST>::values(tmem, slot(at + 1), i > 0, bars, release(ST, at + 1));
-            if (more) Products<D, ST>::scores(tmem, ST ? q1 : q_smem, slot(next), bars, release(ST, next));
-            return true;
-        };
+        const int steps = ST ? s.steps1 : s.steps0;
+        const uint32_t stride = s.alt ? 4 : 2;
+        uint32_t at = pos + (s.alt ? 2 * ST : 0);                          // ring position of the step's K tile; its V tile follows
         if (!wait(kQFull, pieces)) break;
         ++pieces;
-        any = true;
-        if (s.steps0 > 0) {
-            if (!wait_k(place(0, 0))) break;
-            tc_fence_after();
-            Products<D, 0>::scores(tmem, q_smem, slot(place(0, 0)), bars, release(0, place(0, 0)));
-        }
-        if (s.steps1 > 0) {
-            if (!wait_k(place(1, 0))) break;
-            tc_fence_after();
-            Products<D, 1>::scores(tmem, q1, slot(place(1, 0)), bars, release(1, place(1, 0)));
-        }
-        if (steps == 1 && elect_one()) mma_commit(bars + 8 * kQEmpty);
         bool ok = true;
-        for (int i = 0; i < steps && ok; ++i) {
-            ok = step(Stream<0>{}, i) && step(Stream<1>{}, i);
-            if (i + 2 == steps && elect_one()) mma_commit(bars + 8 * kQEmpty);   // the last product with Q is on its way
+        for (int u = 0; u < 2 && u < steps && ok; ++u)
+            if ((ok = full(at + u * stride))) scores(at + u * stride, n + u);
+        any = any || steps > 0;
+        if (!ok) break;
+        if (chosen && steps <= 2) {
+            if (steps > 0) mma_commit(bars + 8 * kQEmpty);
+            else mbar_arrive(bars + 8 * kQEmpty);
         }
+        for (int u = 0; u < steps && ok; ++u, ++n, at += stride) {
+            // everything that can be waited for early comes before the wait for the weights
+            const bool more = u + 2 < steps;
+            ok = full(at + 1) && (!more || full(at + 2 * stride));
+            if (ok && u == 0) {          // the epilogue of the stream's last piece has read O
+                ok = wait(kOFree + ST, o_used ^ 1);
+                o_used ^= 1;
+            }
+            ok = ok && wait(kPReady + 2 * ST + (n & 1), n >> 1);
+            if (!ok) break;
+            values(at + 1, n, u > 0, u + 1 == steps);
+            if (more) scores(at + 2 * stride, n);
+            if (chosen && u + 3 == steps) mma_commit(bars + 8 * kQEmpty);   // the last product with Q is on its way
+        }
+        // tiles that only the other stream sees
+        if (ok && !s.alt)
+            for (int i = steps; i < s.b - s.a && ok; ++i, at += 2)
+                for (uint32_t kv = at; kv < at + 2 && ok; ++kv) {
+                    ok = full(kv);
+                    if (ok && chosen) mbar_arrive(bars + 8 * (kRing + C::kSlots + kv % C::kSlots));
+                }
+        __syncwarp();
         if (!ok) break;
         pos += 2u * (s.b - s.a);
     }
     if (any) {                           // nothing may be running when tensor memory goes away
-        if (elect_one()) mma_commit(bars + 8 * kDrain);
+        if (chosen) mma_commit(bars + 8 * (kDrain + ST));
         __syncwarp();
-        mbar_wait(bars + 8 * kDrain, 0);
+        mbar_wait(bars + 8 * (kDrain + ST), 0);
     }
 }
 
@@ -448,7 +486,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
     const AttendWork work(a);
     Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
     Segment s;
-    uint32_t step = 0, tiles = 0, verdicts = 0, swaps = 0;
+    uint32_t step = 0, tiles = 0, verdicts = 0, swaps = 0, ends = 0;
     // both warpgroups have come here
     auto swap_sync = [&] {
         __syncwarp();
@@ -464,34 +502,36 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
         const int steps = s.steps(st);
         float m = -INFINITY;                                               // in units of the raw scores
         float2 l2 = make_float2(0.f, 0.f);
-        for (int i = 0; i < steps; ++i, ++step) {
-            const int rel = s.alt ? 2 * i + st : i, tile = s.a + rel;
-            if (!warp_wait(bars + 8 * (kSFull + st), step & 1, gave_up, a.status)) return;
+        for (int u = 0; u < steps; ++u, ++step) {
+            const int rel = s.alt ? 2 * u + st : u, first = (s.a + rel) * kKv;
+            const uint32_t buf = 2 * st + (step & 1), t_p = t_s + (step & 1) * kKv;
+            if (!warp_wait(bars + 8 * (kSFull + buf), step >> 1 & 1, gave_up, a.status)) return;
             tc_fence_after();
-            float x[kTile];
-#pragma unroll
-            for (int k = 0; k < kTile; k += 32) tmem_ld32(t_s + k, x + k);
+            float x[kKv];
+            tmem_ld32(t_p, x);
+            tmem_ld32(t_p + 32, x + 32);
             const unsigned mask = ctl->mask[(tiles + rel) % C::kMasks];
             tmem_wait_ld();
-            settle<kTile>(x);
-            if (tile * kTile + kTile > least || mask != 0xffu) {
-                const int limit = sees - tile * kTile;
+            settle<kKv>(x);
+            if (first + kKv > least || mask != 0xfu) {
+                const int limit = sees - first;
 #pragma unroll
-                for (int k = 0; k < kTile; ++k)
+                for (int k = 0; k < kKv; ++k)
                     if (k >= limit || !(mask >> (k / kPage) & 1)) x[k] = -INFINITY;
             }
-            float top[4] = {x[0], x[1], x[2], x[3]};
+            float top[4] = {m, m, m, m};
 #pragma unroll
-            for (int k = 4; k < kTile; k += 8)
+            for (int k = 0; k < kKv; k += 8)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) top[e] = k + 4 + e < kTile ? max3(top[e], x[k + e], x[k + 4 + e]) : fmaxf(top[e], x[k + e]);
-            const float tm = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-            const float mn = fmaxf(m, tm);
+                for (int e = 0; e < 4; ++e) top[e] = max3(top[e], x[k + e], x[k + 4 + e]);
+            const float mn = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
             if (__any_sync(kFull, (mn - m) * sl > kSlack)) {
                 const float f = m == -INFINITY ? 0.f : ex2((m - mn) * sl);
                 m = mn;
                 l2.x *= f, l2.y *= f;
-                if (i > 0) {
+                if (u > 0) {
+                    // O + P V of the last step; the one before is complete (these scores were issued behind it), so the barrier's
+                    // parity says which of two phases it is in
                     if (!warp_wait(bars + 8 * (kODone + st), (step - 1) & 1, gave_up, a.status)) return;
                     tc_fence_after();
 #pragma unroll 1
@@ -507,28 +547,25 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
                 }
             }
             const float off = m == -INFINITY ? 0.f : -m * sl;
+            uint32_t p[kKv / 2];
 #pragma unroll
-            for (int k = 0; k < kTile; k += 64) {
-                uint32_t p[32];
-#pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const float2 y = ffma2(make_float2(x[k + 2 * e], x[k + 2 * e + 1]), make_float2(sl, sl), make_float2(off, off));
-                    const float2 w = make_float2(ex2(y.x), ex2(y.y));
-                    l2 = __fadd2_rn(l2, w);
-                    // the weights enter the product with V as bf16 (8 significant bits), the sum l keeps fp32
-                    const __nv_bfloat162 b = __float22bfloat162_rn(w);
-                    p[e] = *reinterpret_cast<const uint32_t *>(&b);
-                }
-                tmem_st32(t_s + k / 2, p);
+            for (int e = 0; e < kKv / 2; ++e) {
+                const float2 y = ffma2(make_float2(x[2 * e], x[2 * e + 1]), make_float2(sl, sl), make_float2(off, off));
+                const float2 w = make_float2(ex2(y.x), ex2(y.y));
+                l2 = __fadd2_rn(l2, w);
+                // the weights enter the product with V as bf16 (8 significant bits), their sum keeps fp32
+                const __nv_bfloat162 b = __float22bfloat162_rn(w);
+                p[e] = *reinterpret_cast<const uint32_t *>(&b);
             }
+            tmem_st32(t_p, p);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bars + 8 * (kPReady + st));
+            if (lane == 0) mbar_arrive(bars + 8 * (kPReady + buf));
         }
         tiles += s.b - s.a;
         if (steps > 0) {
-            if (!warp_wait(bars + 8 * (kODone + st), (step - 1) & 1, gave_up, a.status)) return;
+            if (!warp_wait(bars + 8 * (kOLast + st), ends++ & 1, gave_up, a.status)) return;
             tc_fence_after();
         }
 
@@ -633,12 +670,12 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
-              const __grid_constant__ CUtensorMap v_map, const __grid_constant__ CUtensorMap k_wide,
-              const __grid_constant__ CUtensorMap v_wide, const __grid_constant__ AttendArgs a) {
+              const __grid_constant__ CUtensorMap k_wide, const __grid_constant__ CUtensorMap v_map,
+              const __grid_constant__ AttendArgs a) {
     using C = Cfg<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t base = smem_u32(smem);
-    Control<D> *ctl = reinterpret_cast<Control<D> *>(smem + 2 * C::kTileBytes + C::kSlots * C::kTileBytes);
+    Control<D> *ctl = reinterpret_cast<Control<D> *>(smem + 2 * C::kTileBytes + C::kSlots * C::kKvBytes);
     const uint32_t bars = smem_u32(ctl->bars);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (base & 1023u) {                  // the swizzle pattern hangs on the address
@@ -648,18 +685,24 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
 
     if (threadIdx.x == 0) {
         mbar_init(bars + 8 * kQFull, 1);
-        mbar_init(bars + 8 * kQEmpty, 1);
+        mbar_init(bars + 8 * kQEmpty, 2);
         for (int st = 0; st < 2; ++st) {
-            mbar_init(bars + 8 * (kSFull + st), 1);
-            mbar_init(bars + 8 * (kPReady + st), 4);
+            for (int buf = 2 * st; buf < 2 * st + 2; ++buf) {
+                mbar_init(bars + 8 * (kSFull + buf), 1);
+                mbar_init(bars + 8 * (kPReady + buf), 4);
+            }
             mbar_init(bars + 8 * (kODone + st), 1);
+            mbar_init(bars + 8 * (kOLast + st), 1);
             mbar_init(bars + 8 * (kOFree + st), 4);
             mbar_init(bars + 8 * (kAll + st), 4);
             mbar_init(bars + 8 * (kVerdict + st), 1);
+            mbar_init(bars + 8 * (kDrain + st), 1);
         }
         mbar_init(bars + 8 * kSwap, 8);
-        mbar_init(bars + 8 * kDrain, 1);
-        for (int i = 0; i < 2 * C::kSlots; ++i) mbar_init(bars + 8 * (kRing + i), 1);
+        for (int i = 0; i < C::kSlots; ++i) {
+            mbar_init(bars + 8 * (kRing + i), 1);
+            mbar_init(bars + 8 * (kRing + C::kSlots + i), 2);
+        }
         mbar_fence_init();
         ctl->gave_up = 0;
     }
@@ -674,12 +717,12 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     tc_fence_after();
 
     if (warp < 8) {
-        regs_up<kRegsSoftmax>();
         softmax_role<D>(a, ctl, bars, warp >> 2);
     } else {
-        regs_down<kRegsOther>();
-        if (warp == kCopyWarp) copy_role<D>(a, &q_map, &k_map, &v_map, &k_wide, &v_wide, ctl, base, base + 2 * C::kTileBytes, bars, lane);
-        else if (warp == kMmaWarp) mma_role<D>(a, ctl, base, base + 2 * C::kTileBytes, bars);
+        if (warp == kKWarp) k_role<D>(a, &q_map, &k_map, &k_wide, ctl, base, base + 2 * C::kTileBytes, bars, lane);
+        else if (warp == kVWarp) v_role<D>(a, &v_map, ctl, base + 2 * C::kTileBytes, bars, lane);
+        else if (warp == kMmaWarp) mma_role<D, 0>(a, ctl, base, base + 2 * C::kTileBytes, bars);
+        else if (warp == kMmaWarp + 1) mma_role<D, 1>(a, ctl, base, base + 2 * C::kTileBytes, bars);
         __syncwarp();
     }
     tc_fence_before();
@@ -695,17 +738,16 @@ template <int D>
 cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t stream) {
     using C = Cfg<D>;
     const int G = p.H_q / p.H_kv;
-    CUtensorMap q_map, k_map, v_map, k_wide, v_wide;
+    CUtensorMap q_map, k_map, k_wide, v_map;
     bool ok = make_rows_map(&q_map, c.q, D, p.H_q, c.total_tokens, c.q_stride, G, kTile / G);
     if (c.page_table) {
         const long long rows = (long long)p.num_phys_pages * p.H_kv * kPage;
-        ok = ok && make_rows_map(&k_map, c.k, D, 1, rows, D, 1, kPage) && make_rows_map(&v_map, c.v, D, 1, rows, D, 1, kPage);
-        k_wide = k_map, v_wide = v_map;                      // not used
+        ok = ok && make_rows_map(&k_map, c.k, D, 1, rows, D, 1, kPage) && make_split_map(&v_map, c.v, D, 1, rows, D, kPage);
+        k_wide = k_map;                                          // not used
     } else {
         ok = ok && make_rows_map(&k_map, c.k, D, p.H_kv, c.total_tokens, c.k_stride, 1, kPage) &&
-             make_rows_map(&v_map, c.v, D, p.H_kv, c.total_tokens, c.v_stride, 1, kPage) &&
-             make_rows_map(&k_wide, c.k, D, p.H_kv, c.total_tokens, c.k_stride, 1, kTile) &&
-             make_rows_map(&v_wide, c.v, D, p.H_kv, c.total_tokens, c.v_stride, 1, kTile);
+             make_split_map(&k_wide, c.k, D, p.H_kv, c.total_tokens, c.k_stride, kKv) &&
+             make_split_map(&v_map, c.v, D, p.H_kv, c.total_tokens, c.v_stride, kPage);
     }
     if (!ok) return cudaErrorInvalidValue;
     AttendArgs a = {};
@@ -717,15 +759,11 @@ cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t 
     a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.G = G, a.T = c.total_tokens, a.max_pages = p.max_pages;
     a.P_phys = p.num_phys_pages, a.scale_log2 = effective_scale(p) * kLog2e;
     auto kern = attend_kernel<D>;
-    // the register split (setmaxnreg) draws on what the block was launched with
-    cudaFuncAttributes attr;
-    cudaError_t e = cudaFuncGetAttributes(&attr, kern);
-    if (e != cudaSuccess) return e;
-    if (attr.numRegs * kThreads < 256 * kRegsSoftmax + 128 * kRegsOther) return cudaErrorInvalidConfiguration;
-    const size_t smem = (2 + C::kSlots) * C::kTileBytes + sizeof(Control<D>);
+    cudaError_t e;
+    const size_t smem = 2 * C::kTileBytes + C::kSlots * C::kKvBytes + sizeof(Control<D>);
     e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    kern<<<kPromptCtas, kThreads, smem, stream>>>(q_map, k_map, v_map, k_wide, v_wide, a);
+    kern<<<kPromptCtas, kThreads, smem, stream>>>(q_map, k_map, k_wide, v_map, a);
     return cudaGetLastError();
 }
 

@@ -82,6 +82,7 @@ struct MassWork {
     }
     __device__ __forceinline__ int unit_at(const TokenRange &, int, long long z) const { return (int)(z / tpt); }
     __device__ __forceinline__ long long min_cost() const { return 4 * tpt; }
+    static constexpr int kCrumb = 2;   // least units of a part of an item
 };
 
 struct Segment {

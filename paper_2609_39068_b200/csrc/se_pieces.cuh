@@ -13,6 +13,7 @@
 //   int units(t, i)                    units of item i
 //   int unit_at(t, i, z)               unit that cost z into the item falls in
 //   long long min_cost()               least cost of a piece
+//   kCrumb                             least units of a part of a split item
 #pragma once
 
 #include "se_device.cuh"
@@ -111,10 +112,10 @@ __device__ __forceinline__ void cut_work(const Work &w, int B, int H_kv, uint32_
         const int units = w.units(t, i);
         unit = w.unit_at(t, i, y - w.cost(t, i));
         item = first[r] + h * items + i;
-        // no crumbs: a piece of an item that is split has two units at least
-        if (unit < 2) {
+        // no crumbs: a part of an item that is split has a few units at least
+        if (unit < Work::kCrumb) {
             unit = 0;
-        } else if (unit > units - 2) {
+        } else if (unit > units - Work::kCrumb) {
             unit = 0, ++item;
             if (++i == items) {
                 i = 0;

@@ -99,6 +99,12 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
         : "memory");
 }
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+        : "memory");
+}
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
@@ -136,6 +142,30 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+// 2^x of a pair without the special-function unit: x = j + f with |f| <= 1/2 (j by adding and taking off 1.5 * 2^23),
+// 2^f by a minimax polynomial of the given degree (own fit; relative error 2.7e-6 for 4, 2.1e-7 for 5, fp32 rounding
+// included), j added to the exponent field.  Below -126 the result stays near 2^-126 instead of reaching 0.
+template <int DEG>
+__device__ __forceinline__ float2 ex2_fma(float2 x) {
+    static_assert(DEG == 4 || DEG == 5, "coefficients");
+    constexpr float kMagic = 12582912.f;
+    x.x = fmaxf(x.x, -126.f), x.y = fmaxf(x.y, -126.f);
+    const float2 t = __fadd2_rn(x, make_float2(kMagic, kMagic));
+    const float2 f = __fadd2_rn(x, ffma2(t, make_float2(-1.f, -1.f), make_float2(kMagic, kMagic)));
+    float2 p;
+    auto step = [&](float c) { p = ffma2(p, f, make_float2(c, c)); };
+    if constexpr (DEG == 4) {
+        p = make_float2(0.009570102207362652f, 0.009570102207362652f);
+        step(0.05591786280274391f), step(0.240247443318367f), step(0.6931217908859253f), step(0.9999992847442627f);
+    } else {
+        p = make_float2(0.0013276472454890609f, 0.0013276472454890609f);
+        step(0.009675541892647743f), step(0.05550713092088699f), step(0.24022120237350464f), step(0.6931469440460205f);
+        step(1.0000001192092896f);
+    }
+    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
+                       __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+}
+
 template <int N>
 __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
@@ -169,6 +199,20 @@ inline bool make_rows_map(CUtensorMap *map, const void *base, int D, long long h
     const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
     const cuuint32_t estr[3] = {1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The same tensor with the channels in blocks of 64, boxes of one head x box_rows x all blocks: [D/64][box_rows][64] in shared
+// memory (the blocks are the slowest dimension of the box although their stride, 128 bytes, is the smallest).
+inline bool make_split_map(CUtensorMap *map, const void *base, int D, long long heads, long long rows, long long stride, int box_rows) {
+    EncodeTiledFn fn = encode_tiled();
+    if (!fn) return false;
+    const cuuint64_t dims[4] = {64, (cuuint64_t)heads, (cuuint64_t)rows, (cuuint64_t)(D / 64)};
+    const cuuint64_t strides[3] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2, 128};
+    const cuuint32_t box[4] = {64, 1, (cuuint32_t)box_rows, (cuuint32_t)(D / 64)};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides, box, estr,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
