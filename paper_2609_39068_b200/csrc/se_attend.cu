@@ -34,7 +34,6 @@ constexpr int kThreads = kPromptThreads;   // 2 softmax warpgroups, K warp, 2 pr
 constexpr int kKWarp = 8, kMmaWarp = 9, kVWarp = 11;
 constexpr int kTile = 128;             // query rows of a tile
 constexpr int kKv = 64;                // tokens of a KV tile
-constexpr int kControlBytes = 2048;    // status word, tickets
 constexpr int kItemCost = 128;         // cost of starting a query tile, in tokens
 constexpr int kMinCost = 512;          // a CTA takes at least 256 tokens of a pair, 512 of a single tile
 // The running maximum may lag: weights up to 2^40 lose nothing (bf16 and fp32 keep their exponents, and 2^40 * 131072
@@ -59,7 +58,7 @@ struct AttendArgs {
     uint16_t *out;
     float *lse;
     float *partials;
-    uint32_t *status, *tickets;
+    PromptControl *ctl;
     int B, H_q, H_kv, G, T, max_pages, P_phys;
     float scale_log2;
 };
@@ -70,7 +69,7 @@ enum Bar { kQFull, kQEmpty, kSFull, kPReady = kSFull + 4, kODone = kPReady + 4, 
 template <int D>
 struct Control {
     uint64_t bars[kRing + 2 * Cfg<D>::kSlots];
-    Pieces pieces;
+    PieceQueue queue;
     uint32_t mask[Cfg<D>::kMasks];     // present 16-token groups of the tiles in flight
     int last[2];
     int gave_up;
@@ -111,21 +110,23 @@ struct Segment {
     TokenRange t;
     int tok0, ntok;        // new tokens of the item, relative to the request
     bool alt;
-    int a, b, nkv;         // KV tiles of this piece, of the item
+    int piece, a, b, nkv;  // piece, its KV tiles of the item, the item's
     int steps0, steps1;    // KV tiles per stream
     __device__ __forceinline__ int steps(int st) const { return st ? steps1 : steps0; }
 };
 
-// This CTA's next piece; every role walks the same list.
-__device__ __forceinline__ bool next_segment(const AttendArgs &a, const AttendWork &w, const Pieces &p, Cursor &c, Segment &s) {
-    if (piece_done(w, a.B, p, c)) return false;
+// The next part of an item in the piece; every role walks the same list.
+__device__ __forceinline__ bool next_segment(Walk<AttendWork> &walk, Segment &s) {
+    if (!walk.item()) return false;
+    const Cursor &c = walk.c;
+    const AttendWork &w = walk.w;
     s.r = c.r, s.h = c.h, s.item = c.item, s.t = c.t;
     s.tok0 = c.i * 2 * w.tpt;
     s.ntok = w.new_tokens(c.t, c.i);
     s.alt = s.ntok <= w.tpt;
     s.nkv = w.units(c.t, c.i);
-    s.a = c.unit;
-    s.b = piece_end(c, p, s.nkv);
+    s.a = c.unit, s.piece = c.piece;
+    s.b = piece_end(c, s.nkv);
     if (s.alt) {
         s.steps0 = (s.b - s.a + 1) / 2;
         s.steps1 = (s.b - s.a) / 2;
@@ -134,7 +135,7 @@ __device__ __forceinline__ bool next_segment(const AttendArgs &a, const AttendWo
         s.steps0 = max(min(s.b, n0) - s.a, 0);
         s.steps1 = s.b - s.a;
     }
-    next_item(w, a.B, a.H_kv, c);
+    walk.next();
     return true;
 }
 
@@ -153,7 +154,7 @@ struct Pages {
         if (!a.page_table) return 0;
         const int pid = a.page_table[(size_t)s.r * a.max_pages + g];
         if (pid >= a.P_phys) {
-            if (report) atomicOr(a.status, SE_DEV_BAD_PAGE_ID);
+            if (report) atomicOr(&a.ctl->status, SE_DEV_BAD_PAGE_ID);
             return -1;
         }
         return pid < 0 ? -1 : pid;
@@ -173,23 +174,36 @@ struct Pages {
     __device__ __forceinline__ int of(int tile, int pg) const { return __shfl_sync(kFull, ids, (tile & 7) * 4 + pg); }
 };
 
+// The end of a copying warp, whose next position would be `pos`: nothing may still be on its way to the CTA's shared memory
+// when the CTA ends - copies, and the products' arrivals on the barriers of the slots they have let go.
+template <int D>
+__device__ __forceinline__ void leave_ring(bool ok, uint32_t pos, uint32_t first, uint32_t bars, volatile int *gave_up,
+                                           const AttendArgs &a) {
+    constexpr uint32_t kSlots = Cfg<D>::kSlots;
+    for (uint32_t p = pos >= kSlots + first ? pos - kSlots : first; p < pos; p += 2) {
+        const uint32_t bar = bars + 8 * (kRing + p % kSlots), parity = p / kSlots & 1;
+        if (ok) ok = warp_wait(bar + 8 * kSlots, parity, gave_up, &a.ctl->status);
+        else mbar_wait(bar, parity);
+    }
+}
+
 template <int D>
 __device__ __forceinline__ void k_role(const AttendArgs &a, const CUtensorMap *q_map, const CUtensorMap *k_map, const CUtensorMap *k_wide,
-                                       Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars, int lane) {
+                                       Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars, int n_pieces, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     const int tpt = kTile / a.G;
     const AttendWork work(a);
-    Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
     Segment s;
     Pages pages;
-    uint32_t pos = 0, tiles = 0, pieces = 0;
+    uint32_t pos = 0, tiles = 0, queries = 0;
     const bool chosen = elect_one();
     bool ok = true;
-    while (ok && next_segment(a, work, ctl->pieces, c, s)) {
+    Walk<AttendWork> walk(work, a.B, a.H_kv, a.ctl, &ctl->queue, gave_up, lane, n_pieces);
+    while (ok && next_segment(walk, s)) {
         const int stop = s.t.past + s.t.n;                                 // tokens of the request
         pages.begin(a, s, s.a, true, lane);
-        ok = warp_wait(bars + 8 * kQEmpty, (pieces & 1) ^ 1, gave_up, a.status);
+        ok = warp_wait(bars + 8 * kQEmpty, (queries & 1) ^ 1, gave_up, &a.ctl->status);
         if (!ok) break;
         if (chosen) {
             mbar_expect_tx(bars + 8 * kQFull, (s.alt ? 1 : 2) * tpt * a.G * D * 2);
@@ -198,7 +212,8 @@ __device__ __forceinline__ void k_role(const AttendArgs &a, const CUtensorMap *q
                     tma_load_3d(q_smem + st * C::kTileBytes + half * (kTile * 128), q_map, half * 64, s.h * a.G,
                                 s.t.start + s.tok0 + st * tpt, bars + 8 * kQFull);
         }
-        ++pieces;
+        __syncwarp();
+        ++queries;
         for (int t = s.a; t < s.b; ++t, ++tiles, pos += 2) {
             const uint32_t slot = pos % C::kSlots, bar = bars + 8 * (kRing + slot), dst = ring + slot * C::kKvBytes;
             pages.reach(a, s, t, true, lane);
@@ -206,7 +221,7 @@ __device__ __forceinline__ void k_role(const AttendArgs &a, const CUtensorMap *q
             int pid[4];
 #pragma unroll
             for (int pg = 0; pg < 4; ++pg) pid[pg] = pages.of(t, pg);
-            ok = warp_wait(bar + 8 * C::kSlots, (pos / C::kSlots & 1) ^ 1, gave_up, a.status);
+            ok = warp_wait(bar + 8 * C::kSlots, (pos / C::kSlots & 1) ^ 1, gave_up, &a.ctl->status);
             if (!ok) break;
             if (chosen) {
                 ctl->mask[tiles % C::kMasks] = mask;
@@ -228,11 +243,10 @@ __device__ __forceinline__ void k_role(const AttendArgs &a, const CUtensorMap *q
             __syncwarp();
         }
     }
-    // no copy may be in flight when the CTA's shared memory goes away
-    if (!ok) {
-        for (uint32_t p = pos > C::kSlots ? pos - C::kSlots : 0; p < pos; p += 2)
-            mbar_wait(bars + 8 * (kRing + p % C::kSlots), p / C::kSlots & 1);
-        if (pieces) mbar_wait(bars + 8 * kQFull, (pieces - 1) & 1);
+    leave_ring<D>(ok, pos, 0, bars, gave_up, a);
+    if (queries) {
+        if (ok) warp_wait(bars + 8 * kQEmpty, (queries - 1) & 1, gave_up, &a.ctl->status);
+        else mbar_wait(bars + 8 * kQFull, (queries - 1) & 1);
     }
 }
 
@@ -241,13 +255,13 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     const AttendWork work(a);
-    Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
     Segment s;
     Pages pages;
     uint32_t pos = 1;
     const bool chosen = elect_one();
     bool ok = true;
-    while (ok && next_segment(a, work, ctl->pieces, c, s)) {
+    Walk<AttendWork> walk(work, a.B, a.H_kv, a.ctl, &ctl->queue, gave_up, lane);
+    while (ok && next_segment(walk, s)) {
         const int stop = s.t.past + s.t.n;                                 // tokens of the request
         pages.begin(a, s, s.a, false, lane);
         for (int t = s.a; t < s.b; ++t, pos += 2) {
@@ -256,7 +270,7 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v
             int pid[4];
 #pragma unroll
             for (int pg = 0; pg < 4; ++pg) pid[pg] = pages.of(t, pg);
-            ok = warp_wait(bar + 8 * C::kSlots, (pos / C::kSlots & 1) ^ 1, gave_up, a.status);
+            ok = warp_wait(bar + 8 * C::kSlots, (pos / C::kSlots & 1) ^ 1, gave_up, &a.ctl->status);
             if (!ok) break;
             // The group that holds the end of the request is copied row by row: what lies behind the end may be anything, and
             // a weight of zero would not hide a NaN.
@@ -296,9 +310,7 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v
             __syncwarp();
         }
     }
-    if (!ok)
-        for (uint32_t p = pos > C::kSlots ? pos - C::kSlots : 1; p < pos; p += 2)
-            mbar_wait(bars + 8 * (kRing + p % C::kSlots), p / C::kSlots & 1);
+    leave_ring<D>(ok, pos, 1, bars, gave_up, a);
 }
 
 // ---- products ----------------------------------------------------------------------
@@ -310,25 +322,19 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v
 // warp for both streams let the tensor cores run dry at every wait.  The whole warp walks the list, so that addresses stay in
 // uniform registers; one elected lane issues.
 template <int D, int ST>
-__device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars) {
+__device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     const uint32_t tmem_s = ctl->tmem + ST * kTile, tmem_o = ctl->tmem + C::kTmemO + ST * D;
     const AttendWork work(a);
-    Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
     Segment s = {};
-    uint32_t pos = 0, pieces = 0, o_used = 0, n = 0;                       // n: steps so far
+    uint32_t pos = 0, queries = 0, o_used = 0, n = 0;                      // n: steps so far
     bool any = false;
     const bool chosen = elect_one();
-    auto wait = [&](int bar, uint32_t parity) { return warp_wait(bars + 8 * bar, parity & 1, gave_up, a.status); };
-    auto full = [&](uint32_t at) { return wait(kRing + at % C::kSlots, at / C::kSlots); };
+    auto wait = [&](int bar, uint32_t parity) { return warp_wait(bars + 8 * bar, parity & 1, gave_up, &a.ctl->status); };
     auto slot = [&](uint32_t at) { return ring + at % C::kSlots * C::kKvBytes; };
-    // a ring slot is free when both streams have let it go; a tile of one stream alone is let go twice by it
-    auto let_go = [&](uint32_t at) {
-        const uint32_t bar = bars + 8 * (kRing + C::kSlots + at % C::kSlots);
-        mma_commit(bar);
-        if (s.alt) mma_commit(bar);
-    };
+    // a ring slot is free when both streams have let it go
+    auto let_go = [&](uint32_t at) { mma_commit(bars + 8 * (kRing + C::kSlots + at % C::kSlots)); };
     // S = Q K^T of the n-th step
     auto scores = [&](uint32_t at, uint32_t n) {
         const uint64_t qd = smem_operand(q_smem + (s.alt ? 0 : ST * C::kTileBytes), 16, 1024), kd = smem_operand(slot(at), 16, 1024);
@@ -342,6 +348,7 @@ __device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, u
             mma_commit(bars + 8 * (kSFull + 2 * ST + (n & 1)));
             let_go(at);
         }
+        __syncwarp();
     };
     // O += P V
     auto values = [&](uint32_t at, uint32_t n, bool accumulate, bool last) {
@@ -351,50 +358,58 @@ __device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, u
         if (chosen) {
 #pragma unroll
             for (int k = 0; k < kKv / 16; ++k) mma_ts(tmem_o, p + k * 8, vd + k * (kPage * D * 2 >> 4), mma_instr(D, true), accumulate || k > 0);
-            mma_commit(bars + 8 * (kODone + ST));
-            if (last) mma_commit(bars + 8 * (kOLast + ST));
+            mma_commit(bars + 8 * ((last ? kOLast : kODone) + ST));
             let_go(at);
         }
+        __syncwarp();
     };
-    while (next_segment(a, work, ctl->pieces, c, s)) {
+    bool ok = true;
+    Walk<AttendWork> walk(work, a.B, a.H_kv, a.ctl, &ctl->queue, gave_up, lane);
+    while (ok && next_segment(walk, s)) {
         const int steps = ST ? s.steps1 : s.steps0;
-        const uint32_t stride = s.alt ? 4 : 2;
-        uint32_t at = pos + (s.alt ? 2 * ST : 0);                          // ring position of the step's K tile; its V tile follows
-        if (!wait(kQFull, pieces)) break;
-        ++pieces;
-        bool ok = true;
+        const int tiles = s.b - s.a, stride = s.alt ? 2 : 1, first = s.alt ? ST : 0;   // this stream's tiles: first, first + stride, ...
+        // Every tile's barriers are waited for, in order, and the tiles of the other stream let go at once: a barrier tells its
+        // phases apart by parity alone, so a warp that left one out could take the phase before for the one it waits for.
+        auto reach = [&](int &next, int last, uint32_t v) {
+            for (; next <= last; ++next) {
+                const uint32_t at = pos + 2 * next + v;
+                if (!wait(kRing + at % C::kSlots, at / C::kSlots)) return false;
+                const bool mine = s.alt ? (next & 1) == ST : next < steps;
+                if (!mine && chosen) mbar_arrive(bars + 8 * (kRing + C::kSlots + at % C::kSlots));
+                __syncwarp();
+            }
+            return true;
+        };
+        int k_next = 0, v_next = 0;
+        ok = wait(kQFull, queries);
+        ++queries;
         for (int u = 0; u < 2 && u < steps && ok; ++u)
-            if ((ok = full(at + u * stride))) scores(at + u * stride, n + u);
+            if ((ok = reach(k_next, first + u * stride, 0))) scores(pos + 2 * (first + u * stride), n + u);
         any = any || steps > 0;
         if (!ok) break;
         if (chosen && steps <= 2) {
             if (steps > 0) mma_commit(bars + 8 * kQEmpty);
             else mbar_arrive(bars + 8 * kQEmpty);
         }
-        for (int u = 0; u < steps && ok; ++u, ++n, at += stride) {
+        __syncwarp();
+        for (int u = 0, t = first; u < steps && ok; ++u, ++n, t += stride) {
             // everything that can be waited for early comes before the wait for the weights
             const bool more = u + 2 < steps;
-            ok = full(at + 1) && (!more || full(at + 2 * stride));
+            ok = reach(v_next, t, 1) && (!more || reach(k_next, t + 2 * stride, 0));
             if (ok && u == 0) {          // the epilogue of the stream's last piece has read O
                 ok = wait(kOFree + ST, o_used ^ 1);
                 o_used ^= 1;
             }
             ok = ok && wait(kPReady + 2 * ST + (n & 1), n >> 1);
             if (!ok) break;
-            values(at + 1, n, u > 0, u + 1 == steps);
-            if (more) scores(at + 2 * stride, n);
+            values(pos + 2 * t + 1, n, u > 0, u + 1 == steps);
+            if (more) scores(pos + 2 * (t + 2 * stride), n);
             if (chosen && u + 3 == steps) mma_commit(bars + 8 * kQEmpty);   // the last product with Q is on its way
+            __syncwarp();
         }
-        // tiles that only the other stream sees
-        if (ok && !s.alt)
-            for (int i = steps; i < s.b - s.a && ok; ++i, at += 2)
-                for (uint32_t kv = at; kv < at + 2 && ok; ++kv) {
-                    ok = full(kv);
-                    if (ok && chosen) mbar_arrive(bars + 8 * (kRing + C::kSlots + kv % C::kSlots));
-                }
+        while (ok && v_next < tiles) ok = reach(k_next, v_next, 0) && reach(v_next, v_next, 1);
         __syncwarp();
-        if (!ok) break;
-        pos += 2u * (s.b - s.a);
+        pos += 2u * tiles;
     }
     if (any) {                           // nothing may be running when tensor memory goes away
         if (chosen) mma_commit(bars + 8 * (kDrain + ST));
@@ -407,8 +422,8 @@ __device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, u
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
 template <int D>
-__device__ __forceinline__ float *partial_slot(const AttendArgs &a, int cta, int kind, int st) {
-    return a.partials + (size_t)((cta * 2 + kind) * 2 + st) * Cfg<D>::kSlotFloats;
+__device__ __forceinline__ float *partial_slot(const AttendArgs &a, int piece, int kind, int st) {
+    return a.partials + (size_t)((piece * 2 + kind) * 2 + st) * Cfg<D>::kSlotFloats;
 }
 
 // Merges the partial results of one query tile and writes its output.  128 threads; warp w takes rows w, w + 4, ...
@@ -484,16 +499,17 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
     const uint32_t t_s = ctl->tmem + lanes + st * kTile, t_o = ctl->tmem + lanes + C::kTmemO + st * D;
     const float sl = a.scale_log2;
     const AttendWork work(a);
-    Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
     Segment s;
     uint32_t step = 0, tiles = 0, verdicts = 0, swaps = 0, ends = 0;
+    uint32_t inner = 0;                                                    // steps so far that were not a piece's last of an item
     // both warpgroups have come here
     auto swap_sync = [&] {
         __syncwarp();
         if (lane == 0) mbar_arrive(bars + 8 * kSwap);
-        return warp_wait(bars + 8 * kSwap, swaps++ & 1, gave_up, a.status);
+        return warp_wait(bars + 8 * kSwap, swaps++ & 1, gave_up, &a.ctl->status);
     };
-    while (next_segment(a, work, ctl->pieces, c, s)) {
+    Walk<AttendWork> walk(work, a.B, a.H_kv, a.ctl, &ctl->queue, gave_up, lane);
+    while (next_segment(walk, s)) {
         const int tok = s.tok0 + (s.alt ? 0 : st * tpt);                   // the tile's first new token
         const int ntok = min(tpt, s.tok0 + s.ntok - tok);
         const int q = min(row / a.G, ntok - 1);
@@ -505,7 +521,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
         for (int u = 0; u < steps; ++u, ++step) {
             const int rel = s.alt ? 2 * u + st : u, first = (s.a + rel) * kKv;
             const uint32_t buf = 2 * st + (step & 1), t_p = t_s + (step & 1) * kKv;
-            if (!warp_wait(bars + 8 * (kSFull + buf), step >> 1 & 1, gave_up, a.status)) return;
+            if (!warp_wait(bars + 8 * (kSFull + buf), step >> 1 & 1, gave_up, &a.ctl->status)) return;
             tc_fence_after();
             float x[kKv];
             tmem_ld32(t_p, x);
@@ -532,7 +548,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
                 if (u > 0) {
                     // O + P V of the last step; the one before is complete (these scores were issued behind it), so the barrier's
                     // parity says which of two phases it is in
-                    if (!warp_wait(bars + 8 * (kODone + st), (step - 1) & 1, gave_up, a.status)) return;
+                    if (!warp_wait(bars + 8 * (kODone + st), (inner + u - 1) & 1, gave_up, &a.ctl->status)) return;
                     tc_fence_after();
 #pragma unroll 1
                     for (int k = 0; k < D; k += 32) {
@@ -562,10 +578,12 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bars + 8 * (kPReady + buf));
+            __syncwarp();
         }
         tiles += s.b - s.a;
+        inner += max(steps - 1, 0);
         if (steps > 0) {
-            if (!warp_wait(bars + 8 * (kOLast + st), ends++ & 1, gave_up, a.status)) return;
+            if (!warp_wait(bars + 8 * (kOLast + st), ends++ & 1, gave_up, &a.ctl->status)) return;
             tc_fence_after();
         }
 
@@ -600,11 +618,12 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bars + 8 * (kOFree + st));
+            __syncwarp();
             continue;
         }
         const int kind = s.a == 0;
         if (steps > 0 || !s.alt) {
-            float *slot = partial_slot<D>(a, blockIdx.x, kind, st);
+            float *slot = partial_slot<D>(a, s.piece, kind, st);
             if (steps > 0) {
 #pragma unroll
                 for (int k = 0; k < D; k += 32) {
@@ -621,6 +640,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bars + 8 * (kOFree + st));
+                __syncwarp();
             }
             __stcg(slot + kTile * D + row, m2);
             __stcg(slot + kTile * D + kTile + row, l);
@@ -628,20 +648,20 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
         if (whole) {
             // alt, all KV tiles in this CTA: the two warpgroups exchange their results and merge half of the rows each
             if (!swap_sync()) return;
-            const float *s0 = partial_slot<D>(a, blockIdx.x, kind, 0), *s1 = partial_slot<D>(a, blockIdx.x, kind, 1);
+            const float *s0 = partial_slot<D>(a, s.piece, kind, 0), *s1 = partial_slot<D>(a, s.piece, kind, 1);
             merge_rows<D>(a, s, st, st * 4 + warp, 8, [&](auto f) { f(s0); f(s1); }, lane);
             if (!swap_sync()) return;                                      // the slots may be written again
             continue;
         }
         if (steps == 0 && s.alt) continue;
-        // the CTAs of the item: from the one that begins it to the one that ends it
-        const int from = first_cta(ctl->pieces, s.item);
-        uint32_t *ticket = a.tickets + 2 * from + (s.alt ? 0 : st);
+        const int from = first_piece_of(a.ctl, s.item, s.piece);
+        uint32_t *ticket = a.ctl->tickets + 2 * from + (s.alt ? 0 : st);
         __threadfence();
         __syncwarp();
         if (lane == 0) mbar_arrive(bars + 8 * (kAll + st));
+        __syncwarp();
         if (warp == 0) {
-            if (!warp_wait(bars + 8 * (kAll + st), verdicts & 1, gave_up, a.status)) return;
+            if (!warp_wait(bars + 8 * (kAll + st), verdicts & 1, gave_up, &a.ctl->status)) return;
             if (lane == 0) {
                 __threadfence();
                 const uint32_t add = s.alt ? steps : s.b - s.a;
@@ -652,12 +672,12 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
             }
             __syncwarp();
         }
-        if (!warp_wait(bars + 8 * (kVerdict + st), verdicts & 1, gave_up, a.status)) return;
+        if (!warp_wait(bars + 8 * (kVerdict + st), verdicts & 1, gave_up, &a.ctl->status)) return;
         ++verdicts;
         if (ctl->last[st]) {
             __threadfence();
             auto each = [&](auto f) {
-                each_cta(ctl->pieces, s.item, s.nkv, from, [&](int y, int ya, int yb) {
+                each_piece_of(a.ctl, s.item, s.nkv, from, lane, [&](int y, int ya, int yb) {
                     f((const float *)partial_slot<D>(a, y, ya == 0, s.alt ? 0 : st));
                     if (s.alt && yb - ya > 1) f((const float *)partial_slot<D>(a, y, ya == 0, 1));
                 });
@@ -679,7 +699,7 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     const uint32_t bars = smem_u32(ctl->bars);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (base & 1023u) {                  // the swizzle pattern hangs on the address
-        if (threadIdx.x == 0) atomicOr(a.status, SE_DEV_WAIT_TIMEOUT);
+        if (threadIdx.x == 0) atomicOr(&a.ctl->status, SE_DEV_WAIT_TIMEOUT);
         return;
     }
 
@@ -703,11 +723,12 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
             mbar_init(bars + 8 * (kRing + i), 1);
             mbar_init(bars + 8 * (kRing + C::kSlots + i), 2);
         }
+        ctl->queue.init(11);
         mbar_fence_init();
         ctl->gave_up = 0;
     }
     if (warp == kMmaWarp) tmem_alloc(smem_u32(&ctl->tmem), 512);
-    cut_work(AttendWork(a), a.B, a.H_kv, a.status, &ctl->pieces, smem + 2 * C::kTileBytes);
+    const int n_pieces = cut_work(AttendWork(a), a.B, a.H_kv, a.ctl, smem + 2 * C::kTileBytes);
     // query rows that no tensor copy fills (G does not divide 128) stay zero
     for (int i = threadIdx.x; i < 2 * C::kTileBytes / 16; i += kThreads)
         reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
@@ -719,10 +740,10 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     if (warp < 8) {
         softmax_role<D>(a, ctl, bars, warp >> 2);
     } else {
-        if (warp == kKWarp) k_role<D>(a, &q_map, &k_map, &k_wide, ctl, base, base + 2 * C::kTileBytes, bars, lane);
+        if (warp == kKWarp) k_role<D>(a, &q_map, &k_map, &k_wide, ctl, base, base + 2 * C::kTileBytes, bars, n_pieces, lane);
         else if (warp == kVWarp) v_role<D>(a, &v_map, ctl, base + 2 * C::kTileBytes, bars, lane);
-        else if (warp == kMmaWarp) mma_role<D, 0>(a, ctl, base, base + 2 * C::kTileBytes, bars);
-        else if (warp == kMmaWarp + 1) mma_role<D, 1>(a, ctl, base, base + 2 * C::kTileBytes, bars);
+        else if (warp == kMmaWarp) mma_role<D, 0>(a, ctl, base, base + 2 * C::kTileBytes, bars, lane);
+        else if (warp == kMmaWarp + 1) mma_role<D, 1>(a, ctl, base, base + 2 * C::kTileBytes, bars, lane);
         __syncwarp();
     }
     tc_fence_before();
@@ -754,8 +775,8 @@ cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t 
     a.cu = c.cu_seqlens, a.seq_lens = c.seq_lens, a.page_table = c.page_table;
     a.v = static_cast<const uint16_t *>(c.v), a.v_stride = c.v_stride;
     a.out = static_cast<uint16_t *>(c.out), a.lse = c.lse;
-    a.status = reinterpret_cast<uint32_t *>(c.workspace), a.tickets = reinterpret_cast<uint32_t *>(c.workspace + 256);
-    a.partials = reinterpret_cast<float *>(c.workspace + kControlBytes);
+    a.ctl = reinterpret_cast<PromptControl *>(c.workspace);
+    a.partials = reinterpret_cast<float *>(c.workspace + kPromptControlBytes);
     a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.G = G, a.T = c.total_tokens, a.max_pages = p.max_pages;
     a.P_phys = p.num_phys_pages, a.scale_log2 = effective_scale(p) * kLog2e;
     auto kern = attend_kernel<D>;
@@ -769,10 +790,10 @@ cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t 
 
 }  // namespace
 
-size_t prompt_workspace_control_bytes() { return kControlBytes; }
+size_t prompt_workspace_control_bytes() { return kPromptControlBytes; }
 size_t prompt_workspace_bytes(const se_params &p) {
     const size_t slot = ((size_t)kTile * p.D + 2 * kTile) * sizeof(float);
-    return kControlBytes + (size_t)kPromptCtas * 4 * slot;
+    return kPromptControlBytes + (size_t)kMaxPieces * 4 * slot;
 }
 
 cudaError_t launch_prompt_attend(const se_params &p, const AttendCall &c, cudaStream_t stream) {

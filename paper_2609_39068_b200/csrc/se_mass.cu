@@ -27,7 +27,6 @@ constexpr int kThreads = kPromptThreads;   // 2 summing warpgroups, copy warp, p
 constexpr int kCopyWarp = 8, kMmaWarp = 9, kLseWarp = 10;
 constexpr int kTile = 128;             // cached tokens of a tile, query rows of a tile
 constexpr int kLseSlots = 2;
-constexpr int kControlBytes = 2048;    // status word, tickets (layout shared with the attention kernel)
 
 template <int D>
 struct Cfg {
@@ -41,7 +40,7 @@ struct MassArgs {
     const int32_t *cu, *seq_lens, *page_table;
     const float *lse;
     float *accum, *partials;
-    uint32_t *status, *tickets;
+    PromptControl *ctl;
     int B, H_q, H_kv, G, T, max_pages, P_phys;
     float scale_log2;
 };
@@ -53,7 +52,7 @@ template <int D>
 struct Control {
     uint64_t bars[kRing + 2 * Cfg<D>::kSlots];
     alignas(16) float lse[kLseSlots][kTile];   // -lse log2 e of the query tiles' rows, -inf for rows that count for nothing
-    Pieces pieces;
+    PieceQueue queue;
     int last[2];
     int gave_up;
     uint32_t tmem;
@@ -89,20 +88,22 @@ struct Segment {
     int r, h, item;
     TokenRange t;
     int pos0;              // first cached token of the item
-    int units, a, b;       // query tiles: all of the item's, this CTA's
+    int piece, units, a, b;   // piece, query tiles: all of the item's, the piece's
     int q0;                // the item's first query tile within the request
     int skip1;             // units before the second tile of cached tokens is seen
 };
 
-__device__ __forceinline__ bool next_segment(const MassArgs &a, const MassWork &w, const Pieces &p, Cursor &c, Segment &s) {
-    if (piece_done(w, a.B, p, c)) return false;
+__device__ __forceinline__ bool next_segment(Walk<MassWork> &walk, Segment &s) {
+    if (!walk.item()) return false;
+    const Cursor &c = walk.c;
+    const MassWork &w = walk.w;
     s.r = c.r, s.h = c.h, s.item = c.item, s.t = c.t;
     s.pos0 = c.i * 2 * kTile;
     s.units = w.units(c.t, c.i);
-    s.a = c.unit, s.b = piece_end(c, p, s.units);
+    s.a = c.unit, s.b = piece_end(c, s.units), s.piece = c.piece;
     s.q0 = w.blind(c.t, s.pos0) / w.tpt;
     s.skip1 = s.pos0 + kTile >= c.t.past + c.t.n ? s.units : w.blind(c.t, s.pos0 + kTile) / w.tpt - s.q0;
-    next_item(w, a.B, a.H_kv, c);
+    walk.next();
     return true;
 }
 
@@ -111,7 +112,7 @@ __device__ __forceinline__ int group_page(const MassArgs &a, const Segment &s, i
     if (g * kPage >= s.t.past + s.t.n) return -1;
     const int pid = a.page_table[(size_t)s.r * a.max_pages + g];
     if (pid >= a.P_phys) {
-        if (report) atomicOr(a.status, SE_DEV_BAD_PAGE_ID);
+        if (report) atomicOr(&a.ctl->status, SE_DEV_BAD_PAGE_ID);
         return -1;
     }
     return pid < 0 ? -1 : pid;
@@ -119,46 +120,59 @@ __device__ __forceinline__ int group_page(const MassArgs &a, const Segment &s, i
 
 template <int D>
 __device__ __forceinline__ void copy_role(const MassArgs &a, const CUtensorMap *q_map, const CUtensorMap *k_map, Control<D> *ctl,
-                                          uint32_t k_smem, uint32_t ring, uint32_t bars, int lane) {
+                                          uint32_t k_smem, uint32_t ring, uint32_t bars, int n_pieces, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     const MassWork work(a);
-    Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
+    Walk<MassWork> walk(work, a.B, a.H_kv, a.ctl, &ctl->queue, gave_up, lane, n_pieces);
     Segment s;
     uint32_t pos = 0, pairs = 0;
+    const bool chosen = elect_one();
     bool ok = true;
-    while (ok && next_segment(a, work, ctl->pieces, c, s)) {
-        // K: 16 groups of 16 tokens; a lane brings a group's 64 channels, D = 128 in two turns.  Absent groups come from behind
-        // the tensor's last row, which reads as zeros.
+    while (ok && next_segment(walk, s)) {
+        // K: 16 groups of 16 tokens.  Absent groups come from behind the tensor's last row, which reads as zeros.
         const int pid = group_page(a, s, s.pos0 / kPage + (lane & 15), lane < 16);
+        const int z = pid >= 0 ? (pid * a.H_kv + s.h) * kPage : a.P_phys * a.H_kv * kPage;
         const uint32_t kb = pairs & 1, kbar = bars + 8 * (kKFull + kb);
-        ok = warp_wait(bars + 8 * (kKEmpty + kb), (pairs >> 1 & 1) ^ 1, gave_up, a.status);
+        ok = warp_wait(bars + 8 * (kKEmpty + kb), (pairs >> 1 & 1) ^ 1, gave_up, &a.ctl->status);
         if (!ok) break;
-        if (lane == 0) mbar_expect_tx(kbar, 2 * C::kTileBytes);
-        __syncwarp();
-        {
-            const int g = lane & 15, half = lane >> 4;
-            if (half < C::kHalves)
-                tma_load_3d(k_smem + (2 * kb + (g >> 3)) * C::kTileBytes + half * (kTile * 128) + (g & 7) * (kPage * 128), k_map,
-                            half * 64, 0, pid >= 0 ? (pid * a.H_kv + s.h) * kPage : a.P_phys * a.H_kv * kPage, kbar);
+        if (chosen) mbar_expect_tx(kbar, 2 * C::kTileBytes);
+#pragma unroll
+        for (int g = 0; g < 16; ++g) {
+            const int row = __shfl_sync(kFull, z, g);
+            if (chosen) {
+#pragma unroll
+                for (int half = 0; half < C::kHalves; ++half)
+                    tma_load_3d(k_smem + (2 * kb + (g >> 3)) * C::kTileBytes + half * (kTile * 128) + (g & 7) * (kPage * 128), k_map,
+                                half * 64, 0, row, kbar);
+            }
+            __syncwarp();
         }
         ++pairs;
         for (int u = s.a; u < s.b; ++u, ++pos) {
             const uint32_t slot = pos % C::kSlots, bar = bars + 8 * (kRing + slot);
-            ok = warp_wait(bar + 8 * C::kSlots, (pos / C::kSlots & 1) ^ 1, gave_up, a.status);
+            ok = warp_wait(bar + 8 * C::kSlots, (pos / C::kSlots & 1) ^ 1, gave_up, &a.ctl->status);
             if (!ok) break;
-            if (lane == 0) mbar_expect_tx(bar, work.tpt * a.G * D * 2);
+            if (chosen) {
+                mbar_expect_tx(bar, work.tpt * a.G * D * 2);
+#pragma unroll
+                for (int half = 0; half < C::kHalves; ++half)
+                    tma_load_3d(ring + slot * C::kTileBytes + half * (kTile * 128), q_map, half * 64, s.h * a.G,
+                                s.t.start + (s.q0 + u) * work.tpt, bar);
+            }
             __syncwarp();
-            if (lane < C::kHalves)
-                tma_load_3d(ring + slot * C::kTileBytes + lane * (kTile * 128), q_map, lane * 64, s.h * a.G,
-                            s.t.start + (s.q0 + u) * work.tpt, bar);
         }
     }
-    // no copy may be in flight when the CTA's shared memory goes away
-    if (!ok) {
-        const uint32_t first = pos > C::kSlots ? pos - C::kSlots : 0;
-        for (uint32_t p = first; p < pos; ++p) mbar_wait(bars + 8 * (kRing + p % C::kSlots), p / C::kSlots & 1);
-        for (uint32_t p = pairs > 2 ? pairs - 2 : 0; p < pairs; ++p) mbar_wait(bars + 8 * (kKFull + (p & 1)), p >> 1 & 1);
+    // nothing may still be on its way to the CTA's shared memory when the CTA ends: copies, and the products' arrivals on the
+    // barriers of the tiles they have let go
+    for (uint32_t p = pos > C::kSlots ? pos - C::kSlots : 0; p < pos; ++p) {
+        const uint32_t bar = bars + 8 * (kRing + p % C::kSlots), parity = p / C::kSlots & 1;
+        if (ok) ok = warp_wait(bar + 8 * C::kSlots, parity, gave_up, &a.ctl->status);
+        else mbar_wait(bar, parity);
+    }
+    for (uint32_t p = pairs > 2 ? pairs - 2 : 0; p < pairs; ++p) {
+        if (ok) ok = warp_wait(bars + 8 * (kKEmpty + (p & 1)), p >> 1 & 1, gave_up, &a.ctl->status);
+        else mbar_wait(bars + 8 * (kKFull + (p & 1)), p >> 1 & 1);
     }
 }
 
@@ -167,11 +181,11 @@ template <int D>
 __device__ __forceinline__ void lse_role(const MassArgs &a, Control<D> *ctl, uint32_t bars, int lane) {
     volatile int *gave_up = &ctl->gave_up;
     const MassWork work(a);
-    Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
+    Walk<MassWork> walk(work, a.B, a.H_kv, a.ctl, &ctl->queue, gave_up, lane);
     Segment s;
     uint32_t tiles = 0;
     const int live = work.tpt * a.G;
-    while (next_segment(a, work, ctl->pieces, c, s)) {
+    while (next_segment(walk, s)) {
         float x[4];
         auto fetch = [&](int u) {
             const int tok = (s.q0 + u) * work.tpt;
@@ -184,7 +198,7 @@ __device__ __forceinline__ void lse_role(const MassArgs &a, Control<D> *ctl, uin
         fetch(s.a);
         for (int u = s.a; u < s.b; ++u, ++tiles) {
             const uint32_t slot = tiles % kLseSlots;
-            if (!warp_wait(bars + 8 * (kLseEmpty + slot), (tiles / kLseSlots & 1) ^ 1, gave_up, a.status)) return;
+            if (!warp_wait(bars + 8 * (kLseEmpty + slot), (tiles / kLseSlots & 1) ^ 1, gave_up, &a.ctl->status)) return;
 #pragma unroll
             for (int k = 0; k < 4; ++k) ctl->lse[slot][lane + 32 * k] = x[k] == -INFINITY ? -INFINITY : -x[k] * kLog2e;
             __syncwarp();
@@ -195,45 +209,52 @@ __device__ __forceinline__ void lse_role(const MassArgs &a, Control<D> *ctl, uin
 }
 
 template <int D>
-__device__ __forceinline__ void mma_role(const MassArgs &a, Control<D> *ctl, uint32_t k_smem, uint32_t ring, uint32_t bars) {
+__device__ __forceinline__ void mma_role(const MassArgs &a, Control<D> *ctl, uint32_t k_smem, uint32_t ring, uint32_t bars, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     constexpr uint32_t kInstr = mma_instr(kTile, false);
     const uint32_t tmem = ctl->tmem;
     const MassWork work(a);
-    Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
+    Walk<MassWork> walk(work, a.B, a.H_kv, a.ctl, &ctl->queue, gave_up, lane);
     Segment s;
     uint32_t pos = 0, pairs = 0, step0 = 0, step1 = 0;
+    const bool chosen = elect_one();
     bool ok = true, any = false;
-    while (ok && next_segment(a, work, ctl->pieces, c, s)) {
+    while (ok && next_segment(walk, s)) {
         const uint32_t kb = pairs & 1;
-        ok = role_wait(bars + 8 * (kKFull + kb), pairs >> 1 & 1, gave_up, a.status);
+        ok = warp_wait(bars + 8 * (kKFull + kb), pairs >> 1 & 1, gave_up, &a.ctl->status);
         ++pairs;
         for (int u = s.a; u < s.b && ok; ++u, ++pos) {
             const uint32_t slot = pos % C::kSlots;
-            ok = role_wait(bars + 8 * (kRing + slot), pos / C::kSlots & 1, gave_up, a.status);
+            ok = warp_wait(bars + 8 * (kRing + slot), pos / C::kSlots & 1, gave_up, &a.ctl->status);
             const uint64_t qd = smem_operand(ring + slot * C::kTileBytes, 16, 1024);
             for (int st = 0; st < 2 && ok; ++st) {
                 if (st == 1 && u < s.skip1) continue;
                 const uint32_t step = st ? step1++ : step0++, buf = 2 * st + (step & 1);
-                ok = role_wait(bars + 8 * (kSFree + buf), (step >> 1 & 1) ^ 1, gave_up, a.status);
+                ok = warp_wait(bars + 8 * (kSFree + buf), (step >> 1 & 1) ^ 1, gave_up, &a.ctl->status);
                 if (!ok) break;
                 tc_fence_after();
                 const uint64_t kd = smem_operand(k_smem + (2 * kb + st) * C::kTileBytes, 16, 1024);
+                if (chosen) {
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t off = (k / 4) * (kTile * 128 >> 4) + (k % 4) * 2;
-                    mma_ss(tmem + buf * kTile, kd + off, qd + off, kInstr, k > 0);
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t off = (k / 4) * (kTile * 128 >> 4) + (k % 4) * 2;
+                        mma_ss(tmem + buf * kTile, kd + off, qd + off, kInstr, k > 0);
+                    }
+                    mma_commit(bars + 8 * (kSFull + buf));
                 }
-                mma_commit(bars + 8 * (kSFull + buf));
+                __syncwarp();
                 any = true;
             }
-            if (ok) mma_commit(bars + 8 * (kRing + C::kSlots + slot));
+            if (ok && chosen) mma_commit(bars + 8 * (kRing + C::kSlots + slot));
+            __syncwarp();
         }
-        if (ok) mma_commit(bars + 8 * (kKEmpty + kb));
+        if (ok && chosen) mma_commit(bars + 8 * (kKEmpty + kb));
+        __syncwarp();
     }
     if (any) {                           // nothing may be running when tensor memory goes away
-        mma_commit(bars + 8 * kDrain);
+        if (chosen) mma_commit(bars + 8 * kDrain);
+        __syncwarp();
         mbar_wait(bars + 8 * kDrain, 0);
     }
 }
@@ -245,23 +266,23 @@ __device__ __forceinline__ void sum_role(const MassArgs &a, Control<D> *ctl, uin
     const uint32_t t_s = ctl->tmem + ((uint32_t)(warp * 32) << 16) + 2 * st * kTile;
     const float2 sl = make_float2(a.scale_log2, a.scale_log2);
     const MassWork work(a);
-    Cursor c = first_piece(work, a.B, a.H_kv, ctl->pieces);
+    Walk<MassWork> walk(work, a.B, a.H_kv, a.ctl, &ctl->queue, gave_up, lane);
     Segment s;
     uint32_t step = 0, tiles = 0, verdicts = 0;
-    while (next_segment(a, work, ctl->pieces, c, s)) {
+    while (next_segment(walk, s)) {
         const int pos = s.pos0 + st * kTile + row;                         // the thread's cached token
         const int pid = group_page(a, s, pos / kPage, false);
         float2 s0 = make_float2(0.f, 0.f), s1 = s0;
         for (int u = s.a; u < s.b; ++u, ++tiles) {
             const uint32_t slot = tiles % kLseSlots;
-            if (!warp_wait(bars + 8 * (kLseFull + slot), tiles / kLseSlots & 1, gave_up, a.status)) return;
+            if (!warp_wait(bars + 8 * (kLseFull + slot), tiles / kLseSlots & 1, gave_up, &a.ctl->status)) return;
             if (st == 0 || u >= s.skip1) {
                 const int tok = (s.q0 + u) * work.tpt;                     // the tile's first new token
                 // columns [from, to) count: the queries at or behind the cached token, and of this request
                 const int from = min(max(pos - s.t.past - tok, 0), kTile) * a.G, to = (s.t.n - tok) * a.G;
                 const bool masked = __any_sync(kFull, from > 0) || to < work.tpt * a.G;
                 const uint32_t buf = step & 1;
-                if (!warp_wait(bars + 8 * (kSFull + 2 * st + buf), step >> 1 & 1, gave_up, a.status)) return;
+                if (!warp_wait(bars + 8 * (kSFull + 2 * st + buf), step >> 1 & 1, gave_up, &a.ctl->status)) return;
                 ++step;
                 tc_fence_after();
                 const float4 *nl = reinterpret_cast<const float4 *>(ctl->lse[slot]);
@@ -276,6 +297,7 @@ __device__ __forceinline__ void sum_role(const MassArgs &a, Control<D> *ctl, uin
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(bars + 8 * (kSFree + 2 * st + buf));
+                        __syncwarp();
                     }
                     float *y = x[k & 1];
                     if (masked) {
@@ -295,6 +317,7 @@ __device__ __forceinline__ void sum_role(const MassArgs &a, Control<D> *ctl, uin
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(bars + 8 * (kLseEmpty + slot));
+            __syncwarp();
         }
         const float sum = (s0.x + s0.y) + (s1.x + s1.y);
         const size_t at = ((size_t)max(pid, 0) * a.H_kv + s.h) * kPage + pos % kPage;
@@ -303,17 +326,18 @@ __device__ __forceinline__ void sum_role(const MassArgs &a, Control<D> *ctl, uin
             if (pid >= 0 && pos < s.t.past + s.t.n) a.accum[at] += sum;
             continue;
         }
-        auto part = [&](int cta, int kind) { return a.partials + (size_t)((cta * 2 + kind) * 2 + st) * kTile + row; };
-        __stcg(part(blockIdx.x, s.a == 0), sum);
-        const int from = first_cta(ctl->pieces, s.item);
+        auto part = [&](int piece, int kind) { return a.partials + (size_t)((piece * 2 + kind) * 2 + st) * kTile + row; };
+        __stcg(part(s.piece, s.a == 0), sum);
+        const int from = first_piece_of(a.ctl, s.item, s.piece);
         __threadfence();
         __syncwarp();
         if (lane == 0) mbar_arrive(bars + 8 * (kAll + st));
+        __syncwarp();
         if (warp == 0) {
-            if (!warp_wait(bars + 8 * (kAll + st), verdicts & 1, gave_up, a.status)) return;
+            if (!warp_wait(bars + 8 * (kAll + st), verdicts & 1, gave_up, &a.ctl->status)) return;
             if (lane == 0) {
                 __threadfence();
-                uint32_t *ticket = a.tickets + 2 * from + st;
+                uint32_t *ticket = a.ctl->tickets + 2 * from + st;
                 const uint32_t add = s.b - s.a;
                 const bool last = atomicAdd(ticket, add) + add == (uint32_t)s.units;
                 if (last) atomicExch(ticket, 0u);
@@ -322,12 +346,12 @@ __device__ __forceinline__ void sum_role(const MassArgs &a, Control<D> *ctl, uin
             }
             __syncwarp();
         }
-        if (!warp_wait(bars + 8 * (kVerdict + st), verdicts & 1, gave_up, a.status)) return;
+        if (!warp_wait(bars + 8 * (kVerdict + st), verdicts & 1, gave_up, &a.ctl->status)) return;
         ++verdicts;
         if (ctl->last[st]) {
             __threadfence();
             float all = 0.f;
-            each_cta(ctl->pieces, s.item, s.units, from, [&](int y, int ya, int) { all += __ldcg(part(y, ya == 0)); });
+            each_piece_of(a.ctl, s.item, s.units, from, lane, [&](int y, int ya, int) { all += __ldcg(part(y, ya == 0)); });
             if (pid >= 0 && pos < s.t.past + s.t.n) a.accum[at] += all;
         }
     }
@@ -344,7 +368,7 @@ mass_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ C
     const uint32_t bars = smem_u32(ctl->bars), ring = base + 2 * C::kPairs * C::kTileBytes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (base & 1023u) {                  // the swizzle pattern hangs on the address
-        if (threadIdx.x == 0) atomicOr(a.status, SE_DEV_WAIT_TIMEOUT);
+        if (threadIdx.x == 0) atomicOr(&a.ctl->status, SE_DEV_WAIT_TIMEOUT);
         return;
     }
     if (threadIdx.x == 0) {
@@ -364,12 +388,13 @@ mass_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ C
         }
         mbar_init(bars + 8 * kDrain, 1);
         for (int i = 0; i < 2 * C::kSlots; ++i) mbar_init(bars + 8 * (kRing + i), 1);
+        ctl->queue.init(10);
         mbar_fence_init();
         ctl->gave_up = 0;
     }
     if (warp == kMmaWarp) tmem_alloc(smem_u32(&ctl->tmem), 512);
     static_assert(kPieceScratch <= kTiles * C::kTileBytes, "the tiles' memory holds the prefix sums first");
-    cut_work(MassWork(a), a.B, a.H_kv, a.status, &ctl->pieces, smem);
+    const int n_pieces = cut_work(MassWork(a), a.B, a.H_kv, a.ctl, smem);
     __syncthreads();
     // query rows that no tensor copy fills (G does not divide 128) stay zero
     for (int i = threadIdx.x; i < C::kSlots * C::kTileBytes / 16; i += kThreads)
@@ -380,9 +405,9 @@ mass_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ C
     tc_fence_after();
 
     if (warp < 8) sum_role<D>(a, ctl, bars, warp >> 2);
-    else if (warp == kCopyWarp) copy_role<D>(a, &q_map, &k_map, ctl, base, ring, bars, lane);
+    else if (warp == kCopyWarp) copy_role<D>(a, &q_map, &k_map, ctl, base, ring, bars, n_pieces, lane);
     else if (warp == kLseWarp) lse_role<D>(a, ctl, bars, lane);
-    else if (warp == kMmaWarp && lane == 0) mma_role<D>(a, ctl, base, ring, bars);
+    else if (warp == kMmaWarp) mma_role<D>(a, ctl, base, ring, bars, lane);
     __syncwarp();
     tc_fence_before();
     __syncthreads();
@@ -403,8 +428,8 @@ cudaError_t launch_mass(const se_params &p, const AttendCall &c, float *score_ac
     MassArgs a = {};
     a.cu = c.cu_seqlens, a.seq_lens = c.seq_lens, a.page_table = c.page_table;
     a.lse = c.lse, a.accum = score_accum;
-    a.status = reinterpret_cast<uint32_t *>(c.workspace), a.tickets = reinterpret_cast<uint32_t *>(c.workspace + 256);
-    a.partials = reinterpret_cast<float *>(c.workspace + kControlBytes);
+    a.ctl = reinterpret_cast<PromptControl *>(c.workspace);
+    a.partials = reinterpret_cast<float *>(c.workspace + kPromptControlBytes);
     a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.G = G, a.T = c.total_tokens, a.max_pages = p.max_pages;
     a.P_phys = p.num_phys_pages, a.scale_log2 = effective_scale(p) * kLog2e;
     const size_t smem = (2 * C::kPairs + C::kSlots) * C::kTileBytes + sizeof(Control<D>);

@@ -14,10 +14,12 @@ constexpr float kLn2 = 0.69314718055994530942f;
 // ---- tensor memory -----------------------------------------------------------------
 // One warp allocates and later frees; the address of the first column lands in shared memory.
 __device__ __forceinline__ void tmem_alloc(uint32_t smem_dst, uint32_t columns) {
+    __syncwarp();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(columns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void tmem_free(uint32_t addr, uint32_t columns) {
+    __syncwarp();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(columns) : "memory");
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -32,8 +34,10 @@ __device__ __forceinline__ void settle(float *v) {
     for (int i = 0; i < N; ++i) asm volatile("" : "+f"(v[i]));
 }
 
-// 32 consecutive 32-bit columns of the warp's 32 lanes: lane i of the warp gets row i.
+// 32 consecutive 32-bit columns of the warp's 32 lanes: lane i of the warp gets row i.  The access is one of the whole warp,
+// which has to be converged; after a branch on the lane only a warp barrier makes sure of that.
 __device__ __forceinline__ void tmem_ld32(uint32_t addr, float *v) {
+    __syncwarp();
     uint32_t *r = reinterpret_cast<uint32_t *>(v);
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
@@ -45,6 +49,7 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, float *v) {
         : "r"(addr));
 }
 __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t *r) {
+    __syncwarp();
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
         "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr),
@@ -110,30 +115,25 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// Wait of one role of a CTA.  Gives up after kWaitLimitNs, or as soon as another role of the CTA has given up
-// (*gave_up != 0, shared memory); the first one to give up reports it.  False: leave the role's loop.
-__device__ __forceinline__ bool role_wait_slow(uint32_t bar, uint32_t parity, volatile int *gave_up, uint32_t *status) {
-    const unsigned long long t0 = globaltimer_ns();
+// Wait of a warp of a role.  Gives up after 400 million cycles (200 ms at 1.97 GHz), or as soon as another role of the CTA has
+// given up (*gave_up != 0, shared memory); the first one to give up reports it.  False: leave the role's loop.
+// The warp stays together, vote by vote: tensor copies and products take their operands from uniform registers, which
+// lanes that ran ahead of the issuing lane would overwrite, and tensor memory is accessed by whole warps.
+constexpr long long kWaitLimitCycles = 400ll * 1000 * 1000;
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *gave_up, uint32_t *status) {
+    if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
+    const long long t0 = clock64();
     for (;;) {
 #pragma unroll 1
         for (int it = 0; it < 64; ++it)
-            if (mbar_try_wait(bar, parity)) return true;
-        if (*gave_up) return false;
-        if (globaltimer_ns() - t0 > kWaitLimitNs) {
+            if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
+        const bool late = __any_sync(kFull, clock64() - t0 > kWaitLimitCycles);
+        if (late) {
             *gave_up = 1;
             atomicOr(status, SE_DEV_WAIT_TIMEOUT);
-            return false;
         }
+        if (__any_sync(kFull, late || *gave_up != 0)) return false;
     }
-}
-__device__ __forceinline__ bool role_wait(uint32_t bar, uint32_t parity, volatile int *gave_up, uint32_t *status) {
-    if (mbar_try_wait(bar, parity)) return true;
-    return role_wait_slow(bar, parity, gave_up, status);
-}
-
-// the same for a whole warp, which stays together
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *gave_up, uint32_t *status) {
-    return __all_sync(kFull, role_wait(bar, parity, gave_up, status));
 }
 
 __device__ __forceinline__ float ex2(float x) {
