@@ -34,6 +34,7 @@ constexpr int kThreads = kPromptThreads;   // 2 softmax warpgroups, K warp, 2 pr
 constexpr int kKWarp = 8, kMmaWarp = 9, kVWarp = 11;
 constexpr int kTile = 128;             // query rows of a tile
 constexpr int kKv = 64;                // tokens of a KV tile
+constexpr int kMaxParts = 320;         // partial results of a query tile: two per piece, 148 pieces of it at most
 constexpr int kItemCost = 128;         // cost of starting a query tile, in tokens
 constexpr int kMinCost = 512;          // a CTA takes at least 256 tokens of a pair, 512 of a single tile
 // The running maximum may lag: weights up to 2^40 lose nothing (bf16 and fp32 keep their exponents, and 2^40 * 131072
@@ -59,6 +60,7 @@ struct AttendArgs {
     float *lse;
     float *partials;
     PromptControl *ctl;
+    uint8_t *prefixes;                 // prefix sums of batches too large for shared memory
     int B, H_q, H_kv, G, T, max_pages, P_phys;
     float scale_log2;
 };
@@ -70,8 +72,10 @@ template <int D>
 struct Control {
     uint64_t bars[kRing + 2 * Cfg<D>::kSlots];
     PieceQueue queue;
+    alignas(8) uint8_t prefix[prefix_bytes(kSmemRequests)];
     uint32_t mask[Cfg<D>::kMasks];     // present 16-token groups of the tiles in flight
-    int last[2];
+    int parts[2];                      // partial results to merge, 0: another CTA does
+    uint16_t part[2][kMaxParts];
     int gave_up;
     uint32_t tmem;
 };
@@ -117,21 +121,20 @@ struct Segment {
 
 // The next part of an item in the piece; every role walks the same list.
 __device__ __forceinline__ bool next_segment(Walk<AttendWork> &walk, Segment &s) {
-    if (!walk.item()) return false;
-    const Cursor &c = walk.c;
-    const AttendWork &w = walk.w;
-    s.r = c.r, s.h = c.h, s.item = c.item, s.t = c.t;
-    s.tok0 = c.i * 2 * w.tpt;
-    s.ntok = w.new_tokens(c.t, c.i);
+    if (!walk.find()) return false;
+    const AttendWork &w = walk.l.w;
+    s.r = walk.r, s.h = walk.h, s.item = walk.item, s.t = walk.t;
+    s.tok0 = walk.i * 2 * w.tpt;
+    s.ntok = w.new_tokens(walk.t, walk.i);
     s.alt = s.ntok <= w.tpt;
-    s.nkv = w.units(c.t, c.i);
-    s.a = c.unit, s.piece = c.piece;
-    s.b = piece_end(c, s.nkv);
+    s.nkv = w.units(walk.t, walk.i);
+    s.a = walk.unit, s.piece = walk.piece;
+    s.b = walk.end_unit(s.nkv);
     if (s.alt) {
         s.steps0 = (s.b - s.a + 1) / 2;
         s.steps1 = (s.b - s.a) / 2;
     } else {
-        const int n0 = (c.t.past + s.tok0 + w.tpt + kKv - 1) / kKv;        // the first tile's tokens see no more than this
+        const int n0 = (walk.t.past + s.tok0 + w.tpt + kKv - 1) / kKv;        // the first tile's tokens see no more than this
         s.steps0 = max(min(s.b, n0) - s.a, 0);
         s.steps1 = s.b - s.a;
     }
@@ -188,18 +191,17 @@ __device__ __forceinline__ void leave_ring(bool ok, uint32_t pos, uint32_t first
 }
 
 template <int D>
-__device__ __forceinline__ void k_role(const AttendArgs &a, const CUtensorMap *q_map, const CUtensorMap *k_map, const CUtensorMap *k_wide,
-                                       Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars, int n_pieces, int lane) {
+__device__ __forceinline__ void k_role(const AttendArgs &a, const List<AttendWork> &list, const CUtensorMap *q_map, const CUtensorMap *k_map, const CUtensorMap *k_wide,
+                                       Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     const int tpt = kTile / a.G;
-    const AttendWork work(a);
     Segment s;
     Pages pages;
     uint32_t pos = 0, tiles = 0, queries = 0;
     const bool chosen = elect_one();
     bool ok = true;
-    Walk<AttendWork> walk(work, a.B, a.H_kv, a.ctl, &ctl->queue, gave_up, lane, n_pieces);
+    Walk<AttendWork> walk(list, a.ctl, &ctl->queue, gave_up, lane, true);
     while (ok && next_segment(walk, s)) {
         const int stop = s.t.past + s.t.n;                                 // tokens of the request
         pages.begin(a, s, s.a, true, lane);
@@ -251,16 +253,15 @@ __device__ __forceinline__ void k_role(const AttendArgs &a, const CUtensorMap *q
 }
 
 template <int D>
-__device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v_map, Control<D> *ctl, uint32_t ring, uint32_t bars, int lane) {
+__device__ __forceinline__ void v_role(const AttendArgs &a, const List<AttendWork> &list, const CUtensorMap *v_map, Control<D> *ctl, uint32_t ring, uint32_t bars, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
-    const AttendWork work(a);
     Segment s;
     Pages pages;
     uint32_t pos = 1;
     const bool chosen = elect_one();
     bool ok = true;
-    Walk<AttendWork> walk(work, a.B, a.H_kv, a.ctl, &ctl->queue, gave_up, lane);
+    Walk<AttendWork> walk(list, a.ctl, &ctl->queue, gave_up, lane, false);
     while (ok && next_segment(walk, s)) {
         const int stop = s.t.past + s.t.n;                                 // tokens of the request
         pages.begin(a, s, s.a, false, lane);
@@ -322,11 +323,10 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v
 // warp for both streams let the tensor cores run dry at every wait.  The whole warp walks the list, so that addresses stay in
 // uniform registers; one elected lane issues.
 template <int D, int ST>
-__device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars, int lane) {
+__device__ __forceinline__ void mma_role(const AttendArgs &a, const List<AttendWork> &list, Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     const uint32_t tmem_s = ctl->tmem + ST * kTile, tmem_o = ctl->tmem + C::kTmemO + ST * D;
-    const AttendWork work(a);
     Segment s = {};
     uint32_t pos = 0, queries = 0, o_used = 0, n = 0;                      // n: steps so far
     bool any = false;
@@ -364,7 +364,7 @@ __device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, u
         __syncwarp();
     };
     bool ok = true;
-    Walk<AttendWork> walk(work, a.B, a.H_kv, a.ctl, &ctl->queue, gave_up, lane);
+    Walk<AttendWork> walk(list, a.ctl, &ctl->queue, gave_up, lane, false);
     while (ok && next_segment(walk, s)) {
         const int steps = ST ? s.steps1 : s.steps0;
         const int tiles = s.b - s.a, stride = s.alt ? 2 : 1, first = s.alt ? ST : 0;   // this stream's tiles: first, first + stride, ...
@@ -421,17 +421,19 @@ __device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, u
 // ---- softmax and epilogue ----------------------------------------------------------
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
+// Partial results: two kinds per piece (of the item that it ends, of the item that it begins) and stream.
+__device__ __forceinline__ int partial_index(int piece, int kind, int st) { return (piece * 2 + kind) * 2 + st; }
 template <int D>
-__device__ __forceinline__ float *partial_slot(const AttendArgs &a, int piece, int kind, int st) {
-    return a.partials + (size_t)((piece * 2 + kind) * 2 + st) * Cfg<D>::kSlotFloats;
+__device__ __forceinline__ float *partial_slot(const AttendArgs &a, int index) {
+    return a.partials + (size_t)index * Cfg<D>::kSlotFloats;
 }
 
-// Merges the partial results of one query tile and writes its output.  128 threads; warp w takes rows w, w + 4, ...
-// `slots`: calls f(pointer) for every contribution, in CTA order.
-template <int D, typename Each>
-__device__ __forceinline__ void merge_rows(const AttendArgs &a, const Segment &s, int st, int row_from, int row_step, Each each,
+// Merges `parts` partial results of one query tile, at(k) their indexes, and writes its output.  A warp takes rows row_from,
+// row_from + row_step, ...
+template <int D, typename At>
+__device__ __forceinline__ void merge_rows(const AttendArgs &a, const Segment &s, int st, int row_from, int row_step, int parts, At at,
                                            int lane) {
-    constexpr int V = D / 32;
+    constexpr int V = D / 32, R = 8;   // channels of a lane, rows at a time
     const int tpt = kTile / a.G;
     const int tok = s.tok0 + (s.alt ? 0 : st * tpt);
     const int rows = min(tpt, s.tok0 + s.ntok - tok) * a.G;
@@ -439,41 +441,45 @@ __device__ __forceinline__ void merge_rows(const AttendArgs &a, const Segment &s
     const int my = row_from + row_step * lane;                             // statistics: a lane per row
     const bool have = my < rows;
     float M = -INFINITY, L = 0.f;
-    each([&](const float *p) {
-        const float m = have ? __ldcg(p + kTile * D + my) : -INFINITY, l = have ? __ldcg(p + kTile * D + kTile + my) : 0.f;
-        if (m == -INFINITY) return;
-        const float top = fmaxf(M, m);
-        L = L * ex2(M - top) + l * ex2(m - top);
+#pragma unroll 4
+    for (int k = 0; k < parts; ++k) {
+        const float *p = partial_slot<D>(a, at(k)) + kTile * D;
+        const float m = have ? __ldcg(p + my) : -INFINITY, l = have ? __ldcg(p + kTile + my) : 0.f;
+        const float top = fmaxf(M, m), ref = top == -INFINITY ? 0.f : top;
+        L = L * ex2(M - ref) + l * ex2(m - ref);
         M = top;
-    });
-    const float inv = L > 0.f ? 1.f / L : 0.f;
+    }
+    const float inv = L > 0.f ? 1.f / L : 0.f, ref = M == -INFINITY ? 0.f : M;
     if (have && a.lse) a.lse[out0 + (long long)(my / a.G) * a.H_q + my % a.G] = L > 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
     const int mine = rows > row_from ? (rows - row_from + row_step - 1) / row_step : 0;
-    for (int k0 = 0; k0 < mine; k0 += 8) {
-        float acc[8][V] = {};
-        each([&](const float *p) {
-            const float m = have ? __ldcg(p + kTile * D + my) : -INFINITY;
-            const float w = m == -INFINITY ? 0.f : ex2(m - M) * inv;
+    for (int k0 = 0; k0 < mine; k0 += R) {
+        float acc[R][V] = {};
+#pragma unroll 2
+        for (int q = 0; q < parts; ++q) {
+            const float *p = partial_slot<D>(a, at(q));
+            const float w = have ? ex2(__ldcg(p + kTile * D + my) - ref) * inv : 0.f;
+            float x[R][V];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float wk = __shfl_sync(kFull, w, k0 + k);
-                if (k0 + k < mine && wk > 0.f) {
-                    const float *src = p + (size_t)(row_from + row_step * (k0 + k)) * D + lane * V;
-                    float x[V];
-                    if constexpr (V == 4) {
-                        const float4 f = __ldcg(reinterpret_cast<const float4 *>(src));
-                        x[0] = f.x, x[1] = f.y, x[2] = f.z, x[3] = f.w;
-                    } else {
-                        const float2 f = __ldcg(reinterpret_cast<const float2 *>(src));
-                        x[0] = f.x, x[1] = f.y;
-                    }
-#pragma unroll
-                    for (int v = 0; v < V; ++v) acc[k][v] += wk * x[v];
+            for (int k = 0; k < R; ++k) {
+                // a row beyond the last is read as the last
+                const float *src = p + (size_t)(row_from + row_step * min(k0 + k, mine - 1)) * D + lane * V;
+                if constexpr (V == 4) {
+                    const float4 f = __ldcg(reinterpret_cast<const float4 *>(src));
+                    x[k][0] = f.x, x[k][1] = f.y, x[k][2] = f.z, x[k][3] = f.w;
+                } else {
+                    const float2 f = __ldcg(reinterpret_cast<const float2 *>(src));
+                    x[k][0] = f.x, x[k][1] = f.y;
                 }
             }
-        });
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < R; ++k) {
+                const float wk = __shfl_sync(kFull, w, min(k0 + k, 31));
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[k][v] += wk > 0.f ? wk * x[k][v] : 0.f;   // a result without weight may be anything
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
             if (k0 + k >= mine) break;
             const int row = row_from + row_step * (k0 + k);
             uint32_t w[V / 2];
@@ -490,7 +496,7 @@ __device__ __forceinline__ void merge_rows(const AttendArgs &a, const Segment &s
 }
 
 template <int D>
-__device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ctl, uint32_t bars, int st) {
+__device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<AttendWork> &list, Control<D> *ctl, uint32_t bars, int st) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     const int row = threadIdx.x & 127, lane = threadIdx.x & 31, warp = row >> 5;
@@ -498,7 +504,6 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     const uint32_t t_s = ctl->tmem + lanes + st * kTile, t_o = ctl->tmem + lanes + C::kTmemO + st * D;
     const float sl = a.scale_log2;
-    const AttendWork work(a);
     Segment s;
     uint32_t step = 0, tiles = 0, verdicts = 0, swaps = 0, ends = 0;
     uint32_t inner = 0;                                                    // steps so far that were not a piece's last of an item
@@ -508,7 +513,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
         if (lane == 0) mbar_arrive(bars + 8 * kSwap);
         return warp_wait(bars + 8 * kSwap, swaps++ & 1, gave_up, &a.ctl->status);
     };
-    Walk<AttendWork> walk(work, a.B, a.H_kv, a.ctl, &ctl->queue, gave_up, lane);
+    Walk<AttendWork> walk(list, a.ctl, &ctl->queue, gave_up, lane, false);
     while (next_segment(walk, s)) {
         const int tok = s.tok0 + (s.alt ? 0 : st * tpt);                   // the tile's first new token
         const int ntok = min(tpt, s.tok0 + s.ntok - tok);
@@ -623,7 +628,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
         }
         const int kind = s.a == 0;
         if (steps > 0 || !s.alt) {
-            float *slot = partial_slot<D>(a, s.piece, kind, st);
+            float *slot = partial_slot<D>(a, partial_index(s.piece, kind, st));
             if (steps > 0) {
 #pragma unroll
                 for (int k = 0; k < D; k += 32) {
@@ -648,41 +653,50 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, Control<D> *ct
         if (whole) {
             // alt, all KV tiles in this CTA: the two warpgroups exchange their results and merge half of the rows each
             if (!swap_sync()) return;
-            const float *s0 = partial_slot<D>(a, s.piece, kind, 0), *s1 = partial_slot<D>(a, s.piece, kind, 1);
-            merge_rows<D>(a, s, st, st * 4 + warp, 8, [&](auto f) { f(s0); f(s1); }, lane);
+            const int slot = partial_index(s.piece, kind, 0);
+            merge_rows<D>(a, s, st, st * 4 + warp, 8, 2, [&](int k) { return slot + k; }, lane);
             if (!swap_sync()) return;                                      // the slots may be written again
             continue;
         }
         if (steps == 0 && s.alt) continue;
-        const int from = first_piece_of(a.ctl, s.item, s.piece);
-        uint32_t *ticket = a.ctl->tickets + 2 * from + (s.alt ? 0 : st);
         __threadfence();
         __syncwarp();
         if (lane == 0) mbar_arrive(bars + 8 * (kAll + st));
         __syncwarp();
         if (warp == 0) {
+            const int from = first_piece_of(list, s.item, s.piece, lane);
             if (!warp_wait(bars + 8 * (kAll + st), verdicts & 1, gave_up, &a.ctl->status)) return;
+            int last = 0;
             if (lane == 0) {
                 __threadfence();
+                uint32_t *ticket = a.ctl->tickets + 2 * from + (s.alt ? 0 : st);
                 const uint32_t add = s.alt ? steps : s.b - s.a;
-                const bool last = atomicAdd(ticket, add) + add == (uint32_t)s.nkv;
+                last = atomicAdd(ticket, add) + add == (uint32_t)s.nkv;
                 if (last) atomicExch(ticket, 0u);
-                ctl->last[st] = last;
+            }
+            int parts = 0;
+            if (__shfl_sync(kFull, last, 0)) {
+                auto add = [&](int index) {
+                    if (lane == 0 && parts < kMaxParts) ctl->part[st][parts] = (uint16_t)index;
+                    ++parts;
+                };
+                each_piece_of(list, s.item, s.nkv, from, lane, [&](int y, int ya, int yb) {
+                    add(partial_index(y, ya == 0, s.alt ? 0 : st));
+                    if (s.alt && yb - ya > 1) add(partial_index(y, ya == 0, 1));
+                });
+            }
+            if (lane == 0) {
+                ctl->parts[st] = min(parts, kMaxParts);
                 mbar_arrive(bars + 8 * (kVerdict + st));
             }
             __syncwarp();
         }
         if (!warp_wait(bars + 8 * (kVerdict + st), verdicts & 1, gave_up, &a.ctl->status)) return;
         ++verdicts;
-        if (ctl->last[st]) {
+        const int parts = ctl->parts[st];
+        if (parts) {
             __threadfence();
-            auto each = [&](auto f) {
-                each_piece_of(a.ctl, s.item, s.nkv, from, lane, [&](int y, int ya, int yb) {
-                    f((const float *)partial_slot<D>(a, y, ya == 0, s.alt ? 0 : st));
-                    if (s.alt && yb - ya > 1) f((const float *)partial_slot<D>(a, y, ya == 0, 1));
-                });
-            };
-            merge_rows<D>(a, s, st, warp, 4, each, lane);
+            merge_rows<D>(a, s, st, warp, 4, parts, [&](int k) { return (int)ctl->part[st][k]; }, lane);
         }
     }
 }
@@ -728,7 +742,9 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
         ctl->gave_up = 0;
     }
     if (warp == kMmaWarp) tmem_alloc(smem_u32(&ctl->tmem), 512);
-    const int n_pieces = cut_work(AttendWork(a), a.B, a.H_kv, a.ctl, smem + 2 * C::kTileBytes);
+    const AttendWork work(a);
+    const List<AttendWork> list = make_list(work, a.B, a.H_kv, a.ctl,
+                                            a.B > kSmemRequests ? a.prefixes + prefix_bytes(a.B) * blockIdx.x : ctl->prefix, smem);
     // query rows that no tensor copy fills (G does not divide 128) stay zero
     for (int i = threadIdx.x; i < 2 * C::kTileBytes / 16; i += kThreads)
         reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
@@ -738,12 +754,12 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     tc_fence_after();
 
     if (warp < 8) {
-        softmax_role<D>(a, ctl, bars, warp >> 2);
+        softmax_role<D>(a, list, ctl, bars, warp >> 2);
     } else {
-        if (warp == kKWarp) k_role<D>(a, &q_map, &k_map, &k_wide, ctl, base, base + 2 * C::kTileBytes, bars, n_pieces, lane);
-        else if (warp == kVWarp) v_role<D>(a, &v_map, ctl, base + 2 * C::kTileBytes, bars, lane);
-        else if (warp == kMmaWarp) mma_role<D, 0>(a, ctl, base, base + 2 * C::kTileBytes, bars, lane);
-        else if (warp == kMmaWarp + 1) mma_role<D, 1>(a, ctl, base, base + 2 * C::kTileBytes, bars, lane);
+        if (warp == kKWarp) k_role<D>(a, list, &q_map, &k_map, &k_wide, ctl, base, base + 2 * C::kTileBytes, bars, lane);
+        else if (warp == kVWarp) v_role<D>(a, list, &v_map, ctl, base + 2 * C::kTileBytes, bars, lane);
+        else if (warp == kMmaWarp) mma_role<D, 0>(a, list, ctl, base, base + 2 * C::kTileBytes, bars, lane);
+        else if (warp == kMmaWarp + 1) mma_role<D, 1>(a, list, ctl, base, base + 2 * C::kTileBytes, bars, lane);
         __syncwarp();
     }
     tc_fence_before();
@@ -777,6 +793,7 @@ cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t 
     a.out = static_cast<uint16_t *>(c.out), a.lse = c.lse;
     a.ctl = reinterpret_cast<PromptControl *>(c.workspace);
     a.partials = reinterpret_cast<float *>(c.workspace + kPromptControlBytes);
+    a.prefixes = c.workspace + prefix_workspace_offset(p.D);
     a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.G = G, a.T = c.total_tokens, a.max_pages = p.max_pages;
     a.P_phys = p.num_phys_pages, a.scale_log2 = effective_scale(p) * kLog2e;
     auto kern = attend_kernel<D>;
@@ -792,8 +809,7 @@ cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t 
 
 size_t prompt_workspace_control_bytes() { return kPromptControlBytes; }
 size_t prompt_workspace_bytes(const se_params &p) {
-    const size_t slot = ((size_t)kTile * p.D + 2 * kTile) * sizeof(float);
-    return kPromptControlBytes + (size_t)kMaxPieces * 4 * slot;
+    return prefix_workspace_offset(p.D) + (prefix_workspace_bytes(p.B) + 255) / 256 * 256;
 }
 
 cudaError_t launch_prompt_attend(const se_params &p, const AttendCall &c, cudaStream_t stream) {

@@ -41,6 +41,7 @@ struct MassArgs {
     const float *lse;
     float *accum, *partials;
     PromptControl *ctl;
+    uint8_t *prefixes;                 // prefix sums of batches too large for shared memory
     int B, H_q, H_kv, G, T, max_pages, P_phys;
     float scale_log2;
 };
@@ -53,6 +54,7 @@ struct Control {
     uint64_t bars[kRing + 2 * Cfg<D>::kSlots];
     alignas(16) float lse[kLseSlots][kTile];   // -lse log2 e of the query tiles' rows, -inf for rows that count for nothing
     PieceQueue queue;
+    alignas(8) uint8_t prefix[prefix_bytes(kSmemRequests)];
     int last[2];
     int gave_up;
     uint32_t tmem;
@@ -94,15 +96,14 @@ struct Segment {
 };
 
 __device__ __forceinline__ bool next_segment(Walk<MassWork> &walk, Segment &s) {
-    if (!walk.item()) return false;
-    const Cursor &c = walk.c;
-    const MassWork &w = walk.w;
-    s.r = c.r, s.h = c.h, s.item = c.item, s.t = c.t;
-    s.pos0 = c.i * 2 * kTile;
-    s.units = w.units(c.t, c.i);
-    s.a = c.unit, s.b = piece_end(c, s.units), s.piece = c.piece;
-    s.q0 = w.blind(c.t, s.pos0) / w.tpt;
-    s.skip1 = s.pos0 + kTile >= c.t.past + c.t.n ? s.units : w.blind(c.t, s.pos0 + kTile) / w.tpt - s.q0;
+    if (!walk.find()) return false;
+    const MassWork &w = walk.l.w;
+    s.r = walk.r, s.h = walk.h, s.item = walk.item, s.t = walk.t;
+    s.pos0 = walk.i * 2 * kTile;
+    s.units = w.units(walk.t, walk.i);
+    s.a = walk.unit, s.b = walk.end_unit(s.units), s.piece = walk.piece;
+    s.q0 = w.blind(walk.t, s.pos0) / w.tpt;
+    s.skip1 = s.pos0 + kTile >= walk.t.past + walk.t.n ? s.units : w.blind(walk.t, s.pos0 + kTile) / w.tpt - s.q0;
     walk.next();
     return true;
 }
@@ -119,12 +120,11 @@ __device__ __forceinline__ int group_page(const MassArgs &a, const Segment &s, i
 }
 
 template <int D>
-__device__ __forceinline__ void copy_role(const MassArgs &a, const CUtensorMap *q_map, const CUtensorMap *k_map, Control<D> *ctl,
-                                          uint32_t k_smem, uint32_t ring, uint32_t bars, int n_pieces, int lane) {
+__device__ __forceinline__ void copy_role(const MassArgs &a, const List<MassWork> &list, const CUtensorMap *q_map, const CUtensorMap *k_map, Control<D> *ctl,
+                                          uint32_t k_smem, uint32_t ring, uint32_t bars, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
-    const MassWork work(a);
-    Walk<MassWork> walk(work, a.B, a.H_kv, a.ctl, &ctl->queue, gave_up, lane, n_pieces);
+    Walk<MassWork> walk(list, a.ctl, &ctl->queue, gave_up, lane, true);
     Segment s;
     uint32_t pos = 0, pairs = 0;
     const bool chosen = elect_one();
@@ -154,11 +154,11 @@ __device__ __forceinline__ void copy_role(const MassArgs &a, const CUtensorMap *
             ok = warp_wait(bar + 8 * C::kSlots, (pos / C::kSlots & 1) ^ 1, gave_up, &a.ctl->status);
             if (!ok) break;
             if (chosen) {
-                mbar_expect_tx(bar, work.tpt * a.G * D * 2);
+                mbar_expect_tx(bar, list.w.tpt * a.G * D * 2);
 #pragma unroll
                 for (int half = 0; half < C::kHalves; ++half)
                     tma_load_3d(ring + slot * C::kTileBytes + half * (kTile * 128), q_map, half * 64, s.h * a.G,
-                                s.t.start + (s.q0 + u) * work.tpt, bar);
+                                s.t.start + (s.q0 + u) * list.w.tpt, bar);
             }
             __syncwarp();
         }
@@ -178,17 +178,16 @@ __device__ __forceinline__ void copy_role(const MassArgs &a, const CUtensorMap *
 
 // The query tiles' log-sum-exps, a tile ahead in registers.
 template <int D>
-__device__ __forceinline__ void lse_role(const MassArgs &a, Control<D> *ctl, uint32_t bars, int lane) {
+__device__ __forceinline__ void lse_role(const MassArgs &a, const List<MassWork> &list, Control<D> *ctl, uint32_t bars, int lane) {
     volatile int *gave_up = &ctl->gave_up;
-    const MassWork work(a);
-    Walk<MassWork> walk(work, a.B, a.H_kv, a.ctl, &ctl->queue, gave_up, lane);
+    Walk<MassWork> walk(list, a.ctl, &ctl->queue, gave_up, lane, false);
     Segment s;
     uint32_t tiles = 0;
-    const int live = work.tpt * a.G;
+    const int live = list.w.tpt * a.G;
     while (next_segment(walk, s)) {
         float x[4];
         auto fetch = [&](int u) {
-            const int tok = (s.q0 + u) * work.tpt;
+            const int tok = (s.q0 + u) * list.w.tpt;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int row = lane + 32 * k, q = tok + row / a.G;
@@ -209,13 +208,12 @@ __device__ __forceinline__ void lse_role(const MassArgs &a, Control<D> *ctl, uin
 }
 
 template <int D>
-__device__ __forceinline__ void mma_role(const MassArgs &a, Control<D> *ctl, uint32_t k_smem, uint32_t ring, uint32_t bars, int lane) {
+__device__ __forceinline__ void mma_role(const MassArgs &a, const List<MassWork> &list, Control<D> *ctl, uint32_t k_smem, uint32_t ring, uint32_t bars, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     constexpr uint32_t kInstr = mma_instr(kTile, false);
     const uint32_t tmem = ctl->tmem;
-    const MassWork work(a);
-    Walk<MassWork> walk(work, a.B, a.H_kv, a.ctl, &ctl->queue, gave_up, lane);
+    Walk<MassWork> walk(list, a.ctl, &ctl->queue, gave_up, lane, false);
     Segment s;
     uint32_t pos = 0, pairs = 0, step0 = 0, step1 = 0;
     const bool chosen = elect_one();
@@ -260,13 +258,12 @@ __device__ __forceinline__ void mma_role(const MassArgs &a, Control<D> *ctl, uin
 }
 
 template <int D>
-__device__ __forceinline__ void sum_role(const MassArgs &a, Control<D> *ctl, uint32_t bars, int st) {
+__device__ __forceinline__ void sum_role(const MassArgs &a, const List<MassWork> &list, Control<D> *ctl, uint32_t bars, int st) {
     volatile int *gave_up = &ctl->gave_up;
     const int row = threadIdx.x & 127, lane = threadIdx.x & 31, warp = row >> 5;
     const uint32_t t_s = ctl->tmem + ((uint32_t)(warp * 32) << 16) + 2 * st * kTile;
     const float2 sl = make_float2(a.scale_log2, a.scale_log2);
-    const MassWork work(a);
-    Walk<MassWork> walk(work, a.B, a.H_kv, a.ctl, &ctl->queue, gave_up, lane);
+    Walk<MassWork> walk(list, a.ctl, &ctl->queue, gave_up, lane, false);
     Segment s;
     uint32_t step = 0, tiles = 0, verdicts = 0;
     while (next_segment(walk, s)) {
@@ -277,10 +274,10 @@ __device__ __forceinline__ void sum_role(const MassArgs &a, Control<D> *ctl, uin
             const uint32_t slot = tiles % kLseSlots;
             if (!warp_wait(bars + 8 * (kLseFull + slot), tiles / kLseSlots & 1, gave_up, &a.ctl->status)) return;
             if (st == 0 || u >= s.skip1) {
-                const int tok = (s.q0 + u) * work.tpt;                     // the tile's first new token
+                const int tok = (s.q0 + u) * list.w.tpt;                     // the tile's first new token
                 // columns [from, to) count: the queries at or behind the cached token, and of this request
                 const int from = min(max(pos - s.t.past - tok, 0), kTile) * a.G, to = (s.t.n - tok) * a.G;
-                const bool masked = __any_sync(kFull, from > 0) || to < work.tpt * a.G;
+                const bool masked = __any_sync(kFull, from > 0) || to < list.w.tpt * a.G;
                 const uint32_t buf = step & 1;
                 if (!warp_wait(bars + 8 * (kSFull + 2 * st + buf), step >> 1 & 1, gave_up, &a.ctl->status)) return;
                 ++step;
@@ -328,7 +325,7 @@ __device__ __forceinline__ void sum_role(const MassArgs &a, Control<D> *ctl, uin
         }
         auto part = [&](int piece, int kind) { return a.partials + (size_t)((piece * 2 + kind) * 2 + st) * kTile + row; };
         __stcg(part(s.piece, s.a == 0), sum);
-        const int from = first_piece_of(a.ctl, s.item, s.piece);
+        const int from = first_piece_of(list, s.item, s.piece, lane);
         __threadfence();
         __syncwarp();
         if (lane == 0) mbar_arrive(bars + 8 * (kAll + st));
@@ -351,7 +348,7 @@ __device__ __forceinline__ void sum_role(const MassArgs &a, Control<D> *ctl, uin
         if (ctl->last[st]) {
             __threadfence();
             float all = 0.f;
-            each_piece_of(a.ctl, s.item, s.units, from, lane, [&](int y, int ya, int) { all += __ldcg(part(y, ya == 0)); });
+            each_piece_of(list, s.item, s.units, from, lane, [&](int y, int ya, int) { all += __ldcg(part(y, ya == 0)); });
             if (pid >= 0 && pos < s.t.past + s.t.n) a.accum[at] += all;
         }
     }
@@ -393,9 +390,9 @@ mass_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ C
         ctl->gave_up = 0;
     }
     if (warp == kMmaWarp) tmem_alloc(smem_u32(&ctl->tmem), 512);
-    static_assert(kPieceScratch <= kTiles * C::kTileBytes, "the tiles' memory holds the prefix sums first");
-    const int n_pieces = cut_work(MassWork(a), a.B, a.H_kv, a.ctl, smem);
-    __syncthreads();
+    const MassWork work(a);
+    const List<MassWork> list = make_list(work, a.B, a.H_kv, a.ctl,
+                                          a.B > kSmemRequests ? a.prefixes + prefix_bytes(a.B) * blockIdx.x : ctl->prefix, smem);
     // query rows that no tensor copy fills (G does not divide 128) stay zero
     for (int i = threadIdx.x; i < C::kSlots * C::kTileBytes / 16; i += kThreads)
         reinterpret_cast<uint4 *>(smem + 2 * C::kPairs * C::kTileBytes)[i] = make_uint4(0, 0, 0, 0);
@@ -404,10 +401,10 @@ mass_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ C
     __syncthreads();
     tc_fence_after();
 
-    if (warp < 8) sum_role<D>(a, ctl, bars, warp >> 2);
-    else if (warp == kCopyWarp) copy_role<D>(a, &q_map, &k_map, ctl, base, ring, bars, n_pieces, lane);
-    else if (warp == kLseWarp) lse_role<D>(a, ctl, bars, lane);
-    else if (warp == kMmaWarp) mma_role<D>(a, ctl, base, ring, bars, lane);
+    if (warp < 8) sum_role<D>(a, list, ctl, bars, warp >> 2);
+    else if (warp == kCopyWarp) copy_role<D>(a, list, &q_map, &k_map, ctl, base, ring, bars, lane);
+    else if (warp == kLseWarp) lse_role<D>(a, list, ctl, bars, lane);
+    else if (warp == kMmaWarp) mma_role<D>(a, list, ctl, base, ring, bars, lane);
     __syncwarp();
     tc_fence_before();
     __syncthreads();
@@ -430,6 +427,7 @@ cudaError_t launch_mass(const se_params &p, const AttendCall &c, float *score_ac
     a.lse = c.lse, a.accum = score_accum;
     a.ctl = reinterpret_cast<PromptControl *>(c.workspace);
     a.partials = reinterpret_cast<float *>(c.workspace + kPromptControlBytes);
+    a.prefixes = c.workspace + prefix_workspace_offset(p.D);
     a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.G = G, a.T = c.total_tokens, a.max_pages = p.max_pages;
     a.P_phys = p.num_phys_pages, a.scale_log2 = effective_scale(p) * kLog2e;
     const size_t smem = (2 * C::kPairs + C::kSlots) * C::kTileBytes + sizeof(Control<D>);
