@@ -2,24 +2,24 @@
 // cache or over contiguous K and V.
 //
 // Mathematics.  A query tile is 128 rows = 128/G tokens x the G query heads of one kv-head, so the heads of a group share
-// every K and V tile.  Over the KV tiles j of 64 tokens:  S = Q K_j^T,  p = 2^(S sl - m)  with sl = sm_scale log2 e,
+// every K and V tile.  Over the KV tiles j of 128 tokens:  S = Q K_j^T,  p = 2^(S sl - m)  with sl = sm_scale log2 e,
 // O += P V_j, l += rowsum p;  out = O / l,  lse = (m + log2 l) ln 2.  m is a row maximum that is moved (and O, l
 // rescaled) only when the scores exceed it by more than 40, so nearly all steps leave O alone.
 //
 // What bounds it.  Per (128 rows x 128 tokens) at D = 128 the two products take 1024 cycles of the tensor cores and
 // the 16384 exponentials 1024 cycles of the special-function units: both have to run all the time.  So a CTA (one per
-// SM, persistent) works on two streams of tiles: two warpgroups do the softmax of one stream each, two warps issue a
-// stream's products each, two warps copy.  S (fp32), P (bf16, in S's columns) and O (fp32) live in tensor memory: 2 x (128 + D)
+// SM, persistent) works on two streams of tiles: two warpgroups do the softmax of one stream each, one warp issues all
+// products, two warps copy.  S (fp32), P (bf16, in S's columns) and O (fp32) live in tensor memory: 2 x (128 + D)
 // of 512 columns.
 //   pair   more than 128 query rows left: the streams are two neighbouring query tiles, K and V tiles are shared
 //   alt    up to 128 rows (decode tokens, short chunks, ends of prompts): both streams are the same query tile, one
 //          takes the even and one the odd KV tiles; their results are merged at the end
 //
 // Split.  The CTAs cut the whole batch's work - query tile pairs in the order (request, kv-head, tile), each as long as
-// the tokens it sees - into equal pieces at KV-tile borders.  A piece that begins or ends inside a query tile leaves
-// fp32 partial results (O, m, l) in the workspace; whichever CTA completes the tile's count of KV tiles merges them, in
-// CTA order, so the result does not depend on who is last.  Long contexts with few rows and long prompts take the same
-// path, and there is no second kernel.
+// the tokens it sees - into pieces at KV-tile borders.  A piece that begins or ends inside a query tile leaves fp32 partial
+// results (O, m, l) in the workspace; whichever CTA completes the tile's count of KV tiles merges them, in the order of the
+// pieces, so the result does not depend on who is last.  Long contexts with few rows and long prompts take the same path, and
+// there is no second kernel.
 #include <math.h>
 
 #include "se_internal.h"
@@ -30,11 +30,13 @@ namespace se {
 
 namespace {
 
-constexpr int kThreads = kPromptThreads;   // 2 softmax warpgroups, K warp, 2 product warps, V warp
-constexpr int kKWarp = 8, kMmaWarp = 9, kVWarp = 11;
+constexpr int kThreads = kPromptThreads;   // 2 softmax warpgroups, K warp, product warp, V warp, idle warp
+constexpr int kKWarp = 8, kMmaWarp = 9, kVWarp = 10;
+constexpr int kRegsSoftmax = 208, kRegsOther = 88;   // 256 * 208 + 128 * 88 = 384 * 168
 constexpr int kTile = 128;             // query rows of a tile
-constexpr int kKv = 64;                // tokens of a KV tile
-constexpr int kMaxParts = 320;         // partial results of a query tile: two per piece, 148 pieces of it at most
+constexpr int kKv = 128;               // tokens of a KV tile
+constexpr int kGroups = kKv / kPage;   // pages of a KV tile
+constexpr int kMaxParts = 304;         // partial results of a query tile: two per piece, little more than 148 pieces of it
 constexpr int kItemCost = 128;         // cost of starting a query tile, in tokens
 constexpr int kMinCost = 512;          // a CTA takes at least 256 tokens of a pair, 512 of a single tile
 // The running maximum may lag: weights up to 2^40 lose nothing (bf16 and fp32 keep their exponents, and 2^40 * 131072
@@ -46,7 +48,8 @@ struct Cfg {
     static constexpr int kHalves = D / 64;
     static constexpr int kTileBytes = kTile * D * 2;              // query tile
     static constexpr int kKvBytes = kKv * D * 2;                  // K or V tile
-    static constexpr int kSlots = 10 * 128 / D;                   // ring of K and V tiles, 160 KB
+    static constexpr int kKSlots = 2 * 128 / D, kVSlots = 3 * 128 / D;   // rings of K and V tiles, 64 and 96 KB
+    static constexpr int kSlots = kKSlots + kVSlots;
     static constexpr int kMasks = 16;
     static constexpr int kSlotFloats = kTile * D + 2 * kTile;     // a partial result: O, m, l
     static constexpr int kTmemO = 256;                            // S0, S1 at columns 0, 128; O0, O1 behind
@@ -65,20 +68,13 @@ struct AttendArgs {
     float scale_log2;
 };
 
-enum Bar { kQFull, kQEmpty, kSFull, kPReady = kSFull + 4, kODone = kPReady + 4, kOLast = kODone + 2, kOFree = kOLast + 2, kAll = kOFree + 2, kVerdict = kAll + 2, kSwap = kVerdict + 2,
-           kDrain, kRing = kDrain + 2 };
-
-template <int D>
-struct Control {
-    uint64_t bars[kRing + 2 * Cfg<D>::kSlots];
-    PieceQueue queue;
-    alignas(8) uint8_t prefix[prefix_bytes(kSmemRequests)];
-    uint32_t mask[Cfg<D>::kMasks];     // present 16-token groups of the tiles in flight
-    int parts[2];                      // partial results to merge, 0: another CTA does
-    uint16_t part[2][kMaxParts];
-    int gave_up;
-    uint32_t tmem;
+template <int N>
+struct Int {
+    static constexpr int value = N;
 };
+
+enum Bar { kQFull, kQEmpty, kSFull, kPReady = kSFull + 2, kOLast = kPReady + 2, kOFree = kOLast + 2, kAll = kOFree + 2,
+           kVerdict = kAll + 2, kSwap = kVerdict + 2, kDrain, kFull };   // kFull: K slots, V slots; then the same for "empty"
 
 // ---- the work list -----------------------------------------------------------------
 // item = two query tiles (the last one of a request may be a single tile), unit = KV tile.  Cost in tokens seen, twice
@@ -106,7 +102,9 @@ struct AttendWork {
         return (int)(z / (kKv * (new_tokens(t, i) > tpt ? 2 : 1)));
     }
     __device__ __forceinline__ long long min_cost() const { return kMinCost; }
-    static constexpr int kCrumb = 4;   // least units of a part of an item
+    static constexpr int kCrumb = 2;   // least units of a part of an item
+    static constexpr bool kShares = true;
+    __device__ __forceinline__ long long longest(const TokenRange &t) const { return 2ll * (t.past + t.n + kItemCost); }
 };
 
 struct Segment {
@@ -119,7 +117,19 @@ struct Segment {
     __device__ __forceinline__ int steps(int st) const { return st ? steps1 : steps0; }
 };
 
-// The next part of an item in the piece; every role walks the same list.
+template <int D>
+struct Control {
+    uint64_t bars[kFull + 2 * Cfg<D>::kSlots];
+    SegmentQueue<Segment> queue;
+    alignas(8) uint8_t prefix[prefix_bytes(kSmemRequests)];
+    uint32_t mask[Cfg<D>::kMasks];     // present 16-token groups of the tiles in flight
+    int parts[2];                      // partial results to merge, 0: another CTA does
+    uint16_t part[2][kMaxParts];
+    int gave_up;
+    uint32_t tmem;
+};
+
+// The next part of an item in the piece.
 __device__ __forceinline__ bool next_segment(Walk<AttendWork> &walk, Segment &s) {
     if (!walk.find()) return false;
     const AttendWork &w = walk.l.w;
@@ -143,9 +153,10 @@ __device__ __forceinline__ bool next_segment(Walk<AttendWork> &walk, Segment &s)
 }
 
 // ---- copies ------------------------------------------------------------------------
-// One warp brings K (and Q), one V: each has every second slot of the ring.  A tile is 64 tokens of one head.  K lies as
-// [D/64][64 tokens][64 channels]: a page is D/64 copies (one for all where K is contiguous).  V lies as
-// [4][D/64][16 tokens][64 channels], because a product takes 16 tokens at a time: a page is one copy.
+// One warp brings K (and Q), one V, each through a ring of its own.  A tile is 128 tokens of one head.  K lies as
+// [D/64][128 tokens][64 channels]: a page is D/64 copies (one for all where K is contiguous).  V lies as
+// [8][D/64][16 tokens][64 channels] where it is paged, because a product takes 16 tokens at a time: a page is one copy; and like
+// K where it is contiguous, a whole tile in one copy.
 // Groups that are absent or past the end come from behind the tensor's last row, which reads as zeros.
 
 // Pages of 32 groups of 16 tokens at a time, a lane each, and of the next 32 ahead.  Contiguous K and V: 0 for "present".
@@ -163,30 +174,29 @@ struct Pages {
         return pid < 0 ? -1 : pid;
     }
     __device__ __forceinline__ void begin(const AttendArgs &a, const Segment &s, int tile, bool report, int lane) {
-        block = tile / 8;
+        block = tile / (32 / kGroups);
         ids = fetch(a, s, block * 32 + lane, report);
         next = fetch(a, s, block * 32 + 32 + lane, report);
     }
     // tiles come in ascending order
     __device__ __forceinline__ void reach(const AttendArgs &a, const Segment &s, int tile, bool report, int lane) {
-        if (tile / 8 == block) return;
+        if (tile / (32 / kGroups) == block) return;
         ++block;
         ids = next;
         next = fetch(a, s, block * 32 + 32 + lane, report);
     }
-    __device__ __forceinline__ int of(int tile, int pg) const { return __shfl_sync(kFull, ids, (tile & 7) * 4 + pg); }
+    __device__ __forceinline__ int of(int tile, int pg) const { return __shfl_sync(se::kFull, ids, tile % (32 / kGroups) * kGroups + pg); }
 };
 
-// The end of a copying warp, whose next position would be `pos`: nothing may still be on its way to the CTA's shared memory
-// when the CTA ends - copies, and the products' arrivals on the barriers of the slots they have let go.
-template <int D>
-__device__ __forceinline__ void leave_ring(bool ok, uint32_t pos, uint32_t first, uint32_t bars, volatile int *gave_up,
-                                           const AttendArgs &a) {
-    constexpr uint32_t kSlots = Cfg<D>::kSlots;
-    for (uint32_t p = pos >= kSlots + first ? pos - kSlots : first; p < pos; p += 2) {
-        const uint32_t bar = bars + 8 * (kRing + p % kSlots), parity = p / kSlots & 1;
-        if (ok) ok = warp_wait(bar + 8 * kSlots, parity, gave_up, &a.ctl->status);
-        else mbar_wait(bar, parity);
+// The end of a copying warp that has filled `filled` slots of a ring of kSlots, whose barriers are full + 8 * slot and
+// empty + 8 * slot: nothing may still be on its way to the CTA's shared memory when the CTA ends - copies, and the
+// products' arrivals for the slots they have let go.
+template <uint32_t kSlots>
+__device__ __forceinline__ void leave_ring(bool ok, uint32_t filled, uint32_t full, uint32_t empty, volatile int *gave_up, const AttendArgs &a) {
+    for (uint32_t n = filled > kSlots ? filled - kSlots : 0; n < filled; ++n) {
+        const uint32_t off = 8 * (n % kSlots), parity = n / kSlots & 1;
+        if (ok) ok = warp_wait(empty + off, parity, gave_up, &a.ctl->status);
+        else mbar_wait(full + off, parity);
     }
 }
 
@@ -198,12 +208,15 @@ __device__ __forceinline__ void k_role(const AttendArgs &a, const List<AttendWor
     const int tpt = kTile / a.G;
     Segment s;
     Pages pages;
-    uint32_t pos = 0, tiles = 0, queries = 0;
+    uint32_t tiles = 0, queries = 0;
+    const uint32_t k_full = bars + 8 * kFull, k_empty = k_full + 8 * C::kSlots;
     const bool chosen = elect_one();
     bool ok = true;
-    Walk<AttendWork> walk(list, a.ctl, &ctl->queue, gave_up, lane, true);
+    Walk<AttendWork> walk(list, a.ctl, lane);
     while (ok && next_segment(walk, s)) {
         const int stop = s.t.past + s.t.n;                                 // tokens of the request
+        ok = ctl->queue.put(queries, &s, gave_up, &a.ctl->status, lane);
+        if (!ok) break;
         pages.begin(a, s, s.a, true, lane);
         ok = warp_wait(bars + 8 * kQEmpty, (queries & 1) ^ 1, gave_up, &a.ctl->status);
         if (!ok) break;
@@ -216,14 +229,14 @@ __device__ __forceinline__ void k_role(const AttendArgs &a, const List<AttendWor
         }
         __syncwarp();
         ++queries;
-        for (int t = s.a; t < s.b; ++t, ++tiles, pos += 2) {
-            const uint32_t slot = pos % C::kSlots, bar = bars + 8 * (kRing + slot), dst = ring + slot * C::kKvBytes;
+        for (int t = s.a; t < s.b; ++t, ++tiles) {
+            const uint32_t slot = tiles % C::kKSlots, bar = k_full + 8 * slot, dst = ring + slot * C::kKvBytes;
             pages.reach(a, s, t, true, lane);
-            const unsigned mask = __ballot_sync(kFull, pages.ids >= 0) >> (t & 7) * 4 & 0xfu;
-            int pid[4];
+            const unsigned mask = __ballot_sync(se::kFull, pages.ids >= 0) >> t % (32 / kGroups) * kGroups & 0xffu;
+            int pid[kGroups];
 #pragma unroll
-            for (int pg = 0; pg < 4; ++pg) pid[pg] = pages.of(t, pg);
-            ok = warp_wait(bar + 8 * C::kSlots, (pos / C::kSlots & 1) ^ 1, gave_up, &a.ctl->status);
+            for (int pg = 0; pg < kGroups; ++pg) pid[pg] = pages.of(t, pg);
+            ok = warp_wait(k_empty + 8 * slot, (tiles / C::kKSlots & 1) ^ 1, gave_up, &a.ctl->status);
             if (!ok) break;
             if (chosen) {
                 ctl->mask[tiles % C::kMasks] = mask;
@@ -232,7 +245,7 @@ __device__ __forceinline__ void k_role(const AttendArgs &a, const List<AttendWor
                     tma_load_4d(dst, k_wide, 0, s.h, s.t.start + t * kKv, 0, bar);
                 } else {
 #pragma unroll
-                    for (int pg = 0; pg < 4; ++pg) {
+                    for (int pg = 0; pg < kGroups; ++pg) {
                         const int y = a.page_table ? 0 : s.h;
                         const int z = pid[pg] < 0 ? (a.page_table ? a.P_phys * a.H_kv * kPage : a.T)
                                                   : a.page_table ? (pid[pg] * a.H_kv + s.h) * kPage : s.t.start + t * kKv + pg * kPage;
@@ -245,7 +258,8 @@ __device__ __forceinline__ void k_role(const AttendArgs &a, const List<AttendWor
             __syncwarp();
         }
     }
-    leave_ring<D>(ok, pos, 0, bars, gave_up, a);
+    if (ok) ok = ctl->queue.put(queries, nullptr, gave_up, &a.ctl->status, lane);
+    leave_ring<C::kKSlots>(ok, tiles, k_full, k_empty, gave_up, a);
     if (queries) {
         if (ok) warp_wait(bars + 8 * kQEmpty, (queries - 1) & 1, gave_up, &a.ctl->status);
         else mbar_wait(bars + 8 * kQFull, (queries - 1) & 1);
@@ -253,36 +267,39 @@ __device__ __forceinline__ void k_role(const AttendArgs &a, const List<AttendWor
 }
 
 template <int D>
-__device__ __forceinline__ void v_role(const AttendArgs &a, const List<AttendWork> &list, const CUtensorMap *v_map, Control<D> *ctl, uint32_t ring, uint32_t bars, int lane) {
+__device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v_map, const CUtensorMap *v_wide, Control<D> *ctl, uint32_t ring, uint32_t bars, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     Segment s;
     Pages pages;
-    uint32_t pos = 1;
+    uint32_t tiles = 0;
+    const uint32_t v_full = bars + 8 * (kFull + C::kKSlots), v_empty = v_full + 8 * C::kSlots;
     const bool chosen = elect_one();
     bool ok = true;
-    Walk<AttendWork> walk(list, a.ctl, &ctl->queue, gave_up, lane, false);
-    while (ok && next_segment(walk, s)) {
+    uint32_t turn = 0;
+    const uint32_t page_step = a.page_table ? kPage * D * 2 : kPage * 128, half_step = a.page_table ? kPage * 128 : kKv * 128;
+    while (ok) {
+        const Segment *next = ctl->queue.get(turn++, gave_up, &a.ctl->status, lane);
+        if (!next) break;
+        s = *next;
         const int stop = s.t.past + s.t.n;                                 // tokens of the request
         pages.begin(a, s, s.a, false, lane);
-        for (int t = s.a; t < s.b; ++t, pos += 2) {
-            const uint32_t slot = pos % C::kSlots, bar = bars + 8 * (kRing + slot), dst = ring + slot * C::kKvBytes;
+        for (int t = s.a; t < s.b; ++t, ++tiles) {
+            const uint32_t slot = tiles % C::kVSlots, bar = v_full + 8 * slot, dst = ring + (C::kKSlots + slot) * C::kKvBytes;
             pages.reach(a, s, t, false, lane);
-            int pid[4];
+            int pid[kGroups];
 #pragma unroll
-            for (int pg = 0; pg < 4; ++pg) pid[pg] = pages.of(t, pg);
-            ok = warp_wait(bar + 8 * C::kSlots, (pos / C::kSlots & 1) ^ 1, gave_up, &a.ctl->status);
+            for (int pg = 0; pg < kGroups; ++pg) pid[pg] = pages.of(t, pg);
+            ok = warp_wait(v_empty + 8 * slot, (tiles / C::kVSlots & 1) ^ 1, gave_up, &a.ctl->status);
             if (!ok) break;
             // The group that holds the end of the request is copied row by row: what lies behind the end may be anything, and
             // a weight of zero would not hide a NaN.
             const int part = stop % kPage && stop / kKv == t ? stop % kKv / kPage : -1;
-            bool by_hand = false;
-#pragma unroll
-            for (int pg = 0; pg < 4; ++pg) {
-                if (pg != part || pid[pg] < 0) continue;
-                by_hand = true;
-                const int tok = t * kKv + pg * kPage;
-                const uint16_t *base = a.page_table ? a.v + ((size_t)pid[pg] * a.H_kv + s.h) * (kPage * D)
+            const int own = part < 0 ? -1 : pages.of(t, part);
+            const bool by_hand = own >= 0;
+            if (by_hand) {
+                const int tok = t * kKv + part * kPage;
+                const uint16_t *base = a.page_table ? a.v + ((size_t)own * a.H_kv + s.h) * (kPage * D)
                                                     : a.v + (long long)(s.t.start + tok) * a.v_stride + s.h * D;
                 const long long pitch = a.page_table ? D : a.v_stride;
                 constexpr int kPieces = D / 8;
@@ -291,7 +308,7 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const List<AttendWor
                     const int e = i * 32 + lane, row = e / kPieces, ch = e % kPieces;
                     uint4 x = make_uint4(0, 0, 0, 0);
                     if (row < stop - tok) x = *reinterpret_cast<const uint4 *>(base + row * pitch + ch * 8);
-                    const uint32_t at = dst + pg * (kPage * D * 2) + (ch >> 3) * (kPage * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4);
+                    const uint32_t at = dst + part * page_step + (ch >> 3) * half_step + row * 128 + (((ch & 7) ^ (row & 7)) << 4);
                     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
                 }
                 fence_async_proxy();
@@ -299,122 +316,130 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const List<AttendWor
             }
             if (chosen) {
                 mbar_expect_tx(bar, C::kKvBytes - (by_hand ? kPage * D * 2 : 0));
+                if (!a.page_table && (t + 1) * kKv <= stop) {
+                    tma_load_4d(dst, v_wide, 0, s.h, s.t.start + t * kKv, 0, bar);
+                } else if (a.page_table) {
 #pragma unroll
-                for (int pg = 0; pg < 4; ++pg) {
-                    if (pg == part && by_hand) continue;
-                    const int y = a.page_table ? 0 : s.h;
-                    const int z = pid[pg] < 0 ? (a.page_table ? a.P_phys * a.H_kv * kPage : a.T)
-                                              : a.page_table ? (pid[pg] * a.H_kv + s.h) * kPage : s.t.start + t * kKv + pg * kPage;
-                    tma_load_4d(dst + pg * (kPage * D * 2), v_map, 0, y, z, 0, bar);
+                    for (int pg = 0; pg < kGroups; ++pg)
+                        if (pg != part || !by_hand)
+                            tma_load_4d(dst + pg * page_step, v_map, 0, 0, (pid[pg] < 0 ? a.P_phys * a.H_kv : pid[pg] * a.H_kv + s.h) * kPage, 0, bar);
+                } else {
+#pragma unroll
+                    for (int pg = 0; pg < kGroups; ++pg)
+#pragma unroll
+                        for (int half = 0; half < C::kHalves; ++half)
+                            if (pg != part || !by_hand)
+                                tma_load_3d(dst + half * half_step + pg * page_step, v_map, half * 64, s.h,
+                                            pid[pg] < 0 ? a.T : s.t.start + t * kKv + pg * kPage, bar);
                 }
             }
             __syncwarp();
         }
     }
-    leave_ring<D>(ok, pos, 1, bars, gave_up, a);
+    leave_ring<C::kVSlots>(ok, tiles, v_full, v_empty, gave_up, a);
 }
 
 // ---- products ----------------------------------------------------------------------
-// The scores of a KV tile of 64 tokens take 64 columns, so every stream has two score buffers, and the next scores are there
-// when the softmax gets to them.  (Tiles of 128 tokens leave room for one buffer: products and softmax of a stream then
-// wait for one another, and the tensor cores stood idle for 40 % of the time.  A score product of 64 columns is bound by
-// shared memory, 49 cycles instead of 32: 20 % of both products, the smaller loss.)
-// One warp per stream issues its products: a wait queues up behind the products that its own warp has issued, so a single
-// warp for both streams let the tensor cores run dry at every wait.  The whole warp walks the list, so that addresses stay in
-// uniform registers; one elected lane issues.
-template <int D, int ST>
-__device__ __forceinline__ void mma_role(const AttendArgs &a, const List<AttendWork> &list, Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars, int lane) {
+// One warp issues all products, in the order of the steps of both streams: it waits for every tile's barriers in order (a
+// barrier tells its phases apart by parity alone, so a warp that left one out could take the phase before for the one it
+// waits for).  The whole warp walks the list, so that addresses stay in uniform registers; one elected lane issues (a role
+// run by a single lane took 82 cycles per instruction to issue, more than the 64 that it computes).
+template <int D>
+__device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, uint32_t q_smem, uint32_t ring,
+                                         uint32_t bars, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
-    const uint32_t tmem_s = ctl->tmem + ST * kTile, tmem_o = ctl->tmem + C::kTmemO + ST * D;
-    Segment s = {};
-    uint32_t pos = 0, queries = 0, o_used = 0, n = 0;                      // n: steps so far
+    const uint32_t tmem = ctl->tmem;
+    uint32_t tiles = 0, queries = 0, p_seen = 0, o_used = 0;               // bit st: parity of the stream's next wait
     bool any = false;
     const bool chosen = elect_one();
+    const uint32_t v_lead = a.page_table ? kPage * 128 : kKv * 128, v_step = (a.page_table ? kPage * D * 2 : kPage * 128) >> 4;
     auto wait = [&](int bar, uint32_t parity) { return warp_wait(bars + 8 * bar, parity & 1, gave_up, &a.ctl->status); };
-    auto slot = [&](uint32_t at) { return ring + at % C::kSlots * C::kKvBytes; };
-    // a ring slot is free when both streams have let it go
-    auto let_go = [&](uint32_t at) { mma_commit(bars + 8 * (kRing + C::kSlots + at % C::kSlots)); };
-    // S = Q K^T of the n-th step
-    auto scores = [&](uint32_t at, uint32_t n) {
-        const uint64_t qd = smem_operand(q_smem + (s.alt ? 0 : ST * C::kTileBytes), 16, 1024), kd = smem_operand(slot(at), 16, 1024);
-        const uint32_t d = tmem_s + (n & 1) * kKv;
-        tc_fence_after();
-        if (chosen) {
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-                mma_ss(d, qd + (k / 4) * (kTile * 128 >> 4) + (k % 4) * 2, kd + (k / 4) * (kKv * 128 >> 4) + (k % 4) * 2, mma_instr(kKv, false),
-                       k > 0);
-            mma_commit(bars + 8 * (kSFull + 2 * ST + (n & 1)));
-            let_go(at);
-        }
-        __syncwarp();
+    // `k_next`, `v_next`: the first tiles not waited for yet
+    uint32_t k_next = 0, v_next = 0;
+    auto wait_k = [&](uint32_t tile) {
+        for (; k_next <= tile; ++k_next)
+            if (!wait(kFull + k_next % C::kKSlots, k_next / C::kKSlots)) return false;
+        return true;
     };
-    // O += P V
-    auto values = [&](uint32_t at, uint32_t n, bool accumulate, bool last) {
-        const uint64_t vd = smem_operand(slot(at), kPage * 128, 1024);
-        const uint32_t p = tmem_s + (n & 1) * kKv;
-        tc_fence_after();
-        if (chosen) {
-#pragma unroll
-            for (int k = 0; k < kKv / 16; ++k) mma_ts(tmem_o, p + k * 8, vd + k * (kPage * D * 2 >> 4), mma_instr(D, true), accumulate || k > 0);
-            mma_commit(bars + 8 * ((last ? kOLast : kODone) + ST));
-            let_go(at);
-        }
-        __syncwarp();
+    auto wait_v = [&](uint32_t tile) {
+        for (; v_next <= tile; ++v_next)
+            if (!wait(kFull + C::kKSlots + v_next % C::kVSlots, v_next / C::kVSlots)) return false;
+        return true;
     };
     bool ok = true;
-    Walk<AttendWork> walk(list, a.ctl, &ctl->queue, gave_up, lane, false);
-    while (ok && next_segment(walk, s)) {
-        const int steps = ST ? s.steps1 : s.steps0;
-        const int tiles = s.b - s.a, stride = s.alt ? 2 : 1, first = s.alt ? ST : 0;   // this stream's tiles: first, first + stride, ...
-        // Every tile's barriers are waited for, in order, and the tiles of the other stream let go at once: a barrier tells its
-        // phases apart by parity alone, so a warp that left one out could take the phase before for the one it waits for.
-        auto reach = [&](int &next, int last, uint32_t v) {
-            for (; next <= last; ++next) {
-                const uint32_t at = pos + 2 * next + v;
-                if (!wait(kRing + at % C::kSlots, at / C::kSlots)) return false;
-                const bool mine = s.alt ? (next & 1) == ST : next < steps;
-                if (!mine && chosen) mbar_arrive(bars + 8 * (kRing + C::kSlots + at % C::kSlots));
-                __syncwarp();
+    while (ok) {
+        const Segment *s = ctl->queue.get(queries, gave_up, &a.ctl->status, lane);
+        if (!s) break;
+        const int steps0 = s->steps0, steps1 = s->steps1, steps = max(steps0, steps1);
+        const bool alt = s->alt;
+        auto place = [&](int st, int i) { return tiles + (alt ? 2 * i + st : i); };
+        // S = Q K^T (the chosen lane)
+        auto scores = [&](auto stream, uint32_t tile) {
+            constexpr int ST = decltype(stream)::value;
+            const uint32_t slot = tile % C::kKSlots;
+            const uint64_t qd = smem_operand(q_smem + (alt ? 0 : ST * C::kTileBytes), 16, 1024);
+            const uint64_t kd = smem_operand(ring + slot * C::kKvBytes, 16, 1024);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                const uint32_t off = (k / 4) * (kTile * 128 >> 4) + (k % 4) * 2;
+                mma_ss(tmem + ST * kTile, qd + off, kd + off, mma_instr(kKv, false), k > 0);
             }
+            mma_commit(bars + 8 * (kSFull + ST));
+            if (alt || ST == 1) mma_commit(bars + 8 * (kFull + C::kSlots + slot));
+        };
+        auto begin = [&](auto stream) {
+            constexpr int ST = decltype(stream)::value;
+            if ((ST ? steps1 : steps0) == 0) return true;
+            if (!wait_k(place(ST, 0))) return false;
+            tc_fence_after();
+            if (chosen) scores(stream, place(ST, 0));
+            __syncwarp();
             return true;
         };
-        int k_next = 0, v_next = 0;
-        ok = wait(kQFull, queries);
-        ++queries;
-        for (int u = 0; u < 2 && u < steps && ok; ++u)
-            if ((ok = reach(k_next, first + u * stride, 0))) scores(pos + 2 * (first + u * stride), n + u);
-        any = any || steps > 0;
-        if (!ok) break;
-        if (chosen && steps <= 2) {
-            if (steps > 0) mma_commit(bars + 8 * kQEmpty);
-            else mbar_arrive(bars + 8 * kQEmpty);
-        }
-        __syncwarp();
-        for (int u = 0, t = first; u < steps && ok; ++u, ++n, t += stride) {
+        // O += P V, and the next scores
+        auto step = [&](auto stream, int i) {
+            constexpr int ST = decltype(stream)::value;
+            const int mine = (ST ? steps1 : steps0);
+            if (i >= mine) return true;
+            const bool more = i + 1 < mine;
+            const uint32_t tile = place(ST, i), slot = tile % C::kVSlots;
+            const uint64_t vd = smem_operand(ring + (C::kKSlots + slot) * C::kKvBytes, v_lead, 1024);
             // everything that can be waited for early comes before the wait for the weights
-            const bool more = u + 2 < steps;
-            ok = reach(v_next, t, 1) && (!more || reach(k_next, t + 2 * stride, 0));
-            if (ok && u == 0) {          // the epilogue of the stream's last piece has read O
-                ok = wait(kOFree + ST, o_used ^ 1);
-                o_used ^= 1;
+            if (!wait_v(tile) || (more && !wait_k(place(ST, i + 1)))) return false;
+            if (i == 0) {                // the epilogue of the stream's last piece has read O
+                if (!wait(kOFree + ST, (o_used >> ST & 1) ^ 1)) return false;
+                o_used ^= 1u << ST;
             }
-            ok = ok && wait(kPReady + 2 * ST + (n & 1), n >> 1);
-            if (!ok) break;
-            values(pos + 2 * t + 1, n, u > 0, u + 1 == steps);
-            if (more) scores(pos + 2 * (t + 2 * stride), n);
-            if (chosen && u + 3 == steps) mma_commit(bars + 8 * kQEmpty);   // the last product with Q is on its way
+            if (!wait(kPReady + ST, p_seen >> ST)) return false;
+            p_seen ^= 1u << ST;
+            tc_fence_after();
+            if (chosen) {
+#pragma unroll
+                for (int k = 0; k < kKv / 16; ++k)
+                    mma_ts(tmem + C::kTmemO + ST * D, tmem + ST * kTile + k * 8, vd + k * v_step, mma_instr(D, true), i > 0 || k > 0);
+                if (alt || ST == 1) mma_commit(bars + 8 * (kFull + C::kSlots + C::kKSlots + slot));
+                if (more) scores(stream, place(ST, i + 1));
+                else mma_commit(bars + 8 * (kOLast + ST));
+            }
+            __syncwarp();
+            return true;
+        };
+        any = true;
+        ok = wait(kQFull, queries++) && begin(Int<0>{}) && begin(Int<1>{});
+        if (ok && chosen && steps == 1) mma_commit(bars + 8 * kQEmpty);
+        __syncwarp();
+        for (int i = 0; i < steps && ok; ++i) {
+            ok = step(Int<0>{}, i) && step(Int<1>{}, i);
+            if (ok && chosen && i + 2 == steps) mma_commit(bars + 8 * kQEmpty);   // the last product with Q is on its way
             __syncwarp();
         }
-        while (ok && v_next < tiles) ok = reach(k_next, v_next, 0) && reach(v_next, v_next, 1);
-        __syncwarp();
-        pos += 2u * tiles;
+        tiles += s->b - s->a;
     }
     if (any) {                           // nothing may be running when tensor memory goes away
-        if (chosen) mma_commit(bars + 8 * (kDrain + ST));
+        if (chosen) mma_commit(bars + 8 * kDrain);
         __syncwarp();
-        mbar_wait(bars + 8 * (kDrain + ST), 0);
+        mbar_wait(bars + 8 * kDrain, 0);
     }
 }
 
@@ -473,7 +498,7 @@ __device__ __forceinline__ void merge_rows(const AttendArgs &a, const Segment &s
             }
 #pragma unroll
             for (int k = 0; k < R; ++k) {
-                const float wk = __shfl_sync(kFull, w, min(k0 + k, 31));
+                const float wk = __shfl_sync(se::kFull, w, min(k0 + k, 31));
 #pragma unroll
                 for (int v = 0; v < V; ++v) acc[k][v] += wk > 0.f ? wk * x[k][v] : 0.f;   // a result without weight may be anything
             }
@@ -504,57 +529,54 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     const uint32_t t_s = ctl->tmem + lanes + st * kTile, t_o = ctl->tmem + lanes + C::kTmemO + st * D;
     const float sl = a.scale_log2;
-    Segment s;
-    uint32_t step = 0, tiles = 0, verdicts = 0, swaps = 0, ends = 0;
-    uint32_t inner = 0;                                                    // steps so far that were not a piece's last of an item
+    uint32_t step = 0, tiles = 0, verdicts = 0, swaps = 0, ends = 0, turn = 0;
     // both warpgroups have come here
     auto swap_sync = [&] {
         __syncwarp();
         if (lane == 0) mbar_arrive(bars + 8 * kSwap);
         return warp_wait(bars + 8 * kSwap, swaps++ & 1, gave_up, &a.ctl->status);
     };
-    Walk<AttendWork> walk(list, a.ctl, &ctl->queue, gave_up, lane, false);
-    while (next_segment(walk, s)) {
+    for (;;) {
+        const Segment *next = ctl->queue.get(turn++, gave_up, &a.ctl->status, lane);
+        if (!next) return;
+        const Segment &s = *next;
         const int tok = s.tok0 + (s.alt ? 0 : st * tpt);                   // the tile's first new token
         const int ntok = min(tpt, s.tok0 + s.ntok - tok);
         const int q = min(row / a.G, ntok - 1);
         const int sees = s.t.past + tok + q + 1;                           // tokens the row sees
-        const int least = __reduce_min_sync(kFull, sees);
+        const int least = __reduce_min_sync(se::kFull, sees);
         const int steps = s.steps(st);
+        const int stride = s.alt ? 2 : 1;
+        int left = sees - (s.a + (s.alt ? st : 0)) * kKv;                  // tokens that the row sees of this tile and the later ones
+        int most = least - (s.a + (s.alt ? st : 0)) * kKv;
+        uint32_t tile = tiles + (s.alt ? st : 0);
         float m = -INFINITY;                                               // in units of the raw scores
         float2 l2 = make_float2(0.f, 0.f);
-        for (int u = 0; u < steps; ++u, ++step) {
-            const int rel = s.alt ? 2 * u + st : u, first = (s.a + rel) * kKv;
-            const uint32_t buf = 2 * st + (step & 1), t_p = t_s + (step & 1) * kKv;
-            if (!warp_wait(bars + 8 * (kSFull + buf), step >> 1 & 1, gave_up, &a.ctl->status)) return;
+        for (int u = 0; u < steps; ++u, ++step, left -= stride * kKv, most -= stride * kKv, tile += stride) {
+            if (!warp_wait(bars + 8 * (kSFull + st), step & 1, gave_up, &a.ctl->status)) return;
             tc_fence_after();
             float x[kKv];
-            tmem_ld32(t_p, x);
-            tmem_ld32(t_p + 32, x + 32);
-            const unsigned mask = ctl->mask[(tiles + rel) % C::kMasks];
+#pragma unroll
+            for (int k = 0; k < kKv; k += 32) tmem_ld32<false>(t_s + k, x + k);   // (converged by the wait)
+            const unsigned mask = ctl->mask[tile % C::kMasks];
             tmem_wait_ld();
             settle<kKv>(x);
-            if (first + kKv > least || mask != 0xfu) {
-                const int limit = sees - first;
+            if (kKv > most || mask != 0xffu) {
 #pragma unroll
                 for (int k = 0; k < kKv; ++k)
-                    if (k >= limit || !(mask >> (k / kPage) & 1)) x[k] = -INFINITY;
+                    if (k >= left || !(mask >> (k / kPage) & 1)) x[k] = -INFINITY;
             }
-            float top[4] = {m, m, m, m};
+            float top[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-            for (int k = 0; k < kKv; k += 8)
+            for (int k = 4; k < kKv; k += 8)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) top[e] = max3(top[e], x[k + e], x[k + 4 + e]);
-            const float mn = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-            if (__any_sync(kFull, (mn - m) * sl > kSlack)) {
+                for (int e = 0; e < 4; ++e) top[e] = k + 4 + e < kKv ? max3(top[e], x[k + e], x[k + 4 + e]) : fmaxf(top[e], x[k + e]);
+            const float mn = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
+            if (__any_sync(se::kFull, (mn - m) * sl > kSlack)) {
                 const float f = m == -INFINITY ? 0.f : ex2((m - mn) * sl);
                 m = mn;
                 l2.x *= f, l2.y *= f;
-                if (u > 0) {
-                    // O + P V of the last step; the one before is complete (these scores were issued behind it), so the barrier's
-                    // parity says which of two phases it is in
-                    if (!warp_wait(bars + 8 * (kODone + st), (inner + u - 1) & 1, gave_up, &a.ctl->status)) return;
-                    tc_fence_after();
+                if (u > 0) {             // the product before these scores is complete: they were issued behind it
 #pragma unroll 1
                     for (int k = 0; k < D; k += 32) {
                         float o[32];
@@ -568,25 +590,27 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
                 }
             }
             const float off = m == -INFINITY ? 0.f : -m * sl;
-            uint32_t p[kKv / 2];
 #pragma unroll
-            for (int e = 0; e < kKv / 2; ++e) {
-                const float2 y = ffma2(make_float2(x[2 * e], x[2 * e + 1]), make_float2(sl, sl), make_float2(off, off));
-                const float2 w = make_float2(ex2(y.x), ex2(y.y));
-                l2 = __fadd2_rn(l2, w);
-                // the weights enter the product with V as bf16 (8 significant bits), their sum keeps fp32
-                const __nv_bfloat162 b = __float22bfloat162_rn(w);
-                p[e] = *reinterpret_cast<const uint32_t *>(&b);
+            for (int k = 0; k < kKv; k += 64) {
+                uint32_t p[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    const float2 y = ffma2(make_float2(x[k + 2 * e], x[k + 2 * e + 1]), make_float2(sl, sl), make_float2(off, off));
+                    const float2 w = make_float2(ex2(y.x), ex2(y.y));
+                    l2 = __fadd2_rn(l2, w);
+                    // the weights enter the product with V as bf16 (8 significant bits), their sum keeps fp32
+                    const __nv_bfloat162 b = __float22bfloat162_rn(w);
+                    p[e] = *reinterpret_cast<const uint32_t *>(&b);
+                }
+                tmem_st32<false>(t_s + k / 2, p);
             }
-            tmem_st32(t_p, p);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bars + 8 * (kPReady + buf));
+            if (lane == 0) mbar_arrive(bars + 8 * (kPReady + st));
             __syncwarp();
         }
         tiles += s.b - s.a;
-        inner += max(steps - 1, 0);
         if (steps > 0) {
             if (!warp_wait(bars + 8 * (kOLast + st), ends++ & 1, gave_up, &a.ctl->status)) return;
             tc_fence_after();
@@ -675,7 +699,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
                 if (last) atomicExch(ticket, 0u);
             }
             int parts = 0;
-            if (__shfl_sync(kFull, last, 0)) {
+            if (__shfl_sync(se::kFull, last, 0)) {
                 auto add = [&](int index) {
                     if (lane == 0 && parts < kMaxParts) ctl->part[st][parts] = (uint16_t)index;
                     ++parts;
@@ -705,7 +729,7 @@ template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
               const __grid_constant__ CUtensorMap k_wide, const __grid_constant__ CUtensorMap v_map,
-              const __grid_constant__ AttendArgs a) {
+              const __grid_constant__ CUtensorMap v_wide, const __grid_constant__ AttendArgs a) {
     using C = Cfg<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t base = smem_u32(smem);
@@ -719,25 +743,19 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
 
     if (threadIdx.x == 0) {
         mbar_init(bars + 8 * kQFull, 1);
-        mbar_init(bars + 8 * kQEmpty, 2);
+        mbar_init(bars + 8 * kQEmpty, 1);
         for (int st = 0; st < 2; ++st) {
-            for (int buf = 2 * st; buf < 2 * st + 2; ++buf) {
-                mbar_init(bars + 8 * (kSFull + buf), 1);
-                mbar_init(bars + 8 * (kPReady + buf), 4);
-            }
-            mbar_init(bars + 8 * (kODone + st), 1);
+            mbar_init(bars + 8 * (kSFull + st), 1);
+            mbar_init(bars + 8 * (kPReady + st), 4);
             mbar_init(bars + 8 * (kOLast + st), 1);
             mbar_init(bars + 8 * (kOFree + st), 4);
             mbar_init(bars + 8 * (kAll + st), 4);
             mbar_init(bars + 8 * (kVerdict + st), 1);
-            mbar_init(bars + 8 * (kDrain + st), 1);
         }
         mbar_init(bars + 8 * kSwap, 8);
-        for (int i = 0; i < C::kSlots; ++i) {
-            mbar_init(bars + 8 * (kRing + i), 1);
-            mbar_init(bars + 8 * (kRing + C::kSlots + i), 2);
-        }
-        ctl->queue.init(11);
+        mbar_init(bars + 8 * kDrain, 1);
+        for (int i = 0; i < 2 * C::kSlots; ++i) mbar_init(bars + 8 * (kFull + i), 1);
+        ctl->queue.init(10);
         mbar_fence_init();
         ctl->gave_up = 0;
     }
@@ -754,12 +772,14 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     tc_fence_after();
 
     if (warp < 8) {
+        regs_up<kRegsSoftmax>();
         softmax_role<D>(a, list, ctl, bars, warp >> 2);
     } else {
-        if (warp == kKWarp) k_role<D>(a, list, &q_map, &k_map, &k_wide, ctl, base, base + 2 * C::kTileBytes, bars, lane);
-        else if (warp == kVWarp) v_role<D>(a, list, &v_map, ctl, base + 2 * C::kTileBytes, bars, lane);
-        else if (warp == kMmaWarp) mma_role<D, 0>(a, list, ctl, base, base + 2 * C::kTileBytes, bars, lane);
-        else if (warp == kMmaWarp + 1) mma_role<D, 1>(a, list, ctl, base, base + 2 * C::kTileBytes, bars, lane);
+        regs_down<kRegsOther>();
+        const uint32_t ring = base + 2 * C::kTileBytes;
+        if (warp == kKWarp) k_role<D>(a, list, &q_map, &k_map, &k_wide, ctl, base, ring, bars, lane);
+        else if (warp == kVWarp) v_role<D>(a, &v_map, &v_wide, ctl, ring, bars, lane);
+        else if (warp == kMmaWarp) mma_role<D>(a, ctl, base, ring, bars, lane);
         __syncwarp();
     }
     tc_fence_before();
@@ -775,16 +795,17 @@ template <int D>
 cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t stream) {
     using C = Cfg<D>;
     const int G = p.H_q / p.H_kv;
-    CUtensorMap q_map, k_map, k_wide, v_map;
+    CUtensorMap q_map, k_map, k_wide, v_map, v_wide;
     bool ok = make_rows_map(&q_map, c.q, D, p.H_q, c.total_tokens, c.q_stride, G, kTile / G);
     if (c.page_table) {
         const long long rows = (long long)p.num_phys_pages * p.H_kv * kPage;
         ok = ok && make_rows_map(&k_map, c.k, D, 1, rows, D, 1, kPage) && make_split_map(&v_map, c.v, D, 1, rows, D, kPage);
-        k_wide = k_map;                                          // not used
+        k_wide = k_map, v_wide = v_map;                          // not used
     } else {
         ok = ok && make_rows_map(&k_map, c.k, D, p.H_kv, c.total_tokens, c.k_stride, 1, kPage) &&
              make_split_map(&k_wide, c.k, D, p.H_kv, c.total_tokens, c.k_stride, kKv) &&
-             make_split_map(&v_map, c.v, D, p.H_kv, c.total_tokens, c.v_stride, kPage);
+             make_rows_map(&v_map, c.v, D, p.H_kv, c.total_tokens, c.v_stride, 1, kPage) &&
+             make_split_map(&v_wide, c.v, D, p.H_kv, c.total_tokens, c.v_stride, kKv);
     }
     if (!ok) return cudaErrorInvalidValue;
     AttendArgs a = {};
@@ -797,11 +818,16 @@ cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t 
     a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.G = G, a.T = c.total_tokens, a.max_pages = p.max_pages;
     a.P_phys = p.num_phys_pages, a.scale_log2 = effective_scale(p) * kLog2e;
     auto kern = attend_kernel<D>;
-    cudaError_t e;
-    const size_t smem = 2 * C::kTileBytes + C::kSlots * C::kKvBytes + sizeof(Control<D>);
+    // the register split (setmaxnreg) draws on what the block was launched with
+    cudaFuncAttributes attr;
+    cudaError_t e = cudaFuncGetAttributes(&attr, kern);
+    if (e != cudaSuccess) return e;
+    if (attr.numRegs * kThreads < 256 * kRegsSoftmax + 128 * kRegsOther) return cudaErrorInvalidConfiguration;
+    constexpr size_t smem = 2 * C::kTileBytes + C::kSlots * C::kKvBytes + sizeof(Control<D>);
+    static_assert(smem <= 227 * 1024, "shared memory of a CTA");
     e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    kern<<<kPromptCtas, kThreads, smem, stream>>>(q_map, k_map, k_wide, v_map, a);
+    kern<<<kPromptCtas, kThreads, smem, stream>>>(q_map, k_map, k_wide, v_map, v_wide, a);
     return cudaGetLastError();
 }
 

@@ -49,17 +49,6 @@ struct MassArgs {
 enum Bar { kSFull, kSFree = kSFull + 4, kLseFull = kSFree + 4, kLseEmpty = kLseFull + kLseSlots, kKFull = kLseEmpty + kLseSlots,
            kKEmpty = kKFull + 2, kAll = kKEmpty + 2, kVerdict = kAll + 2, kDrain = kVerdict + 2, kRing };
 
-template <int D>
-struct Control {
-    uint64_t bars[kRing + 2 * Cfg<D>::kSlots];
-    alignas(16) float lse[kLseSlots][kTile];   // -lse log2 e of the query tiles' rows, -inf for rows that count for nothing
-    PieceQueue queue;
-    alignas(8) uint8_t prefix[prefix_bytes(kSmemRequests)];
-    int last[2];
-    int gave_up;
-    uint32_t tmem;
-};
-
 struct MassWork {
     const int32_t *cu, *seq_lens;
     int T, max_tokens, tpt;            // tpt: new tokens of a query tile
@@ -84,6 +73,7 @@ struct MassWork {
     __device__ __forceinline__ int unit_at(const TokenRange &, int, long long z) const { return (int)(z / tpt); }
     __device__ __forceinline__ long long min_cost() const { return 4 * tpt; }
     static constexpr int kCrumb = 2;   // least units of a part of an item
+    static constexpr bool kShares = false;
 };
 
 struct Segment {
@@ -93,6 +83,17 @@ struct Segment {
     int piece, units, a, b;   // piece, query tiles: all of the item's, the piece's
     int q0;                // the item's first query tile within the request
     int skip1;             // units before the second tile of cached tokens is seen
+};
+
+template <int D>
+struct Control {
+    uint64_t bars[kRing + 2 * Cfg<D>::kSlots];
+    alignas(16) float lse[kLseSlots][kTile];   // -lse log2 e of the query tiles' rows, -inf for rows that count for nothing
+    SegmentQueue<Segment> queue;
+    alignas(8) uint8_t prefix[prefix_bytes(kSmemRequests)];
+    int last[2];
+    int gave_up;
+    uint32_t tmem;
 };
 
 __device__ __forceinline__ bool next_segment(Walk<MassWork> &walk, Segment &s) {
@@ -124,12 +125,14 @@ __device__ __forceinline__ void copy_role(const MassArgs &a, const List<MassWork
                                           uint32_t k_smem, uint32_t ring, uint32_t bars, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
-    Walk<MassWork> walk(list, a.ctl, &ctl->queue, gave_up, lane, true);
+    Walk<MassWork> walk(list, a.ctl, lane);
     Segment s;
     uint32_t pos = 0, pairs = 0;
     const bool chosen = elect_one();
     bool ok = true;
     while (ok && next_segment(walk, s)) {
+        ok = ctl->queue.put(pairs, &s, gave_up, &a.ctl->status, lane);
+        if (!ok) break;
         // K: 16 groups of 16 tokens.  Absent groups come from behind the tensor's last row, which reads as zeros.
         const int pid = group_page(a, s, s.pos0 / kPage + (lane & 15), lane < 16);
         const int z = pid >= 0 ? (pid * a.H_kv + s.h) * kPage : a.P_phys * a.H_kv * kPage;
@@ -163,6 +166,7 @@ __device__ __forceinline__ void copy_role(const MassArgs &a, const List<MassWork
             __syncwarp();
         }
     }
+    if (ok) ok = ctl->queue.put(pairs, nullptr, gave_up, &a.ctl->status, lane);
     // nothing may still be on its way to the CTA's shared memory when the CTA ends: copies, and the products' arrivals on the
     // barriers of the tiles they have let go
     for (uint32_t p = pos > C::kSlots ? pos - C::kSlots : 0; p < pos; ++p) {
@@ -180,11 +184,12 @@ __device__ __forceinline__ void copy_role(const MassArgs &a, const List<MassWork
 template <int D>
 __device__ __forceinline__ void lse_role(const MassArgs &a, const List<MassWork> &list, Control<D> *ctl, uint32_t bars, int lane) {
     volatile int *gave_up = &ctl->gave_up;
-    Walk<MassWork> walk(list, a.ctl, &ctl->queue, gave_up, lane, false);
-    Segment s;
-    uint32_t tiles = 0;
+    uint32_t tiles = 0, turn = 0;
     const int live = list.w.tpt * a.G;
-    while (next_segment(walk, s)) {
+    for (;;) {
+        const Segment *next = ctl->queue.get(turn++, gave_up, &a.ctl->status, lane);
+        if (!next) break;
+        const Segment s = *next;
         float x[4];
         auto fetch = [&](int u) {
             const int tok = (s.q0 + u) * list.w.tpt;
@@ -208,17 +213,18 @@ __device__ __forceinline__ void lse_role(const MassArgs &a, const List<MassWork>
 }
 
 template <int D>
-__device__ __forceinline__ void mma_role(const MassArgs &a, const List<MassWork> &list, Control<D> *ctl, uint32_t k_smem, uint32_t ring, uint32_t bars, int lane) {
+__device__ __forceinline__ void mma_role(const MassArgs &a, Control<D> *ctl, uint32_t k_smem, uint32_t ring, uint32_t bars, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     constexpr uint32_t kInstr = mma_instr(kTile, false);
     const uint32_t tmem = ctl->tmem;
-    Walk<MassWork> walk(list, a.ctl, &ctl->queue, gave_up, lane, false);
-    Segment s;
     uint32_t pos = 0, pairs = 0, step0 = 0, step1 = 0;
     const bool chosen = elect_one();
     bool ok = true, any = false;
-    while (ok && next_segment(walk, s)) {
+    while (ok) {
+        const Segment *next = ctl->queue.get(pairs, gave_up, &a.ctl->status, lane);
+        if (!next) break;
+        const Segment s = *next;
         const uint32_t kb = pairs & 1;
         ok = warp_wait(bars + 8 * (kKFull + kb), pairs >> 1 & 1, gave_up, &a.ctl->status);
         ++pairs;
@@ -263,10 +269,11 @@ __device__ __forceinline__ void sum_role(const MassArgs &a, const List<MassWork>
     const int row = threadIdx.x & 127, lane = threadIdx.x & 31, warp = row >> 5;
     const uint32_t t_s = ctl->tmem + ((uint32_t)(warp * 32) << 16) + 2 * st * kTile;
     const float2 sl = make_float2(a.scale_log2, a.scale_log2);
-    Walk<MassWork> walk(list, a.ctl, &ctl->queue, gave_up, lane, false);
-    Segment s;
-    uint32_t step = 0, tiles = 0, verdicts = 0;
-    while (next_segment(walk, s)) {
+    uint32_t step = 0, tiles = 0, verdicts = 0, turn = 0;
+    for (;;) {
+        const Segment *next = ctl->queue.get(turn++, gave_up, &a.ctl->status, lane);
+        if (!next) break;
+        const Segment s = *next;
         const int pos = s.pos0 + st * kTile + row;                         // the thread's cached token
         const int pid = group_page(a, s, pos / kPage, false);
         float2 s0 = make_float2(0.f, 0.f), s1 = s0;
@@ -404,7 +411,7 @@ mass_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ C
     if (warp < 8) sum_role<D>(a, list, ctl, bars, warp >> 2);
     else if (warp == kCopyWarp) copy_role<D>(a, list, &q_map, &k_map, ctl, base, ring, bars, lane);
     else if (warp == kLseWarp) lse_role<D>(a, list, ctl, bars, lane);
-    else if (warp == kMmaWarp) mma_role<D>(a, list, ctl, base, ring, bars, lane);
+    else if (warp == kMmaWarp) mma_role<D>(a, ctl, base, ring, bars, lane);
     __syncwarp();
     tc_fence_before();
     __syncthreads();

@@ -5,8 +5,9 @@
 //
 // Pieces of equal cost do not take equal time: SMs differ in their distance to the data, and no cost model knows every short
 // item.  With one piece per CTA the slowest CTA took 9 % (one long prompt) to 29 % (mixed batches) longer than the mean.
-// So a large batch is cut three times: 148 pieces with 7/10 of the cost, 148 with 2/10, 148 with 1/10; a CTA begins with
-// the piece of its number and then takes the next one that nobody has.
+// So a large batch can be cut twice: 148 pieces with 9/10 of the cost, 148 with the rest; a CTA begins with the piece of its
+// number and then takes the next one that nobody has.  Attention over eight packed prompts took 403 us with it, 410 us with one
+// piece each, 428 us with three sizes (7/10, 2/10, 1/10); 2048 tokens over 65536: 1880 to 1935, 1940, 1945 us.
 //
 // A border is found by a search, because an item's cost has a closed form: every CTA makes one prefix sum over the
 // requests, and looks up the borders of the pieces that it takes or merges.  There is no planning kernel, and no table that
@@ -20,6 +21,8 @@
 //   int unit_at(t, i, z)               unit that cost z into the item falls in
 //   long long min_cost()               least cost of a piece
 //   kCrumb                             least units of a part of a split item
+//   kShares                            whether a large batch is cut into pieces of two sizes;
+//   long long longest(t)               then: a bound on the cost of the request's items
 #pragma once
 
 #include "se_tc.cuh"
@@ -28,7 +31,7 @@ namespace se {
 
 constexpr int kPromptCtas = 148;       // one per SM
 constexpr int kPromptThreads = 384;
-constexpr int kMaxPieces = 3 * kPromptCtas;
+constexpr int kMaxPieces = 2 * kPromptCtas;
 constexpr int kSmemRequests = 96;      // batches up to here keep their prefix sums in shared memory
 
 // Head of the workspace of the prompt calls (zero when no call is running).
@@ -63,13 +66,10 @@ struct List {
     long long total, size;             // size: cost of a piece where all are equal
 
     __device__ __forceinline__ Border border(int p) const {
-        const int level = p / kPromptCtas, k = p - level * kPromptCtas;
-        const long long tenth = total / 10;
+        const long long large = total / 10 * 9;
         const long long at = pieces == kPromptCtas ? size * p
-                             : level == 0          ? tenth * 7 * k / kPromptCtas
-                             : level == 1          ? tenth * 7 + tenth * 2 * k / kPromptCtas
-                             : level == 2          ? tenth * 9 + (total - tenth * 9) * k / kPromptCtas
-                                                   : total;
+                             : p < kPromptCtas     ? large * p / kPromptCtas
+                                                   : large + (total - large) * (p - kPromptCtas) / kPromptCtas;
         Border b = {first[B], 0, B, 0, 0};
         if (at >= total) return b;
         int lo = 0, hi = B;                // last request whose cost begins at or before `at`
@@ -110,17 +110,18 @@ struct List {
 };
 
 // The list of a batch; all threads of the CTA.  `own` holds the prefix sums for good: shared memory, or the CTA's part of the
-// workspace; sums: 144 bytes of shared memory, free afterwards.  Ends with a barrier.
+// workspace; sums: 240 bytes of shared memory, free afterwards.  Ends with a barrier.
 template <class Work>
 __device__ __forceinline__ List<Work> make_list(const Work &w, int B, int H_kv, PromptControl *ctl, void *own, void *sums) {
     constexpr int kWarps = kPromptThreads / 32;
     long long *cost = reinterpret_cast<long long *>(own);
     int *first = reinterpret_cast<int *>(cost + B + 1);
     long long *s_cost = reinterpret_cast<long long *>(sums);
-    int *s_items = reinterpret_cast<int *>(s_cost + kWarps);
+    long long *s_long = s_cost + kWarps;
+    int *s_items = reinterpret_cast<int *>(s_long + kWarps);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (B + kPromptThreads - 1) / kPromptThreads;
-    long long sum = 0;
+    long long sum = 0, longest = 0;
     int n = 0;
     for (int k = 0; k < per; ++k) {
         const int r = tid * per + k;
@@ -131,6 +132,7 @@ __device__ __forceinline__ List<Work> make_list(const Work &w, int B, int H_kv, 
         const long long c = t.n ? w.cost(t, items) : 0;
         cost[r] = c, first[r] = items;
         sum += c * H_kv, n += items * H_kv;
+        if constexpr (Work::kShares) longest = max(longest, t.n ? w.longest(t) : 0ll);
     }
     long long si = sum;
     int ni = n;
@@ -139,12 +141,14 @@ __device__ __forceinline__ List<Work> make_list(const Work &w, int B, int H_kv, 
         const long long x = __shfl_up_sync(kFull, si, o);
         const int y = __shfl_up_sync(kFull, ni, o);
         if (lane >= o) si += x, ni += y;
+        longest = max(longest, __shfl_xor_sync(kFull, longest, o));
     }
-    if (lane == 31) s_cost[warp] = si, s_items[warp] = ni;
+    if (lane == 31) s_cost[warp] = si, s_items[warp] = ni, s_long[warp] = longest;
     __syncthreads();
     long long sb = si - sum;
     int nb = ni - n;
     for (int k = 0; k < warp; ++k) sb += s_cost[k], nb += s_items[k];
+    for (int k = 0; k < kWarps; ++k) longest = max(longest, s_long[k]);
     for (int k = 0; k < per; ++k) {
         const int r = tid * per + k;
         if (r >= B) break;
@@ -156,106 +160,101 @@ __device__ __forceinline__ List<Work> make_list(const Work &w, int B, int H_kv, 
     if (tid == kPromptThreads - 1) cost[B] = sb, first[B] = nb;
     __syncthreads();
     List<Work> l = {w, B, H_kv, cost, first, kMaxPieces, cost[B], 0};
-    // the small pieces have to be worth their partial results
-    if (l.total / 10 < (long long)kPromptCtas * 5 * w.min_cost()) l.pieces = kPromptCtas;
+    // the small pieces have to be worth their partial results, and no item may fall into more than 148 of them and a few others
+    if (!Work::kShares || l.total / 10 < (long long)kPromptCtas * 5 * w.min_cost() || l.total / 10 < longest) l.pieces = kPromptCtas;
     l.size = (l.total + kPromptCtas - 1) / kPromptCtas;
     if (l.size < w.min_cost()) l.size = w.min_cost();
     return l;
 }
 
-// Pieces on their way through the roles of a CTA: one warp takes them, the others (listeners) hear of them through shared
-// memory, two at a time.
-struct PieceQueue {
-    uint64_t full[2], empty[2];
-    struct {
-        int piece;         // -1: no more
-        Border begin;
-        int e_item, e_unit;
-    } entry[2];
+// The parts of items that a CTA works on (a `Segment` of the kernel), on their way from the warp that walks the CTA's pieces to
+// the other roles, a few at a time: the roles read what they need where they need it, and keep their registers.
+template <class Segment>
+struct SegmentQueue {
+    static constexpr uint32_t kDepth = 4;
+    uint64_t full[kDepth], empty[kDepth];
+    Segment entry[kDepth];
+    int more[kDepth];                  // 0: the list has ended
 
     __device__ __forceinline__ void init(int listeners) {
-        for (int k = 0; k < 2; ++k) {
+        for (uint32_t k = 0; k < kDepth; ++k) {
             mbar_init(smem_u32(&full[k]), 1);
             mbar_init(smem_u32(&empty[k]), listeners);
         }
     }
+    // by the warp that walks, the n-th entry; false: a wait gave up
+    __device__ __forceinline__ bool put(uint32_t n, const Segment *s, volatile int *gave_up, uint32_t *status, int lane) {
+        const uint32_t k = n % kDepth;
+        if (!warp_wait(smem_u32(&empty[k]), (n / kDepth & 1) ^ 1, gave_up, status)) return false;
+        if (lane == 0) {
+            if (s) entry[k] = *s;
+            more[k] = s != nullptr;
+            mbar_arrive(smem_u32(&full[k]));
+        }
+        __syncwarp();
+        return true;
+    }
+    // by the other warps, one entry after the other; nullptr: no more, or a wait gave up
+    __device__ __forceinline__ const Segment *get(uint32_t n, volatile int *gave_up, uint32_t *status, int lane) {
+        if (n > 0) {                   // done with the one before
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&empty[(n - 1) % kDepth]));
+            __syncwarp();
+        }
+        const uint32_t k = n % kDepth;
+        if (!warp_wait(smem_u32(&full[k]), n / kDepth & 1, gave_up, status) || !*(volatile int *)&more[k]) return nullptr;
+        return &entry[k];
+    }
 };
 
-// A role's way through the items of its CTA's pieces; every role does it for itself.  An item that an earlier piece began comes
-// last: whole items and the item that a later piece ends are walked from their first unit, and what is left of the first item
-// then falls on the units that the neighbours are at, so CTAs that share a head read the same tiles at about the same time
-// and all but one of them find the tile in L2.
+// One warp's way through the items of its CTA's pieces.  An item that an earlier piece began comes last: whole items and the
+// item that a later piece ends are walked from their first unit, and what is left of the first item then falls on the units
+// that the neighbours are at, so CTAs that share a head read the same tiles at about the same time and all but one of them
+// find the tile in L2.
 template <class Work>
 struct Walk {
     const List<Work> &l;
     PromptControl *ctl;
-    PieceQueue *queue;
-    volatile int *gave_up;
     int lane;
-    bool taker;
-    uint32_t turn = 0;                 // pieces so far
+    bool begun = false;
+    Border first;                      // of the piece
+    int end_item, end_unit_;
     // the item that the walk has come to
     int r, h, i, unit, item, piece;
     TokenRange t;
     int late = 2;                      // 0 no item to come back to, 1 still to come, 2 being done
 
-    __device__ __forceinline__ Walk(const List<Work> &l, PromptControl *ctl, PieceQueue *queue, volatile int *gave_up, int lane, bool taker)
-        : l(l), ctl(ctl), queue(queue), gave_up(gave_up), lane(lane), taker(taker) {}
+    __device__ __forceinline__ Walk(const List<Work> &l, PromptControl *ctl, int lane) : l(l), ctl(ctl), lane(lane) {}
 
-    __device__ __forceinline__ volatile int *entry() const {
-        return reinterpret_cast<volatile int *>(&queue->entry[(turn - 1) & 1]);
-    }
     __device__ __forceinline__ void to_begin() {
-        const volatile int *e = entry();
-        item = e[1], unit = e[2], r = e[3], h = e[4], i = e[5];
+        item = first.item, unit = first.unit, r = first.r, h = first.h, i = first.i;
         t = TokenRange{0, 0, 0, false};
         if (r < l.B) t = l.w.tokens(r);
     }
-    // One piece taken and announced; false: no more, or a wait gave up.
     __device__ __forceinline__ bool take() {
-        int p = blockIdx.x;
-        if (turn > 0) {
-            p = -1;
-            if (l.pieces > (int)gridDim.x) {
-                if (lane == 0) p = (int)(gridDim.x + atomicAdd(&ctl->next_piece, 1u));
-                p = __shfl_sync(kFull, p, 0);
-                if (p >= l.pieces) p = -1;
+        piece = blockIdx.x;
+        if (begun) {
+            if (l.pieces == (int)gridDim.x) return false;
+            if (lane == 0) piece = (int)(gridDim.x + atomicAdd(&ctl->next_piece, 1u));
+            piece = __shfl_sync(kFull, piece, 0);
+            if (piece >= l.pieces) {
+                // the last CTA to see the end leaves the counters as it found them
+                if (lane == 0 && atomicInc(&ctl->ended, gridDim.x - 1) == gridDim.x - 1) atomicExch(&ctl->next_piece, 0u);
+                __syncwarp();
+                return false;
             }
         }
+        begun = true;
         Border b = {};
-        if (p >= 0 && lane < 2) b = l.border(p + lane);
+        if (lane < 2) b = l.border(piece + lane);
         __syncwarp();
-        const uint32_t k = turn & 1;
-        if (!warp_wait(smem_u32(&queue->empty[k]), (turn >> 1 & 1) ^ 1, gave_up, &ctl->status)) return false;
-        volatile int *e = reinterpret_cast<volatile int *>(&queue->entry[k]);
-        if (lane == 0) e[0] = p, e[1] = b.item, e[2] = b.unit, e[3] = b.r, e[4] = b.h, e[5] = b.i;
-        if (lane == 1) e[6] = b.item, e[7] = b.unit;
-        __syncwarp();
-        if (lane == 0) {
-            mbar_arrive(smem_u32(&queue->full[k]));
-            // the last CTA to see the end leaves the counters as it found them
-            if (p < 0 && l.pieces > (int)gridDim.x && atomicInc(&ctl->ended, gridDim.x - 1) == gridDim.x - 1) atomicExch(&ctl->next_piece, 0u);
-        }
-        __syncwarp();
-        ++turn;
-        piece = p;
-        return p >= 0;
-    }
-    __device__ __forceinline__ bool hear() {
-        if (turn > 0) {                // done with the last one
-            if (lane == 0) mbar_arrive(smem_u32(&queue->empty[(turn - 1) & 1]));
-            __syncwarp();
-        }
-        if (!warp_wait(smem_u32(&queue->full[turn & 1]), turn >> 1 & 1, gave_up, &ctl->status)) return false;
-        ++turn;
-        piece = entry()[0];
-        return piece >= 0;
+        first = Border{__shfl_sync(kFull, b.item, 0), __shfl_sync(kFull, b.unit, 0), __shfl_sync(kFull, b.r, 0), __shfl_sync(kFull, b.h, 0),
+                       __shfl_sync(kFull, b.i, 0)};
+        end_item = __shfl_sync(kFull, b.item, 1), end_unit_ = __shfl_sync(kFull, b.unit, 1);
+        return true;
     }
     // Units of the item that belong to the piece end here.
-    __device__ __forceinline__ int end_unit(int units) const {
-        const volatile int *e = entry();
-        return item == e[6] ? min(e[7], units) : units;
-    }
+    __device__ __forceinline__ int end_unit(int units) const { return item == end_item ? min(end_unit_, units) : units; }
     __device__ __forceinline__ void next() {
         unit = 0;
         ++item;
@@ -267,21 +266,20 @@ struct Walk {
             if (++r < l.B) t = l.w.tokens(r);
         } while (r < l.B && t.n == 0);
     }
-    // On an item (or a part of one) to work on; false: no more, or a wait gave up.
+    // On an item (or a part of one) to work on; false: no more.
     __device__ __forceinline__ bool find() {
         for (;;) {
-            if (turn > 0) {
-                const volatile int *e = entry();
-                if (late < 2 && r < l.B && (item < e[6] || (item == e[6] && unit < e[7]))) return true;
+            if (begun) {
+                if (late < 2 && r < l.B && (item < end_item || (item == end_item && unit < end_unit_))) return true;
                 if (late == 1) {
                     to_begin();
                     late = 2;
                     return true;
                 }
             }
-            if (!(taker ? take() : hear())) return false;
+            if (!take()) return false;
             to_begin();
-            late = r < l.B && unit > 0 && item < entry()[6];
+            late = r < l.B && unit > 0 && item < end_item;
             if (late) next();
         }
     }

@@ -35,9 +35,11 @@ __device__ __forceinline__ void settle(float *v) {
 }
 
 // 32 consecutive 32-bit columns of the warp's 32 lanes: lane i of the warp gets row i.  The access is one of the whole warp,
-// which has to be converged; after a branch on the lane only a warp barrier makes sure of that.
+// which has to be converged; after a branch on the lane only a warp barrier makes sure of that (SYNC = false: none since the
+// last one).
+template <bool SYNC = true>
 __device__ __forceinline__ void tmem_ld32(uint32_t addr, float *v) {
-    __syncwarp();
+    if (SYNC) __syncwarp();
     uint32_t *r = reinterpret_cast<uint32_t *>(v);
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
@@ -48,8 +50,9 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, float *v) {
           "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(addr));
 }
+template <bool SYNC = true>
 __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t *r) {
-    __syncwarp();
+    if (SYNC) __syncwarp();
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
         "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr),
@@ -117,53 +120,32 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 
 // Wait of a warp of a role.  Gives up after 400 million cycles (200 ms at 1.97 GHz), or as soon as another role of the CTA has
 // given up (*gave_up != 0, shared memory); the first one to give up reports it.  False: leave the role's loop.
-// The warp stays together, vote by vote: tensor copies and products take their operands from uniform registers, which
-// lanes that ran ahead of the issuing lane would overwrite, and tensor memory is accessed by whole warps.
+// The warp leaves it together: tensor copies and products take their operands from uniform registers, which lanes that ran ahead
+// of the issuing lane would overwrite, and tensor memory is accessed by whole warps.  (A vote at every look took 2 to 10 % of
+// the attention kernel's time.)
 constexpr long long kWaitLimitCycles = 400ll * 1000 * 1000;
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *gave_up, uint32_t *status) {
-    if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
-    const long long t0 = clock64();
-    for (;;) {
+    bool got = mbar_try_wait(bar, parity);
+    if (!got) {
+        const long long t0 = clock64();
+        for (;;) {
 #pragma unroll 1
-        for (int it = 0; it < 64; ++it)
-            if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
-        const bool late = __any_sync(kFull, clock64() - t0 > kWaitLimitCycles);
-        if (late) {
-            *gave_up = 1;
-            atomicOr(status, SE_DEV_WAIT_TIMEOUT);
+            for (int it = 0; it < 64 && !got; ++it) got = mbar_try_wait(bar, parity);
+            if (got || *gave_up) break;
+            if (clock64() - t0 > kWaitLimitCycles) {
+                *gave_up = 1;
+                atomicOr(status, SE_DEV_WAIT_TIMEOUT);
+                break;
+            }
         }
-        if (__any_sync(kFull, late || *gave_up != 0)) return false;
     }
+    return __all_sync(kFull, got);
 }
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
-}
-
-// 2^x of a pair without the special-function unit: x = j + f with |f| <= 1/2 (j by adding and taking off 1.5 * 2^23),
-// 2^f by a minimax polynomial of the given degree (own fit; relative error 2.7e-6 for 4, 2.1e-7 for 5, fp32 rounding
-// included), j added to the exponent field.  Below -126 the result stays near 2^-126 instead of reaching 0.
-template <int DEG>
-__device__ __forceinline__ float2 ex2_fma(float2 x) {
-    static_assert(DEG == 4 || DEG == 5, "coefficients");
-    constexpr float kMagic = 12582912.f;
-    x.x = fmaxf(x.x, -126.f), x.y = fmaxf(x.y, -126.f);
-    const float2 t = __fadd2_rn(x, make_float2(kMagic, kMagic));
-    const float2 f = __fadd2_rn(x, ffma2(t, make_float2(-1.f, -1.f), make_float2(kMagic, kMagic)));
-    float2 p;
-    auto step = [&](float c) { p = ffma2(p, f, make_float2(c, c)); };
-    if constexpr (DEG == 4) {
-        p = make_float2(0.009570102207362652f, 0.009570102207362652f);
-        step(0.05591786280274391f), step(0.240247443318367f), step(0.6931217908859253f), step(0.9999992847442627f);
-    } else {
-        p = make_float2(0.0013276472454890609f, 0.0013276472454890609f);
-        step(0.009675541892647743f), step(0.05550713092088699f), step(0.24022120237350464f), step(0.6931469440460205f);
-        step(1.0000001192092896f);
-    }
-    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
-                       __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 
 template <int N>
