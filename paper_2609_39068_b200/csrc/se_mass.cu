@@ -9,7 +9,9 @@
 // What bounds it: per 128 x 128 tile one product of 512 tensor cycles (D = 128) and 16384 exponentials = 1024 cycles of
 // the special-function units; K is read once per item, the queries come from L2.  A CTA works on two tiles of cached tokens
 // (one warpgroup each) that share every query tile.  Scores are double-buffered in tensor memory (4 x 128 columns), so the
-// products of the next query tile run under the exponentials of this one.
+// products of the next query tile run under the exponentials of this one, and a quarter of the exponentials is taken off the
+// special-function units.  Prompt of 16384 tokens (32 heads over 8, D = 128): 1412 us; with all exponentials on the
+// special-function units 1492 us, their bound being 1.2 ms at the 1.8 GHz that the power limit leaves.
 //
 // Item = 256 cached tokens of one (request, kv-head), unit = query tile; pieces and merging as in se_pieces.cuh (a partial
 // result is one number per cached token).
@@ -22,6 +24,29 @@
 namespace se {
 
 namespace {
+
+// One pair of weights in four is computed without the special-function unit, which bounds the kernel (prompt of 16384: none
+// 1497 us, one in four 1408 us, one in two 1690 us).
+// 2^x of a pair: x = j + f with |f| <= 1/2 (j by adding and taking off 1.5 * 2^23), 2^f by a
+// minimax polynomial of degree 5 with 2^0 = 1 (own fit; relative error 1.6e-7, fp32 rounding included), j added to the exponent
+// field.  x is held to [-127, 128], where the exponent field comes out as 0 and as that of infinity; below -126 the result is
+// less than 2^-126.  The integer arithmetic loses a NaN, so `nan` collects them: 0, or NaN once x has been one.
+__device__ __forceinline__ float2 ex2_fma(float2 x, float2 &nan) {
+    constexpr float kMagic = 12582912.f;
+    auto hold = [](float v) {
+        asm("max.NaN.f32 %0, %0, 0fC2FE0000;\n\tmin.NaN.f32 %0, %0, 0f43000000;" : "+f"(v));
+        return v;
+    };
+    x = make_float2(hold(x.x), hold(x.y));
+    nan = ffma2(x, make_float2(0.f, 0.f), nan);
+    const float2 t = __fadd2_rn(x, make_float2(kMagic, kMagic));
+    const float2 f = __fadd2_rn(x, ffma2(t, make_float2(-1.f, -1.f), make_float2(kMagic, kMagic)));
+    float2 p = make_float2(0.0013274633092805743f, 0.0013274633092805743f);
+    auto step = [&](float k) { p = ffma2(p, f, make_float2(k, k)); };
+    step(0.009671961888670921f), step(0.055506784468889236f), step(0.24022234976291656f), step(0.6931470632553101f), step(1.f);
+    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
+                       __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+}
 
 constexpr int kThreads = kPromptThreads;   // 2 summing warpgroups, copy warp, product warp, lse warp, idle warp
 constexpr int kCopyWarp = 8, kMmaWarp = 9, kLseWarp = 10;
@@ -276,7 +301,7 @@ __device__ __forceinline__ void sum_role(const MassArgs &a, const List<MassWork>
         const Segment s = *next;
         const int pos = s.pos0 + st * kTile + row;                         // the thread's cached token
         const int pid = group_page(a, s, pos / kPage, false);
-        float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+        float sum = 0.f, lost = 0.f;   // of the query tiles so far, and what rounding took from it (Kahan)
         for (int u = s.a; u < s.b; ++u, ++tiles) {
             const uint32_t slot = tiles % kLseSlots;
             if (!warp_wait(bars + 8 * (kLseFull + slot), tiles / kLseSlots & 1, gave_up, &a.ctl->status)) return;
@@ -290,6 +315,7 @@ __device__ __forceinline__ void sum_role(const MassArgs &a, const List<MassWork>
                 ++step;
                 tc_fence_after();
                 const float4 *nl = reinterpret_cast<const float4 *>(ctl->lse[slot]);
+                float2 s0 = make_float2(0.f, 0.f), s1 = s0, nan = s0;
                 float x[2][32];
                 tmem_ld32(t_s + buf * kTile, x[0]);
 #pragma unroll
@@ -315,15 +341,18 @@ __device__ __forceinline__ void sum_role(const MassArgs &a, const List<MassWork>
                         const float2 z0 = ffma2(make_float2(y[e], y[e + 1]), sl, make_float2(n.x, n.y));
                         const float2 z1 = ffma2(make_float2(y[e + 2], y[e + 3]), sl, make_float2(n.z, n.w));
                         s0 = __fadd2_rn(s0, make_float2(ex2(z0.x), ex2(z0.y)));
-                        s1 = __fadd2_rn(s1, make_float2(ex2(z1.x), ex2(z1.y)));
+                        s1 = __fadd2_rn(s1, e % 8 == 0 ? ex2_fma(z1, nan) : make_float2(ex2(z1.x), ex2(z1.y)));
                     }
                 }
+                // 65536 weights added one after the other would lose 5e-6 of the sum
+                const float y = __fsub_rn((s0.x + s0.y) + (s1.x + s1.y) + (nan.x + nan.y), lost), next = __fadd_rn(sum, y);
+                lost = __fsub_rn(__fsub_rn(next, sum), y);
+                sum = next;
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(bars + 8 * (kLseEmpty + slot));
             __syncwarp();
         }
-        const float sum = (s0.x + s0.y) + (s1.x + s1.y);
         const size_t at = ((size_t)max(pid, 0) * a.H_kv + s.h) * kPage + pos % kPage;
         if (s.a == 0 && s.b == s.units) {
             // the only addition to this token in this call

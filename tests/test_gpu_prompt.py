@@ -100,6 +100,14 @@ def test_long_prompt_and_large_batch():
     check_attention(Calls(ref.make_batch(42, new, past, 4, 1, 64, spare=2)))
 
 
+@pytest.mark.parametrize("new,past", [
+    ([600, 1] * 12 + [1, 2] * 4 + [37], [1400, 4000] * 12 + [4100, 900] * 4 + [0]),   # long and short items side by side
+    ([64] * 100 + [1] * 20, [1950] * 110 + [2500] * 10),
+], ids=["chunks_and_tokens", "many_requests"])
+def test_batches_large_enough_for_pieces_of_two_sizes(new, past):
+    check_attention(Calls(ref.make_batch(44, new, past, 32, 8, 64, spare=1)))
+
+
 def test_absent_pages_and_rows_that_see_nothing():
     # request 0 has lost its first page and its query page, so its first rows see nothing; request 1 has nothing at all
     b = ref.make_batch(51, [20, 5, 40], [0, 30, 400], 8, 2, 128, absent=[(0, 0), (1, 0), (1, 1), (1, 2), (2, 3), (2, 9), (2, 10)])
@@ -212,6 +220,45 @@ def test_accumulated_weights_of_rows_that_see_nothing():
     want, tol = ref.accumulate(b, lse, u)
     c.mass(lse, u)
     held(u, want, tol, "score_accum")
+
+
+@pytest.mark.parametrize("at", range(16))
+def test_a_bad_query_reaches_the_tokens_that_it_sees_and_no_others(at):
+    b = ref.make_batch(95, [16], [200], 2, 2, 64)
+    c = Calls(b)
+    lse = ref.attend(b)[2].float()
+    for value in (math.nan, math.inf):
+        # a NaN query, and a log-sum-exp that makes all of its weights overflow
+        x, y = b.qkv.clone(), lse.clone()
+        if math.isnan(value):
+            b.qkv[at, 0] = value
+        else:
+            y[at, 0] = -1e4
+        u = torch.zeros(b.P, 2, 16, device="cuda")
+        c.mass(y, u)
+        got = u[b.page_table[0].long()].transpose(0, 1).reshape(2, -1)
+        hit = got[0].isnan() if math.isnan(value) else got[0] == value
+        assert bool(hit[:200 + at + 1].all()) and bool((got[0, 200 + at + 1:216].abs() <= 16).all())
+        assert bool((got[1, :216].abs() <= 16.01).all()) and bool((got[:, 216:] == 0).all())
+        b.qkv.copy_(x)
+
+
+def test_weights_of_many_queries_add_up_without_loss():
+    # a token that every query sees alike: with equal logits the weights are 1 / (number of tokens seen)
+    n = 12000
+    b = ref.make_batch(96, [n], [0], 8, 1, 64, nan_tail=False)
+    b.qkv.zero_()
+    c = Calls(b)
+    seen = torch.arange(1, n + 1, dtype=torch.float64, device="cuda")
+    lse = seen.log().float()[:, None].expand(n, 8).contiguous()
+    u = torch.zeros(b.P, 1, 16, device="cuda")
+    c.mass(lse, u)
+    got = u[b.page_table[0].long()].reshape(-1)[:n].double()
+    # the logarithm's rounding is the input's: at most 2^-24 * 9.4 relative in a weight.  On top of it the argument of
+    # the exponential is rounded twice (2 * 2^-24 * 13.6 in powers of two), the exponential is good to 2^-22, and sums
+    # of 32 weights in a chain add 32 * 2^-24
+    want = torch.exp(-lse[:, 0].double()).flip(0).cumsum(0).flip(0) * 8
+    assert float(((got - want).abs() / want).max()) <= 2 * 2.0 ** -24 * 13.6 + 2.0 ** -22 + 32 * 2.0 ** -24 + 4 * 2.0 ** -24
 
 
 def rope_inputs(b, axes, rot, seed, far=0):
