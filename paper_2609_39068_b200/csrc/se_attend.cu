@@ -30,7 +30,7 @@ namespace se {
 
 namespace {
 
-constexpr int kThreads = kPromptThreads;   // 2 softmax warpgroups, K warp, product warp, V warp, idle warp
+constexpr int kThreads = 384;            // 2 softmax warpgroups, K warp, product warp, V warp, idle warp
 constexpr int kKWarp = 8, kMmaWarp = 9, kVWarp = 10;
 constexpr int kRegsSoftmax = 208, kRegsOther = 88;   // 256 * 208 + 128 * 88 = 384 * 168
 constexpr int kTile = 128;             // query rows of a tile
@@ -761,7 +761,7 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     }
     if (warp == kMmaWarp) tmem_alloc(smem_u32(&ctl->tmem), 512);
     const AttendWork work(a);
-    const List<AttendWork> list = make_list(work, a.B, a.H_kv, a.ctl,
+    const List<AttendWork> list = make_list<kThreads>(work, a.B, a.H_kv, a.ctl,
                                             a.B > kSmemRequests ? a.prefixes + prefix_bytes(a.B) * blockIdx.x : ctl->prefix, smem);
     // query rows that no tensor copy fills (G does not divide 128) stay zero
     for (int i = threadIdx.x; i < 2 * C::kTileBytes / 16; i += kThreads)

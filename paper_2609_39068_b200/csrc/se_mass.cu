@@ -3,15 +3,16 @@
 //
 // The sum runs over queries, so the tile is laid the other way round than in the attention kernel: a tile of 128 cached
 // tokens is the M side (tensor-memory lanes), a query tile of 128/G tokens x G heads the N side (columns), S^T = K Q^T.
-// A thread owns one cached token and adds up 2^(S sl - lse log2 e) along its columns in a register: no reduction between
-// threads, no atomics, no second pass, and the result does not depend on timing.
+// A thread owns one cached token and adds up 2^(S sl - lse log2 e) along half of its columns in a register: no reduction
+// between threads but the one addition of the halves, no atomics, no second pass, and the result does not depend on timing.
 //
 // What bounds it: per 128 x 128 tile one product of 512 tensor cycles (D = 128) and 16384 exponentials = 1024 cycles of
 // the special-function units; K is read once per item, the queries come from L2.  A CTA works on two tiles of cached tokens
-// (one warpgroup each) that share every query tile.  Scores are double-buffered in tensor memory (4 x 128 columns), so the
-// products of the next query tile run under the exponentials of this one, and a quarter of the exponentials is taken off the
-// special-function units.  Prompt of 16384 tokens (32 heads over 8, D = 128): 1412 us; with all exponentials on the
-// special-function units 1492 us, their bound being 1.2 ms at the 1.8 GHz that the power limit leaves.
+// (two warpgroups each) that share every query tile.  Scores are double-buffered in tensor memory (4 x 128 columns), so the
+// products of the next query tile run under the exponentials of this one.
+// Prompt of 16384 tokens (32 heads over 8, D = 128): 1320 us, 417 TFLOP/s of products counted below the diagonal; chunks of
+// four requests over 32768 cached tokens: 566 us, the special-function units busy for 52 % of the cycles, the tensor cores for
+// 34 %, an instruction issued in 62 % of them.  With one warpgroup per tile (all columns in a thread) 1412 and 599 us.
 //
 // Item = 256 cached tokens of one (request, kv-head), unit = query tile; pieces and merging as in se_pieces.cuh (a partial
 // result is one number per cached token).
@@ -25,8 +26,8 @@ namespace se {
 
 namespace {
 
-// One pair of weights in four is computed without the special-function unit, which bounds the kernel (prompt of 16384: none
-// 1497 us, one in four 1408 us, one in two 1690 us).
+// One pair of weights in eight is computed without the special-function units (prompt of 16384: none 1350 us, one in eight
+// 1320 us, one in four 1408 us, where the issue of instructions becomes the bound).
 // 2^x of a pair: x = j + f with |f| <= 1/2 (j by adding and taking off 1.5 * 2^23), 2^f by a
 // minimax polynomial of degree 5 with 2^0 = 1 (own fit; relative error 1.6e-7, fp32 rounding included), j added to the exponent
 // field.  x is held to [-127, 128], where the exponent field comes out as 0 and as that of infinity; below -126 the result is
@@ -48,8 +49,9 @@ __device__ __forceinline__ float2 ex2_fma(float2 x, float2 &nan) {
                        __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 
-constexpr int kThreads = kPromptThreads;   // 2 summing warpgroups, copy warp, product warp, lse warp, idle warp
-constexpr int kCopyWarp = 8, kMmaWarp = 9, kLseWarp = 10;
+constexpr int kThreads = 640;          // 4 summing warpgroups, copy warp, product warp, lse warp, idle warp
+constexpr int kCopyWarp = 16, kMmaWarp = 17, kLseWarp = 18;
+constexpr int kRegsSum = 104, kRegsOther = 64;   // 512 * 104 + 128 * 64 = 640 * 96
 constexpr int kTile = 128;             // cached tokens of a tile, query rows of a tile
 constexpr int kLseSlots = 2;
 
@@ -72,7 +74,7 @@ struct MassArgs {
 };
 
 enum Bar { kSFull, kSFree = kSFull + 4, kLseFull = kSFree + 4, kLseEmpty = kLseFull + kLseSlots, kKFull = kLseEmpty + kLseSlots,
-           kKEmpty = kKFull + 2, kAll = kKEmpty + 2, kVerdict = kAll + 2, kDrain = kVerdict + 2, kRing };
+           kKEmpty = kKFull + 2, kAll = kKEmpty + 2, kVerdict = kAll + 2, kHalfFull = kVerdict + 2, kHalfFree = kHalfFull + 2, kDrain = kHalfFree + 2, kRing };
 
 struct MassWork {
     const int32_t *cu, *seq_lens;
@@ -289,12 +291,15 @@ __device__ __forceinline__ void mma_role(const MassArgs &a, Control<D> *ctl, uin
 }
 
 template <int D>
-__device__ __forceinline__ void sum_role(const MassArgs &a, const List<MassWork> &list, Control<D> *ctl, uint32_t bars, int st) {
+__device__ __forceinline__ void sum_role(const MassArgs &a, const List<MassWork> &list, Control<D> *ctl, uint32_t bars, int st, int half) {
     volatile int *gave_up = &ctl->gave_up;
     const int row = threadIdx.x & 127, lane = threadIdx.x & 31, warp = row >> 5;
-    const uint32_t t_s = ctl->tmem + ((uint32_t)(warp * 32) << 16) + 2 * st * kTile;
+    const int col = half * (kTile / 2);                                    // the warpgroup's first column
+    const uint32_t t_s = ctl->tmem + ((uint32_t)(warp * 32) << 16) + 2 * st * kTile + col;
     const float2 sl = make_float2(a.scale_log2, a.scale_log2);
-    uint32_t step = 0, tiles = 0, verdicts = 0, turn = 0;
+    uint32_t step = 0, tiles = 0, verdicts = 0, halves = 0, turn = 0;
+    // the second half's sum on its way to the first half (behind the partial results; shared memory is full)
+    volatile float *other = a.partials + (size_t)kMaxPieces * 4 * kTile + (blockIdx.x * 2 + st) * kTile + row;
     for (;;) {
         const Segment *next = ctl->queue.get(turn++, gave_up, &a.ctl->status, lane);
         if (!next) break;
@@ -308,22 +313,22 @@ __device__ __forceinline__ void sum_role(const MassArgs &a, const List<MassWork>
             if (st == 0 || u >= s.skip1) {
                 const int tok = (s.q0 + u) * list.w.tpt;                     // the tile's first new token
                 // columns [from, to) count: the queries at or behind the cached token, and of this request
-                const int from = min(max(pos - s.t.past - tok, 0), kTile) * a.G, to = (s.t.n - tok) * a.G;
-                const bool masked = __any_sync(kFull, from > 0) || to < list.w.tpt * a.G;
+                const int from = min(max(pos - s.t.past - tok, 0), kTile) * a.G - col, to = (s.t.n - tok) * a.G - col;
+                const bool masked = __any_sync(kFull, from > 0) || to < min(list.w.tpt * a.G - col, kTile / 2);
                 const uint32_t buf = step & 1;
                 if (!warp_wait(bars + 8 * (kSFull + 2 * st + buf), step >> 1 & 1, gave_up, &a.ctl->status)) return;
                 ++step;
                 tc_fence_after();
-                const float4 *nl = reinterpret_cast<const float4 *>(ctl->lse[slot]);
+                const float4 *nl = reinterpret_cast<const float4 *>(ctl->lse[slot] + col);
                 float2 s0 = make_float2(0.f, 0.f), s1 = s0, nan = s0;
                 float x[2][32];
                 tmem_ld32(t_s + buf * kTile, x[0]);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < 2; ++k) {
                     tmem_wait_ld();
                     settle<32>(x[k & 1]);
-                    if (k < 3) tmem_ld32(t_s + buf * kTile + 32 * (k + 1), x[(k + 1) & 1]);
-                    if (k == 3) {
+                    if (k == 0) tmem_ld32(t_s + buf * kTile + 32, x[1]);
+                    if (k == 1) {
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(bars + 8 * (kSFree + 2 * st + buf));
@@ -341,7 +346,7 @@ __device__ __forceinline__ void sum_role(const MassArgs &a, const List<MassWork>
                         const float2 z0 = ffma2(make_float2(y[e], y[e + 1]), sl, make_float2(n.x, n.y));
                         const float2 z1 = ffma2(make_float2(y[e + 2], y[e + 3]), sl, make_float2(n.z, n.w));
                         s0 = __fadd2_rn(s0, make_float2(ex2(z0.x), ex2(z0.y)));
-                        s1 = __fadd2_rn(s1, e % 8 == 0 ? ex2_fma(z1, nan) : make_float2(ex2(z1.x), ex2(z1.y)));
+                        s1 = __fadd2_rn(s1, e % 16 == 0 ? ex2_fma(z1, nan) : make_float2(ex2(z1.x), ex2(z1.y)));
                     }
                 }
                 // 65536 weights added one after the other would lose 5e-6 of the sum
@@ -353,6 +358,20 @@ __device__ __forceinline__ void sum_role(const MassArgs &a, const List<MassWork>
             if (lane == 0) mbar_arrive(bars + 8 * (kLseEmpty + slot));
             __syncwarp();
         }
+        // the two halves of the columns
+        if (half == 1) {
+            if (!warp_wait(bars + 8 * (kHalfFree + st), (halves++ & 1) ^ 1, gave_up, &a.ctl->status)) return;
+            *other = sum;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bars + 8 * (kHalfFull + st));
+            __syncwarp();
+            continue;
+        }
+        if (!warp_wait(bars + 8 * (kHalfFull + st), halves++ & 1, gave_up, &a.ctl->status)) return;
+        sum += *other;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bars + 8 * (kHalfFree + st));
+        __syncwarp();
         const size_t at = ((size_t)max(pid, 0) * a.H_kv + s.h) * kPage + pos % kPage;
         if (s.a == 0 && s.b == s.units) {
             // the only addition to this token in this call
@@ -407,27 +426,29 @@ mass_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ C
     if (threadIdx.x == 0) {
         for (int i = 0; i < 4; ++i) {
             mbar_init(bars + 8 * (kSFull + i), 1);
-            mbar_init(bars + 8 * (kSFree + i), 4);
+            mbar_init(bars + 8 * (kSFree + i), 8);
         }
         for (int i = 0; i < kLseSlots; ++i) {
             mbar_init(bars + 8 * (kLseFull + i), 1);
-            mbar_init(bars + 8 * (kLseEmpty + i), 8);
+            mbar_init(bars + 8 * (kLseEmpty + i), 16);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bars + 8 * (kKFull + i), 1);
             mbar_init(bars + 8 * (kKEmpty + i), 1);
             mbar_init(bars + 8 * (kAll + i), 4);
             mbar_init(bars + 8 * (kVerdict + i), 1);
+            mbar_init(bars + 8 * (kHalfFull + i), 4);
+            mbar_init(bars + 8 * (kHalfFree + i), 4);
         }
         mbar_init(bars + 8 * kDrain, 1);
         for (int i = 0; i < 2 * C::kSlots; ++i) mbar_init(bars + 8 * (kRing + i), 1);
-        ctl->queue.init(10);
+        ctl->queue.init(18);
         mbar_fence_init();
         ctl->gave_up = 0;
     }
     if (warp == kMmaWarp) tmem_alloc(smem_u32(&ctl->tmem), 512);
     const MassWork work(a);
-    const List<MassWork> list = make_list(work, a.B, a.H_kv, a.ctl,
+    const List<MassWork> list = make_list<kThreads>(work, a.B, a.H_kv, a.ctl,
                                           a.B > kSmemRequests ? a.prefixes + prefix_bytes(a.B) * blockIdx.x : ctl->prefix, smem);
     // query rows that no tensor copy fills (G does not divide 128) stay zero
     for (int i = threadIdx.x; i < C::kSlots * C::kTileBytes / 16; i += kThreads)
@@ -437,10 +458,15 @@ mass_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ C
     __syncthreads();
     tc_fence_after();
 
-    if (warp < 8) sum_role<D>(a, list, ctl, bars, warp >> 2);
-    else if (warp == kCopyWarp) copy_role<D>(a, list, &q_map, &k_map, ctl, base, ring, bars, lane);
-    else if (warp == kLseWarp) lse_role<D>(a, list, ctl, bars, lane);
-    else if (warp == kMmaWarp) mma_role<D>(a, ctl, base, ring, bars, lane);
+    if (warp < 16) {
+        regs_up<kRegsSum>();
+        sum_role<D>(a, list, ctl, bars, warp >> 2 & 1, warp >> 3);
+    } else {
+        regs_down<kRegsOther>();
+        if (warp == kCopyWarp) copy_role<D>(a, list, &q_map, &k_map, ctl, base, ring, bars, lane);
+        else if (warp == kLseWarp) lse_role<D>(a, list, ctl, bars, lane);
+        else if (warp == kMmaWarp) mma_role<D>(a, ctl, base, ring, bars, lane);
+    }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
@@ -466,9 +492,15 @@ cudaError_t launch_mass(const se_params &p, const AttendCall &c, float *score_ac
     a.prefixes = c.workspace + prefix_workspace_offset(p.D);
     a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.G = G, a.T = c.total_tokens, a.max_pages = p.max_pages;
     a.P_phys = p.num_phys_pages, a.scale_log2 = effective_scale(p) * kLog2e;
-    const size_t smem = (2 * C::kPairs + C::kSlots) * C::kTileBytes + sizeof(Control<D>);
+    constexpr size_t smem = (2 * C::kPairs + C::kSlots) * C::kTileBytes + sizeof(Control<D>);
+    static_assert(smem <= 227 * 1024, "shared memory of a CTA");
     auto kern = mass_kernel<D>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    // the register split (setmaxnreg) draws on what the block was launched with
+    cudaFuncAttributes attr;
+    cudaError_t e = cudaFuncGetAttributes(&attr, kern);
+    if (e != cudaSuccess) return e;
+    if (attr.numRegs * kThreads < 512 * kRegsSum + 128 * kRegsOther) return cudaErrorInvalidConfiguration;
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     kern<<<kPromptCtas, kThreads, smem, stream>>>(q_map, k_map, a);
     return cudaGetLastError();

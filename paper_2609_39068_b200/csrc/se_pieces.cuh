@@ -30,7 +30,6 @@
 namespace se {
 
 constexpr int kPromptCtas = 148;       // one per SM
-constexpr int kPromptThreads = 384;
 constexpr int kMaxPieces = 2 * kPromptCtas;
 constexpr int kSmemRequests = 96;      // batches up to here keep their prefix sums in shared memory
 
@@ -110,17 +109,17 @@ struct List {
 };
 
 // The list of a batch; all threads of the CTA.  `own` holds the prefix sums for good: shared memory, or the CTA's part of the
-// workspace; sums: 240 bytes of shared memory, free afterwards.  Ends with a barrier.
-template <class Work>
+// workspace; sums: 20 bytes of shared memory a warp, free afterwards.  Ends with a barrier.
+template <int kThreads, class Work>
 __device__ __forceinline__ List<Work> make_list(const Work &w, int B, int H_kv, PromptControl *ctl, void *own, void *sums) {
-    constexpr int kWarps = kPromptThreads / 32;
+    constexpr int kWarps = kThreads / 32;
     long long *cost = reinterpret_cast<long long *>(own);
     int *first = reinterpret_cast<int *>(cost + B + 1);
     long long *s_cost = reinterpret_cast<long long *>(sums);
     long long *s_long = s_cost + kWarps;
     int *s_items = reinterpret_cast<int *>(s_long + kWarps);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = (B + kPromptThreads - 1) / kPromptThreads;
+    const int per = (B + kThreads - 1) / kThreads;
     long long sum = 0, longest = 0;
     int n = 0;
     for (int k = 0; k < per; ++k) {
@@ -157,7 +156,7 @@ __device__ __forceinline__ List<Work> make_list(const Work &w, int B, int H_kv, 
         cost[r] = sb, first[r] = nb;
         sb += c * H_kv, nb += items * H_kv;
     }
-    if (tid == kPromptThreads - 1) cost[B] = sb, first[B] = nb;
+    if (tid == kThreads - 1) cost[B] = sb, first[B] = nb;
     __syncthreads();
     List<Work> l = {w, B, H_kv, cost, first, kMaxPieces, cost[B], 0};
     // the small pieces have to be worth their partial results, and no item may fall into more than 148 of them and a few others
