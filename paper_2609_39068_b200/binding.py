@@ -369,112 +369,117 @@ def _rows(t: torch.Tensor, heads: int, D: int, name: str):
         raise SparseEngineError("%s must be a CUDA tensor" % name)
     if t.dtype != torch.bfloat16:
         raise SparseEngineError("%s must have dtype torch.bfloat16, got %s" % (name, t.dtype))
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != D:
-        raise SparseEngineError("%s must have shape [T, %d, %d], got %s" % (name, heads, D, tuple(t.shape)))
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != D):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != D:
+        raise SparseEngineError("%s must have shape [T, %d, %d], got %s" % (name, heads, D, tuple(shape)))
+    if stride[2] != 1 or (heads > 1 and stride[1] != D):
         raise SparseEngineError("the rows [H, D] of %s must be contiguous" % name)
     # a dimension of one row has no stride to speak of
-    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else heads * D)
+    return t.data_ptr(), (stride[0] if shape[0] > 1 else heads * D)
 
 
-def _shape(t: Optional[torch.Tensor], shape, name: str) -> None:
-    if t is not None and tuple(t.shape) != tuple(shape):
+def _shape(t: Optional[torch.Tensor], shape: tuple, name: str) -> None:
+    if t is not None and t.shape != shape:
         raise SparseEngineError("%s must have shape %s, got %s" % (name, list(shape), list(t.shape)))
 
 
-def _one_device(workspace: torch.Tensor, tensors) -> torch.device:
-    """The workspace's device, after a check that every other tensor is there too."""
-    for t in tensors:
-        if t is not None and t.device != workspace.device:
-            raise SparseEngineError("all tensors must be on %s, got one on %s" % (workspace.device, t.device))
-    return workspace.device
-
-
 def _prompt_common(p: SeParams, workspace: torch.Tensor, cu_seqlens, page_table=None, seq_lens=None, k_cache=None, v_cache=None):
-    _shape(cu_seqlens, [p.B + 1], "cu_seqlens")
-    _shape(page_table, [p.B, p.max_pages], "page_table")
-    _shape(seq_lens, [p.B], "seq_lens")
-    _shape(k_cache, [p.num_phys_pages, p.H_kv, 16, p.D], "k_cache")
-    _shape(v_cache, [p.num_phys_pages, p.H_kv, 16, p.D], "v_cache")
+    B, cache = p.B, (p.num_phys_pages, p.H_kv, 16, p.D)
+    _shape(cu_seqlens, (B + 1,), "cu_seqlens")
+    _shape(page_table, (B, p.max_pages), "page_table")
+    _shape(seq_lens, (B,), "seq_lens")
+    _shape(k_cache, cache, "k_cache")
+    _shape(v_cache, cache, "v_cache")
     if workspace.numel() < se_prompt_workspace_bytes(p):
         raise SparseEngineError("workspace is smaller than se_prompt_workspace_bytes")
+
+
+def _call(entry: str, workspace: torch.Tensor, tensors, *args) -> None:
+    """The call on the current stream of the workspace's device, where every other tensor has to be too.  (The device is
+    switched only where it has to be: torch.cuda.device and the default current_stream took 5 us of a small call.)"""
+    dev = workspace.device
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise SparseEngineError("all tensors must be on %s, got one on %s" % (dev, t.device))
+    f = getattr(load(), entry)
+    ws = _ptr(workspace, torch.uint8, "workspace")
+    if dev.index == torch.cuda.current_device():
+        rc = f(*args, ws, torch.cuda.current_stream(dev.index).cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            rc = f(*args, ws, torch.cuda.current_stream(dev.index).cuda_stream)
+    _check(rc, entry)
 
 
 def se_rope_append(p, q, k, v, cu_seqlens, seq_lens, page_table, positions, inv_freq, pair_axis, q_out, k_cache,
                    v_cache, workspace, meta=None, k_out=None, interleaved=False) -> None:
     """``q``, ``k``, ``v`` may be views of one [T, H_q + 2*H_kv, D] projection output; rot_dim is twice the length of
     ``inv_freq``; ``positions`` is [n_axes, T]."""
-    T = q.shape[0]
+    T, H_q, H_kv, D = q.shape[0], p.H_q, p.H_kv, p.D
+    axes, pairs = positions.shape[0], inv_freq.numel()
     _prompt_common(p, workspace, cu_seqlens, page_table, seq_lens, k_cache, v_cache)
-    _shape(positions, [positions.shape[0], T], "positions")
-    _shape(k, [T, p.H_kv, p.D], "k")
-    _shape(v, [T, p.H_kv, p.D], "v")
-    _shape(q_out, [T, p.H_q, p.D], "q_out")
-    _shape(k_out, [T, p.H_kv, p.D], "k_out")
-    _shape(meta, [p.num_phys_pages, p.H_kv, 2, p.D], "meta")
+    _shape(positions, (axes, T), "positions")
+    _shape(k, (T, H_kv, D), "k")
+    _shape(v, (T, H_kv, D), "v")
+    _shape(q_out, (T, H_q, D), "q_out")
+    _shape(k_out, (T, H_kv, D), "k_out")
+    _shape(meta, (p.num_phys_pages, H_kv, 2, D), "meta")
     _shape(pair_axis, inv_freq.shape, "pair_axis")
-    (qp, qs), (kp, ks), (vp_, vs) = _rows(q, p.H_q, p.D, "q"), _rows(k, p.H_kv, p.D, "k"), _rows(v, p.H_kv, p.D, "v")
+    (qp, qs), (kp, ks), (vp_, vs) = _rows(q, H_q, D, "q"), _rows(k, H_kv, D, "k"), _rows(v, H_kv, D, "v")
     if T == 0:           # an empty tensor has no address
         return
-    with torch.cuda.device(_one_device(workspace, (q, k, v, cu_seqlens, seq_lens, page_table, positions, inv_freq, pair_axis,
-                                                   q_out, k_cache, v_cache, meta, k_out))):
-        _check(load().se_rope_append(ctypes.byref(p), qp, qs, kp, ks, vp_, vs, T, _ptr(cu_seqlens, torch.int32, "cu_seqlens"),
-                                     _ptr(seq_lens, torch.int32, "seq_lens"), _ptr(page_table, torch.int32, "page_table"),
-                                     _ptr(positions, torch.int32, "positions"), positions.shape[0],
-                                     _ptr(inv_freq, torch.float64, "inv_freq"), _ptr(pair_axis, torch.int32, "pair_axis"),
-                                     2 * inv_freq.numel(), int(bool(interleaved)), _ptr(q_out, torch.bfloat16, "q_out"),
-                                     _ptr(k_out, torch.bfloat16, "k_out"), _ptr(k_cache, torch.bfloat16, "k_cache"),
-                                     _ptr(v_cache, torch.bfloat16, "v_cache"), _ptr(meta, torch.bfloat16, "meta"),
-                                     _ptr(workspace, torch.uint8, "workspace"), _stream()), "se_rope_append")
+    i32, bf16 = torch.int32, torch.bfloat16
+    _call("se_rope_append", workspace, (q, k, v, cu_seqlens, seq_lens, page_table, positions, inv_freq, pair_axis, q_out, k_cache,
+                                        v_cache, meta, k_out),
+          ctypes.byref(p), qp, qs, kp, ks, vp_, vs, T, _ptr(cu_seqlens, i32, "cu_seqlens"), _ptr(seq_lens, i32, "seq_lens"),
+          _ptr(page_table, i32, "page_table"), _ptr(positions, i32, "positions"), axes, _ptr(inv_freq, torch.float64, "inv_freq"),
+          _ptr(pair_axis, i32, "pair_axis"), 2 * pairs, int(bool(interleaved)), _ptr(q_out, bf16, "q_out"),
+          _ptr(k_out, bf16, "k_out"), _ptr(k_cache, bf16, "k_cache"), _ptr(v_cache, bf16, "v_cache"), _ptr(meta, bf16, "meta"))
 
 
 def se_chunk_attend(p, q, cu_seqlens, k_cache, v_cache, page_table, seq_lens, out, workspace, lse=None) -> None:
-    T = q.shape[0]
+    T, H_q, D = q.shape[0], p.H_q, p.D
     _prompt_common(p, workspace, cu_seqlens, page_table, seq_lens, k_cache, v_cache)
-    _shape(out, [T, p.H_q, p.D], "out")
-    _shape(lse, [T, p.H_q], "lse")
-    qp, qs = _rows(q, p.H_q, p.D, "q")
+    _shape(out, (T, H_q, D), "out")
+    _shape(lse, (T, H_q), "lse")
+    qp, qs = _rows(q, H_q, D, "q")
     if T == 0:           # an empty tensor has no address
         return
-    with torch.cuda.device(_one_device(workspace, (q, cu_seqlens, k_cache, v_cache, page_table, seq_lens, out, lse))):
-        _check(load().se_chunk_attend(ctypes.byref(p), qp, qs, T, _ptr(cu_seqlens, torch.int32, "cu_seqlens"),
-                                      _ptr(k_cache, torch.bfloat16, "k_cache"), _ptr(v_cache, torch.bfloat16, "v_cache"),
-                                      _ptr(page_table, torch.int32, "page_table"), _ptr(seq_lens, torch.int32, "seq_lens"),
-                                      _ptr(out, torch.bfloat16, "out"), _ptr(lse, torch.float32, "lse"),
-                                      _ptr(workspace, torch.uint8, "workspace"), _stream()), "se_chunk_attend")
+    i32, bf16 = torch.int32, torch.bfloat16
+    _call("se_chunk_attend", workspace, (q, cu_seqlens, k_cache, v_cache, page_table, seq_lens, out, lse),
+          ctypes.byref(p), qp, qs, T, _ptr(cu_seqlens, i32, "cu_seqlens"), _ptr(k_cache, bf16, "k_cache"),
+          _ptr(v_cache, bf16, "v_cache"), _ptr(page_table, i32, "page_table"), _ptr(seq_lens, i32, "seq_lens"),
+          _ptr(out, bf16, "out"), _ptr(lse, torch.float32, "lse"))
 
 
 def se_prompt_attend(p, q, k, v, cu_seqlens, out, workspace, lse=None) -> None:
-    T = q.shape[0]
+    T, H_q, H_kv, D = q.shape[0], p.H_q, p.H_kv, p.D
     _prompt_common(p, workspace, cu_seqlens)
-    _shape(k, [T, p.H_kv, p.D], "k")
-    _shape(v, [T, p.H_kv, p.D], "v")
-    _shape(out, [T, p.H_q, p.D], "out")
-    _shape(lse, [T, p.H_q], "lse")
-    (qp, qs), (kp, ks), (vp_, vs) = _rows(q, p.H_q, p.D, "q"), _rows(k, p.H_kv, p.D, "k"), _rows(v, p.H_kv, p.D, "v")
+    _shape(k, (T, H_kv, D), "k")
+    _shape(v, (T, H_kv, D), "v")
+    _shape(out, (T, H_q, D), "out")
+    _shape(lse, (T, H_q), "lse")
+    (qp, qs), (kp, ks), (vp_, vs) = _rows(q, H_q, D, "q"), _rows(k, H_kv, D, "k"), _rows(v, H_kv, D, "v")
     if T == 0:           # an empty tensor has no address
         return
-    with torch.cuda.device(_one_device(workspace, (q, k, v, cu_seqlens, out, lse))):
-        _check(load().se_prompt_attend(ctypes.byref(p), qp, qs, kp, ks, vp_, vs, T,
-                                       _ptr(cu_seqlens, torch.int32, "cu_seqlens"), _ptr(out, torch.bfloat16, "out"),
-                                       _ptr(lse, torch.float32, "lse"), _ptr(workspace, torch.uint8, "workspace"), _stream()),
-               "se_prompt_attend")
+    _call("se_prompt_attend", workspace, (q, k, v, cu_seqlens, out, lse),
+          ctypes.byref(p), qp, qs, kp, ks, vp_, vs, T, _ptr(cu_seqlens, torch.int32, "cu_seqlens"),
+          _ptr(out, torch.bfloat16, "out"), _ptr(lse, torch.float32, "lse"))
 
 
 def se_h2o_accumulate(p, q, cu_seqlens, k_cache, page_table, seq_lens, lse, score_accum, workspace) -> None:
-    T = q.shape[0]
+    T, H_q, D = q.shape[0], p.H_q, p.D
     _prompt_common(p, workspace, cu_seqlens, page_table, seq_lens, k_cache)
-    _shape(lse, [T, p.H_q], "lse")
-    _shape(score_accum, [p.num_phys_pages, p.H_kv, 16], "score_accum")
-    qp, qs = _rows(q, p.H_q, p.D, "q")
+    _shape(lse, (T, H_q), "lse")
+    _shape(score_accum, (p.num_phys_pages, p.H_kv, 16), "score_accum")
+    qp, qs = _rows(q, H_q, D, "q")
     if T == 0:           # an empty tensor has no address
         return
-    with torch.cuda.device(_one_device(workspace, (q, cu_seqlens, k_cache, page_table, seq_lens, lse, score_accum))):
-        _check(load().se_h2o_accumulate(ctypes.byref(p), qp, qs, T, _ptr(cu_seqlens, torch.int32, "cu_seqlens"),
-                                        _ptr(k_cache, torch.bfloat16, "k_cache"), _ptr(page_table, torch.int32, "page_table"),
-                                        _ptr(seq_lens, torch.int32, "seq_lens"), _ptr(lse, torch.float32, "lse"),
-                                        _ptr(score_accum, torch.float32, "score_accum"),
-                                        _ptr(workspace, torch.uint8, "workspace"), _stream()), "se_h2o_accumulate")
+    i32 = torch.int32
+    _call("se_h2o_accumulate", workspace, (q, cu_seqlens, k_cache, page_table, seq_lens, lse, score_accum),
+          ctypes.byref(p), qp, qs, T, _ptr(cu_seqlens, i32, "cu_seqlens"), _ptr(k_cache, torch.bfloat16, "k_cache"),
+          _ptr(page_table, i32, "page_table"), _ptr(seq_lens, i32, "seq_lens"), _ptr(lse, torch.float32, "lse"),
+          _ptr(score_accum, torch.float32, "score_accum"))
 
 
 def se_last_device_status(workspace) -> int:

@@ -99,7 +99,7 @@ struct AttendWork {
         return (t.past + i * 2 * tpt + new_tokens(t, i) + kKv - 1) / kKv;
     }
     __device__ __forceinline__ int unit_at(const TokenRange &t, int i, long long z) const {
-        return (int)(z / (kKv * (new_tokens(t, i) > tpt ? 2 : 1)));
+        return (int)((z / kKv) >> (new_tokens(t, i) > tpt ? 1 : 0));
     }
     __device__ __forceinline__ long long min_cost() const { return kMinCost; }
     static constexpr int kCrumb = 2;   // least units of a part of an item
@@ -453,6 +453,13 @@ __device__ __forceinline__ float *partial_slot(const AttendArgs &a, int index) {
     return a.partials + (size_t)index * Cfg<D>::kSlotFloats;
 }
 
+// 32 bytes of a thread's own row: half the instructions, each of which takes a cycle per row, of two stores of 16 bytes.
+__device__ __forceinline__ void store32(void *dst, const uint32_t *w) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+                 "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+}
+
 // Merges `parts` partial results of one query tile, at(k) their indexes, and writes its output.  A warp takes rows row_from,
 // row_from + row_step, ...
 template <int D, typename At>
@@ -466,7 +473,7 @@ __device__ __forceinline__ void merge_rows(const AttendArgs &a, const Segment &s
     const int my = row_from + row_step * lane;                             // statistics: a lane per row
     const bool have = my < rows;
     float M = -INFINITY, L = 0.f;
-#pragma unroll 4
+#pragma unroll 8
     for (int k = 0; k < parts; ++k) {
         const float *p = partial_slot<D>(a, at(k)) + kTile * D;
         const float m = have ? __ldcg(p + my) : -INFINITY, l = have ? __ldcg(p + kTile + my) : 0.f;
@@ -479,7 +486,7 @@ __device__ __forceinline__ void merge_rows(const AttendArgs &a, const Segment &s
     const int mine = rows > row_from ? (rows - row_from + row_step - 1) / row_step : 0;
     for (int k0 = 0; k0 < mine; k0 += R) {
         float acc[R][V] = {};
-#pragma unroll 2
+#pragma unroll 4
         for (int q = 0; q < parts; ++q) {
             const float *p = partial_slot<D>(a, at(q));
             const float w = have ? ex2(__ldcg(p + kTile * D + my) - ref) * inv : 0.f;
@@ -626,6 +633,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
             if (s.alt && st == 1) continue;                                // a single KV tile: stream 0 has it all
             const float inv = l > 0.f ? 1.f / l : 0.f;
             uint4 *dst = reinterpret_cast<uint4 *>(a.out + orow * D);
+            const bool wide = ((uintptr_t)a.out & 31) == 0;
 #pragma unroll
             for (int k = 0; k < D; k += 32) {
                 float o[32];
@@ -640,7 +648,14 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
                 }
                 if (live) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) dst[k / 8 + e] = make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+                    for (int e = 0; e < 4; e += 2) {
+                        if (wide) {
+                            store32(dst + k / 8 + e, w + 4 * e);
+                        } else {
+                            dst[k / 8 + e] = make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+                            dst[k / 8 + e + 1] = make_uint4(w[4 * e + 4], w[4 * e + 5], w[4 * e + 6], w[4 * e + 7]);
+                        }
+                    }
                 }
             }
             if (live && a.lse) a.lse[orow] = l > 0.f ? (m2 + log2f(l)) * kLn2 : -INFINITY;
@@ -661,9 +676,8 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
                     tmem_wait_ld();
                     settle<32>(o);
                     if (live) {
-                        float4 *dst = reinterpret_cast<float4 *>(slot + (size_t)row * D + k);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) __stcg(dst + e, make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]));
+                        for (int e = 0; e < 32; e += 8) store32(slot + (size_t)row * D + k + e, reinterpret_cast<const uint32_t *>(o + e));
                     }
                 }
                 tc_fence_before();
@@ -741,30 +755,26 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
         return;
     }
 
-    if (threadIdx.x == 0) {
-        mbar_init(bars + 8 * kQFull, 1);
-        mbar_init(bars + 8 * kQEmpty, 1);
-        for (int st = 0; st < 2; ++st) {
-            mbar_init(bars + 8 * (kSFull + st), 1);
-            mbar_init(bars + 8 * (kPReady + st), 4);
-            mbar_init(bars + 8 * (kOLast + st), 1);
-            mbar_init(bars + 8 * (kOFree + st), 4);
-            mbar_init(bars + 8 * (kAll + st), 4);
-            mbar_init(bars + 8 * (kVerdict + st), 1);
-        }
-        mbar_init(bars + 8 * kSwap, 8);
-        mbar_init(bars + 8 * kDrain, 1);
-        for (int i = 0; i < 2 * C::kSlots; ++i) mbar_init(bars + 8 * (kFull + i), 1);
+    static_assert(kFull + 2 * C::kSlots <= kThreads, "a thread per barrier");
+    if (threadIdx.x < kFull + 2 * C::kSlots) {
+        const int i = threadIdx.x;
+        const bool by_warp = (i >= kPReady && i < kPReady + 2) || (i >= kOFree && i < kOFree + 2) || (i >= kAll && i < kAll + 2);
+        mbar_init(bars + 8 * i, i == kSwap ? 8 : by_warp ? 4 : 1);
+        mbar_fence_init();
+    }
+    if (threadIdx.x == 32) {
         ctl->queue.init(10);
         mbar_fence_init();
         ctl->gave_up = 0;
     }
     if (warp == kMmaWarp) tmem_alloc(smem_u32(&ctl->tmem), 512);
+    if (threadIdx.x == 32 * kKWarp) prefetch_map(&q_map), prefetch_map(&k_map);
+    if (threadIdx.x == 32 * kVWarp) prefetch_map(&v_map);
     const AttendWork work(a);
     const List<AttendWork> list = make_list<kThreads>(work, a.B, a.H_kv, a.ctl,
                                             a.B > kSmemRequests ? a.prefixes + prefix_bytes(a.B) * blockIdx.x : ctl->prefix, smem);
     // query rows that no tensor copy fills (G does not divide 128) stay zero
-    for (int i = threadIdx.x; i < 2 * C::kTileBytes / 16; i += kThreads)
+    for (int i = threadIdx.x; i < (work.tpt * a.G == kTile ? 0 : 2 * C::kTileBytes / 16); i += kThreads)
         reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
     fence_async_proxy();
     tc_fence_before();
@@ -813,7 +823,7 @@ cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t 
     a.v = static_cast<const uint16_t *>(c.v), a.v_stride = c.v_stride;
     a.out = static_cast<uint16_t *>(c.out), a.lse = c.lse;
     a.ctl = reinterpret_cast<PromptControl *>(c.workspace);
-    a.partials = reinterpret_cast<float *>(c.workspace + kPromptControlBytes);
+    a.partials = partials_of(c.workspace);
     a.prefixes = c.workspace + prefix_workspace_offset(p.D);
     a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.G = G, a.T = c.total_tokens, a.max_pages = p.max_pages;
     a.P_phys = p.num_phys_pages, a.scale_log2 = effective_scale(p) * kLog2e;

@@ -10,7 +10,7 @@
 // the special-function units; K is read once per item, the queries come from L2.  A CTA works on two tiles of cached tokens
 // (two warpgroups each) that share every query tile.  Scores are double-buffered in tensor memory (4 x 128 columns), so the
 // products of the next query tile run under the exponentials of this one.
-// Prompt of 16384 tokens (32 heads over 8, D = 128): 1320 us, 417 TFLOP/s of products counted below the diagonal; chunks of
+// Prompt of 16384 tokens (32 heads over 8, D = 128): 1320 us, 833 TFLOP/s of products counted below the diagonal; chunks of
 // four requests over 32768 cached tokens: 566 us, the special-function units busy for 52 % of the cycles, the tensor cores for
 // 34 %, an instruction issued in 62 % of them.  With one warpgroup per tile (all columns in a thread) 1412 and 599 us.
 //
@@ -488,7 +488,7 @@ cudaError_t launch_mass(const se_params &p, const AttendCall &c, float *score_ac
     a.cu = c.cu_seqlens, a.seq_lens = c.seq_lens, a.page_table = c.page_table;
     a.lse = c.lse, a.accum = score_accum;
     a.ctl = reinterpret_cast<PromptControl *>(c.workspace);
-    a.partials = reinterpret_cast<float *>(c.workspace + kPromptControlBytes);
+    a.partials = partials_of(c.workspace);
     a.prefixes = c.workspace + prefix_workspace_offset(p.D);
     a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.G = G, a.T = c.total_tokens, a.max_pages = p.max_pages;
     a.P_phys = p.num_phys_pages, a.scale_log2 = effective_scale(p) * kLog2e;

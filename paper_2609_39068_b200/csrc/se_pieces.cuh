@@ -45,9 +45,13 @@ constexpr size_t prefix_bytes(int B) { return ((size_t)(B + 1) * 12 + 15) / 16 *
 // workspace for the prefix sums of all CTAs (each has its own)
 inline size_t prefix_workspace_bytes(int B) { return B > kSmemRequests ? prefix_bytes(B) * kPromptCtas : 0; }
 
-// Behind the partial results: up to two per piece and stream, each of 128 rows of D channels and two statistics.
+// The partial results, from a border of 32 bytes (the workspace begins on one of 16): up to two per piece and stream, each of
+// 128 rows of D channels and two statistics.  The prefix sums lie behind them.
+inline float *partials_of(uint8_t *workspace) {
+    return reinterpret_cast<float *>(((uintptr_t)workspace + kPromptControlBytes + 31) & ~(uintptr_t)31);
+}
 inline size_t prefix_workspace_offset(int D) {
-    return kPromptControlBytes + (size_t)kMaxPieces * 4 * ((size_t)128 * D + 256) * sizeof(float);
+    return kPromptControlBytes + 32 + (size_t)kMaxPieces * 4 * ((size_t)128 * D + 256) * sizeof(float);
 }
 
 // Where a piece begins: number of the item in the list, unit in it; request (B: the end of the list), kv-head, index.
@@ -80,7 +84,8 @@ struct List {
         const TokenRange t = w.tokens(b.r);
         const int items = w.items(t);
         const long long each = w.cost(t, items), x = at - cost[b.r];
-        b.h = (int)(x / each);
+        // (a division of 64 bits is a hundred instructions)
+        b.h = (x | each) >> 32 ? (int)(x / each) : (int)((uint32_t)x / (uint32_t)each);
         const long long y = x - b.h * each;
         int i0 = 0, i1 = items;
         while (i1 - i0 > 1) {

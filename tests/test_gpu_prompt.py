@@ -108,6 +108,22 @@ def test_batches_large_enough_for_pieces_of_two_sizes(new, past):
     check_attention(Calls(ref.make_batch(44, new, past, 32, 8, 64, spare=1)))
 
 
+def test_buffers_that_begin_on_16_bytes():
+    b = ref.make_batch(45, [40, 1, 200], [900, 5000, 0], 8, 2, 128)
+    c = Calls(b)
+    room = torch.zeros(c.ws.numel() + 16, dtype=torch.uint8, device="cuda")
+    c.ws = room[16:]
+    binding.se_prompt_workspace_init(c.p, c.ws)
+    c.out = torch.full((c.out.numel() + 8,), NAN, dtype=torch.bfloat16, device="cuda")[8:].view(c.out.shape)
+    assert c.ws.data_ptr() % 32 == 16 and c.out.data_ptr() % 32 == 16
+    check_attention(c)
+    lse = ref.attend(b)[2].float()
+    u = torch.zeros(b.P, 2, 16, device="cuda")
+    want, tol = ref.accumulate(b, lse, u)
+    c.mass(lse, u)
+    held(u, want, tol, "score_accum")
+
+
 def test_absent_pages_and_rows_that_see_nothing():
     # request 0 has lost its first page and its query page, so its first rows see nothing; request 1 has nothing at all
     b = ref.make_batch(51, [20, 5, 40], [0, 30, 400], 8, 2, 128, absent=[(0, 0), (1, 0), (1, 1), (1, 2), (2, 3), (2, 9), (2, 10)])
