@@ -569,9 +569,18 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
             tmem_wait_ld();
             settle<kKv>(x);
             if (kKv > most || mask != 0xffu) {
+                // (a branch per page: pruned contexts come here in most tiles, and a test per element took 300 instructions)
 #pragma unroll
-                for (int k = 0; k < kKv; ++k)
-                    if (k >= left || !(mask >> (k / kPage) & 1)) x[k] = -INFINITY;
+                for (int pg = 0; pg < kGroups; ++pg)
+                    if (!(mask >> pg & 1)) {
+#pragma unroll
+                        for (int k = 0; k < kPage; ++k) x[pg * kPage + k] = -INFINITY;
+                    }
+                if (kKv > most) {
+#pragma unroll
+                    for (int k = 0; k < kKv; ++k)
+                        if (k >= left) x[k] = -INFINITY;
+                }
             }
             float top[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
