@@ -394,7 +394,7 @@ int se_h2o_compact(const se_params *p, void *k_cache, void *v_cache, float *scor
  *    (>= H*D, a multiple of 8), so that the calls read views of one [T, H_q + 2*H_kv, D] projection output.
  *  - Of se_params they use B, H_q, H_kv, D, max_pages, num_phys_pages and sm_scale; the other fields only
  *    have to be valid.
- *  - They take a workspace of their own kind: se_prompt_workspace_bytes bytes (256-byte aligned), initialised
+ *  - They take a workspace of their own kind: se_prompt_workspace_bytes bytes (80 MB at D = 128), initialised
  *    once by se_prompt_workspace_init, then good for any number of calls with the same se_params that are ordered
  *    on the device.  se_last_device_status reads its status word.  After a call that reported
  *    SE_DEV_WAIT_TIMEOUT it has to be initialised again.

@@ -51,7 +51,7 @@ inline float *partials_of(uint8_t *workspace) {
     return reinterpret_cast<float *>(((uintptr_t)workspace + kPromptControlBytes + 31) & ~(uintptr_t)31);
 }
 inline size_t prefix_workspace_offset(int D) {
-    return kPromptControlBytes + 32 + (size_t)kMaxPieces * 4 * ((size_t)128 * D + 256) * sizeof(float);
+    return kPromptControlBytes + 256 + (size_t)kMaxPieces * 4 * ((size_t)128 * D + 256) * sizeof(float);
 }
 
 // Where a piece begins: number of the item in the list, unit in it; request (B: the end of the list), kv-head, index.
