@@ -415,8 +415,8 @@ int se_prompt_workspace_init(const se_params *p, void *workspace, void *stream);
  *   k_out  [total_tokens, H_kv, D] bf16 or NULL: rotated K also in token order (for se_prompt_attend)
  * k_cache / v_cache slots of the new tokens are written; a token whose page is absent or out of range is
  * left out of the cache and reported (SE_DEV_BAD_PAGE_ID).  With meta != NULL the summaries of the touched pages
- * become those of se_meta_update over the page's tokens below seq_lens[r] (bit for bit).  Pages that receive tokens
- * must not be shared between requests.
+ * become those of se_meta_update over the page's tokens below seq_lens[r] (bit for bit).  A page that receives tokens
+ * must appear once in the page table.
  */
 int se_rope_append(const se_params *p, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                    const void *v, int64_t v_stride, int32_t total_tokens, const int32_t *cu_seqlens,
@@ -454,7 +454,7 @@ int se_prompt_attend(const se_params *p, const void *q, int64_t q_stride, const 
  * se_chunk_attend left it for the same q and cache,
  *     score_accum[pid(j),h,j%16] += sum over the new tokens i >= j and the heads a of group h of exp(z_ij^a - lse_i^a).
  * After the last chunk of a prompt this is the statistic that se_h2o_retain ranks and the decode steps go on with.
- * The physical pages of different requests must be distinct.  The sum's order is fixed: equal inputs give equal bits.
+ * A physical page must appear once among the requests' pages.  The sum's order is fixed: equal inputs give equal bits.
  */
 int se_h2o_accumulate(const se_params *p, const void *q, int64_t q_stride, int32_t total_tokens,
                       const int32_t *cu_seqlens, const void *k_cache, const int32_t *page_table,

@@ -445,3 +445,57 @@ def test_a_replayed_graph_follows_changed_lengths():
         out, tol, lse, ltol = ref.attend(b)
         held(c.lse, lse, ltol, "lse")
         held(c.out, out, tol, "out")
+
+
+def test_calls_at_once_on_two_streams_give_the_same_bits():
+    # large enough for pieces that CTAs take as they become free; each stream has its workspace
+    b = ref.make_batch(131, [600, 1] * 12 + [1, 2] * 4 + [37], [1400, 4000] * 12 + [4100, 900] * 4 + [0], 32, 8, 64)
+    first = Calls(b)
+    first.chunk()
+    u0 = torch.zeros(b.P, 8, 16, device="cuda")
+    first.mass(first.lse, u0)
+    torch.cuda.synchronize()
+    sides = [(Calls(b), torch.zeros_like(u0), torch.cuda.Stream()) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for c, u, stream in sides:
+            with torch.cuda.stream(stream):
+                c.out.fill_(NAN)
+                u.zero_()
+                c.chunk()
+                c.mass(c.lse, u)
+    torch.cuda.synchronize()
+    for c, u, _ in sides:
+        assert torch.equal(c.out, first.out) and torch.equal(c.lse, first.lse) and torch.equal(u, u0)
+        assert c.status() == 0
+
+
+def test_a_page_read_twice_and_by_two_requests():
+    # an aliased prefix, and one physical page at two logical positions
+    b = ref.make_batch(132, [20, 30], [300, 500], 8, 2, 128)
+    b.page_table[1, :10] = b.page_table[0, :10]
+    b.page_table[1, 12] = b.page_table[1, 11]
+    check_attention(Calls(b))
+
+
+def test_largest_batch_of_short_requests():
+    n = 8192
+    b = ref.make_batch(133, [r % 3 for r in range(n)], [0 if r % 5 else 20 for r in range(n)], 2, 1, 64, spare=2)
+    c = Calls(b)
+    c.chunk()
+    torch.cuda.synchronize()
+    assert c.status() == 0
+    pick = [0, 1, 2, 5, 95, 96, 97, 4096, 8189, 8190, 8191]
+    want = {}
+    for r in pick:                       # the reference goes request by request: only some of them
+        one = ref.Batch(b.H_q, b.H_kv, b.D, [b.new[r]], [b.total[r]], b.new[r], b.max_pages, b.P, b.qkv[b.rows(r)],
+                        None, None, b.page_table[r:r + 1], b.k_cache, b.v_cache)
+        want[r] = ref.attend(one)
+    for r, (out, tol, lse, ltol) in want.items():
+        rows = b.rows(r)
+        held(c.lse[rows], lse, ltol, "lse of request %d" % r)
+        held(c.out[rows], out, tol, "out of request %d" % r)
+    assert bool(c.out[:sum(b.new)].isfinite().all()) and bool(c.out[sum(b.new):].isnan().all())
+    u = torch.zeros(b.P, 1, 16, device="cuda")
+    c.mass(c.lse[:b.T].clone(), u)
+    assert abs(float(u.double().sum()) - sum(b.new) * 2) < 1e-4 * sum(b.new) * 2
