@@ -124,7 +124,7 @@ def _ptr(t: Optional[torch.Tensor], dtype, name: str):
         raise SparseEngineError("%s must have dtype %s, got %s" % (name, dtype, t.dtype))
     if not t.is_contiguous():
         raise SparseEngineError("%s must be contiguous" % name)
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _stream():
@@ -397,17 +397,16 @@ def _prompt_common(p: SeParams, workspace: torch.Tensor, cu_seqlens, page_table=
 def _call(entry: str, workspace: torch.Tensor, tensors, *args) -> None:
     """The call on the current stream of the workspace's device, where every other tensor has to be too.  (The device is
     switched only where it has to be: torch.cuda.device and the default current_stream took 5 us of a small call.)"""
-    dev = workspace.device
+    ws, dev = _ptr(workspace, torch.uint8, "workspace"), workspace.get_device()
     for t in tensors:
-        if t is not None and t.device != dev:
-            raise SparseEngineError("all tensors must be on %s, got one on %s" % (dev, t.device))
+        if t is not None and t.get_device() != dev:
+            raise SparseEngineError("all tensors must be on %s, got one on %s" % (workspace.device, t.device))
     f = getattr(load(), entry)
-    ws = _ptr(workspace, torch.uint8, "workspace")
-    if dev.index == torch.cuda.current_device():
-        rc = f(*args, ws, torch.cuda.current_stream(dev.index).cuda_stream)
+    if dev == torch.cuda.current_device():
+        rc = f(*args, ws, torch.cuda.current_stream(dev).cuda_stream)
     else:
         with torch.cuda.device(dev):
-            rc = f(*args, ws, torch.cuda.current_stream(dev.index).cuda_stream)
+            rc = f(*args, ws, torch.cuda.current_stream(dev).cuda_stream)
     _check(rc, entry)
 
 

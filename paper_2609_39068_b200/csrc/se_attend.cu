@@ -38,7 +38,10 @@ constexpr int kKv = 128;               // tokens of a KV tile
 constexpr int kGroups = kKv / kPage;   // pages of a KV tile
 constexpr int kMaxParts = 304;         // partial results of a query tile: two per piece, little more than 148 pieces of it
 constexpr int kItemCost = 128;         // cost of starting a query tile, in tokens
-constexpr int kMinCost = 512;          // a CTA takes at least 256 tokens of a pair, 512 of a single tile
+// A CTA takes at least 256 tokens (a short item has a CTA of its own), but where pieces are small, items are split at multiples
+// of four KV tiles only: the parts have to be merged, which takes as long as a dozen tiles.  Six short prompts: 14.0 us, with
+// pieces of 512 tokens 17.2 us; one token over 2048: 20.3 us, split at every second tile 21.7 us.
+constexpr int kMinCost = 256, kCoarse = 2048;
 // The running maximum may lag: weights up to 2^40 lose nothing (bf16 and fp32 keep their exponents, and 2^40 * 131072
 // tokens is far from the end of the range).
 constexpr float kSlack = 40.f;
@@ -103,7 +106,10 @@ struct AttendWork {
     }
     __device__ __forceinline__ long long min_cost() const { return kMinCost; }
     static constexpr int kCrumb = 2;   // least units of a part of an item
+    static constexpr int kGrain = 4;
+    __device__ __forceinline__ long long coarse() const { return kCoarse; }
     static constexpr bool kShares = true;
+    static constexpr long long kShareCost = 2560;
     __device__ __forceinline__ long long longest(const TokenRange &t) const { return 2ll * (t.past + t.n + kItemCost); }
 };
 

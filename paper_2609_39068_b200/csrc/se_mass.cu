@@ -100,6 +100,8 @@ struct MassWork {
     __device__ __forceinline__ int unit_at(const TokenRange &, int, long long z) const { return (int)(z / tpt); }
     __device__ __forceinline__ long long min_cost() const { return 4 * tpt; }
     static constexpr int kCrumb = 2;   // least units of a part of an item
+    static constexpr int kGrain = 1;
+    __device__ __forceinline__ long long coarse() const { return 0; }
     static constexpr bool kShares = false;
 };
 

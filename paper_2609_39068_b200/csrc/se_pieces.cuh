@@ -21,7 +21,9 @@
 //   int unit_at(t, i, z)               unit that cost z into the item falls in
 //   long long min_cost()               least cost of a piece
 //   kCrumb                             least units of a part of a split item
+//   kGrain, long long coarse()         pieces of less cost than coarse() begin and end at multiples of kGrain units
 //   kShares                            whether a large batch is cut into pieces of two sizes;
+//   kShareCost                         then: least cost of the small ones
 //   long long longest(t)               then: a bound on the cost of the request's items
 #pragma once
 
@@ -95,6 +97,7 @@ struct List {
         b.i = i0;
         const int units = w.units(t, b.i);
         b.unit = w.unit_at(t, b.i, y - w.cost(t, b.i));
+        if (size < w.coarse()) b.unit -= b.unit % Work::kGrain;
         b.item = first[b.r] + b.h * items + b.i;
         // no crumbs: a part of an item that is split has a few units at least
         if (b.unit < Work::kCrumb) {
@@ -165,7 +168,11 @@ __device__ __forceinline__ List<Work> make_list(const Work &w, int B, int H_kv, 
     __syncthreads();
     List<Work> l = {w, B, H_kv, cost, first, kMaxPieces, cost[B], 0};
     // the small pieces have to be worth their partial results, and no item may fall into more than 148 of them and a few others
-    if (!Work::kShares || l.total / 10 < (long long)kPromptCtas * 5 * w.min_cost() || l.total / 10 < longest) l.pieces = kPromptCtas;
+    if constexpr (Work::kShares) {
+        if (l.total / 10 < kPromptCtas * Work::kShareCost || l.total / 10 < longest) l.pieces = kPromptCtas;
+    } else {
+        l.pieces = kPromptCtas;
+    }
     l.size = (l.total + kPromptCtas - 1) / kPromptCtas;
     if (l.size < w.min_cost()) l.size = w.min_cost();
     return l;
