@@ -20,6 +20,12 @@
 // results (O, m, l) in the workspace; whichever CTA completes the tile's count of KV tiles merges them, in the order of the
 // pieces, so the result does not depend on who is last.  Long contexts with few rows and long prompts take the same path, and
 // there is no second kernel.
+//
+// Measured (32 heads over 8, D = 128): prompt of 32768 tokens 7.7-8.25 ms (1.07-1.14 PFLOP/s), 2048 tokens over 65536 1.8-1.95 ms,
+// eight packed prompts of 500-4000 tokens 370 us, eight times five drafted tokens over 32768 194 us (5.5 TB/s).  A step of both
+// streams takes 3350 cycles where products and exponentials take 2048 each: a stream's chain of scores, softmax and product is
+// what bounds it.  KV tiles of 64 tokens with two score buffers per stream took 465-497 us for the packed prompts, a product that
+// begins with half of the weights 399-410 us, exponentials on the FMA units (one pair in eight) 386 us.
 #include <math.h>
 
 #include "se_internal.h"
