@@ -82,8 +82,9 @@ struct Int {
     static constexpr int value = N;
 };
 
+// kRing: full barriers of the K slots and of the V slots, then the empty ones in the same order
 enum Bar { kQFull, kQEmpty, kSFull, kPReady = kSFull + 2, kOLast = kPReady + 2, kOFree = kOLast + 2, kAll = kOFree + 2,
-           kVerdict = kAll + 2, kSwap = kVerdict + 2, kDrain, kFull };   // kFull: K slots, V slots; then the same for "empty"
+           kVerdict = kAll + 2, kSwap = kVerdict + 2, kDrain, kRing };
 
 // ---- the work list -----------------------------------------------------------------
 // item = two query tiles (the last one of a request may be a single tile), unit = KV tile.  Cost in tokens seen, twice
@@ -131,7 +132,7 @@ struct Segment {
 
 template <int D>
 struct Control {
-    uint64_t bars[kFull + 2 * Cfg<D>::kSlots];
+    uint64_t bars[kRing + 2 * Cfg<D>::kSlots];
     SegmentQueue<Segment> queue;
     alignas(8) uint8_t prefix[prefix_bytes(kSmemRequests)];
     uint32_t mask[Cfg<D>::kMasks];     // present 16-token groups of the tiles in flight
@@ -197,7 +198,7 @@ struct Pages {
         ids = next;
         next = fetch(a, s, block * 32 + 32 + lane, report);
     }
-    __device__ __forceinline__ int of(int tile, int pg) const { return __shfl_sync(se::kFull, ids, tile % (32 / kGroups) * kGroups + pg); }
+    __device__ __forceinline__ int of(int tile, int pg) const { return __shfl_sync(kFull, ids, tile % (32 / kGroups) * kGroups + pg); }
 };
 
 // The end of a copying warp that has filled `filled` slots of a ring of kSlots, whose barriers are full + 8 * slot and
@@ -221,7 +222,7 @@ __device__ __forceinline__ void k_role(const AttendArgs &a, const List<AttendWor
     Segment s;
     Pages pages;
     uint32_t tiles = 0, queries = 0;
-    const uint32_t k_full = bars + 8 * kFull, k_empty = k_full + 8 * C::kSlots;
+    const uint32_t k_full = bars + 8 * kRing, k_empty = k_full + 8 * C::kSlots;
     const bool chosen = elect_one();
     bool ok = true;
     Walk<AttendWork> walk(list, a.ctl, lane);
@@ -244,7 +245,7 @@ __device__ __forceinline__ void k_role(const AttendArgs &a, const List<AttendWor
         for (int t = s.a; t < s.b; ++t, ++tiles) {
             const uint32_t slot = tiles % C::kKSlots, bar = k_full + 8 * slot, dst = ring + slot * C::kKvBytes;
             pages.reach(a, s, t, true, lane);
-            const unsigned mask = __ballot_sync(se::kFull, pages.ids >= 0) >> t % (32 / kGroups) * kGroups & 0xffu;
+            const unsigned mask = __ballot_sync(kFull, pages.ids >= 0) >> t % (32 / kGroups) * kGroups & 0xffu;
             int pid[kGroups];
 #pragma unroll
             for (int pg = 0; pg < kGroups; ++pg) pid[pg] = pages.of(t, pg);
@@ -285,7 +286,7 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v
     Segment s;
     Pages pages;
     uint32_t tiles = 0;
-    const uint32_t v_full = bars + 8 * (kFull + C::kKSlots), v_empty = v_full + 8 * C::kSlots;
+    const uint32_t v_full = bars + 8 * (kRing + C::kKSlots), v_empty = v_full + 8 * C::kSlots;
     const bool chosen = elect_one();
     bool ok = true;
     uint32_t turn = 0;
@@ -371,12 +372,12 @@ __device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, u
     uint32_t k_next = 0, v_next = 0;
     auto wait_k = [&](uint32_t tile) {
         for (; k_next <= tile; ++k_next)
-            if (!wait(kFull + k_next % C::kKSlots, k_next / C::kKSlots)) return false;
+            if (!wait(kRing + k_next % C::kKSlots, k_next / C::kKSlots)) return false;
         return true;
     };
     auto wait_v = [&](uint32_t tile) {
         for (; v_next <= tile; ++v_next)
-            if (!wait(kFull + C::kKSlots + v_next % C::kVSlots, v_next / C::kVSlots)) return false;
+            if (!wait(kRing + C::kKSlots + v_next % C::kVSlots, v_next / C::kVSlots)) return false;
         return true;
     };
     bool ok = true;
@@ -398,7 +399,7 @@ __device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, u
                 mma_ss(tmem + ST * kTile, qd + off, kd + off, mma_instr(kKv, false), k > 0);
             }
             mma_commit(bars + 8 * (kSFull + ST));
-            if (alt || ST == 1) mma_commit(bars + 8 * (kFull + C::kSlots + slot));
+            if (alt || ST == 1) mma_commit(bars + 8 * (kRing + C::kSlots + slot));
         };
         auto begin = [&](auto stream) {
             constexpr int ST = decltype(stream)::value;
@@ -430,7 +431,7 @@ __device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, u
 #pragma unroll
                 for (int k = 0; k < kKv / 16; ++k)
                     mma_ts(tmem + C::kTmemO + ST * D, tmem + ST * kTile + k * 8, vd + k * v_step, mma_instr(D, true), i > 0 || k > 0);
-                if (alt || ST == 1) mma_commit(bars + 8 * (kFull + C::kSlots + C::kKSlots + slot));
+                if (alt || ST == 1) mma_commit(bars + 8 * (kRing + C::kSlots + C::kKSlots + slot));
                 if (more) scores(stream, place(ST, i + 1));
                 else mma_commit(bars + 8 * (kOLast + ST));
             }
@@ -517,7 +518,7 @@ __device__ __forceinline__ void merge_rows(const AttendArgs &a, const Segment &s
             }
 #pragma unroll
             for (int k = 0; k < R; ++k) {
-                const float wk = __shfl_sync(se::kFull, w, min(k0 + k, 31));
+                const float wk = __shfl_sync(kFull, w, min(k0 + k, 31));
 #pragma unroll
                 for (int v = 0; v < V; ++v) acc[k][v] += wk > 0.f ? wk * x[k][v] : 0.f;   // a result without weight may be anything
             }
@@ -563,7 +564,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
         const int ntok = min(tpt, s.tok0 + s.ntok - tok);
         const int q = min(row / a.G, ntok - 1);
         const int sees = s.t.past + tok + q + 1;                           // tokens the row sees
-        const int least = __reduce_min_sync(se::kFull, sees);
+        const int least = __reduce_min_sync(kFull, sees);
         const int steps = s.steps(st);
         const int stride = s.alt ? 2 : 1;
         int left = sees - (s.a + (s.alt ? st : 0)) * kKv;                  // tokens that the row sees of this tile and the later ones
@@ -600,7 +601,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
 #pragma unroll
                 for (int e = 0; e < 4; ++e) top[e] = k + 4 + e < kKv ? max3(top[e], x[k + e], x[k + 4 + e]) : fmaxf(top[e], x[k + e]);
             const float mn = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
-            if (__any_sync(se::kFull, (mn - m) * sl > kSlack)) {
+            if (__any_sync(kFull, (mn - m) * sl > kSlack)) {
                 const float f = m == -INFINITY ? 0.f : ex2((m - mn) * sl);
                 m = mn;
                 l2.x *= f, l2.y *= f;
@@ -734,7 +735,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
                 if (last) atomicExch(ticket, 0u);
             }
             int parts = 0;
-            if (__shfl_sync(se::kFull, last, 0)) {
+            if (__shfl_sync(kFull, last, 0)) {
                 auto add = [&](int index) {
                     if (lane == 0 && parts < kMaxParts) ctl->part[st][parts] = (uint16_t)index;
                     ++parts;
@@ -776,8 +777,8 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
         return;
     }
 
-    static_assert(kFull + 2 * C::kSlots <= kThreads, "a thread per barrier");
-    if (threadIdx.x < kFull + 2 * C::kSlots) {
+    static_assert(kRing + 2 * C::kSlots <= kThreads, "a thread per barrier");
+    if (threadIdx.x < kRing + 2 * C::kSlots) {
         const int i = threadIdx.x;
         const bool by_warp = (i >= kPReady && i < kPReady + 2) || (i >= kOFree && i < kOFree + 2) || (i >= kAll && i < kAll + 2);
         mbar_init(bars + 8 * i, i == kSwap ? 8 : by_warp ? 4 : 1);

@@ -14,8 +14,11 @@
 // head (the two halves of eight rotation pairs), a warp reads all 16 tokens before it computes, so 8 x 16 bytes per
 // lane are in flight.  The K warps fold min and max of what they wrote, and of the page's older keys, with shuffles.
 //
-// Bound by HBM for prompts: 24K tokens of 32 + 2 x 8 heads, D = 128, 131.7 us for 662 MB = 5.0 TB/s, 0.78 of a plain copy.  Small
-// calls are four dependent round trips: 64 single tokens 7.8 us.
+// Bound by HBM for prompts: 24K tokens of 32 + 2 x 8 heads, D = 128, 121.5 us for 662 MB = 5.4 TB/s, 0.84 of a plain copy.  Small
+// calls are four dependent round trips: 64 single tokens 7.2 us.  (Loading the next rows while a row is turned, with the registers
+// that takes, was slower: 8.2 and 128.5 us.)
+#include <type_traits>
+
 #include "se_internal.h"
 
 namespace se {
@@ -76,8 +79,9 @@ __device__ __forceinline__ uint4 shfl_xor4(const uint4 &w, int m) {
                       __shfl_xor_sync(kFull, w.w, m));
 }
 
-template <int D, bool INTERLEAVED>
-__global__ void __launch_bounds__(kRopeThreads)
+// CTAS per SM: a CTA's latency is shorter with two (128 registers), more bytes are in flight with three (80 registers).
+template <int D, bool INTERLEAVED, int CTAS>
+__global__ void __launch_bounds__(kRopeThreads, CTAS)
 rope_append_kernel(const RopeArgs a) {
     constexpr int LPR = D / 16;            // lanes per token: two 16-byte pieces each
     constexpr int RP = 32 / LPR;           // tokens per warp pass
@@ -220,11 +224,22 @@ cudaError_t launch_rope_append(const se_params &p, const RopeCall &c, cudaStream
     a.P_phys = p.num_phys_pages, a.n_axes = c.n_axes, a.rot = c.rot_dim;
     // a request touches at most ceil((n + 15) / 16) pages
     const long long items = (long long)c.total_tokens / kPage + 2ll * p.B;
-    const long long cap = 4ll * device_sm_count();
+    const int sms = device_sm_count();
+    // 64 single tokens: 7.2 us with two CTAs per SM, 8.4 us with three; 24K tokens of prompts: 126.8 and 121.5 us.  (Until each
+    // CTA has several pages the latency of one counts.)
+    const bool many = items > 8ll * sms;
+    const long long cap = (many ? 3ll : 2ll) * sms;
     const unsigned grid = (unsigned)(items < cap ? items : cap);
     const size_t smem = ((size_t)p.B + 1) * sizeof(int);
-    auto kern = p.D == 128 ? (c.interleaved ? rope_append_kernel<128, true> : rope_append_kernel<128, false>)
-                           : (c.interleaved ? rope_append_kernel<64, true> : rope_append_kernel<64, false>);
+    auto pick = [&](auto d, auto ctas) {
+        constexpr int D = decltype(d)::value, CTAS = decltype(ctas)::value;
+        return c.interleaved ? rope_append_kernel<D, true, CTAS> : rope_append_kernel<D, false, CTAS>;
+    };
+    using Two = std::integral_constant<int, 2>;
+    using Three = std::integral_constant<int, 3>;
+    using D64 = std::integral_constant<int, 64>;
+    using D128 = std::integral_constant<int, 128>;
+    auto kern = p.D == 128 ? (many ? pick(D128{}, Three{}) : pick(D128{}, Two{})) : (many ? pick(D64{}, Three{}) : pick(D64{}, Two{}));
     kern<<<grid, kRopeThreads, smem, stream>>>(a);
     return cudaGetLastError();
 }

@@ -322,6 +322,12 @@ def test_rope_append(name, H_q, H_kv, D, rot, axes, inter):
     assert torch.equal(meta.view(torch.int16), rebuilt.view(torch.int16))
 
 
+@pytest.mark.parametrize("D,inter", [(128, False), (64, True)])
+def test_rope_append_of_many_pages(D, inter, monkeypatch):
+    monkeypatch.setitem(SHAPES, "many_pages", ([180, 17, 1] * 100, [5, 0, 130] * 100))
+    test_rope_append("many_pages", 8, 2, D, D, 2, inter)
+
+
 def test_rope_far_positions_and_in_place():
     b = ref.make_batch(111, [50], [3], 4, 2, 128)
     c = Calls(b)
