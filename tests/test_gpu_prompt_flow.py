@@ -1,5 +1,9 @@
 """The prompt-side operators together, as a serving step uses them: a prompt enters in chunks (rotation and append,
 attention, accumulated weights), is evicted down to its budget, and decoding goes on over what is left."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -123,3 +127,39 @@ def test_contiguous_and_paged_attention_of_a_prompt_agree():
     binding.se_prompt_attend(p, q, k, b.v, b.cu, out[1], ws, lse=lse[1])
     assert binding.se_last_device_status(ws) == 0
     assert torch.equal(out[0], out[1]) and torch.equal(lse[0], lse[1])      # the same tiles in the same order
+
+
+FIRST_CALLS = """
+import torch, prompt_ref as ref
+from paper_2609_39068_b200 import binding
+b = ref.make_batch(5, [7, 40], [100, 3], 8, 2, 128)
+p = binding.make_params(b.B, b.H_q, b.H_kv, b.D, b.max_pages, b.P, 1)
+ws = binding.alloc_prompt_workspace(p)
+out, first = (torch.zeros(b.T, 8, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+lse, u = torch.zeros(b.T, 8, device="cuda"), torch.zeros(b.P, 2, 16, device="cuda")
+pos = torch.zeros(1, b.T, dtype=torch.int32, device="cuda")
+freq, axis = torch.ones(64, dtype=torch.float64, device="cuda"), torch.zeros(64, dtype=torch.int32, device="cuda")
+q, k, v = torch.empty_like(out), b.k_cache.clone(), b.v_cache.clone()
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    binding.se_rope_append(p, b.q, b.k, b.v, b.cu, b.seq_lens, b.page_table, pos, freq, axis, q, k, v, ws)
+    binding.se_prompt_attend(p, b.q, b.k, b.v, b.cu, first, ws)
+    binding.se_chunk_attend(p, b.q, b.cu, b.k_cache, b.v_cache, b.page_table, b.seq_lens, out, ws, lse=lse)
+    binding.se_h2o_accumulate(p, b.q, b.cu, b.k_cache, b.page_table, b.seq_lens, lse, u, ws)
+g.replay()
+torch.cuda.synchronize()
+want, tol, _, _ = ref.attend(b)
+assert bool(((out.double() - want).abs() <= tol).all()) and binding.se_last_device_status(ws) == 0
+assert torch.equal(q, b.q) and abs(float(u.double().sum()) - 47 * 8) < 0.04
+b.total = list(b.new)                  # whole prompts: nothing lies before the rows
+want, tol, _, _ = ref.attend(b, paged=False)
+assert bool(((first.double() - want).abs() <= tol).all())
+"""
+
+
+def test_the_first_calls_of_a_process_may_be_captured():
+    here = os.path.dirname(os.path.abspath(__file__))
+    env = dict(os.environ, PYTHONPATH=os.pathsep.join([here, os.path.dirname(here)]))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], env=env, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
