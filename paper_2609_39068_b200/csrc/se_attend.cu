@@ -214,8 +214,8 @@ __device__ __forceinline__ void leave_ring(bool ok, uint32_t filled, uint32_t fu
 }
 
 template <int D>
-__device__ __forceinline__ void k_role(const AttendArgs &a, const List<AttendWork> &list, const CUtensorMap *q_map, const CUtensorMap *k_map, const CUtensorMap *k_wide,
-                                       Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars, int lane) {
+__device__ __forceinline__ void k_role(const AttendArgs &a, const List<AttendWork> &list, const CUtensorMap *q_map, const CUtensorMap *k_map,
+                                       const CUtensorMap *k_wide, Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     const int tpt = kTile / a.G;
@@ -280,7 +280,8 @@ __device__ __forceinline__ void k_role(const AttendArgs &a, const List<AttendWor
 }
 
 template <int D>
-__device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v_map, const CUtensorMap *v_wide, Control<D> *ctl, uint32_t ring, uint32_t bars, int lane) {
+__device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v_map, const CUtensorMap *v_wide, Control<D> *ctl, uint32_t ring,
+                                       uint32_t bars, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     Segment s;
@@ -335,7 +336,8 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v
 #pragma unroll
                     for (int pg = 0; pg < kGroups; ++pg)
                         if (pg != part || !by_hand)
-                            tma_load_4d(dst + pg * page_step, v_map, 0, 0, (pid[pg] < 0 ? a.P_phys * a.H_kv : pid[pg] * a.H_kv + s.h) * kPage, 0, bar);
+                            tma_load_4d(dst + pg * page_step, v_map, 0, 0,
+                                        (pid[pg] < 0 ? a.P_phys * a.H_kv : pid[pg] * a.H_kv + s.h) * kPage, 0, bar);
                 } else {
 #pragma unroll
                     for (int pg = 0; pg < kGroups; ++pg)

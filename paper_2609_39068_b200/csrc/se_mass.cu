@@ -74,7 +74,8 @@ struct MassArgs {
 };
 
 enum Bar { kSFull, kSFree = kSFull + 4, kLseFull = kSFree + 4, kLseEmpty = kLseFull + kLseSlots, kKFull = kLseEmpty + kLseSlots,
-           kKEmpty = kKFull + 2, kAll = kKEmpty + 2, kVerdict = kAll + 2, kHalfFull = kVerdict + 2, kHalfFree = kHalfFull + 2, kDrain = kHalfFree + 2, kRing };
+           kKEmpty = kKFull + 2, kAll = kKEmpty + 2, kVerdict = kAll + 2, kHalfFull = kVerdict + 2,
+           kHalfFree = kHalfFull + 2, kDrain = kHalfFree + 2, kRing };
 
 struct MassWork {
     const int32_t *cu, *seq_lens;
@@ -150,8 +151,8 @@ __device__ __forceinline__ int group_page(const MassArgs &a, const Segment &s, i
 }
 
 template <int D>
-__device__ __forceinline__ void copy_role(const MassArgs &a, const List<MassWork> &list, const CUtensorMap *q_map, const CUtensorMap *k_map, Control<D> *ctl,
-                                          uint32_t k_smem, uint32_t ring, uint32_t bars, int lane) {
+__device__ __forceinline__ void copy_role(const MassArgs &a, const List<MassWork> &list, const CUtensorMap *q_map, const CUtensorMap *k_map,
+                                          Control<D> *ctl, uint32_t k_smem, uint32_t ring, uint32_t bars, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     Walk<MassWork> walk(list, a.ctl, lane);
