@@ -56,8 +56,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
-# A second build of the same sources with -DSE_TEST_SHORT_TX: the scoring kernel's waits run out (see
-# se_select.cu).  Only tests/test_gpu_timeout.py loads it.
+# A second build of the same sources with -DSE_TEST_SHORT_TX: waits of the scoring kernel (se_select.cu) and of the prompt
+# kernels (se_tc.cuh) run out.  Only the tests of the bounded waits load it.
 LIB_SHORT_TX = os.path.join(HERE, "libsparse_engine_shorttx.so")
 
 

@@ -203,13 +203,14 @@ struct Pages {
 
 // The end of a copying warp that has filled `filled` slots of a ring of kSlots, whose barriers are full + 8 * slot and
 // empty + 8 * slot: nothing may still be on its way to the CTA's shared memory when the CTA ends - copies, and the
-// products' arrivals for the slots they have let go.
+// products' arrivals for the slots they have let go.  A slot that is let go has been filled; where the products have given up
+// (also just now, in the wait for this very slot) the copy itself is waited for.
 template <uint32_t kSlots>
 __device__ __forceinline__ void leave_ring(bool ok, uint32_t filled, uint32_t full, uint32_t empty, volatile int *gave_up, const AttendArgs &a) {
     for (uint32_t n = filled > kSlots ? filled - kSlots : 0; n < filled; ++n) {
         const uint32_t off = 8 * (n % kSlots), parity = n / kSlots & 1;
-        if (ok) ok = warp_wait(empty + off, parity, gave_up, &a.ctl->status);
-        else mbar_wait(full + off, parity);
+        ok = ok && warp_wait(empty + off, parity, gave_up, &a.ctl->status);
+        if (!ok) mbar_wait(full + off, parity);
     }
 }
 
@@ -274,8 +275,8 @@ __device__ __forceinline__ void k_role(const AttendArgs &a, const List<AttendWor
     if (ok) ok = ctl->queue.put(queries, nullptr, gave_up, &a.ctl->status, lane);
     leave_ring<C::kKSlots>(ok, tiles, k_full, k_empty, gave_up, a);
     if (queries) {
-        if (ok) warp_wait(bars + 8 * kQEmpty, (queries - 1) & 1, gave_up, &a.ctl->status);
-        else mbar_wait(bars + 8 * kQFull, (queries - 1) & 1);
+        ok = ok && warp_wait(bars + 8 * kQEmpty, (queries - 1) & 1, gave_up, &a.ctl->status);
+        if (!ok) mbar_wait(bars + 8 * kQFull, (queries - 1) & 1);
     }
 }
 
@@ -329,7 +330,7 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v
                 __syncwarp();
             }
             if (chosen) {
-                mbar_expect_tx(bar, C::kKvBytes - (by_hand ? kPage * D * 2 : 0));
+                mbar_expect_tx(bar, C::kKvBytes - (by_hand ? kPage * D * 2 : 0) + (tiles == 0 ? kTestExtraTx : 0));
                 if (!a.page_table && (t + 1) * kKv <= stop) {
                     tma_load_4d(dst, v_wide, 0, s.h, s.t.start + t * kKv, 0, bar);
                 } else if (a.page_table) {

@@ -187,7 +187,7 @@ __device__ __forceinline__ void copy_role(const MassArgs &a, const List<MassWork
             ok = warp_wait(bar + 8 * C::kSlots, (pos / C::kSlots & 1) ^ 1, gave_up, &a.ctl->status);
             if (!ok) break;
             if (chosen) {
-                mbar_expect_tx(bar, list.w.tpt * a.G * D * 2);
+                mbar_expect_tx(bar, list.w.tpt * a.G * D * 2 + (pos == 0 ? kTestExtraTx : 0));
 #pragma unroll
                 for (int half = 0; half < C::kHalves; ++half)
                     tma_load_3d(ring + slot * C::kTileBytes + half * (kTile * 128), q_map, half * 64, s.h * a.G,
@@ -198,15 +198,16 @@ __device__ __forceinline__ void copy_role(const MassArgs &a, const List<MassWork
     }
     if (ok) ok = ctl->queue.put(pairs, nullptr, gave_up, &a.ctl->status, lane);
     // nothing may still be on its way to the CTA's shared memory when the CTA ends: copies, and the products' arrivals on the
-    // barriers of the tiles they have let go
+    // barriers of the tiles they have let go.  A tile that is let go has been filled; where the products have given up (also
+    // just now, in the wait for this very tile) the copy itself is waited for.
     for (uint32_t p = pos > C::kSlots ? pos - C::kSlots : 0; p < pos; ++p) {
         const uint32_t bar = bars + 8 * (kRing + p % C::kSlots), parity = p / C::kSlots & 1;
-        if (ok) ok = warp_wait(bar + 8 * C::kSlots, parity, gave_up, &a.ctl->status);
-        else mbar_wait(bar, parity);
+        ok = ok && warp_wait(bar + 8 * C::kSlots, parity, gave_up, &a.ctl->status);
+        if (!ok) mbar_wait(bar, parity);
     }
     for (uint32_t p = pairs > 2 ? pairs - 2 : 0; p < pairs; ++p) {
-        if (ok) ok = warp_wait(bars + 8 * (kKEmpty + (p & 1)), p >> 1 & 1, gave_up, &a.ctl->status);
-        else mbar_wait(bars + 8 * (kKFull + (p & 1)), p >> 1 & 1);
+        ok = ok && warp_wait(bars + 8 * (kKEmpty + (p & 1)), p >> 1 & 1, gave_up, &a.ctl->status);
+        if (!ok) mbar_wait(bars + 8 * (kKFull + (p & 1)), p >> 1 & 1);
     }
 }
 

@@ -8,6 +8,14 @@
 
 namespace se {
 
+// Fault injection for the test of the bounded waits (a second build of the library, -DSE_TEST_SHORT_TX, never the product): a
+// copy announces 16 bytes more than it delivers, so the wait for it runs out.
+#ifdef SE_TEST_SHORT_TX
+constexpr uint32_t kTestExtraTx = 16;
+#else
+constexpr uint32_t kTestExtraTx = 0;
+#endif
+
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
