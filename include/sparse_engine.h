@@ -397,7 +397,8 @@ int se_h2o_compact(const se_params *p, void *k_cache, void *v_cache, float *scor
  *  - They take a workspace of their own kind: se_prompt_workspace_bytes bytes (80 MB at D = 128), initialised
  *    once by se_prompt_workspace_init, then good for any number of calls with the same se_params that are ordered
  *    on the device.  se_last_device_status reads its status word.  After a call that reported
- *    SE_DEV_WAIT_TIMEOUT it has to be initialised again.
+ *    SE_DEV_WAIT_TIMEOUT it has to be initialised again: until then se_chunk_attend, se_prompt_attend and
+ *    se_h2o_accumulate write nothing and report SE_DEV_WAIT_TIMEOUT each time.
  */
 size_t se_prompt_workspace_bytes(const se_params *p);
 int se_prompt_workspace_init(const se_params *p, void *workspace, void *stream);

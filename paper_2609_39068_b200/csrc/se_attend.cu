@@ -139,6 +139,7 @@ struct Control {
     int parts[2];                      // partial results to merge, 0: another CTA does
     uint16_t part[2][kMaxParts];
     int gave_up;
+    uint32_t refused;                  // the workspace has to be initialised first
     uint32_t tmem;
 };
 
@@ -792,6 +793,8 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
         mbar_fence_init();
         ctl->gave_up = 0;
     }
+    // (read ahead: it is here when the list is)
+    const uint32_t refused = threadIdx.x == 32 ? *(volatile uint32_t *)&a.ctl->needs_init : 0u;
     if (warp == kMmaWarp) tmem_alloc(smem_u32(&ctl->tmem), 512);
     if (threadIdx.x == 32 * kKWarp) prefetch_map(&q_map), prefetch_map(&k_map);
     if (threadIdx.x == 32 * kVWarp) prefetch_map(&v_map);
@@ -801,12 +804,15 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     // query rows that no tensor copy fills (G does not divide 128) stay zero
     for (int i = threadIdx.x; i < (work.tpt * a.G == kTile ? 0 : 2 * C::kTileBytes / 16); i += kThreads)
         reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
+    if (threadIdx.x == 32) ctl->refused = refused;
     fence_async_proxy();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
 
-    if (warp < 8) {
+    if (ctl->refused) {
+        if (threadIdx.x == 0 && blockIdx.x == 0) atomicOr(&a.ctl->status, SE_DEV_WAIT_TIMEOUT);
+    } else if (warp < 8) {
         regs_up<kRegsSoftmax>();
         softmax_role<D>(a, list, ctl, bars, warp >> 2);
     } else {

@@ -123,6 +123,7 @@ struct Control {
     alignas(8) uint8_t prefix[prefix_bytes(kSmemRequests)];
     int last[2];
     int gave_up;
+    uint32_t refused;                  // the workspace has to be initialised first
     uint32_t tmem;
 };
 
@@ -450,6 +451,8 @@ mass_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ C
         mbar_fence_init();
         ctl->gave_up = 0;
     }
+    // (read ahead: it is here when the list is)
+    const uint32_t refused = threadIdx.x == 32 ? *(volatile uint32_t *)&a.ctl->needs_init : 0u;
     if (warp == kMmaWarp) tmem_alloc(smem_u32(&ctl->tmem), 512);
     const MassWork work(a);
     const List<MassWork> list = make_list<kThreads>(work, a.B, a.H_kv, a.ctl,
@@ -457,12 +460,15 @@ mass_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ C
     // query rows that no tensor copy fills (G does not divide 128) stay zero
     for (int i = threadIdx.x; i < C::kSlots * C::kTileBytes / 16; i += kThreads)
         reinterpret_cast<uint4 *>(smem + 2 * C::kPairs * C::kTileBytes)[i] = make_uint4(0, 0, 0, 0);
+    if (threadIdx.x == 32) ctl->refused = refused;
     fence_async_proxy();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
 
-    if (warp < 16) {
+    if (ctl->refused) {
+        if (threadIdx.x == 0 && blockIdx.x == 0) atomicOr(&a.ctl->status, SE_DEV_WAIT_TIMEOUT);
+    } else if (warp < 16) {
         regs_up<kRegsSum>();
         sum_role<D>(a, list, ctl, bars, warp >> 2 & 1, warp >> 3);
     } else {

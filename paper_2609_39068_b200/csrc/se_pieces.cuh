@@ -27,6 +27,8 @@
 //   long long longest(t)               then: a bound on the cost of the request's items
 #pragma once
 
+#include <stddef.h>
+
 #include "se_tc.cuh"
 
 namespace se {
@@ -35,11 +37,14 @@ constexpr int kPromptCtas = 148;       // one per SM
 constexpr int kMaxPieces = 2 * kPromptCtas;
 constexpr int kSmemRequests = 96;      // batches up to here keep their prefix sums in shared memory
 
-// Head of the workspace of the prompt calls (zero when no call is running).
+// Head of the workspace of the prompt calls.  The counters are zero when no call is running, unless a call gave up a wait: then
+// needs_init is set, and the kernels that count do nothing but report SE_DEV_WAIT_TIMEOUT until the workspace is initialised
+// again (reading the status word does not clear it).
 struct PromptControl {
-    uint32_t status, next_piece, ended, pad[61];
+    uint32_t status, needs_init, next_piece, ended, pad[60];
     uint32_t tickets[2 * kMaxPieces];
 };
+static_assert(offsetof(PromptControl, needs_init) == kNeedsInitWord * sizeof(uint32_t), "the word that warp_wait sets");
 constexpr size_t kPromptControlBytes = (sizeof(PromptControl) + 255) / 256 * 256;
 
 // Prefix sums over the requests: cost and number of items before each, [B + 1].

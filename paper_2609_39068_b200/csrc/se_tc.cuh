@@ -131,10 +131,12 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 }
 
 // Wait of a warp of a role.  Gives up after 400 million cycles (200 ms at 1.97 GHz), or as soon as another role of the CTA has
-// given up (*gave_up != 0, shared memory); the first one to give up reports it.  False: leave the role's loop.
+// given up (*gave_up != 0, shared memory); the first one to give up reports it in the status word, and marks the workspace in
+// the word behind it: the call's counters stay half counted, so no later call may use them.  False: leave the role's loop.
 // The warp leaves it together: tensor copies and products take their operands from uniform registers, which lanes that ran ahead
 // of the issuing lane would overwrite, and tensor memory is accessed by whole warps.  (A vote at every look took 2 to 10 % of
 // the attention kernel's time.)
+constexpr int kNeedsInitWord = 1;
 constexpr long long kWaitLimitCycles = 400ll * 1000 * 1000;
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *gave_up, uint32_t *status) {
     bool got = mbar_try_wait(bar, parity);
@@ -146,6 +148,7 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
             if (got || *gave_up) break;
             if (clock64() - t0 > kWaitLimitCycles) {
                 *gave_up = 1;
+                atomicExch(status + kNeedsInitWord, 1u);
                 atomicOr(status, SE_DEV_WAIT_TIMEOUT);
                 break;
             }

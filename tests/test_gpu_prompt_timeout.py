@@ -86,3 +86,41 @@ def test_wait_that_never_completes_times_out(short, name, op):
         torch.cuda.synchronize()
         assert c.status() == 0
         assert all(torch.equal(x, y) for x, y in zip(good, again))
+
+
+@pytest.mark.parametrize("op", ["chunk", "prompt", "mass"])
+def test_after_a_timeout_calls_refuse_until_the_workspace_is_initialised(short, op):
+    new, past, H_q, H_kv, D = BATCHES["two_sizes"]
+    b = ref.make_batch(3, new, past, H_q, H_kv, D, nan_tail=False)
+    c, ops = operators(b)
+    good = [x.clone() for x in ops[op]()]
+    short(ops[op])
+    assert c.status() == binding.SE_DEV_WAIT_TIMEOUT and c.status() == 0      # the reading has cleared the word ...
+    for _ in range(2):
+        c.out.fill_(7.0)
+        c.lse.fill_(7.0)
+        outputs = ops[op]()
+        torch.cuda.synchronize()
+        assert c.status() == binding.SE_DEV_WAIT_TIMEOUT                      # ... but the workspace is not fit for use
+        assert all(bool((x == (0.0 if op == "mass" else 7.0)).all()) for x in outputs)
+    binding.se_prompt_workspace_init(c.p, c.ws)
+    again = ops[op]()
+    torch.cuda.synchronize()
+    assert c.status() == 0 and all(torch.equal(x, y) for x, y in zip(good, again))
+
+
+def test_the_mark_is_the_workspace_s_own():
+    # set from the host; a workspace beside it goes on, and the append, which counts nothing, goes on with the marked one
+    b = ref.make_batch(4, [20, 1], [30, 0], 8, 2, 64)
+    marked, other = Calls(b), Calls(b)
+    marked.ws[:8].view(torch.int32)[1] = 1
+    marked.chunk()
+    other.chunk()
+    torch.cuda.synchronize()
+    assert marked.status() == binding.SE_DEV_WAIT_TIMEOUT and bool(marked.out.isnan().all())
+    assert other.status() == 0 and bool(other.out.isfinite().all())
+    pos = torch.zeros(1, b.T, dtype=torch.int32, device="cuda")
+    freq, axis = torch.ones(32, dtype=torch.float64, device="cuda"), torch.zeros(32, dtype=torch.int32, device="cuda")
+    binding.se_rope_append(marked.p, b.q, b.k, b.v, b.cu, b.seq_lens, b.page_table, pos, freq, axis, marked.out, b.k_cache.clone(),
+                           b.v_cache.clone(), marked.ws)
+    assert marked.status() == 0 and torch.equal(marked.out, b.q)
