@@ -139,7 +139,7 @@ struct Control {
     int parts[2];                      // partial results to merge, 0: another CTA does
     uint16_t part[2][kMaxParts];
     int gave_up;
-    uint32_t refused;                  // the workspace has to be initialised first
+    List<AttendWork> list;             // (in registers it made the compiler spill: 252 bytes of loads, here 28)
     uint32_t tmem;
 };
 
@@ -805,20 +805,25 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     if (threadIdx.x == 32 * kKWarp) prefetch_map(&q_map), prefetch_map(&k_map);
     if (threadIdx.x == 32 * kVWarp) prefetch_map(&v_map);
     const AttendWork work(a);
-    const List<AttendWork> list = make_list<kThreads>(work, a.B, a.H_kv, a.ctl,
+    List<AttendWork> made = make_list<kThreads>(work, a.B, a.H_kv, a.ctl,
                                             a.B > kSmemRequests ? a.prefixes + prefix_bytes(a.B) * blockIdx.x : ctl->prefix, smem);
     // query rows that no tensor copy fills (G does not divide 128) stay zero
     for (int i = threadIdx.x; i < (work.tpt * a.G == kTile ? 0 : 2 * C::kTileBytes / 16); i += kThreads)
         reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
-    if (threadIdx.x == 32) ctl->refused = refused;
+    if (threadIdx.x == 32) {
+        if (refused) {                   // an empty list: the roles find nothing to do, and no counter moves
+            made.total = 0, made.pieces = kPromptCtas;
+            if (blockIdx.x == 0) atomicOr(&a.ctl->status, SE_DEV_WAIT_TIMEOUT);
+        }
+        ctl->list = made;
+    }
     fence_async_proxy();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    const List<AttendWork> &list = ctl->list;
 
-    if (ctl->refused) {
-        if (threadIdx.x == 0 && blockIdx.x == 0) atomicOr(&a.ctl->status, SE_DEV_WAIT_TIMEOUT);
-    } else if (warp < 8) {
+    if (warp < 8) {
         regs_up<kRegsSoftmax>();
         softmax_role<D>(a, list, ctl, bars, warp >> 2);
     } else {

@@ -35,7 +35,7 @@ namespace se {
 
 constexpr int kPromptCtas = 148;       // one per SM
 constexpr int kMaxPieces = 2 * kPromptCtas;
-constexpr int kSmemRequests = 96;      // batches up to here keep their prefix sums in shared memory
+constexpr int kSmemRequests = 88;      // batches up to here keep their prefix sums in shared memory
 
 // Head of the workspace of the prompt calls.  The counters are zero when no call is running, unless a call gave up a wait: then
 // needs_init is set, and the kernels that count do nothing but report SE_DEV_WAIT_TIMEOUT until the workspace is initialised
@@ -68,7 +68,7 @@ struct Border {
 
 template <class Work>
 struct List {
-    const Work &w;
+    Work w;
     int B, H_kv;
     const long long *cost;
     const int *first;
