@@ -435,6 +435,9 @@ int se_rope_append(const se_params *p, const void *q, int64_t q_stride, const vo
  *   out  [total_tokens, H_q, D] bf16 (the next operation of a layer is a bf16 product)
  *   lse  [total_tokens, H_q] fp32, or NULL
  * Cache slots past a request's length may hold anything, NaN included.  n_r = 1 is a dense decode step.
+ * A row with a NaN among its logits, or one of +infinity, has out = lse = NaN, however the batch was cut, and no
+ * request reaches another one's rows.  (V has to be finite: an infinity or NaN of a new token's V also reaches rows
+ * of its request that do not see it, where they share its tile of 128 tokens.)
  */
 int se_chunk_attend(const se_params *p, const void *q, int64_t q_stride, int32_t total_tokens,
                     const int32_t *cu_seqlens, const void *k_cache, const void *v_cache,

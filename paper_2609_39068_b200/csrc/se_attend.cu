@@ -498,15 +498,18 @@ __device__ __forceinline__ void merge_rows(const AttendArgs &a, const Segment &s
         L = L * ex2(M - ref) + l * ex2(m - ref);
         M = top;
     }
-    const float inv = L > 0.f ? 1.f / L : 0.f, ref = M == -INFINITY ? 0.f : M;
-    if (have && a.lse) a.lse[out0 + (long long)(my / a.G) * a.H_q + my % a.G] = L > 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
+    // a sum of exactly 0: nothing was seen; a NaN goes on into the row and its lse
+    const float inv = L == 0.f ? 0.f : 1.f / L, ref = M == -INFINITY ? 0.f : M;
+    if (have && a.lse) a.lse[out0 + (long long)(my / a.G) * a.H_q + my % a.G] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
     const int mine = rows > row_from ? (rows - row_from + row_step - 1) / row_step : 0;
     for (int k0 = 0; k0 < mine; k0 += R) {
         float acc[R][V] = {};
 #pragma unroll 4
         for (int q = 0; q < parts; ++q) {
             const float *p = partial_slot<D>(a, at(q));
-            const float w = have ? ex2(__ldcg(p + kTile * D + my) - ref) * inv : 0.f;
+            // -1: the part saw nothing, and what lies in its place may be anything
+            const float m = have ? __ldcg(p + kTile * D + my) : -INFINITY;
+            const float w = m == -INFINITY ? -1.f : ex2(m - ref) * inv;
             float x[R][V];
 #pragma unroll
             for (int k = 0; k < R; ++k) {
@@ -524,7 +527,7 @@ __device__ __forceinline__ void merge_rows(const AttendArgs &a, const Segment &s
             for (int k = 0; k < R; ++k) {
                 const float wk = __shfl_sync(kFull, w, min(k0 + k, 31));
 #pragma unroll
-                for (int v = 0; v < V; ++v) acc[k][v] += wk > 0.f ? wk * x[k][v] : 0.f;   // a result without weight may be anything
+                for (int v = 0; v < V; ++v) acc[k][v] += wk < 0.f ? 0.f : wk * x[k][v];
             }
         }
 #pragma unroll
@@ -656,14 +659,15 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
         }
 
         // ---- epilogue ----
-        const float m2 = m == -INFINITY ? m : m * sl;
+        // -infinity says that nothing was seen, so a sum that is NaN goes with another maximum
+        const float m2 = l != l ? INFINITY : m == -INFINITY ? m : m * sl;
         const bool live = row < ntok * a.G;
         const bool whole = s.a == 0 && s.b == s.nkv;
         const bool direct = whole && (!s.alt || s.nkv == 1);
         const long long orow = (long long)(s.t.start + tok + q) * a.H_q + s.h * a.G + row % a.G;
         if (direct) {
             if (s.alt && st == 1) continue;                                // a single KV tile: stream 0 has it all
-            const float inv = l > 0.f ? 1.f / l : 0.f;
+            const float inv = l == 0.f ? 0.f : 1.f / l;                    // 0: nothing was seen; a NaN goes on
             uint4 *dst = reinterpret_cast<uint4 *>(a.out + orow * D);
             const bool wide = ((uintptr_t)a.out & 31) == 0;
 #pragma unroll
@@ -690,7 +694,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
                     }
                 }
             }
-            if (live && a.lse) a.lse[orow] = l > 0.f ? (m2 + log2f(l)) * kLn2 : -INFINITY;
+            if (live && a.lse) a.lse[orow] = l == 0.f ? -INFINITY : (m2 + log2f(l)) * kLn2;
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bars + 8 * (kOFree + st));
