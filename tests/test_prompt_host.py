@@ -83,3 +83,12 @@ def test_binding_refuses_tensors_that_are_not_on_a_gpu():
         binding._rows(x, 32, 128, "q")
     with pytest.raises(binding.SparseEngineError):
         binding._shape(x, [3, 32, 64], "q")
+
+
+def test_shapes_are_compared_by_value():
+    x = torch.zeros(3, 32, 128, dtype=torch.bfloat16)
+    binding._shape(x, (3, 32, 128), "q")
+    binding._shape(None, (3, 32, 128), "lse")
+    for bad in ((3, 32, 64), (3, 32), (3, 32, 128, 1), (4, 32, 128), ()):
+        with pytest.raises(binding.SparseEngineError, match=r"q must have shape \["):
+            binding._shape(x, bad, "q")
