@@ -413,7 +413,8 @@ int se_prompt_workspace_init(const se_params *p, void *workspace, void *stream);
  * interleaved = 0: pair c is channels (c, c + rot_dim/2); 1: channels (2c, 2c+1).  Angles are reduced in fp64, the
  * rotation is fp32, the result is rounded once to bf16.
  *   q_out  [total_tokens, H_q, D]  bf16       may be q itself when q_stride == H_q*D
- *   k_out  [total_tokens, H_kv, D] bf16 or NULL: rotated K also in token order (for se_prompt_attend)
+ *   k_out  [total_tokens, H_kv, D] bf16 or NULL: rotated K also in token order (for se_prompt_attend);
+ *                                        may be k itself when k_stride == H_kv*D
  * k_cache / v_cache slots of the new tokens are written; a token whose page is absent or out of range is
  * left out of the cache and reported (SE_DEV_BAD_PAGE_ID).  With meta != NULL the summaries of the touched pages
  * become those of se_meta_update over the page's tokens below seq_lens[r] (bit for bit).  A page that receives tokens

@@ -468,7 +468,8 @@ int se_rope_append(const se_params *p, const void *q, int64_t q_stride, const vo
         return SE_ERR_MISALIGNED;
     if (total_tokens < 0 || bad_stride(q_stride, p->H_q, p->D) || bad_stride(k_stride, p->H_kv, p->D) ||
         bad_stride(v_stride, p->H_kv, p->D) || n_axes < 1 || n_axes > 4 || rot_dim < 16 || rot_dim > p->D ||
-        rot_dim % 16 != 0 || (interleaved != 0 && interleaved != 1) || (q_out == q && q_stride != (int64_t)p->H_q * p->D))
+        rot_dim % 16 != 0 || (interleaved != 0 && interleaved != 1) || (q_out == q && q_stride != (int64_t)p->H_q * p->D) ||
+        (k_out == k && k_stride != (int64_t)p->H_kv * p->D))
         return SE_ERR_INVALID_ARG;
     if (total_tokens == 0) return SE_OK;
     RopeCall c = {};

@@ -92,3 +92,10 @@ def test_shapes_are_compared_by_value():
     for bad in ((3, 32, 64), (3, 32), (3, 32, 128, 1), (4, 32, 128), ()):
         with pytest.raises(binding.SparseEngineError, match=r"q must have shape \["):
             binding._shape(x, bad, "q")
+
+
+def test_rotated_keys_in_place_of_a_strided_view():
+    # k_out may be k itself only where the rows of both lie at the same places
+    args = changed("se_rope_append", 18, OK)
+    args[3], args[4] = OK, 6144
+    assert call("se_rope_append", args) == -1
