@@ -458,7 +458,7 @@ mass_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ C
     const List<MassWork> list = make_list<kThreads>(work, a.B, a.H_kv, a.ctl,
                                           a.B > kSmemRequests ? a.prefixes + prefix_bytes(a.B) * blockIdx.x : ctl->prefix, smem);
     // query rows that no tensor copy fills (G does not divide 128) stay zero
-    for (int i = threadIdx.x; i < C::kSlots * C::kTileBytes / 16; i += kThreads)
+    for (int i = threadIdx.x; i < (work.tpt * a.G == kTile ? 0 : C::kSlots * C::kTileBytes / 16); i += kThreads)
         reinterpret_cast<uint4 *>(smem + 2 * C::kPairs * C::kTileBytes)[i] = make_uint4(0, 0, 0, 0);
     if (threadIdx.x == 32) ctl->refused = refused;
     fence_async_proxy();
