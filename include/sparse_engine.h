@@ -435,6 +435,9 @@ int se_rope_append(const se_params *p, const void *q, int64_t q_stride, const vo
  * The new tokens' own K and V are in the cache already (se_rope_append).  No visible position: out = 0, lse = -inf.
  *   out  [total_tokens, H_q, D] bf16 (the next operation of a layer is a bf16 product)
  *   lse  [total_tokens, H_q] fp32, or NULL
+ * Precision: scores, the weights' sum and lse are fp32.  Each weight is rounded to bf16 (to nearest, at most 2^-8
+ * relative) before its product with V, as the tensor cores take V and the weights in one type; products are summed
+ * in fp32, and out is rounded once to bf16.
  * Cache slots past a request's length may hold anything, NaN included.  n_r = 1 is a dense decode step.
  * A row with a NaN among its logits, or one of +infinity, has out = lse = NaN, however the batch was cut, and no
  * request reaches another one's rows.  (V has to be finite: an infinity or NaN of a new token's V also reaches rows
@@ -447,7 +450,7 @@ int se_chunk_attend(const se_params *p, const void *q, int64_t q_stride, int32_t
 
 /*
  * The same for whole prompts whose K and V are still contiguous [total_tokens, H_kv, D] (a method that prunes the
- * prompt before it caches anything, an encoder pass without a cache): token i of a request attends its tokens 0..i.
+ * prompt before it caches anything, a pass that keeps no cache): token i of a request attends its tokens 0..i.
  */
 int se_prompt_attend(const se_params *p, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                      const void *v, int64_t v_stride, int32_t total_tokens, const int32_t *cu_seqlens, void *out,

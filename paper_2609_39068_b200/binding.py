@@ -437,6 +437,8 @@ def se_rope_append(p, q, k, v, cu_seqlens, seq_lens, page_table, positions, inv_
 
 
 def se_chunk_attend(p, q, cu_seqlens, k_cache, v_cache, page_table, seq_lens, out, workspace, lse=None) -> None:
+    """Causal attention of the new tokens over the paged cache.  ``out`` is bf16; the weights are rounded to bf16 before their
+    product with V, their sum and ``lse`` are fp32."""
     T, H_q, D = q.shape[0], p.H_q, p.D
     _prompt_common(p, workspace, cu_seqlens, page_table, seq_lens, k_cache, v_cache)
     _shape(out, (T, H_q, D), "out")
@@ -452,6 +454,7 @@ def se_chunk_attend(p, q, cu_seqlens, k_cache, v_cache, page_table, seq_lens, ou
 
 
 def se_prompt_attend(p, q, k, v, cu_seqlens, out, workspace, lse=None) -> None:
+    """Causal attention of packed whole prompts over contiguous K and V, with the precision of ``se_chunk_attend``."""
     T, H_q, H_kv, D = q.shape[0], p.H_q, p.H_kv, p.D
     _prompt_common(p, workspace, cu_seqlens)
     _shape(k, (T, H_kv, D), "k")
