@@ -21,11 +21,13 @@
 // pieces, so the result does not depend on who is last.  Long contexts with few rows and long prompts take the same path, and
 // there is no second kernel.
 //
-// Measured (32 heads over 8, D = 128): prompt of 32768 tokens 7.7-8.25 ms (1.07-1.14 PFLOP/s), 2048 tokens over 65536 1.8-1.95 ms,
-// eight packed prompts of 500-4000 tokens 370 us, eight times five drafted tokens over 32768 194 us (5.5 TB/s).  A step of both
+// Measured (32 heads over 8, D = 128; device time in graphs, calls issued one by one on changing inputs in brackets): prompt of
+// 32768 tokens 8.1-8.4 ms (8.3-8.4; 1.05-1.09 PFLOP/s), 2048 tokens over 65536 1.9-2.0 ms (2.02-2.05), eight packed prompts of
+// 500-4000 tokens 366 us (387-390), eight times five drafted tokens over 32768 197 us (203-213; 5.0-5.4 TB/s).  A step of both
 // streams takes 3350 cycles where products and exponentials take 2048 each: a stream's chain of scores, softmax and product is
-// what bounds it.  KV tiles of 64 tokens with two score buffers per stream took 465-497 us for the packed prompts, a product that
-// begins with half of the weights 399-410 us, exponentials on the FMA units (one pair in eight) 386 us.
+// what bounds it.  Compared on builds that took 372 us for the packed prompts: KV tiles of 64 tokens with two score buffers per
+// stream 465-497 us, a product that begins with half of the weights 399-410 us, exponentials on the FMA units (one pair in
+// eight) 386 us.
 #include <math.h>
 
 #include "se_internal.h"
@@ -47,8 +49,8 @@ constexpr int kGroups = kKv / kPage;   // pages of a KV tile
 constexpr int kMaxParts = 304;         // partial results of a query tile: two per piece, little more than 148 pieces of it
 constexpr int kItemCost = 128;         // cost of starting a query tile, in tokens
 // A CTA takes at least 256 tokens (a short item has a CTA of its own), but where pieces are small, items are split at multiples
-// of four KV tiles only: the parts have to be merged, which takes as long as a dozen tiles.  Six short prompts: 14.0 us, with
-// pieces of 512 tokens 17.2 us; one token over 2048: 20.3 us, split at every second tile 21.7 us.
+// of four KV tiles only: the parts have to be merged, which takes as long as a dozen tiles.  Six short prompts: 16.4 us, with
+// pieces of 512 tokens 19.5 us; one token over 2048: 21.8 us, split at every second tile 23.7 us.
 constexpr int kMinCost = 256, kCoarse = 2048;
 // The running maximum may lag: weights up to 2^40 lose nothing (bf16 and fp32 keep their exponents, and 2^40 * 131072
 // tokens is far from the end of the range).
@@ -649,7 +651,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
             if (lane == 0) mbar_arrive(bars + 8 * (kPReady + st));
             __syncwarp();
             // The tile's sum joins the others in one compensated step: equal weights added one after the other over 32768 tokens
-            // lost up to 2e-4 of the sum, 5e-4 over 65536 (now 6e-6 and less).
+            // lost up to 2e-4 of the sum, 5e-4 over 65536 (now less than 2e-6).
             const float y = __fsub_rn(l2.x + l2.y, lost), next_l = __fadd_rn(l, y);
             lost = __fsub_rn(__fsub_rn(next_l, l), y);
             l = next_l;

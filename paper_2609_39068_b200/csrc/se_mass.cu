@@ -6,13 +6,14 @@
 // A thread owns one cached token and adds up 2^(S sl - lse log2 e) along half of its columns in a register: no reduction
 // between threads but the one addition of the halves, no atomics, no second pass, and the result does not depend on timing.
 //
-// What bounds it: per 128 x 128 tile one product of 512 tensor cycles (D = 128) and 16384 exponentials = 1024 cycles of
-// the special-function units; K is read once per item, the queries come from L2.  A CTA works on two tiles of cached tokens
-// (two warpgroups each) that share every query tile.  Scores are double-buffered in tensor memory (4 x 128 columns), so the
-// products of the next query tile run under the exponentials of this one.
-// Prompt of 16384 tokens (32 heads over 8, D = 128): 1320 us, 833 TFLOP/s of products counted below the diagonal; chunks of
-// four requests over 32768 cached tokens: 566 us, the special-function units busy for 52 % of the cycles, the tensor cores for
-// 34 %, an instruction issued in 62 % of them.  With one warpgroup per tile (all columns in a thread) 1412 and 599 us.
+// What bounds it: per 128 x 128 tile one product of 512 tensor cycles (D = 128) and 16384 exponentials, seven in eight of them
+// on the special-function units, which takes those 896 cycles; K is read once per item, the queries come from L2.  A CTA works
+// on two tiles of cached tokens (two warpgroups each) that share every query tile.  Scores are double-buffered in tensor memory
+// (4 x 128 columns), so the products of the next query tile run under the exponentials of this one.
+// Prompt of 16384 tokens (32 heads over 8, D = 128): 1320-1430 us in graphs, 1460-1475 as calls on changing inputs (750 TFLOP/s of
+// products counted below the diagonal); chunks of four requests over 32768 cached tokens: 571-576 and 597-605 us.  Of the latter's
+// cycles the special-function units are busy for 59 %, the tensor cores for 33 %, and an instruction is issued in 52 %.  With one
+// warpgroup per tile (all columns in a thread) 1412 and 599 us in graphs, on a build that took 1320 and 566.
 //
 // Item = 256 cached tokens of one (request, kv-head), unit = query tile; pieces and merging as in se_pieces.cuh (a partial
 // result is one number per cached token).
@@ -26,8 +27,8 @@ namespace se {
 
 namespace {
 
-// One pair of weights in eight is computed without the special-function units (prompt of 16384: none 1350 us, one in eight
-// 1320 us, one in four 1408 us, where the issue of instructions becomes the bound).
+// One pair of weights in eight is computed without the special-function units (side by side, prompt of 16384: none 1350 us, one
+// in eight 1320 us, one in four 1408 us, where the issue of instructions becomes the bound).
 // 2^x of a pair: x = j + f with |f| <= 1/2 (j by adding and taking off 1.5 * 2^23), 2^f by a
 // minimax polynomial of degree 5 with 2^0 = 1 (own fit; relative error 1.6e-7, fp32 rounding included), j added to the exponent
 // field.  x is held to [-127, 128], where the exponent field comes out as 0 and as that of infinity; below -126 the result is

@@ -6,8 +6,9 @@
 // Pieces of equal cost do not take equal time: SMs differ in their distance to the data, and no cost model knows every short
 // item.  With one piece per CTA the slowest CTA took 9 % (one long prompt) to 29 % (mixed batches) longer than the mean.
 // So a large batch can be cut twice: 148 pieces with 9/10 of the cost, 148 with the rest; a CTA begins with the piece of its
-// number and then takes the next one that nobody has.  Attention over eight packed prompts took 403 us with it, 410 us with one
-// piece each, 428 us with three sizes (7/10, 2/10, 1/10); 2048 tokens over 65536: 1880 to 1935, 1940, 1945 us.
+// number and then takes the next one that nobody has.  Attention with it, and with one piece each: eight packed prompts 366-372
+// and 371-375 us, mixed batch 1252 and 1265 us, prompt of 32768 8.37 and 8.43 ms; 2048 tokens over 65536 take 2.0 ms either way.
+// (Three sizes, 7/10, 2/10 and 1/10, were slower than one on an earlier build: 428 us where two took 403 and one 410.)
 //
 // A border is found by a search, because an item's cost has a closed form: every CTA makes one prefix sum over the
 // requests, and looks up the borders of the pieces that it takes or merges.  There is no planning kernel, and no table that

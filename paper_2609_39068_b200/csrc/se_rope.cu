@@ -14,9 +14,9 @@
 // head (the two halves of eight rotation pairs), a warp reads all 16 tokens before it computes, so 8 x 16 bytes per
 // lane are in flight.  The K warps fold min and max of what they wrote, and of the page's older keys, with shuffles.
 //
-// Bound by HBM for prompts: 24K tokens of 32 + 2 x 8 heads, D = 128, 121.5 us for 662 MB = 5.4 TB/s, 0.84 of a plain copy.  Small
-// calls are four dependent round trips: 64 single tokens 7.2 us.  (Loading the next rows while a row is turned, with the registers
-// that takes, was slower: 8.2 and 128.5 us.)
+// Bound by HBM for prompts: 24K tokens of 32 + 2 x 8 heads, D = 128, 122 us for 662 MB = 5.4 TB/s, 0.84 of a plain copy (124-125 us
+// as calls on changing inputs).  Small calls are four dependent round trips: 64 single tokens 7.7 us.  (Loading the next rows
+// while a row is turned, with the registers that takes, was slower: 8.2 us where 7.2 were taken, 128.5 us for 121.5.)
 #include <type_traits>
 
 #include "se_internal.h"
@@ -225,8 +225,8 @@ cudaError_t launch_rope_append(const se_params &p, const RopeCall &c, cudaStream
     // a request touches at most ceil((n + 15) / 16) pages
     const long long items = (long long)c.total_tokens / kPage + 2ll * p.B;
     const int sms = device_sm_count();
-    // 64 single tokens: 7.2 us with two CTAs per SM, 8.4 us with three; 24K tokens of prompts: 126.8 and 121.5 us.  (Until each
-    // CTA has several pages the latency of one counts.)
+    // Side by side, 64 single tokens: 7.2 us with two CTAs per SM, 8.4 us with three; 24K tokens of prompts: 126.8 and 121.5 us.
+    // (Until each CTA has several pages the latency of one counts.)
     const bool many = items > 8ll * sms;
     const long long cap = (many ? 3ll : 2ll) * sms;
     const unsigned grid = (unsigned)(items < cap ? items : cap);
