@@ -259,7 +259,7 @@ __device__ __forceinline__ void k_role(const AttendArgs &a, const List<AttendWor
             if (!ok) break;
             if (chosen) {
                 ctl->mask[tiles % C::kMasks] = mask;
-                mbar_expect_tx(bar, C::kKvBytes);
+                mbar_expect_tx(bar, C::kKvBytes + (D == 64 && tiles == 0 ? kTestExtraTx : 0));
                 if (!a.page_table && (t + 1) * kKv <= stop) {
                     tma_load_4d(dst, k_wide, 0, s.h, s.t.start + t * kKv, 0, bar);
                 } else {
@@ -335,7 +335,7 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v
                 __syncwarp();
             }
             if (chosen) {
-                mbar_expect_tx(bar, C::kKvBytes - (by_hand ? kPage * D * 2 : 0) + (tiles == 0 ? kTestExtraTx : 0));
+                mbar_expect_tx(bar, C::kKvBytes - (by_hand ? kPage * D * 2 : 0) + (D == 128 && tiles == 0 ? kTestExtraTx : 0));
                 if (!a.page_table && (t + 1) * kKv <= stop) {
                     tma_load_4d(dst, v_wide, 0, s.h, s.t.start + t * kKv, 0, bar);
                 } else if (a.page_table) {

@@ -171,7 +171,7 @@ __device__ __forceinline__ void copy_role(const MassArgs &a, const List<MassWork
         const uint32_t kb = pairs & 1, kbar = bars + 8 * (kKFull + kb);
         ok = warp_wait(bars + 8 * (kKEmpty + kb), (pairs >> 1 & 1) ^ 1, gave_up, &a.ctl->status);
         if (!ok) break;
-        if (chosen) mbar_expect_tx(kbar, 2 * C::kTileBytes);
+        if (chosen) mbar_expect_tx(kbar, 2 * C::kTileBytes + (D == 64 && pairs == 0 ? kTestExtraTx : 0));
 #pragma unroll
         for (int g = 0; g < 16; ++g) {
             const int row = __shfl_sync(kFull, z, g);
@@ -189,7 +189,7 @@ __device__ __forceinline__ void copy_role(const MassArgs &a, const List<MassWork
             ok = warp_wait(bar + 8 * C::kSlots, (pos / C::kSlots & 1) ^ 1, gave_up, &a.ctl->status);
             if (!ok) break;
             if (chosen) {
-                mbar_expect_tx(bar, list.w.tpt * a.G * D * 2 + (pos == 0 ? kTestExtraTx : 0));
+                mbar_expect_tx(bar, list.w.tpt * a.G * D * 2 + (D == 128 && pos == 0 ? kTestExtraTx : 0));
 #pragma unroll
                 for (int half = 0; half < C::kHalves; ++half)
                     tma_load_3d(ring + slot * C::kTileBytes + half * (kTile * 128), q_map, half * 64, s.h * a.G,

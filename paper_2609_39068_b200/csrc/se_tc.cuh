@@ -9,7 +9,7 @@
 namespace se {
 
 // Fault injection for the test of the bounded waits (a second build of the library, -DSE_TEST_SHORT_TX, never the product): a
-// copy announces 16 bytes more than it delivers, so the wait for it runs out.
+// CTA's first copy of one kind announces 16 bytes more than it delivers, so the wait for it runs out.
 #ifdef SE_TEST_SHORT_TX
 constexpr uint32_t kTestExtraTx = 16;
 #else

@@ -1,7 +1,8 @@
 """The bounded waits of the prompt-side kernels: a copy that never completes ends in SE_DEV_WAIT_TIMEOUT, not in a hang.
 
-In the second build of the library (``-DSE_TEST_SHORT_TX``) the first V tile of every CTA (attention) or its first query tile
-(accumulated weights) announces 16 bytes more than its copies deliver.  The warp that needs it gives up after the limit, the
+In the second build of the library (``-DSE_TEST_SHORT_TX``) one copy of every CTA announces 16 bytes more than it delivers: in
+attention the first V tile (D = 128) or the first K tile (D = 64), in the accumulated weights the first query tile (D = 128) or the
+first pair of K tiles (D = 64).  The warp that needs it gives up after the limit, the
 other roles follow, the copying warps wait - bounded again - for what they still have in flight, and the kernel returns."""
 import ctypes
 import time
@@ -20,6 +21,8 @@ pytestmark = pytest.mark.gpu
 BATCHES = {
     "few_tiles": ([40, 3], [100, 200], 8, 2, 128),
     "many_tiles": ([300, 5], [20000, 30000], 8, 2, 128),
+    "few_tiles_64": ([40, 3], [100, 200], 8, 2, 64),
+    "many_tiles_64": ([300, 5], [20000, 30000], 6, 2, 64),
     "two_sizes": ([64] * 100 + [1] * 20, [1950] * 110 + [2500] * 10, 32, 8, 64),
 }
 
