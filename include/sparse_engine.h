@@ -469,6 +469,46 @@ int se_h2o_accumulate(const se_params *p, const void *q, int64_t q_stride, int32
                       const int32_t *seq_lens, const float *lse, float *score_accum, void *workspace, void *stream);
 
 /*
+ * 8-bit cache.  (The paper has no counterpart: Appendix A fixes the attention that is computed, not the type that K and V
+ * are held in.)  The calls below read and write a cache of half the bytes:
+ *   k_cache, v_cache  [P_phys, H_kv, 16, D]  e4m3 codes (4 exponent bits, 3 mantissa bits, largest value 448)
+ *   scales            [P_phys, H_kv, 2]      fp32, of K and of V: value = code * scale
+ * A scale is a power of two, 2^-64 .. 2^7, so every value is exact in bf16: page summaries (meta) stay bf16, and
+ * se_page_select works on them as it does on those of a bf16 cache.  They take the workspace of the prompt calls
+ * (se_prompt_workspace_bytes).
+ */
+
+/*
+ * se_rope_append into an 8-bit cache: same arguments and rules, codes and scales in the place of the bf16 pages.  K is rotated
+ * and rounded to bf16 as se_rope_append does (k_out, if given, gets these), then for every touched page and kv-head, for K
+ * and V apart,
+ *     s = the smallest 2^e, -64 <= e <= 7, with max |x| <= 448 s over the page's new tokens; not below the page's scale so far,
+ *         if the page held tokens of the request before (what it holds of earlier owners does not count),
+ *     code = x / s rounded to the nearest code, ties to even; magnitudes above 448 s (57344 and more) become 448 s.
+ * Where the scale of a page grows, the codes of its older tokens are brought to it (code * s_old / s, rounded again: exact but
+ * for codes that become subnormal).  With meta != NULL the touched pages' summaries are the minimum and maximum of code * s
+ * over the page's tokens below seq_lens[r].  A page that receives tokens must appear once in the page table.
+ */
+int se_kv8_append(const se_params *p, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                  int64_t v_stride, int32_t total_tokens, const int32_t *cu_seqlens, const int32_t *seq_lens,
+                  const int32_t *page_table, const int32_t *positions, int32_t n_axes, const double *inv_freq,
+                  const int32_t *pair_axis, int32_t rot_dim, int32_t interleaved, void *q_out, void *k_out, void *k_cache,
+                  void *v_cache, float *scales, void *meta, void *workspace, void *stream);
+
+/*
+ * Attention of one token per request over an 8-bit cache (se_sparse_decode's equations): with sel_idx / sel_cnt over the pages
+ * that se_page_select left there ([B, H_kv, k_max], [B, H_kv]); with both NULL over every present page of the request (a dense
+ * layer; k_max is not used).  out fp32, lse fp32; scores, statistics and sums are fp32, each weight enters its product with V
+ * as two halves (22 significant bits).  No token (length 0, an empty selection, no present page): out = 0, lse = -inf.  Absent
+ * pages are left out; an entry of sel_idx outside the request is skipped and reported (SE_DEV_BAD_SELECTION), as is a sel_cnt
+ * above k_max (the first k_max entries count); a length outside 0 .. 16*max_pages is reported (SE_DEV_BAD_LENGTH).  Equal inputs
+ * give equal bits.
+ */
+int se_kv8_decode(const se_params *p, const void *q, const void *k_cache, const void *v_cache, const float *scales,
+                  const int32_t *page_table, const int32_t *seq_lens, const int32_t *sel_idx, const int32_t *sel_cnt,
+                  float *out, float *lse, void *workspace, void *stream);
+
+/*
  * Measurement aid (no counterpart in the paper): a read-only gather with the access pattern and
  * pipeline shape of the library's kernels and no arithmetic, to find what the memory system of a
  * given GPU allows for that pattern.  Piece i of the list lives at base + piece_idx[i]*piece_bytes

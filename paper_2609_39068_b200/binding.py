@@ -28,7 +28,7 @@ EXPORTS = ("se_version", "se_strerror", "se_workspace_bytes", "se_decode_num_spl
            "se_token_decode",
            "se_page_select_static", "se_decode_step", "se_decode_step_launches", "se_probe_gather",
            "se_prompt_workspace_bytes", "se_prompt_workspace_init", "se_rope_append", "se_chunk_attend",
-           "se_prompt_attend", "se_h2o_accumulate")
+           "se_prompt_attend", "se_h2o_accumulate", "se_kv8_append", "se_kv8_decode")
 SE_STATIC_SCRATCH_BYTES = 4 * 1024 * 1024
 
 
@@ -96,6 +96,8 @@ def load(build_if_missing: bool = True):
     lib.se_prompt_workspace_init.argtypes = [pp, vp, vp]
     lib.se_rope_append.argtypes = [pp, vp, i64, vp, i64, vp, i64, i32, i32p, i32p, i32p, i32p, i32, vp, i32p, i32, i32,
                                    vp, vp, vp, vp, vp, vp, vp]
+    lib.se_kv8_append.argtypes = lib.se_rope_append.argtypes[:-2] + [vp, vp, vp]
+    lib.se_kv8_decode.argtypes = [pp, vp, vp, vp, fp, i32p, i32p, i32p, i32p, fp, fp, vp, vp]
     lib.se_chunk_attend.argtypes = [pp, vp, i64, i32, i32p, vp, vp, i32p, i32p, vp, fp, vp, vp]
     lib.se_prompt_attend.argtypes = [pp, vp, i64, vp, i64, vp, i64, i32, i32p, vp, fp, vp, vp]
     lib.se_h2o_accumulate.argtypes = [pp, vp, i64, i32, i32p, vp, i32p, i32p, fp, fp, vp, vp]
@@ -104,7 +106,7 @@ def load(build_if_missing: bool = True):
                  "se_h2o_retain", "se_h2o_compact", "se_decode_num_splits", "se_page_select_static",
                  "se_observe_decode", "se_token_select", "se_token_decode", "se_page_select_scores",
                  "se_page_select_topk", "se_decode_step", "se_decode_step_launches", "se_prompt_workspace_init",
-                 "se_rope_append", "se_chunk_attend", "se_prompt_attend", "se_h2o_accumulate"):
+                 "se_rope_append", "se_chunk_attend", "se_prompt_attend", "se_h2o_accumulate", "se_kv8_append", "se_kv8_decode"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -410,10 +412,8 @@ def _call(entry: str, workspace: torch.Tensor, tensors, *args) -> None:
     _check(rc, entry)
 
 
-def se_rope_append(p, q, k, v, cu_seqlens, seq_lens, page_table, positions, inv_freq, pair_axis, q_out, k_cache,
-                   v_cache, workspace, meta=None, k_out=None, interleaved=False) -> None:
-    """``q``, ``k``, ``v`` may be views of one [T, H_q + 2*H_kv, D] projection output; rot_dim is twice the length of
-    ``inv_freq``; ``positions`` is [n_axes, T]."""
+def _append(entry, p, q, k, v, cu_seqlens, seq_lens, page_table, positions, inv_freq, pair_axis, q_out, k_cache, v_cache,
+            workspace, meta, k_out, interleaved, kind, scales) -> None:
     T, H_q, H_kv, D = q.shape[0], p.H_q, p.H_kv, p.D
     axes, pairs = positions.shape[0], inv_freq.numel()
     _prompt_common(p, workspace, cu_seqlens, page_table, seq_lens, k_cache, v_cache)
@@ -428,12 +428,21 @@ def se_rope_append(p, q, k, v, cu_seqlens, seq_lens, page_table, positions, inv_
     if T == 0:           # an empty tensor has no address
         return
     i32, bf16 = torch.int32, torch.bfloat16
-    _call("se_rope_append", workspace, (q, k, v, cu_seqlens, seq_lens, page_table, positions, inv_freq, pair_axis, q_out, k_cache,
-                                        v_cache, meta, k_out),
+    _call(entry, workspace, (q, k, v, cu_seqlens, seq_lens, page_table, positions, inv_freq, pair_axis, q_out, k_cache, v_cache, meta,
+                             k_out) + scales,
           ctypes.byref(p), qp, qs, kp, ks, vp_, vs, T, _ptr(cu_seqlens, i32, "cu_seqlens"), _ptr(seq_lens, i32, "seq_lens"),
           _ptr(page_table, i32, "page_table"), _ptr(positions, i32, "positions"), axes, _ptr(inv_freq, torch.float64, "inv_freq"),
           _ptr(pair_axis, i32, "pair_axis"), 2 * pairs, int(bool(interleaved)), _ptr(q_out, bf16, "q_out"),
-          _ptr(k_out, bf16, "k_out"), _ptr(k_cache, bf16, "k_cache"), _ptr(v_cache, bf16, "v_cache"), _ptr(meta, bf16, "meta"))
+          _ptr(k_out, bf16, "k_out"), _ptr(k_cache, kind, "k_cache"), _ptr(v_cache, kind, "v_cache"),
+          *[_ptr(t, torch.float32, "scales") for t in scales], _ptr(meta, bf16, "meta"))
+
+
+def se_rope_append(p, q, k, v, cu_seqlens, seq_lens, page_table, positions, inv_freq, pair_axis, q_out, k_cache,
+                   v_cache, workspace, meta=None, k_out=None, interleaved=False) -> None:
+    """``q``, ``k``, ``v`` may be views of one [T, H_q + 2*H_kv, D] projection output; rot_dim is twice the length of
+    ``inv_freq``; ``positions`` is [n_axes, T]."""
+    _append("se_rope_append", p, q, k, v, cu_seqlens, seq_lens, page_table, positions, inv_freq, pair_axis, q_out, k_cache, v_cache,
+            workspace, meta, k_out, interleaved, torch.bfloat16, ())
 
 
 def se_chunk_attend(p, q, cu_seqlens, k_cache, v_cache, page_table, seq_lens, out, workspace, lse=None) -> None:
@@ -482,6 +491,33 @@ def se_h2o_accumulate(p, q, cu_seqlens, k_cache, page_table, seq_lens, lse, scor
           ctypes.byref(p), qp, qs, T, _ptr(cu_seqlens, i32, "cu_seqlens"), _ptr(k_cache, torch.bfloat16, "k_cache"),
           _ptr(page_table, i32, "page_table"), _ptr(seq_lens, i32, "seq_lens"), _ptr(lse, torch.float32, "lse"),
           _ptr(score_accum, torch.float32, "score_accum"))
+
+
+# ---- 8-bit cache: e4m3 codes, a power-of-two scale for each (page, kv-head) of K and of V -------------
+
+def se_kv8_append(p, q, k, v, cu_seqlens, seq_lens, page_table, positions, inv_freq, pair_axis, q_out, k_cache, v_cache,
+                  scales, workspace, meta=None, k_out=None, interleaved=False) -> None:
+    """``se_rope_append`` into an 8-bit cache: ``k_cache``, ``v_cache`` are torch.float8_e4m3fn, ``scales`` [P, H_kv, 2] fp32."""
+    _shape(scales, (p.num_phys_pages, p.H_kv, 2), "scales")
+    _append("se_kv8_append", p, q, k, v, cu_seqlens, seq_lens, page_table, positions, inv_freq, pair_axis, q_out, k_cache, v_cache,
+            workspace, meta, k_out, interleaved, torch.float8_e4m3fn, (scales,))
+
+
+def se_kv8_decode(p, q, k_cache, v_cache, scales, page_table, seq_lens, out, lse, workspace, sel_idx=None, sel_cnt=None) -> None:
+    """One token per request over an 8-bit cache: the selected pages, or all present ones where ``sel_idx`` is None."""
+    B, H_q, D = p.B, p.H_q, p.D
+    _prompt_common(p, workspace, None, page_table, seq_lens, k_cache, v_cache)
+    _shape(q, (B, H_q, D), "q")
+    _shape(scales, (p.num_phys_pages, p.H_kv, 2), "scales")
+    _shape(out, (B, H_q, D), "out")
+    _shape(lse, (B, H_q), "lse")
+    _shape(sel_idx, (B, p.H_kv, p.k_max), "sel_idx")
+    _shape(sel_cnt, (B, p.H_kv), "sel_cnt")
+    i32, f32, codes = torch.int32, torch.float32, torch.float8_e4m3fn
+    _call("se_kv8_decode", workspace, (q, k_cache, v_cache, scales, page_table, seq_lens, out, lse, sel_idx, sel_cnt),
+          ctypes.byref(p), _ptr(q, torch.bfloat16, "q"), _ptr(k_cache, codes, "k_cache"), _ptr(v_cache, codes, "v_cache"),
+          _ptr(scales, f32, "scales"), _ptr(page_table, i32, "page_table"), _ptr(seq_lens, i32, "seq_lens"), _ptr(sel_idx, i32, "sel_idx"),
+          _ptr(sel_cnt, i32, "sel_cnt"), _ptr(out, f32, "out"), _ptr(lse, f32, "lse"))
 
 
 def se_last_device_status(workspace) -> int:

@@ -450,11 +450,11 @@ int se_prompt_workspace_init(const se_params *p, void *workspace, void *stream) 
     return e == cudaSuccess ? SE_OK : SE_ERR_CUDA;
 }
 
-int se_rope_append(const se_params *p, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+static int rope_append(const se_params *p, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                    const void *v, int64_t v_stride, int32_t total_tokens, const int32_t *cu_seqlens,
                    const int32_t *seq_lens, const int32_t *page_table, const int32_t *positions, int32_t n_axes,
                    const double *inv_freq, const int32_t *pair_axis, int32_t rot_dim, int32_t interleaved,
-                   void *q_out, void *k_out, void *k_cache, void *v_cache, void *meta, void *workspace,
+                   void *q_out, void *k_out, void *k_cache, void *v_cache, float *scales, void *meta, void *workspace,
                    void *stream) {
     int rc = validate(p);
     if (rc != SE_OK) return rc;
@@ -477,10 +477,21 @@ int se_rope_append(const se_params *p, const void *q, int64_t q_stride, const vo
     c.total_tokens = total_tokens, c.n_axes = n_axes, c.rot_dim = rot_dim, c.interleaved = interleaved != 0;
     c.cu_seqlens = cu_seqlens, c.seq_lens = seq_lens, c.page_table = page_table, c.positions = positions;
     c.pair_axis = pair_axis, c.inv_freq = inv_freq;
-    c.q_out = q_out, c.k_out = k_out, c.k_cache = k_cache, c.v_cache = v_cache, c.meta = meta;
+    c.q_out = q_out, c.k_out = k_out, c.k_cache = k_cache, c.v_cache = v_cache, c.scales = scales, c.meta = meta;
     c.status = static_cast<uint32_t *>(workspace);
     cudaError_t e = launch_rope_append(*p, c, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? SE_OK : SE_ERR_CUDA;
+}
+
+int se_rope_append(const se_params *p, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                   const void *v, int64_t v_stride, int32_t total_tokens, const int32_t *cu_seqlens,
+                   const int32_t *seq_lens, const int32_t *page_table, const int32_t *positions, int32_t n_axes,
+                   const double *inv_freq, const int32_t *pair_axis, int32_t rot_dim, int32_t interleaved,
+                   void *q_out, void *k_out, void *k_cache, void *v_cache, void *meta, void *workspace,
+                   void *stream) {
+    return rope_append(p, q, q_stride, k, k_stride, v, v_stride, total_tokens, cu_seqlens, seq_lens, page_table, positions,
+                       n_axes, inv_freq, pair_axis, rot_dim, interleaved, q_out, k_out, k_cache, v_cache, nullptr, meta,
+                       workspace, stream);
 }
 
 int se_chunk_attend(const se_params *p, const void *q, int64_t q_stride, int32_t total_tokens,
@@ -542,6 +553,40 @@ int se_h2o_accumulate(const se_params *p, const void *q, int64_t q_stride, int32
     c.cu_seqlens = cu_seqlens, c.seq_lens = seq_lens, c.page_table = page_table;
     c.lse = const_cast<float *>(lse), c.workspace = static_cast<uint8_t *>(workspace);
     cudaError_t e = launch_h2o_accumulate(*p, c, score_accum, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? SE_OK : SE_ERR_CUDA;
+}
+
+// ---- 8-bit cache ----
+int se_kv8_append(const se_params *p, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                  int64_t v_stride, int32_t total_tokens, const int32_t *cu_seqlens, const int32_t *seq_lens,
+                  const int32_t *page_table, const int32_t *positions, int32_t n_axes, const double *inv_freq,
+                  const int32_t *pair_axis, int32_t rot_dim, int32_t interleaved, void *q_out, void *k_out, void *k_cache,
+                  void *v_cache, float *scales, void *meta, void *workspace, void *stream) {
+    int rc = validate(p);
+    if (rc != SE_OK) return rc;
+    if (!scales) return SE_ERR_NULL_POINTER;
+    if (!aligned16(scales)) return SE_ERR_MISALIGNED;
+    return rope_append(p, q, q_stride, k, k_stride, v, v_stride, total_tokens, cu_seqlens, seq_lens, page_table, positions,
+                       n_axes, inv_freq, pair_axis, rot_dim, interleaved, q_out, k_out, k_cache, v_cache, scales, meta,
+                       workspace, stream);
+}
+
+int se_kv8_decode(const se_params *p, const void *q, const void *k_cache, const void *v_cache, const float *scales,
+                  const int32_t *page_table, const int32_t *seq_lens, const int32_t *sel_idx, const int32_t *sel_cnt,
+                  float *out, float *lse, void *workspace, void *stream) {
+    int rc = validate(p);
+    if (rc != SE_OK) return rc;
+    if (!q || !k_cache || !v_cache || !scales || !page_table || !seq_lens || !out || !lse || !workspace ||
+        (sel_idx == nullptr) != (sel_cnt == nullptr))
+        return SE_ERR_NULL_POINTER;
+    if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(scales) || !aligned16(page_table) ||
+        !aligned16(seq_lens) || !aligned16(sel_idx) || !aligned16(sel_cnt) || !aligned16(out) || !aligned16(lse) ||
+        !aligned16(workspace))
+        return SE_ERR_MISALIGNED;
+    Kv8DecodeCall c = {};
+    c.q = q, c.k_cache = k_cache, c.v_cache = v_cache, c.scales = scales, c.page_table = page_table, c.seq_lens = seq_lens;
+    c.sel_idx = sel_idx, c.sel_cnt = sel_cnt, c.out = out, c.lse = lse, c.workspace = static_cast<uint8_t *>(workspace);
+    cudaError_t e = launch_kv8_decode(*p, c, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? SE_OK : SE_ERR_CUDA;
 }
 

@@ -91,6 +91,7 @@ struct RopeCall {
     const int32_t *cu_seqlens, *seq_lens, *page_table, *positions, *pair_axis;
     const double *inv_freq;
     void *q_out, *k_out, *k_cache, *v_cache, *meta;
+    float *scales;                               // nullptr: k_cache, v_cache are bf16; otherwise e4m3 codes with these scales
     uint32_t *status;
 };
 cudaError_t launch_rope_append(const se_params &p, const RopeCall &c, cudaStream_t stream);
@@ -108,6 +109,16 @@ struct AttendCall {
 cudaError_t launch_prompt_attend(const se_params &p, const AttendCall &c, cudaStream_t stream);
 // score_accum += the queries' weights on every cached token (k, lse of `c` are read, v and out are not used)
 cudaError_t launch_h2o_accumulate(const se_params &p, const AttendCall &c, float *score_accum, cudaStream_t stream);
+
+// 8-bit cache: attention of one token per request over the selected pages (sel_idx nullptr: all pages)
+struct Kv8DecodeCall {
+    const void *q, *k_cache, *v_cache;
+    const float *scales;
+    const int32_t *page_table, *seq_lens, *sel_idx, *sel_cnt;
+    float *out, *lse;
+    uint8_t *workspace;
+};
+cudaError_t launch_kv8_decode(const se_params &p, const Kv8DecodeCall &c, cudaStream_t stream);
 size_t prompt_workspace_bytes(const se_params &p);
 size_t prompt_workspace_control_bytes();
 

@@ -1,0 +1,527 @@
+// Attention of one token per request over an 8-bit paged cache (Appendix A, "Attention over Selected Positions", with K and V
+// held as e4m3 codes with a power-of-two scale per page and kv-head): over the pages of a selection, or over all present pages.
+//
+// Mathematics.  For a page with scales s_K, s_V and codes c:  z_j = sm_scale s_K (q . c_j),  out = sum_j p_j s_V c_j / sum_j p_j,
+// p_j = 2^(z_j log2 e - m).  The scales stay outside of the products, once per page: s_K multiplies 16 logits per head, s_V the
+// page's sum of p_j c_j.  The products run on mma.sync with halves, because a code is a half exactly:
+//   q     is brought to a maximum of 2^13..2^14 per head by a power of two; its 8 significant bits fit a half for everything
+//         above 2^-30 of the maximum, so nothing that fp32 sums could show is lost
+//   p_j   enters as two halves, p = hi + lo (22 bits), as the output is fp32.
+//
+// What bounds it: HBM, 2 * 2 * D bytes per token and kv-head and a few cycles of everything else: per page and head at D = 128
+// 64 conversions of two codes, 24 matrix instructions, 32 fp32 FMAs per warp.
+//
+// Split.  The list of all (request, kv-head) pairs' pages is cut into 148 runs of equal length, one per CTA; a CTA's pages go
+// round its eight warps, each of which keeps a ring of pages in flight (tensor copies, 128-byte swizzle) across the borders of
+// pairs.  At the end of a pair's run the warps merge through shared memory; a pair that several CTAs share leaves partial
+// results in the workspace, and the CTA that arrives last merges them in order.
+#include <math.h>
+
+#include "se_internal.h"
+#include "se_kv8.cuh"
+#include "se_pieces.cuh"
+
+namespace se {
+
+namespace {
+
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kChunks = 2048;          // prefix sums that a CTA keeps: of every pair, or of runs of pairs
+constexpr float kSlack = 8.f;          // the running maximum may lag: weights up to 2^8 stay far inside a half's range
+
+template <int D>
+struct Cfg {
+    static constexpr int kPageBytes = kPage * D;                    // of K or of V, one head
+    static constexpr int kStages = D == 128 ? 5 : 8;
+    static constexpr int kRowsPerPage = kPageBytes / 128;
+    static constexpr int kTiles = D / 16;                           // 16-channel tiles of the output
+    static constexpr int kPitch = D + 4;                            // floats of a head's row in the merge buffer
+    static constexpr int kPartFloats = 8 * D + 16;                  // a partial result: O, m, l
+    static constexpr size_t kRing = (size_t)kWarps * kStages * 2 * kPageBytes;
+    static constexpr size_t kSmem = kRing + (size_t)kWarps * (8 * kPitch + 16) * 4 + (kChunks + 1) * 8 + kWarps * kStages * 8 + 64 * 4;
+};
+
+struct Args {
+    const uint16_t *q;
+    const float2 *scales;
+    const int32_t *page_table, *seq_lens, *sel_idx, *sel_cnt;
+    float *out, *lse, *partials;
+    PromptControl *ctl;
+    int B, H_q, H_kv, G, max_pages, P_phys, k_max;
+    float scale_log2;
+};
+
+// D(16x8, fp32) += A(16x16, half, row) * B(16x8, half, col)
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t at) {
+    uint2 v;
+    asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ uint32_t pack_half2(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ float2 unpack_half2(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
+
+// ---- the list of pages: pairs (request, kv-head) in order, each with its pages ---------
+struct Pairs {
+    const Args &a;
+    const long long *pre;              // shared: pages before each chunk of `per` pairs, [chunks + 1]
+    int per, chunks;
+
+    __device__ __forceinline__ int pages_of(int r) const {
+        const int len = a.seq_lens[r];
+        return len < 0 || len > a.max_pages * kPage ? 0 : (len + kPage - 1) / kPage;
+    }
+    __device__ __forceinline__ int count(int pair) const {
+        if (!a.sel_cnt) return pages_of(pair / a.H_kv);
+        return min(max(a.sel_cnt[pair], 0), a.k_max);
+    }
+    // the pair that holds page u of the list, and its first page
+    __device__ __forceinline__ int find(long long u, long long &first) const {
+        int lo = 0, hi = chunks;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (pre[mid] <= u) lo = mid; else hi = mid;
+        }
+        first = pre[lo];
+        int x = lo * per;
+        if (per > 1)
+            for (int n = count(x); first + n <= u; n = count(++x)) first += n;
+        return x;
+    }
+    __device__ __forceinline__ int count_known(int pair) const { return per > 1 ? count(pair) : (int)(pre[pair + 1] - pre[pair]); }
+};
+
+// what a lane knows of one page of its warp
+struct Page {
+    int row;                           // page * H_kv + head, -1: not present
+    int tokens;                        // below the request's length, 1..16
+    float2 scale;
+};
+__device__ __forceinline__ Page look_up(const Args &a, const Pairs &ps, long long u0, int n, int i) {
+    Page p = {-1, 0, make_float2(0.f, 0.f)};
+    if (i >= n) return p;
+    long long first;
+    const int pair = ps.find(u0 + i, first);
+    const int r = pair / a.H_kv, h = pair - r * a.H_kv;
+    int b = (int)(u0 + i - first);
+    const int len = a.seq_lens[r];
+    if (a.sel_idx) {
+        b = a.sel_idx[(size_t)pair * a.k_max + b];
+        if (b < 0 || b >= a.max_pages || b * kPage >= len) {
+            atomicOr(&a.ctl->status, SE_DEV_BAD_SELECTION);
+            return p;
+        }
+    }
+    const int pid = a.page_table[(size_t)r * a.max_pages + b];
+    if (pid >= a.P_phys) atomicOr(&a.ctl->status, SE_DEV_BAD_PAGE_ID);
+    if (pid < 0 || pid >= a.P_phys) return p;
+    p.row = pid * a.H_kv + h;
+    p.tokens = min(kPage, len - b * kPage);
+    p.scale = a.scales[p.row];
+    return p;
+}
+
+template <int D>
+__device__ __forceinline__ void load_q(const Args &a, int pair, int g, int t, uint4 (&raw)[D / 32]) {
+    const int r = pair / a.H_kv, h = pair - r * a.H_kv;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+        const uint4 *src = reinterpret_cast<const uint4 *>(a.q + ((size_t)r * a.H_q + h * a.G + min(g, a.G - 1)) * D + 64 * i + 16 * t);
+        raw[2 * i] = src[0], raw[2 * i + 1] = src[1];
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const __grid_constant__ Args a) {
+    using C = Cfg<D>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    float *s_merge = reinterpret_cast<float *>(smem + C::kRing);                        // [warp][8][kPitch], then m and l
+    long long *s_pre = reinterpret_cast<long long *>(s_merge + kWarps * (8 * C::kPitch + 16));
+    uint64_t *s_bars = reinterpret_cast<uint64_t *>(s_pre + kChunks + 1);
+    int *s_misc = reinterpret_cast<int *>(s_bars + kWarps * C::kStages);                // sums of a scan, verdict of a merge
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const uint32_t ring = smem_u32(smem) + warp * (C::kStages * 2 * C::kPageBytes);
+    const uint32_t bars = smem_u32(s_bars) + warp * (C::kStages * 8);
+
+    if ((smem_u32(smem) & 1023u) || *(volatile uint32_t *)&a.ctl->needs_init) {         // the swizzle pattern hangs on the address
+        if (tid == 0 && blockIdx.x == 0) atomicOr(&a.ctl->status, SE_DEV_WAIT_TIMEOUT);
+        return;
+    }
+    if (lane < C::kStages) mbar_init(bars + 8 * lane, 1);
+    if (tid == 0) prefetch_map(&k_map), prefetch_map(&v_map);
+    mbar_fence_init();
+
+    // pages before every pair (or every run of pairs, where there are more than 2048)
+    const int pairs = a.B * a.H_kv;
+    Pairs ps = {a, s_pre, (pairs + kChunks - 1) / kChunks, 0};
+    ps.chunks = (pairs + ps.per - 1) / ps.per;
+    {
+        const int each = (ps.chunks + kThreads - 1) / kThreads;
+        const int c0 = min(tid * each, ps.chunks), c1 = min(c0 + each, ps.chunks);
+        long long sum = 0;
+        for (int c = c0; c < c1; ++c) {
+            s_pre[c] = sum;
+            for (int x = c * ps.per; x < min((c + 1) * ps.per, pairs); ++x) {
+                if (blockIdx.x == 0) {
+                    const int len = a.seq_lens[x / a.H_kv];
+                    if (len < 0 || len > a.max_pages * kPage) atomicOr(&a.ctl->status, SE_DEV_BAD_LENGTH);
+                    if (a.sel_cnt && (a.sel_cnt[x] < 0 || a.sel_cnt[x] > a.k_max)) atomicOr(&a.ctl->status, SE_DEV_BAD_SELECTION);
+                }
+                sum += ps.count(x);
+            }
+        }
+        long long inc = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long x = __shfl_up_sync(kFull, inc, o);
+            if (lane >= o) inc += x;
+        }
+        long long *tot = reinterpret_cast<long long *>(s_misc);
+        if (lane == 31) tot[warp] = inc;
+        __syncthreads();
+        long long before = inc - sum;
+        for (int w = 0; w < warp; ++w) before += tot[w];
+        for (int c = c0; c < c1; ++c) s_pre[c] += before;
+        if (tid == kThreads - 1) s_pre[ps.chunks] = before + sum;
+        __syncthreads();
+    }
+    // pairs without a page
+    for (int x0 = blockIdx.x * 32 + warp * 32 * gridDim.x; x0 < pairs; x0 += 32 * kWarps * gridDim.x) {
+        unsigned none = __ballot_sync(kFull, x0 + lane < pairs && ps.count_known(min(x0 + lane, pairs - 1)) == 0);
+        for (; none; none &= none - 1) {
+            const int x = x0 + __ffs(none) - 1;
+            const size_t row = (size_t)(x / a.H_kv) * a.H_q + x % a.H_kv * a.G;
+            for (int e = lane; e < a.G * D; e += 32) a.out[row * D + e] = 0.f;
+            if (lane < a.G) a.lse[row + lane] = -INFINITY;
+        }
+    }
+
+    const long long total = s_pre[ps.chunks];
+    const long long size = max((total + gridDim.x - 1) / gridDim.x, (long long)kWarps);  // pages of a CTA: a warp has one at least
+    const long long u0 = size * blockIdx.x;
+    if (u0 >= total) return;
+    const int n = (int)min(size, total - u0);
+    const int mine = n > warp ? (n - warp + kWarps - 1) / kWarps : 0;                    // page k of the warp is page k * kWarps + warp
+    Page now = look_up(a, ps, u0, n, lane * kWarps + warp), next = look_up(a, ps, u0, n, (32 + lane) * kWarps + warp);
+    int block = 0, issue = 0;          // block of 32 pages that `now` describes; next page to be fetched
+    uint32_t sent = 0, used = 0;       // pages fetched, pages consumed
+    bool ok = true;
+    const bool chosen = elect_one();
+    auto send = [&] {
+        while (ok && issue < mine && sent - used < C::kStages && issue < (block + 2) * 32) {
+            const int row = __shfl_sync(kFull, issue / 32 == block ? now.row : next.row, issue & 31);
+            if (row >= 0) {
+                if (chosen) {
+                    const uint32_t slot = sent % C::kStages, dst = ring + slot * (2 * C::kPageBytes);
+                    mbar_expect_tx(bars + 8 * slot, 2 * C::kPageBytes + (sent == 0 ? kTestExtraTx : 0));
+                    tma_load_2d(dst, &k_map, 0, row * C::kRowsPerPage, bars + 8 * slot);
+                    tma_load_2d(dst + C::kPageBytes, &v_map, 0, row * C::kRowsPerPage, bars + 8 * slot);
+                }
+                __syncwarp();
+                ++sent;
+            }
+            ++issue;
+        }
+    };
+    send();
+
+    long long first;
+    int pair = ps.find(u0, first);
+    uint4 raw[D / 32];
+    load_q<D>(a, pair, g, t, raw);
+    int k = 0;
+    for (int done = 0; done < n;) {
+        const int pages = ps.count_known(pair);
+        const int stop = (int)min((long long)n, first + pages - u0);                     // end of the pair's pages in the CTA
+        // q as halves: head g, channels 64 i + 16 t .. + 15
+        uint32_t qh[D / 8];
+        float f0, f1;                  // heads 2 t and 2 t + 1: logit in powers of two = sum * f * s_K
+        {
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) top = bmax2(top, largest8(raw[i]));
+            top = max(top & 0xffffu, top >> 16);
+            top = max(top, __shfl_xor_sync(kFull, top, 1));
+            top = max(top, __shfl_xor_sync(kFull, top, 2));
+            const int e = max((int)(top >> 7), 20);                                      // maximum 1.x * 2^(e - 127)
+            const float up = __uint_as_float((uint32_t)(140 - e + 127) << 23);           // 2^(140 - e)
+            const float down = __uint_as_float((uint32_t)(e - 140 + 127) << 23);
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float2 x = bf16x2_to_f2(w[j]);
+                    qh[4 * i + j] = g < a.G ? pack_half2(x.x * up, x.y * up) : 0u;
+                }
+            }
+            const float f = down * a.scale_log2;
+            f0 = __shfl_sync(kFull, f, 8 * t), f1 = __shfl_sync(kFull, f, 8 * t + 4);
+        }
+        float acc[C::kTiles][4];
+#pragma unroll
+        for (int i = 0; i < C::kTiles; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+        float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+
+        for (; k < mine && k * kWarps + warp < stop; ++k) {
+            if (k / 32 != block) {
+                ++block;
+                now = next;
+                next = look_up(a, ps, u0, n, ((block + 1) * 32 + lane) * kWarps + warp);
+                send();
+            }
+            const int row = __shfl_sync(kFull, now.row, k & 31);
+            if (row < 0) continue;
+            const int tokens = __shfl_sync(kFull, now.tokens, k & 31);
+            const float sk = __shfl_sync(kFull, now.scale.x, k & 31), sv = __shfl_sync(kFull, now.scale.y, k & 31);
+            const uint32_t slot = used % C::kStages, at = ring + slot * (2 * C::kPageBytes);
+            if (ok && !__all_sync(kFull, mbar_wait(bars + 8 * slot, used / C::kStages & 1))) {
+                ok = false;
+                if (lane == 0) atomicOr(&a.ctl->status, SE_DEV_WAIT_TIMEOUT);
+            }
+            if (!ok) continue;
+            // ---- logits: rows are tokens, columns are heads.  Row x of the product is token x for even x, x ^ 4 for odd x (and the
+            // same 8 further on): with the swizzle, lanes that load at the same time then never meet in a bank, here and for V.
+            const int tok = g & 1 ? g ^ 4 : g;
+            float c[2][4] = {};
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) {
+                uint4 x, y;
+                if constexpr (D == 128) {
+                    const uint32_t off = at + tok * 128 + (((t + 4 * i) ^ tok) << 4);
+                    x = lds128(off), y = lds128(off + 1024);
+                } else {
+                    const uint32_t line = tok >> 1, off = (((tok & 1) * 4 + t) ^ line) << 4;
+                    x = lds128(at + line * 128 + off), y = lds128(at + 512 + line * 128 + (off ^ 64));
+                }
+                const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+                    mma_f16(c[s & 1], half2_of_e4m3x2(xw[s] & 0xffffu), half2_of_e4m3x2(yw[s] & 0xffffu), half2_of_e4m3x2(xw[s] >> 16),
+                            half2_of_e4m3x2(yw[s] >> 16), qh[8 * i + 2 * s], qh[8 * i + 2 * s + 1]);
+            }
+            const float g0 = fmaxf(f0 * sk, 1e-37f), g1 = fmaxf(f1 * sk, 1e-37f);        // (0 times a masked logit would be NaN)
+            float z[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[e] = c[0][e] + c[1][e];
+            if (tokens < kPage) {
+                if (tok >= tokens) z[0] = z[1] = -INFINITY;
+                if (tok + 8 >= tokens) z[2] = z[3] = -INFINITY;
+            }
+            const float t0 = fmaxf(z[0], z[2]) * g0, t1 = fmaxf(z[1], z[3]) * g1;
+            if (__any_sync(kFull, t0 > m0 + kSlack || t1 > m1 + kSlack)) {
+                float n0 = fmaxf(m0, t0), n1 = fmaxf(m1, t1);
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) {
+                    n0 = fmaxf(n0, __shfl_xor_sync(kFull, n0, o));
+                    n1 = fmaxf(n1, __shfl_xor_sync(kFull, n1, o));
+                }
+                const float r0 = ex2(m0 - n0), r1 = ex2(m1 - n1);                        // (a page has a token, so n is a number)
+                m0 = n0, m1 = n1;
+                l0 *= r0, l1 *= r1;
+#pragma unroll
+                for (int i = 0; i < C::kTiles; ++i) acc[i][0] *= r0, acc[i][1] *= r1, acc[i][2] *= r0, acc[i][3] *= r1;
+            }
+            const float p0 = ex2(fmaf(z[0], g0, -m0)), p1 = ex2(fmaf(z[1], g1, -m1));
+            const float p2 = ex2(fmaf(z[2], g0, -m0)), p3 = ex2(fmaf(z[3], g1, -m1));
+            l0 += p0 + p2, l1 += p1 + p3;
+            // weights as hi + lo, two halves; transposed, they are the second operand: rows tokens, columns heads
+            const uint32_t h0 = pack_half2(p0, p1), h1 = pack_half2(p2, p3);
+            const float2 u = unpack_half2(h0), w = unpack_half2(h1);
+            const uint32_t b0 = transpose8x8(h0), b1 = transpose8x8(h1);
+            const uint32_t e0 = transpose8x8(pack_half2(p0 - u.x, p1 - u.y)), e1 = transpose8x8(pack_half2(p2 - w.x, p3 - w.y));
+            // ---- output: rows are channels, columns are heads
+            uint32_t va[D / 32], vb[D / 32], vc[D / 32], vd[D / 32];                     // tokens of columns 2 t, 2 t + 1, and 8 further on
+            const int ta = 2 * t, tb = (2 * t + 1) ^ 4;
+            auto fetch = [&](int tk, uint32_t (&dst)[D / 32]) {
+                if constexpr (D == 128) {
+                    const uint4 x = lds128(at + C::kPageBytes + tk * 128 + ((g ^ (tk & 7)) << 4));
+                    dst[0] = x.x, dst[1] = x.y, dst[2] = x.z, dst[3] = x.w;
+                } else {
+                    const uint32_t line = tk >> 1;
+                    const uint2 x = lds64(at + C::kPageBytes + line * 128 + ((((tk & 1) * 4 + (g >> 1)) ^ line) << 4) + (g & 1) * 8);
+                    dst[0] = x.x, dst[1] = x.y;
+                }
+            };
+            fetch(ta, va), fetch(tb, vb), fetch(ta + 8, vc), fetch(tb + 8, vd);
+            __syncwarp();
+            ++used;                    // the page's bytes are in registers: its slot may be filled again
+            send();
+            if (tokens < kPage) {      // what lies behind the end may be anything, and a weight of zero would not hide a NaN
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j) {
+                    if (ta >= tokens) va[j] = 0;
+                    if (tb >= tokens) vb[j] = 0;
+                    if (ta + 8 >= tokens) vc[j] = 0;
+                    if (tb + 8 >= tokens) vd[j] = 0;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < C::kTiles; ++i) {                                        // rows g, g + 8: channels (D / 8) g + 2 i, + 1
+                const uint32_t sel = i & 1 ? 0x7362u : 0x5140u;
+                const uint32_t x = __byte_perm(va[i / 2], vb[i / 2], sel), y = __byte_perm(vc[i / 2], vd[i / 2], sel);
+                const uint32_t a0 = half2_of_e4m3x2(x & 0xffffu), a1 = half2_of_e4m3x2(x >> 16);
+                const uint32_t a2 = half2_of_e4m3x2(y & 0xffffu), a3 = half2_of_e4m3x2(y >> 16);
+                float o[4] = {};
+                mma_f16(o, a0, a1, a2, a3, e0, e1);
+                mma_f16(o, a0, a1, a2, a3, b0, b1);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][e] = fmaf(o[e], sv, acc[i][e]);
+            }
+        }
+
+        // ---- end of the pair's pages in this CTA ----
+        const bool more = stop < n;
+        int after = pair;
+        long long after_first = first + pages;
+        if (more) {
+            while (ps.count_known(++after) == 0) {}
+            load_q<D>(a, after, g, t, raw);
+        }
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l0 += __shfl_xor_sync(kFull, l0, o), l1 += __shfl_xor_sync(kFull, l1, o);
+        float *own = s_merge + warp * (8 * C::kPitch + 16);
+        if (g == 0) own[8 * C::kPitch + 2 * t] = m0, own[8 * C::kPitch + 2 * t + 1] = m1, own[8 * C::kPitch + 8 + 2 * t] = l0, own[8 * C::kPitch + 9 + 2 * t] = l1;
+#pragma unroll
+        for (int j = 0; j < C::kTiles / 2; ++j) {
+            const int ch = (D / 8) * g + 4 * j;
+            *reinterpret_cast<float4 *>(own + (2 * t) * C::kPitch + ch) = make_float4(acc[2 * j][0], acc[2 * j][2], acc[2 * j + 1][0], acc[2 * j + 1][2]);
+            *reinterpret_cast<float4 *>(own + (2 * t + 1) * C::kPitch + ch) = make_float4(acc[2 * j][1], acc[2 * j][3], acc[2 * j + 1][1], acc[2 * j + 1][3]);
+        }
+        __syncthreads();
+        const int c0 = (int)(first / size), c1 = (int)((first + pages - 1) / size);      // CTAs that share the pair
+        const int r = pair / a.H_kv, h = pair - r * a.H_kv;
+        const size_t row0 = (size_t)r * a.H_q + h * a.G;
+        float *part = a.partials + (size_t)(blockIdx.x * 2 + (c0 == (int)blockIdx.x ? 1 : 0)) * C::kPartFloats;
+        for (int e = tid; e < a.G * (D / 4); e += kThreads) {
+            const int head = e / (D / 4), ch = e % (D / 4) * 4;
+            float M = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_merge[w * (8 * C::kPitch + 16) + 8 * C::kPitch + head]);
+            const float ref = M == -INFINITY ? 0.f : M;
+            float L = 0.f;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float *src = s_merge + w * (8 * C::kPitch + 16);
+                const float x = ex2(src[8 * C::kPitch + head] - ref);
+                L = fmaf(x, src[8 * C::kPitch + 8 + head], L);
+                const float4 v = *reinterpret_cast<const float4 *>(src + head * C::kPitch + ch);
+                o.x = fmaf(x, v.x, o.x), o.y = fmaf(x, v.y, o.y), o.z = fmaf(x, v.z, o.z), o.w = fmaf(x, v.w, o.w);
+            }
+            if (c0 == c1) {
+                const float inv = L == 0.f ? 0.f : 1.f / L;
+                *reinterpret_cast<float4 *>(a.out + (row0 + head) * D + ch) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+                if (ch == 0) a.lse[row0 + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+            } else {
+                __stcg(reinterpret_cast<float4 *>(part + head * D + ch), o);
+                if (ch == 0) __stcg(part + 8 * D + head, M), __stcg(part + 8 * D + 8 + head, L);
+            }
+        }
+        if (c0 != c1) {
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                __threadfence();
+                uint32_t *ticket = a.ctl->tickets + c0;
+                const int last = atomicAdd(ticket, 1u) == (uint32_t)(c1 - c0);
+                if (last) atomicExch(ticket, 0u);
+                s_misc[0] = last;
+            }
+            __syncthreads();
+            if (s_misc[0]) {
+                __threadfence();
+                for (int e = tid; e < a.G * (D / 4); e += kThreads) {
+                    const int head = e / (D / 4), ch = e % (D / 4) * 4;
+                    float M = -INFINITY, L = 0.f;
+                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                    for (int x = c0; x <= c1; ++x) {
+                        const float *src = a.partials + (size_t)(x * 2 + (x == c0 ? 1 : 0)) * C::kPartFloats;
+                        const float mx = __ldcg(src + 8 * D + head), lx = __ldcg(src + 8 * D + 8 + head);
+                        const float4 v = __ldcg(reinterpret_cast<const float4 *>(src + head * D + ch));
+                        const float top = fmaxf(M, mx), ref = top == -INFINITY ? 0.f : top;
+                        const float fo = ex2(M - ref), fx = ex2(mx - ref);
+                        M = top, L = L * fo + lx * fx;
+                        o.x = o.x * fo + v.x * fx, o.y = o.y * fo + v.y * fx, o.z = o.z * fo + v.z * fx, o.w = o.w * fo + v.w * fx;
+                    }
+                    const float inv = L == 0.f ? 0.f : 1.f / L;
+                    *reinterpret_cast<float4 *>(a.out + (row0 + head) * D + ch) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+                    if (ch == 0) a.lse[row0 + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+                }
+            }
+        }
+        __syncthreads();               // the merge buffer is written again
+        pair = after, first = after_first;
+        done = stop;
+    }
+    // a wait that gave up: the copies that are still on their way end before the CTA does
+    for (; used != sent; ++used) mbar_wait(bars + 8 * (used % C::kStages), used / C::kStages & 1);
+}
+
+// the cache as lines of 128 bytes, boxes of one page of one head
+bool make_lines_map(CUtensorMap *map, const void *base, long long bytes, int lines) {
+    EncodeTiledFn fn = encode_tiled();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {128, (cuuint64_t)(bytes / 128)};
+    const cuuint64_t strides[1] = {128};
+    const cuuint32_t box[2] = {128, (cuuint32_t)lines};
+    const cuuint32_t estr[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+cudaError_t launch(const se_params &p, const Kv8DecodeCall &c, cudaStream_t stream) {
+    using C = Cfg<D>;
+    CUtensorMap k_map, v_map;
+    const long long bytes = (long long)p.num_phys_pages * p.H_kv * C::kPageBytes;
+    if (!make_lines_map(&k_map, c.k_cache, bytes, C::kRowsPerPage) || !make_lines_map(&v_map, c.v_cache, bytes, C::kRowsPerPage))
+        return cudaErrorInvalidValue;
+    Args a = {};
+    a.q = static_cast<const uint16_t *>(c.q), a.scales = reinterpret_cast<const float2 *>(c.scales);
+    a.page_table = c.page_table, a.seq_lens = c.seq_lens, a.sel_idx = c.sel_idx, a.sel_cnt = c.sel_cnt;
+    a.out = c.out, a.lse = c.lse, a.partials = partials_of(c.workspace), a.ctl = reinterpret_cast<PromptControl *>(c.workspace);
+    a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.G = p.H_q / p.H_kv, a.max_pages = p.max_pages, a.P_phys = p.num_phys_pages;
+    a.k_max = p.k_max, a.scale_log2 = effective_scale(p) * kLog2e;
+    static_assert(C::kSmem <= 227 * 1024, "shared memory of a CTA");
+    static_assert(2 * C::kPartFloats <= 8 * (128 * D + 256), "partial results of a CTA fit where the prompt kernels keep theirs");
+    auto kern = kv8_decode_kernel<D>;
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
+    if (e != cudaSuccess) return e;
+    kern<<<kPromptCtas, kThreads, C::kSmem, stream>>>(k_map, v_map, a);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_kv8_decode(const se_params &p, const Kv8DecodeCall &c, cudaStream_t stream) {
+    return p.D == 128 ? launch<128>(p, c, stream) : launch<64>(p, c, stream);
+}
+
+}  // namespace se

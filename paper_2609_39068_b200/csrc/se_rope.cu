@@ -17,9 +17,15 @@
 // Bound by HBM for prompts: 24K tokens of 32 + 2 x 8 heads, D = 128, 122 us for 662 MB = 5.4 TB/s, 0.84 of a plain copy (124-125 us
 // as calls on changing inputs).  Small calls are four dependent round trips: 64 single tokens 7.7 us.  (Loading the next rows
 // while a row is turned, with the registers that takes, was slower: 8.2 us where 7.2 were taken, 128.5 us for 121.5.)
+//
+// The same kernel fills a cache of e4m3 codes (KV8): a warp holds all tokens of a (page, head), so it has the page's largest
+// magnitude after five shuffles, picks the power-of-two scale, quantises, and brings older codes of the page to a scale that
+// has grown.  A power of two costs e4m3 no precision (its relative step is the same in every binade), makes the older codes'
+// second rounding exact but for subnormal codes, and makes every dequantised value a bf16 number.
 #include <type_traits>
 
 #include "se_internal.h"
+#include "se_kv8.cuh"
 
 namespace se {
 
@@ -32,7 +38,10 @@ struct RopeArgs {
     long long q_stride, k_stride, v_stride;      // elements between tokens
     const int32_t *cu, *seq_lens, *page_table, *positions, *pair_axis;
     const double *inv_freq;
-    uint16_t *q_out, *k_out, *k_cache, *v_cache, *meta;
+    uint16_t *q_out, *k_out;
+    void *k_cache, *v_cache;                     // bf16, or e4m3 codes
+    float *scales;                               // codes: [P_phys, H_kv, 2]
+    uint16_t *meta;
     uint32_t *status;
     int B, H_q, H_kv, T, max_pages, P_phys, n_axes, rot;
 };
@@ -80,7 +89,7 @@ __device__ __forceinline__ uint4 shfl_xor4(const uint4 &w, int m) {
 }
 
 // CTAS per SM: a CTA's latency is shorter with two (128 registers), more bytes are in flight with three (80 registers).
-template <int D, bool INTERLEAVED, int CTAS>
+template <int D, bool INTERLEAVED, int CTAS, bool KV8>
 __global__ void __launch_bounds__(kRopeThreads, CTAS)
 rope_append_kernel(const RopeArgs a) {
     constexpr int LPR = D / 16;            // lanes per token: two 16-byte pieces each
@@ -168,11 +177,23 @@ rope_append_kernel(const RopeArgs a) {
                 if (t >= s0 && t < s1) {
                     const uint4 *row = reinterpret_cast<const uint4 *>(src + (row0 + t) * stride);
                     x[i] = row[c_lo], y[i] = row[c_hi];
-                } else if (want_meta && t < s0) {          // older keys of the page
-                    const uint4 *row = reinterpret_cast<const uint4 *>(a.k_cache + page + (size_t)t * D);
-                    x[i] = row[c_lo], y[i] = row[c_hi];
+                } else if (KV8 ? !is_q && cached && t < s0 : want_meta && t < s0) {          // older tokens of the page
+                    if constexpr (KV8) {
+                        const uint2 *row = reinterpret_cast<const uint2 *>((const uint8_t *)(is_k ? a.k_cache : a.v_cache) + page + (size_t)t * D);
+                        const uint2 u = row[c_lo], w = row[c_hi];
+                        x[i] = make_uint4(u.x, u.y, 0, 0), y[i] = make_uint4(w.x, w.y, 0, 0);
+                    } else {
+                        const uint4 *row = reinterpret_cast<const uint4 *>((const uint16_t *)a.k_cache + page + (size_t)t * D);
+                        x[i] = row[c_lo], y[i] = row[c_hi];
+                    }
                 }
             }
+            [[maybe_unused]] float *sp = nullptr, old_scale = 0.f;
+            if constexpr (KV8) {
+                sp = a.scales + ((size_t)max(pid, 0) * a.H_kv + max(h, 0)) * 2 + (is_k ? 0 : 1);
+                if (!is_q && cached && s0 > 0) old_scale = *sp;
+            }
+            [[maybe_unused]] uint32_t top = 0;     // KV8: largest magnitudes so far, two bf16
             uint4 mnx = make_uint4(0x7f807f80u, 0x7f807f80u, 0x7f807f80u, 0x7f807f80u), mny = mnx;   // +inf pairs
             uint4 mxx = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u), mxy = mxx;   // -inf pairs
 #pragma unroll
@@ -185,14 +206,50 @@ rope_append_kernel(const RopeArgs a) {
                                                                   : a.k_out + ((row0 + t) * a.H_kv + h) * D);
                         o[c_lo] = x[i], o[c_hi] = y[i];
                     }
-                    if (!is_q && cached) {
-                        uint4 *o = reinterpret_cast<uint4 *>((is_k ? a.k_cache : a.v_cache) + page + (size_t)t * D);
+                    if constexpr (KV8) {
+                        top = bmax2(top, bmax2(largest8(x[i]), largest8(y[i])));
+                    } else if (!is_q && cached) {
+                        uint4 *o = reinterpret_cast<uint4 *>((uint16_t *)(is_k ? a.k_cache : a.v_cache) + page + (size_t)t * D);
                         o[c_lo] = x[i], o[c_hi] = y[i];
                     }
                 }
-                if (want_meta && t < s1) {
+                if (!KV8 && want_meta && t < s1) {
                     fold_min(mnx, x[i]), fold_min(mny, y[i]);
                     fold_max(mxx, x[i]), fold_max(mxy, y[i]);
+                }
+            }
+            if constexpr (KV8) {
+                if (!is_q && cached) {
+#pragma unroll
+                    for (int m = 16; m; m >>= 1) top = bmax2(top, __shfl_xor_sync(kFull, top, m));
+                    const float own = kv8_scale(max(top & 0xffffu, top >> 16));
+                    const float scale = s0 > 0 ? fmaxf(old_scale, own) : own;      // (a scale that is no number counts as none)
+                    const float inv = __uint_as_float(0x7f000000u - __float_as_uint(scale));     // 1 / 2^e
+                    const bool grown = s0 > 0 && scale != old_scale;
+                    const float again = old_scale * inv;
+                    uint8_t *codes = (uint8_t *)(is_k ? a.k_cache : a.v_cache) + page;
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) {
+                        const int t = i * RP + tq;
+                        if (t >= s1) continue;
+                        uint2 u, w;
+                        if (t >= s0) {
+                            u = kv8_codes(x[i], inv), w = kv8_codes(y[i], inv);
+                        } else {
+                            u = make_uint2(x[i].x, x[i].y), w = make_uint2(y[i].x, y[i].y);
+                            if (grown) u = kv8_again(u, again), w = kv8_again(w, again);
+                        }
+                        if (t >= s0 || grown) {
+                            uint2 *o = reinterpret_cast<uint2 *>(codes + (size_t)t * D);
+                            o[c_lo] = u, o[c_hi] = w;
+                        }
+                        if (want_meta) {
+                            x[i] = kv8_values(u, scale), y[i] = kv8_values(w, scale);
+                            fold_min(mnx, x[i]), fold_min(mny, y[i]);
+                            fold_max(mxx, x[i]), fold_max(mxy, y[i]);
+                        }
+                    }
+                    if (lane == 0) *sp = scale;
                 }
             }
             if (want_meta) {
@@ -218,8 +275,8 @@ cudaError_t launch_rope_append(const se_params &p, const RopeCall &c, cudaStream
     a.q_stride = c.q_stride, a.k_stride = c.k_stride, a.v_stride = c.v_stride;
     a.cu = c.cu_seqlens, a.seq_lens = c.seq_lens, a.page_table = c.page_table, a.positions = c.positions;
     a.pair_axis = c.pair_axis, a.inv_freq = c.inv_freq;
-    a.q_out = (uint16_t *)c.q_out, a.k_out = (uint16_t *)c.k_out, a.k_cache = (uint16_t *)c.k_cache;
-    a.v_cache = (uint16_t *)c.v_cache, a.meta = (uint16_t *)c.meta, a.status = c.status;
+    a.q_out = (uint16_t *)c.q_out, a.k_out = (uint16_t *)c.k_out, a.k_cache = c.k_cache, a.v_cache = c.v_cache;
+    a.scales = c.scales, a.meta = (uint16_t *)c.meta, a.status = c.status;
     a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.T = c.total_tokens, a.max_pages = p.max_pages;
     a.P_phys = p.num_phys_pages, a.n_axes = c.n_axes, a.rot = c.rot_dim;
     // a request touches at most ceil((n + 15) / 16) pages
@@ -233,7 +290,8 @@ cudaError_t launch_rope_append(const se_params &p, const RopeCall &c, cudaStream
     const size_t smem = ((size_t)p.B + 1) * sizeof(int);
     auto pick = [&](auto d, auto ctas) {
         constexpr int D = decltype(d)::value, CTAS = decltype(ctas)::value;
-        return c.interleaved ? rope_append_kernel<D, true, CTAS> : rope_append_kernel<D, false, CTAS>;
+        if (c.scales) return c.interleaved ? rope_append_kernel<D, true, CTAS, true> : rope_append_kernel<D, false, CTAS, true>;
+        return c.interleaved ? rope_append_kernel<D, true, CTAS, false> : rope_append_kernel<D, false, CTAS, false>;
     };
     using Two = std::integral_constant<int, 2>;
     using Three = std::integral_constant<int, 3>;
