@@ -28,10 +28,11 @@ __device__ __forceinline__ uint32_t largest8(const uint4 &w) {
 __device__ __forceinline__ uint32_t e4m3x2(float a, float b) {
     return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
-// two codes (the lower 16 bits) as two halves: exact
-__device__ __forceinline__ uint32_t half2_of_e4m3x2(uint32_t codes) {
-    const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3);
-    return (uint32_t)r.x | (uint32_t)r.y << 16;
+// four codes as four halves (lower two, upper two): exact
+__device__ __forceinline__ void halves_of_e4m3x4(uint32_t codes, uint32_t &lo, uint32_t &hi) {
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+        : "=r"(lo), "=r"(hi)
+        : "r"(codes));
 }
 __device__ __forceinline__ float2 float2_of_e4m3x2(uint32_t codes) {
     return __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3)));

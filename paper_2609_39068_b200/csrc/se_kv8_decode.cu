@@ -11,10 +11,10 @@
 // What bounds it: HBM, 2 * 2 * D bytes per token and kv-head and a few cycles of everything else: per page and head at D = 128
 // 64 conversions of two codes, 24 matrix instructions, 32 fp32 FMAs per warp.
 //
-// Split.  The list of all (request, kv-head) pairs' pages is cut into 148 runs of equal length, one per CTA; a CTA's pages go
-// round its eight warps, each of which keeps a ring of pages in flight (tensor copies, 128-byte swizzle) across the borders of
-// pairs.  At the end of a pair's run the warps merge through shared memory; a pair that several CTAs share leaves partial
-// results in the workspace, and the CTA that arrives last merges them in order.
+// Split.  The list of all (request, kv-head) pairs' pages is cut into 592 runs of equal length, one per group of four warps; a
+// group's pages go round its warps, each of which keeps a ring of pages in flight (tensor copies, 128-byte swizzle) across the
+// borders of pairs.  At the end of a pair's run the warps merge through shared memory; a pair that several groups share leaves
+// partial results in the workspace, and the group that arrives last merges them in order.
 #include <math.h>
 
 #include "se_internal.h"
@@ -25,20 +25,23 @@ namespace se {
 
 namespace {
 
-constexpr int kWarps = 8, kThreads = 32 * kWarps;
-constexpr int kChunks = 2048;          // prefix sums that a CTA keeps: of every pair, or of runs of pairs
+constexpr int kWarps = 16, kThreads = 32 * kWarps;
+constexpr int kTeam = 4, kTeams = kWarps / kTeam;      // warps that share a run of pages, runs of a CTA
+constexpr int kLeast = 2 * kTeam;      // pages of a run
+constexpr int kChunks = 1024;          // prefix sums that a CTA keeps: of every pair, or of runs of pairs
 constexpr float kSlack = 8.f;          // the running maximum may lag: weights up to 2^8 stay far inside a half's range
 
 template <int D>
 struct Cfg {
     static constexpr int kPageBytes = kPage * D;                    // of K or of V, one head
-    static constexpr int kStages = D == 128 ? 5 : 8;
+    static constexpr int kStages = D == 128 ? 2 : 4;
     static constexpr int kRowsPerPage = kPageBytes / 128;
     static constexpr int kTiles = D / 16;                           // 16-channel tiles of the output
     static constexpr int kPitch = D + 4;                            // floats of a head's row in the merge buffer
     static constexpr int kPartFloats = 8 * D + 16;                  // a partial result: O, m, l
     static constexpr size_t kRing = (size_t)kWarps * kStages * 2 * kPageBytes;
-    static constexpr size_t kSmem = kRing + (size_t)kWarps * (8 * kPitch + 16) * 4 + (kChunks + 1) * 8 + kWarps * kStages * 8 + 64 * 4;
+    static constexpr size_t kMerge = (size_t)kWarps * (8 * kPitch + 16) * 4, kQ = (size_t)kTeams * 2 * 8 * D * 2;
+    static constexpr size_t kSmem = kRing + kMerge + kQ + (kChunks + 1) * 8 + kWarps * kStages * 8 + 64 * 4;
 };
 
 struct Args {
@@ -57,6 +60,13 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// the same without an addend
+__device__ __forceinline__ void mma_f16_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
     uint32_t d;
@@ -121,6 +131,7 @@ struct Page {
     int tokens;                        // below the request's length, 1..16
     float2 scale;
 };
+__device__ __forceinline__ void team_sync(int team) { asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(32 * kTeam) : "memory"); }
 __device__ __forceinline__ Page look_up(const Args &a, const Pairs &ps, long long u0, int n, int i) {
     Page p = {-1, 0, make_float2(0.f, 0.f)};
     if (i >= n) return p;
@@ -128,13 +139,11 @@ __device__ __forceinline__ Page look_up(const Args &a, const Pairs &ps, long lon
     const int pair = ps.find(u0 + i, first);
     const int r = pair / a.H_kv, h = pair - r * a.H_kv;
     int b = (int)(u0 + i - first);
-    const int len = a.seq_lens[r];
-    if (a.sel_idx) {
-        b = a.sel_idx[(size_t)pair * a.k_max + b];
-        if (b < 0 || b >= a.max_pages || b * kPage >= len) {
-            atomicOr(&a.ctl->status, SE_DEV_BAD_SELECTION);
-            return p;
-        }
+    const int chosen = a.sel_idx ? a.sel_idx[(size_t)pair * a.k_max + b] : b, len = a.seq_lens[r];
+    b = chosen;
+    if (b < 0 || b >= a.max_pages || b * kPage >= len) {                                 // (only a selection can be wrong here)
+        atomicOr(&a.ctl->status, SE_DEV_BAD_SELECTION);
+        return p;
     }
     const int pid = a.page_table[(size_t)r * a.max_pages + b];
     if (pid >= a.P_phys) atomicOr(&a.ctl->status, SE_DEV_BAD_PAGE_ID);
@@ -145,13 +154,37 @@ __device__ __forceinline__ Page look_up(const Args &a, const Pairs &ps, long lon
     return p;
 }
 
+// A pair's query heads on their way to shared memory, by the team's threads.
 template <int D>
-__device__ __forceinline__ void load_q(const Args &a, int pair, int g, int t, uint4 (&raw)[D / 32]) {
+__device__ __forceinline__ void fetch_q(const Args &a, int pair, uint32_t dst, int tt) {
     const int r = pair / a.H_kv, h = pair - r * a.H_kv;
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
-        const uint4 *src = reinterpret_cast<const uint4 *>(a.q + ((size_t)r * a.H_q + h * a.G + min(g, a.G - 1)) * D + 64 * i + 16 * t);
-        raw[2 * i] = src[0], raw[2 * i + 1] = src[1];
+    if (tt < a.G * D / 8)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + tt * 16), "l"(a.q + ((size_t)r * a.H_q + h * a.G) * D + tt * 8) : "memory");
+    asm volatile("cp.async.commit_group;" ::: "memory");
+}
+
+// Merges the parts of a pair that the runs c0 .. c1 have left, in their order, by the team's threads.
+template <int D>
+__device__ __noinline__ void merge_parts(const Args &a, int pair, int c0, int c1, int tt) {
+    using C = Cfg<D>;
+    const size_t row0 = (size_t)(pair / a.H_kv) * a.H_q + pair % a.H_kv * a.G;
+    for (int e = tt; e < a.G * (D / 4); e += 32 * kTeam) {
+        const int head = e / (D / 4), ch = e % (D / 4) * 4;
+        float M = -INFINITY, L = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int x = c0; x <= c1; ++x) {
+            const float *src = a.partials + (size_t)(x * 2 + (x == c0 ? 1 : 0)) * C::kPartFloats;
+            const float mx = __ldcg(src + 8 * D + head), lx = __ldcg(src + 8 * D + 8 + head);
+            const float4 v = __ldcg(reinterpret_cast<const float4 *>(src + head * D + ch));
+            const float top = fmaxf(M, mx), ref = top == -INFINITY ? 0.f : top;
+            const float fo = ex2(M - ref), fx = ex2(mx - ref);
+            M = top, L = L * fo + lx * fx;
+            o.x = o.x * fo + v.x * fx, o.y = o.y * fo + v.y * fx, o.z = o.z * fo + v.z * fx, o.w = o.w * fo + v.w * fx;
+        }
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        *reinterpret_cast<float4 *>(a.out + (row0 + head) * D + ch) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+        if (ch == 0) a.lse[row0 + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
     }
 }
 
@@ -161,10 +194,13 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     using C = Cfg<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
     float *s_merge = reinterpret_cast<float *>(smem + C::kRing);                        // [warp][8][kPitch], then m and l
-    long long *s_pre = reinterpret_cast<long long *>(s_merge + kWarps * (8 * C::kPitch + 16));
+    const uint32_t s_q = smem_u32(smem) + (uint32_t)(C::kRing + C::kMerge);             // [team][2][8][D] bf16
+    long long *s_pre = reinterpret_cast<long long *>(smem + C::kRing + C::kMerge + C::kQ);
     uint64_t *s_bars = reinterpret_cast<uint64_t *>(s_pre + kChunks + 1);
     int *s_misc = reinterpret_cast<int *>(s_bars + kWarps * C::kStages);                // sums of a scan, verdict of a merge
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const int team = warp / kTeam, mate = warp % kTeam, tt = tid % (32 * kTeam);         // team, warp and thread of the team
+    const int runs = gridDim.x * kTeams, run = team * gridDim.x + blockIdx.x;            // (few runs: on SMs of their own)
     const uint32_t ring = smem_u32(smem) + warp * (C::kStages * 2 * C::kPageBytes);
     const uint32_t bars = smem_u32(s_bars) + warp * (C::kStages * 8);
 
@@ -176,7 +212,7 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     if (tid == 0) prefetch_map(&k_map), prefetch_map(&v_map);
     mbar_fence_init();
 
-    // pages before every pair (or every run of pairs, where there are more than 2048)
+    // pages before every pair (or every run of pairs, where there are more than 1024)
     const int pairs = a.B * a.H_kv;
     Pairs ps = {a, s_pre, (pairs + kChunks - 1) / kChunks, 0};
     ps.chunks = (pairs + ps.per - 1) / ps.per;
@@ -222,18 +258,22 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     }
 
     const long long total = s_pre[ps.chunks];
-    const long long size = max((total + gridDim.x - 1) / gridDim.x, (long long)kWarps);  // pages of a CTA: a warp has one at least
-    const long long u0 = size * blockIdx.x;
+    const long long size = max((total + runs - 1) / runs, (long long)kLeast);
+    const long long u0 = size * run;
     if (u0 >= total) return;
     const int n = (int)min(size, total - u0);
-    const int mine = n > warp ? (n - warp + kWarps - 1) / kWarps : 0;                    // page k of the warp is page k * kWarps + warp
-    Page now = look_up(a, ps, u0, n, lane * kWarps + warp), next = look_up(a, ps, u0, n, (32 + lane) * kWarps + warp);
-    int block = 0, issue = 0;          // block of 32 pages that `now` describes; next page to be fetched
+    const int mine = n > mate ? (n - mate + kTeam - 1) / kTeam : 0;                      // page k of the warp is page k * kTeam + mate of the run
+    long long first;
+    int pair = ps.find(u0, first);
+    const uint32_t q_at = s_q + team * (2 * 8 * D * 2);
+    fetch_q<D>(a, pair, q_at, tt);     // (ahead of the pages: behind the rings' first fill it took 4 us)
+    Page now = look_up(a, ps, u0, n, lane * kTeam + mate), next = {-1, 0, make_float2(0.f, 0.f)};
+    int block = 0, known = 32, issue = 0;                                                // block of 32 pages that `now` describes, pages looked up; next page to fetch
     uint32_t sent = 0, used = 0;       // pages fetched, pages consumed
     bool ok = true;
     const bool chosen = elect_one();
     auto send = [&] {
-        while (ok && issue < mine && sent - used < C::kStages && issue < (block + 2) * 32) {
+        while (ok && issue < mine && sent - used < C::kStages && issue < known) {
             const int row = __shfl_sync(kFull, issue / 32 == block ? now.row : next.row, issue & 31);
             if (row >= 0) {
                 if (chosen) {
@@ -250,18 +290,29 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     };
     send();
 
-    long long first;
-    int pair = ps.find(u0, first);
-    uint4 raw[D / 32];
-    load_q<D>(a, pair, g, t, raw);
+    if (mine > 32) next = look_up(a, ps, u0, n, (32 + lane) * kTeam + mate);
+    known = 64;
     int k = 0;
-    for (int done = 0; done < n;) {
+    int begun = -1, begun_c0 = 0, begun_c1 = 0;        // the run's first pair, where earlier runs hold a part of it
+    for (int done = 0, turn = 0;; ++turn) {
         const int pages = ps.count_known(pair);
-        const int stop = (int)min((long long)n, first + pages - u0);                     // end of the pair's pages in the CTA
+        const int stop = (int)min((long long)n, first + pages - u0);                     // end of the pair's pages in the run
+        // q is here, and the team has read the merge buffer; the next pair's q is on its way a whole pair ahead
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        team_sync(team);
+        int after = pair;
+        if (stop < n) {
+            while (ps.count_known(++after) == 0) {}
+            fetch_q<D>(a, after, q_at + (turn + 1 & 1) * (8 * D * 2), tt);
+        }
         // q as halves: head g, channels 64 i + 16 t .. + 15
         uint32_t qh[D / 8];
         float f0, f1;                  // heads 2 t and 2 t + 1: logit in powers of two = sum * f * s_K
         {
+            uint4 raw[D / 32];
+            const uint32_t src = q_at + (turn & 1) * (8 * D * 2) + min(g, a.G - 1) * (2 * D) + 32 * t;
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) raw[2 * i] = lds128(src + 128 * i), raw[2 * i + 1] = lds128(src + 128 * i + 16);
             uint32_t top = 0;
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) top = bmax2(top, largest8(raw[i]));
@@ -283,16 +334,17 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             const float f = down * a.scale_log2;
             f0 = __shfl_sync(kFull, f, 8 * t), f1 = __shfl_sync(kFull, f, 8 * t + 4);
         }
-        float acc[C::kTiles][4];
+        float2 acc[C::kTiles][2];      // [tile][channel (D / 8) g + 2 tile, + 1]: heads 2 t, 2 t + 1
 #pragma unroll
-        for (int i = 0; i < C::kTiles; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+        for (int i = 0; i < C::kTiles; ++i) acc[i][0] = acc[i][1] = make_float2(0.f, 0.f);
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
 
-        for (; k < mine && k * kWarps + warp < stop; ++k) {
+        for (; k < mine && k * kTeam + mate < stop; ++k) {
             if (k / 32 != block) {
                 ++block;
                 now = next;
-                next = look_up(a, ps, u0, n, ((block + 1) * 32 + lane) * kWarps + warp);
+                next = look_up(a, ps, u0, n, ((block + 1) * 32 + lane) * kTeam + mate);
+                known += 32;
                 send();
             }
             const int row = __shfl_sync(kFull, now.row, k & 31);
@@ -308,7 +360,7 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             // ---- logits: rows are tokens, columns are heads.  Row x of the product is token x for even x, x ^ 4 for odd x (and the
             // same 8 further on): with the swizzle, lanes that load at the same time then never meet in a bank, here and for V.
             const int tok = g & 1 ? g ^ 4 : g;
-            float c[2][4] = {};
+            float c[2][4];
 #pragma unroll
             for (int i = 0; i < D / 64; ++i) {
                 uint4 x, y;
@@ -321,9 +373,12 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 }
                 const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-                for (int s = 0; s < 4; ++s)
-                    mma_f16(c[s & 1], half2_of_e4m3x2(xw[s] & 0xffffu), half2_of_e4m3x2(yw[s] & 0xffffu), half2_of_e4m3x2(xw[s] >> 16),
-                            half2_of_e4m3x2(yw[s] >> 16), qh[8 * i + 2 * s], qh[8 * i + 2 * s + 1]);
+                for (int s = 0; s < 4; ++s) {
+                    uint32_t a0, a1, a2, a3;
+                    halves_of_e4m3x4(xw[s], a0, a2), halves_of_e4m3x4(yw[s], a1, a3);
+                    if (i == 0 && s < 2) mma_f16_first(c[s & 1], a0, a1, a2, a3, qh[8 * i + 2 * s], qh[8 * i + 2 * s + 1]);
+                    else mma_f16(c[s & 1], a0, a1, a2, a3, qh[8 * i + 2 * s], qh[8 * i + 2 * s + 1]);
+                }
             }
             const float g0 = fmaxf(f0 * sk, 1e-37f), g1 = fmaxf(f1 * sk, 1e-37f);        // (0 times a masked logit would be NaN)
             float z[4];
@@ -345,7 +400,9 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 m0 = n0, m1 = n1;
                 l0 *= r0, l1 *= r1;
 #pragma unroll
-                for (int i = 0; i < C::kTiles; ++i) acc[i][0] *= r0, acc[i][1] *= r1, acc[i][2] *= r0, acc[i][3] *= r1;
+                for (int i = 0; i < C::kTiles; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) acc[i][e].x *= r0, acc[i][e].y *= r1;
             }
             const float p0 = ex2(fmaf(z[0], g0, -m0)), p1 = ex2(fmaf(z[1], g1, -m1));
             const float p2 = ex2(fmaf(z[2], g0, -m0)), p3 = ex2(fmaf(z[3], g1, -m1));
@@ -385,50 +442,44 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             for (int i = 0; i < C::kTiles; ++i) {                                        // rows g, g + 8: channels (D / 8) g + 2 i, + 1
                 const uint32_t sel = i & 1 ? 0x7362u : 0x5140u;
                 const uint32_t x = __byte_perm(va[i / 2], vb[i / 2], sel), y = __byte_perm(vc[i / 2], vd[i / 2], sel);
-                const uint32_t a0 = half2_of_e4m3x2(x & 0xffffu), a1 = half2_of_e4m3x2(x >> 16);
-                const uint32_t a2 = half2_of_e4m3x2(y & 0xffffu), a3 = half2_of_e4m3x2(y >> 16);
-                float o[4] = {};
-                mma_f16(o, a0, a1, a2, a3, e0, e1);
+                uint32_t a0, a1, a2, a3;
+                halves_of_e4m3x4(x, a0, a1), halves_of_e4m3x4(y, a2, a3);
+                float o[4];
+                mma_f16_first(o, a0, a1, a2, a3, e0, e1);
                 mma_f16(o, a0, a1, a2, a3, b0, b1);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][e] = fmaf(o[e], sv, acc[i][e]);
+                acc[i][0] = ffma2(make_float2(o[0], o[1]), make_float2(sv, sv), acc[i][0]);
+                acc[i][1] = ffma2(make_float2(o[2], o[3]), make_float2(sv, sv), acc[i][1]);
             }
         }
 
-        // ---- end of the pair's pages in this CTA ----
-        const bool more = stop < n;
-        int after = pair;
-        long long after_first = first + pages;
-        if (more) {
-            while (ps.count_known(++after) == 0) {}
-            load_q<D>(a, after, g, t, raw);
-        }
+        // ---- end of the pair's pages in this run ----
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) l0 += __shfl_xor_sync(kFull, l0, o), l1 += __shfl_xor_sync(kFull, l1, o);
+        const float *team_merge = s_merge + team * kTeam * (8 * C::kPitch + 16);
         float *own = s_merge + warp * (8 * C::kPitch + 16);
         if (g == 0) own[8 * C::kPitch + 2 * t] = m0, own[8 * C::kPitch + 2 * t + 1] = m1, own[8 * C::kPitch + 8 + 2 * t] = l0, own[8 * C::kPitch + 9 + 2 * t] = l1;
 #pragma unroll
         for (int j = 0; j < C::kTiles / 2; ++j) {
             const int ch = (D / 8) * g + 4 * j;
-            *reinterpret_cast<float4 *>(own + (2 * t) * C::kPitch + ch) = make_float4(acc[2 * j][0], acc[2 * j][2], acc[2 * j + 1][0], acc[2 * j + 1][2]);
-            *reinterpret_cast<float4 *>(own + (2 * t + 1) * C::kPitch + ch) = make_float4(acc[2 * j][1], acc[2 * j][3], acc[2 * j + 1][1], acc[2 * j + 1][3]);
+            *reinterpret_cast<float4 *>(own + (2 * t) * C::kPitch + ch) = make_float4(acc[2 * j][0].x, acc[2 * j][1].x, acc[2 * j + 1][0].x, acc[2 * j + 1][1].x);
+            *reinterpret_cast<float4 *>(own + (2 * t + 1) * C::kPitch + ch) = make_float4(acc[2 * j][0].y, acc[2 * j][1].y, acc[2 * j + 1][0].y, acc[2 * j + 1][1].y);
         }
-        __syncthreads();
-        const int c0 = (int)(first / size), c1 = (int)((first + pages - 1) / size);      // CTAs that share the pair
+        team_sync(team);
+        const int c0 = (int)(first / size), c1 = (int)((first + pages - 1) / size);      // runs that share the pair
         const int r = pair / a.H_kv, h = pair - r * a.H_kv;
         const size_t row0 = (size_t)r * a.H_q + h * a.G;
-        float *part = a.partials + (size_t)(blockIdx.x * 2 + (c0 == (int)blockIdx.x ? 1 : 0)) * C::kPartFloats;
-        for (int e = tid; e < a.G * (D / 4); e += kThreads) {
+        float *part = a.partials + (size_t)(run * 2 + (c0 == run ? 1 : 0)) * C::kPartFloats;
+        for (int e = tt; e < a.G * (D / 4); e += 32 * kTeam) {
             const int head = e / (D / 4), ch = e % (D / 4) * 4;
             float M = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_merge[w * (8 * C::kPitch + 16) + 8 * C::kPitch + head]);
+            for (int w = 0; w < kTeam; ++w) M = fmaxf(M, team_merge[w * (8 * C::kPitch + 16) + 8 * C::kPitch + head]);
             const float ref = M == -INFINITY ? 0.f : M;
             float L = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const float *src = s_merge + w * (8 * C::kPitch + 16);
+            for (int w = 0; w < kTeam; ++w) {
+                const float *src = team_merge + w * (8 * C::kPitch + 16);
                 const float x = ex2(src[8 * C::kPitch + head] - ref);
                 L = fmaf(x, src[8 * C::kPitch + 8 + head], L);
                 const float4 v = *reinterpret_cast<const float4 *>(src + head * C::kPitch + ch);
@@ -443,42 +494,37 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 if (ch == 0) __stcg(part + 8 * D + head, M), __stcg(part + 8 * D + 8 + head, L);
             }
         }
-        if (c0 != c1) {
-            __threadfence();
-            __syncthreads();
-            if (tid == 0) {
-                __threadfence();
-                uint32_t *ticket = a.ctl->tickets + c0;
-                const int last = atomicAdd(ticket, 1u) == (uint32_t)(c1 - c0);
-                if (last) atomicExch(ticket, 0u);
-                s_misc[0] = last;
-            }
-            __syncthreads();
-            if (s_misc[0]) {
-                __threadfence();
-                for (int e = tid; e < a.G * (D / 4); e += kThreads) {
-                    const int head = e / (D / 4), ch = e % (D / 4) * 4;
-                    float M = -INFINITY, L = 0.f;
-                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-                    for (int x = c0; x <= c1; ++x) {
-                        const float *src = a.partials + (size_t)(x * 2 + (x == c0 ? 1 : 0)) * C::kPartFloats;
-                        const float mx = __ldcg(src + 8 * D + head), lx = __ldcg(src + 8 * D + 8 + head);
-                        const float4 v = __ldcg(reinterpret_cast<const float4 *>(src + head * D + ch));
-                        const float top = fmaxf(M, mx), ref = top == -INFINITY ? 0.f : top;
-                        const float fo = ex2(M - ref), fx = ex2(mx - ref);
-                        M = top, L = L * fo + lx * fx;
-                        o.x = o.x * fo + v.x * fx, o.y = o.y * fo + v.y * fx, o.z = o.z * fo + v.z * fx, o.w = o.w * fo + v.w * fx;
-                    }
-                    const float inv = L == 0.f ? 0.f : 1.f / L;
-                    *reinterpret_cast<float4 *>(a.out + (row0 + head) * D + ch) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-                    if (ch == 0) a.lse[row0 + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
-                }
-            }
-        }
-        __syncthreads();               // the merge buffer is written again
-        pair = after, first = after_first;
+        if (c0 < run) begun = pair, begun_c0 = c0, begun_c1 = c1;
         done = stop;
+        if (done == n) {
+            // The parts of pairs that other runs share are all written: one round of fence and tickets for both (after each pair it
+            // took the team 6 to 9 us, under load, with nothing else to do).
+            const bool ends = c1 > run && c0 == run;                                     // later runs go on with a pair that begins here
+            if (begun >= 0 || ends) {
+                __threadfence();
+                team_sync(team);
+                if (tt == 0) {
+                    __threadfence();
+                    int verdict = 0;
+                    if (begun >= 0 && atomicAdd(a.ctl->tickets + begun_c0, 1u) == (uint32_t)(begun_c1 - begun_c0)) {
+                        atomicExch(a.ctl->tickets + begun_c0, 0u);
+                        verdict = 1;
+                    }
+                    if (ends && atomicAdd(a.ctl->tickets + c0, 1u) == (uint32_t)(c1 - c0)) {
+                        atomicExch(a.ctl->tickets + c0, 0u);
+                        verdict |= 2;
+                    }
+                    s_misc[team] = verdict;
+                }
+                team_sync(team);
+                const int verdict = s_misc[team];
+                if (verdict) __threadfence();
+                if (verdict & 1) merge_parts<D>(a, begun, begun_c0, begun_c1, tt);
+                if (verdict & 2) merge_parts<D>(a, pair, c0, c1, tt);
+            }
+            break;
+        }
+        pair = after, first += pages;
     }
     // a wait that gave up: the copies that are still on their way end before the CTA does
     for (; used != sent; ++used) mbar_wait(bars + 8 * (used % C::kStages), used / C::kStages & 1);
@@ -510,7 +556,8 @@ cudaError_t launch(const se_params &p, const Kv8DecodeCall &c, cudaStream_t stre
     a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.G = p.H_q / p.H_kv, a.max_pages = p.max_pages, a.P_phys = p.num_phys_pages;
     a.k_max = p.k_max, a.scale_log2 = effective_scale(p) * kLog2e;
     static_assert(C::kSmem <= 227 * 1024, "shared memory of a CTA");
-    static_assert(2 * C::kPartFloats <= 8 * (128 * D + 256), "partial results of a CTA fit where the prompt kernels keep theirs");
+    static_assert(2 * kTeams * C::kPartFloats <= 8 * (128 * D + 256), "partial results of a CTA fit where the prompt kernels keep theirs");
+    static_assert(kTeams * kPromptCtas <= 2 * kMaxPieces, "a ticket per run");
     auto kern = kv8_decode_kernel<D>;
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
     if (e != cudaSuccess) return e;
