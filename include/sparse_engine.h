@@ -72,6 +72,7 @@ extern "C" {
 #define SE_DEV_BAD_SELECTION        2u  /* sel_idx entry outside the request / sel_cnt > k_max */
 #define SE_DEV_WAIT_TIMEOUT         4u  /* a bounded wait (200 ms) on an asynchronous copy gave up */
 #define SE_DEV_BAD_LENGTH           8u  /* prompt calls: cu_seqlens / seq_lens / pair_axis entry out of range */
+#define SE_DEV_NO_PAGES            16u  /* se_pages_update: fewer free pages than asked for, nothing was changed */
 
 typedef struct se_params {
     int32_t B;               /* requests in the batch, 1..8192                              */
@@ -507,6 +508,67 @@ int se_kv8_append(const se_params *p, const void *q, int64_t q_stride, const voi
 int se_kv8_decode(const se_params *p, const void *q, const void *k_cache, const void *v_cache, const float *scales,
                   const int32_t *page_table, const int32_t *seq_lens, const int32_t *sel_idx, const int32_t *sel_cnt,
                   float *out, float *lse, void *workspace, void *stream);
+
+/*
+ * The pool's pages: which request owns which physical page.  (Appendix A, "Logical Positions and Physical Blocks", has the
+ * mapping; the paper leaves the pool to the engine.)  They work on any cache of this library, or several at once: whatever has
+ * one entry per physical page is a buffer.
+ *   ref_count [P_phys] int32   entries of the page table that refer to a page, plus one for every other holder (a prefix cache
+ *                              that keeps a page alive); 0 = free
+ * A row of the page table owns its first ceil(seq_lens[r] / 16) entries; -1 among them is a page that was pruned.
+ * Of se_params they use B, max_pages and num_phys_pages; the other fields only have to be valid.  They take a workspace of
+ * their own kind: se_pages_workspace_bytes bytes (24 per page, and a little), initialised once by se_pages_workspace_init,
+ * then good for any number of calls with the same se_params that are ordered on the device; se_last_device_status reads its
+ * status word.  After a call that reported SE_DEV_WAIT_TIMEOUT it has to be initialised again: until then the calls do nothing
+ * and report it each time.  The kernels have grid-wide barriers (cooperative launches, at most one CTA per SM).
+ */
+#define SE_MAX_PAGE_BUFFERS 512
+typedef struct se_page_buffer {
+    void   *base;                /* device pointer, 16-byte aligned: page i is the bytes_per_page bytes from i * bytes_per_page on */
+    int64_t bytes_per_page;      /* a multiple of 4 (of 16: copied in wide pieces), at most 2^30                                  */
+} se_page_buffer;
+size_t se_pages_workspace_bytes(const se_params *p);
+int se_pages_workspace_init(const se_params *p, void *workspace, void *stream);
+
+/*
+ * Requests fork, end, shrink and grow.  Slot r of the batch goes on with the first keep = min(seq_lens[parent[r]], new_lens[r])
+ * tokens of slot parent[r] (-1: of nothing), and has room for new_lens[r] tokens afterwards:
+ *   page_table_out[r]    the parent's first ceil(keep / 16) entries, then new pages up to ceil(new_lens[r] / 16), then -1
+ *   seq_lens_out[r]      new_lens[r]
+ *   ref_count_out        with the entries of page_table_out in the place of those of page_table
+ * parent == NULL: every slot goes on with its own row.  Examples: parent[r] = r and new_lens[r] = seq_lens[r] + 1 before a decode
+ * step; parent[r] = -1, new_lens[r] = 0 ends a request and frees its pages; several slots with one parent fork it (beams, samples
+ * of one prompt); a smaller length takes back drafted tokens.
+ * Copy on write: a row that ends inside a page (keep not a multiple of 16) will write into it, so where anything else refers to that
+ * page the row gets a copy of it, in all `buffers` (host array of n_buffers <= SE_MAX_PAGE_BUFFERS; every layer's K, V, summaries,
+ * scales, ... of the pool).  Of rows that share the page only with rows that end inside it too, the first keeps it.  Whole pages stay
+ * shared.
+ * New pages are the lowest-numbered free ones, handed out slot by slot in ascending logical order (the copy of a slot's last page
+ * first); pages that this call frees count as free.  free_pages ([1], device) receives the number of free pages left.  If more are
+ * asked for than there are, nothing is changed - the outputs are the inputs, no buffer is written -, free_pages is negative (what is
+ * missing) and SE_DEV_NO_PAGES is reported.
+ * A slot with parent[r] outside -1 .. B-1, or a length outside 0 .. 16*max_pages, stays as it is and is reported
+ * (SE_DEV_BAD_LENGTH); an entry that is no page of the pool counts as absent, is carried along and reported (SE_DEV_BAD_PAGE_ID).
+ * The outputs may be the inputs themselves: ref_count_out always, the others only without `parent` (refused with it).
+ * New pages' contents are whatever they held before.
+ */
+int se_pages_update(const se_params *p, const int32_t *page_table, const int32_t *seq_lens, const int32_t *ref_count,
+                    const int32_t *parent, const int32_t *new_lens, int32_t *page_table_out, int32_t *seq_lens_out,
+                    int32_t *ref_count_out, int32_t *free_pages, const se_page_buffer *buffers, int32_t n_buffers,
+                    void *workspace, void *stream);
+
+/*
+ * Live pages (ref_count > 0) move to the front of the pool: with n of them, the i-th live page with a number >= n becomes the
+ * i-th free number below n, in all buffers, and everything from page n on is free.
+ *   page_table_out   the rows' entries with their pages' new numbers (entries behind a row's length are copied)
+ *   ref_count_out    the counts at the pages' new numbers
+ *   page_map         [P_phys] int32: new number of every live page, -1 for the others (for holders outside the page table)
+ *   live_pages       [1] int32: n
+ * page_table_out and ref_count_out may be the inputs themselves.
+ */
+int se_pages_compact(const se_params *p, const int32_t *page_table, const int32_t *seq_lens, const int32_t *ref_count,
+                     int32_t *page_table_out, int32_t *ref_count_out, int32_t *page_map, int32_t *live_pages,
+                     const se_page_buffer *buffers, int32_t n_buffers, void *workspace, void *stream);
 
 /*
  * Measurement aid (no counterpart in the paper): a read-only gather with the access pattern and

@@ -20,6 +20,7 @@ SE_DEV_BAD_PAGE_ID = 1
 SE_DEV_BAD_SELECTION = 2
 SE_DEV_WAIT_TIMEOUT = 4
 SE_DEV_BAD_LENGTH = 8
+SE_DEV_NO_PAGES = 16
 
 EXPORTS = ("se_version", "se_strerror", "se_workspace_bytes", "se_decode_num_splits", "se_workspace_init",
            "se_meta_update",
@@ -28,7 +29,8 @@ EXPORTS = ("se_version", "se_strerror", "se_workspace_bytes", "se_decode_num_spl
            "se_token_decode",
            "se_page_select_static", "se_decode_step", "se_decode_step_launches", "se_probe_gather",
            "se_prompt_workspace_bytes", "se_prompt_workspace_init", "se_rope_append", "se_chunk_attend",
-           "se_prompt_attend", "se_h2o_accumulate", "se_kv8_append", "se_kv8_decode")
+           "se_prompt_attend", "se_h2o_accumulate", "se_kv8_append", "se_kv8_decode", "se_pages_workspace_bytes",
+           "se_pages_workspace_init", "se_pages_update", "se_pages_compact")
 SE_STATIC_SCRATCH_BYTES = 4 * 1024 * 1024
 
 
@@ -38,6 +40,10 @@ class SeParams(ctypes.Structure):
                 ("num_phys_pages", ctypes.c_int32), ("k_max", ctypes.c_int32),
                 ("sm_scale", ctypes.c_float), ("flags", ctypes.c_uint32),
                 ("sink_pages", ctypes.c_int32), ("recent_pages", ctypes.c_int32)]
+
+
+class SePageBuffer(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("bytes_per_page", ctypes.c_int64)]
 
 
 class SparseEngineError(RuntimeError):
@@ -98,6 +104,11 @@ def load(build_if_missing: bool = True):
                                    vp, vp, vp, vp, vp, vp, vp]
     lib.se_kv8_append.argtypes = lib.se_rope_append.argtypes[:-2] + [vp, vp, vp]
     lib.se_kv8_decode.argtypes = [pp, vp, vp, vp, fp, i32p, i32p, i32p, i32p, fp, fp, vp, vp]
+    lib.se_pages_workspace_bytes.restype = ctypes.c_size_t
+    lib.se_pages_workspace_bytes.argtypes = [pp]
+    lib.se_pages_workspace_init.argtypes = [pp, vp, vp]
+    lib.se_pages_update.argtypes = [pp] + [i32p] * 9 + [vp, i32, vp, vp]
+    lib.se_pages_compact.argtypes = [pp] + [i32p] * 7 + [vp, i32, vp, vp]
     lib.se_chunk_attend.argtypes = [pp, vp, i64, i32, i32p, vp, vp, i32p, i32p, vp, fp, vp, vp]
     lib.se_prompt_attend.argtypes = [pp, vp, i64, vp, i64, vp, i64, i32, i32p, vp, fp, vp, vp]
     lib.se_h2o_accumulate.argtypes = [pp, vp, i64, i32, i32p, vp, i32p, i32p, fp, fp, vp, vp]
@@ -106,7 +117,8 @@ def load(build_if_missing: bool = True):
                  "se_h2o_retain", "se_h2o_compact", "se_decode_num_splits", "se_page_select_static",
                  "se_observe_decode", "se_token_select", "se_token_decode", "se_page_select_scores",
                  "se_page_select_topk", "se_decode_step", "se_decode_step_launches", "se_prompt_workspace_init",
-                 "se_rope_append", "se_chunk_attend", "se_prompt_attend", "se_h2o_accumulate", "se_kv8_append", "se_kv8_decode"):
+                 "se_rope_append", "se_chunk_attend", "se_prompt_attend", "se_h2o_accumulate", "se_kv8_append", "se_kv8_decode", "se_pages_workspace_bytes",
+           "se_pages_workspace_init", "se_pages_update", "se_pages_compact"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -518,6 +530,85 @@ def se_kv8_decode(p, q, k_cache, v_cache, scales, page_table, seq_lens, out, lse
           ctypes.byref(p), _ptr(q, torch.bfloat16, "q"), _ptr(k_cache, codes, "k_cache"), _ptr(v_cache, codes, "v_cache"),
           _ptr(scales, f32, "scales"), _ptr(page_table, i32, "page_table"), _ptr(seq_lens, i32, "seq_lens"), _ptr(sel_idx, i32, "sel_idx"),
           _ptr(sel_cnt, i32, "sel_cnt"), _ptr(out, f32, "out"), _ptr(lse, f32, "lse"))
+
+
+# ---- the pool's pages --------------------------------------------------------------------------------
+
+def se_pages_workspace_bytes(p: SeParams) -> int:
+    return int(load().se_pages_workspace_bytes(ctypes.byref(p)))
+
+
+def se_pages_workspace_init(p: SeParams, workspace: torch.Tensor) -> None:
+    with torch.cuda.device(workspace.device):
+        _check(load().se_pages_workspace_init(ctypes.byref(p), _ptr(workspace, torch.uint8, "workspace"), _stream()),
+               "se_pages_workspace_init")
+
+
+def alloc_pages_workspace(p: SeParams, device="cuda") -> torch.Tensor:
+    """Allocates (through torch) and initialises a workspace of the page calls for ``p``."""
+    n = se_pages_workspace_bytes(p)
+    if n == 0:
+        raise SparseEngineError("invalid se_params")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    se_pages_workspace_init(p, ws)
+    return ws
+
+
+class PageBuffers:
+    """What moves with a page: contiguous CUDA tensors [num_phys_pages, ...] of any type (every layer's K, V, summaries,
+    scales, statistics of one pool).  Made once, used by every call."""
+
+    def __init__(self, tensors):
+        self.tensors = tuple(tensors)
+        self.entries = (SePageBuffer * max(1, len(self.tensors)))()
+        for i, t in enumerate(self.tensors):
+            if not t.is_cuda or not t.is_contiguous() or t.dim() < 1 or t.shape[0] < 1 or t.device != self.tensors[0].device:
+                raise SparseEngineError("page buffers must be contiguous CUDA tensors [num_phys_pages, ...] on one device")
+            self.entries[i] = SePageBuffer(t.data_ptr(), t.numel() // t.shape[0] * t.element_size())
+
+
+def page_buffers(tensors) -> PageBuffers:
+    return tensors if isinstance(tensors, PageBuffers) else PageBuffers(tensors)
+
+
+def _pages_common(p, workspace, page_table, seq_lens, ref_count, buffers) -> PageBuffers:
+    _shape(page_table, (p.B, p.max_pages), "page_table")
+    _shape(seq_lens, (p.B,), "seq_lens")
+    _shape(ref_count, (p.num_phys_pages,), "ref_count")
+    if workspace.numel() < se_pages_workspace_bytes(p):
+        raise SparseEngineError("workspace is smaller than se_pages_workspace_bytes")
+    buffers = page_buffers(buffers)
+    for t in buffers.tensors:
+        if t.shape[0] != p.num_phys_pages:
+            raise SparseEngineError("a page buffer must have %d pages, got shape %s" % (p.num_phys_pages, list(t.shape)))
+    return buffers
+
+
+def se_pages_update(p, page_table, seq_lens, ref_count, new_lens, page_table_out, seq_lens_out, ref_count_out, free_pages, workspace,
+                    parent=None, buffers=()) -> None:
+    """Slot r goes on with row parent[r], cut or grown to new_lens[r] tokens; open pages that others refer to are copied in all
+    ``buffers`` (tensors [num_phys_pages, ...], or a ``page_buffers`` handle)."""
+    buffers = _pages_common(p, workspace, page_table, seq_lens, ref_count, buffers)
+    for t, like, name in ((new_lens, seq_lens, "new_lens"), (parent, seq_lens, "parent"), (page_table_out, page_table, "page_table_out"),
+                          (seq_lens_out, seq_lens, "seq_lens_out"), (ref_count_out, ref_count, "ref_count_out")):
+        _shape(t, tuple(like.shape), name)
+    _shape(free_pages, (1,), "free_pages")
+    tensors = (page_table, seq_lens, ref_count, parent, new_lens, page_table_out, seq_lens_out, ref_count_out, free_pages)
+    _call("se_pages_update", workspace, tensors + buffers.tensors[:1], ctypes.byref(p),
+          *[_ptr(t, torch.int32, "page table, lengths and counts") for t in tensors], buffers.entries, len(buffers.tensors))
+
+
+def se_pages_compact(p, page_table, seq_lens, ref_count, page_table_out, ref_count_out, page_map, live_pages, workspace,
+                     buffers=()) -> None:
+    """Live pages to the front of the pool, in all ``buffers``."""
+    buffers = _pages_common(p, workspace, page_table, seq_lens, ref_count, buffers)
+    for t, like, name in ((page_table_out, page_table, "page_table_out"), (ref_count_out, ref_count, "ref_count_out"),
+                          (page_map, ref_count, "page_map")):
+        _shape(t, tuple(like.shape), name)
+    _shape(live_pages, (1,), "live_pages")
+    tensors = (page_table, seq_lens, ref_count, page_table_out, ref_count_out, page_map, live_pages)
+    _call("se_pages_compact", workspace, tensors + buffers.tensors[:1], ctypes.byref(p),
+          *[_ptr(t, torch.int32, "page table, lengths and counts") for t in tensors], buffers.entries, len(buffers.tensors))
 
 
 def se_last_device_status(workspace) -> int:

@@ -590,6 +590,80 @@ int se_kv8_decode(const se_params *p, const void *q, const void *k_cache, const 
     return e == cudaSuccess ? SE_OK : SE_ERR_CUDA;
 }
 
+// ---- the pool's pages ----
+size_t se_pages_workspace_bytes(const se_params *p) {
+    if (validate(p) != SE_OK) return 0;
+    return pages_workspace_bytes(*p);
+}
+
+int se_pages_workspace_init(const se_params *p, void *workspace, void *stream) {
+    int rc = validate(p);
+    if (rc != SE_OK) return rc;
+    if (!workspace) return SE_ERR_NULL_POINTER;
+    if (!aligned16(workspace)) return SE_ERR_MISALIGNED;
+    cudaError_t e = cudaMemsetAsync(workspace, 0, pages_workspace_zeroed_bytes(*p), static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? SE_OK : SE_ERR_CUDA;
+}
+
+static int check_buffers(const se_page_buffer *buffers, int32_t n) {
+    if (n < 0 || n > SE_MAX_PAGE_BUFFERS) return SE_ERR_INVALID_ARG;
+    if (n > 0 && !buffers) return SE_ERR_NULL_POINTER;
+    int64_t all = 0;
+    for (int32_t k = 0; k < n; ++k) {
+        if (!buffers[k].base) return SE_ERR_NULL_POINTER;
+        if (!aligned16(buffers[k].base)) return SE_ERR_MISALIGNED;
+        if (buffers[k].bytes_per_page < 4 || buffers[k].bytes_per_page % 4 != 0 || buffers[k].bytes_per_page > (1ll << 30))
+            return SE_ERR_INVALID_ARG;
+        all += buffers[k].bytes_per_page;
+    }
+    return all > (1ll << 40) ? SE_ERR_INVALID_ARG : SE_OK;     // pieces of a page are counted in 32 bits
+}
+
+int se_pages_update(const se_params *p, const int32_t *page_table, const int32_t *seq_lens, const int32_t *ref_count,
+                    const int32_t *parent, const int32_t *new_lens, int32_t *page_table_out, int32_t *seq_lens_out,
+                    int32_t *ref_count_out, int32_t *free_pages, const se_page_buffer *buffers, int32_t n_buffers,
+                    void *workspace, void *stream) {
+    int rc = validate(p);
+    if (rc != SE_OK) return rc;
+    if (!page_table || !seq_lens || !ref_count || !new_lens || !page_table_out || !seq_lens_out || !ref_count_out ||
+        !free_pages || !workspace)
+        return SE_ERR_NULL_POINTER;
+    if (!aligned16(page_table) || !aligned16(seq_lens) || !aligned16(ref_count) || !aligned16(parent) || !aligned16(new_lens) ||
+        !aligned16(page_table_out) || !aligned16(seq_lens_out) || !aligned16(ref_count_out) || !aligned16(free_pages) ||
+        !aligned16(workspace))
+        return SE_ERR_MISALIGNED;
+    rc = check_buffers(buffers, n_buffers);
+    if (rc != SE_OK) return rc;
+    // rows that go to other slots are read after some have been written
+    if (parent && (page_table_out == page_table || seq_lens_out == seq_lens)) return SE_ERR_INVALID_ARG;
+    PagesUpdateCall c = {};
+    c.page_table = page_table, c.seq_lens = seq_lens, c.ref_count = ref_count, c.parent = parent, c.new_lens = new_lens;
+    c.page_table_out = page_table_out, c.seq_lens_out = seq_lens_out, c.ref_count_out = ref_count_out, c.free_pages = free_pages;
+    c.buffers = buffers, c.n_buffers = n_buffers, c.workspace = static_cast<uint8_t *>(workspace);
+    cudaError_t e = launch_pages_update(*p, c, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? SE_OK : SE_ERR_CUDA;
+}
+
+int se_pages_compact(const se_params *p, const int32_t *page_table, const int32_t *seq_lens, const int32_t *ref_count,
+                     int32_t *page_table_out, int32_t *ref_count_out, int32_t *page_map, int32_t *live_pages,
+                     const se_page_buffer *buffers, int32_t n_buffers, void *workspace, void *stream) {
+    int rc = validate(p);
+    if (rc != SE_OK) return rc;
+    if (!page_table || !seq_lens || !ref_count || !page_table_out || !ref_count_out || !page_map || !live_pages || !workspace)
+        return SE_ERR_NULL_POINTER;
+    if (!aligned16(page_table) || !aligned16(seq_lens) || !aligned16(ref_count) || !aligned16(page_table_out) ||
+        !aligned16(ref_count_out) || !aligned16(page_map) || !aligned16(live_pages) || !aligned16(workspace))
+        return SE_ERR_MISALIGNED;
+    rc = check_buffers(buffers, n_buffers);
+    if (rc != SE_OK) return rc;
+    PagesCompactCall c = {};
+    c.page_table = page_table, c.seq_lens = seq_lens, c.ref_count = ref_count;
+    c.page_table_out = page_table_out, c.ref_count_out = ref_count_out, c.page_map = page_map, c.live_pages = live_pages;
+    c.buffers = buffers, c.n_buffers = n_buffers, c.workspace = static_cast<uint8_t *>(workspace);
+    cudaError_t e = launch_pages_compact(*p, c, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? SE_OK : SE_ERR_CUDA;
+}
+
 int se_last_device_status(void *workspace, void *stream, int32_t *host_out) {
     if (!workspace || !host_out) return SE_ERR_NULL_POINTER;
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -119,6 +119,26 @@ struct Kv8DecodeCall {
     uint8_t *workspace;
 };
 cudaError_t launch_kv8_decode(const se_params &p, const Kv8DecodeCall &c, cudaStream_t stream);
+
+// the pool's pages
+struct PagesUpdateCall {
+    const int32_t *page_table, *seq_lens, *ref_count, *parent, *new_lens;   // parent nullptr: every slot goes on with its own row
+    int32_t *page_table_out, *seq_lens_out, *ref_count_out, *free_pages;
+    const se_page_buffer *buffers;
+    int n_buffers;
+    uint8_t *workspace;
+};
+struct PagesCompactCall {
+    const int32_t *page_table, *seq_lens, *ref_count;
+    int32_t *page_table_out, *ref_count_out, *page_map, *live_pages;
+    const se_page_buffer *buffers;
+    int n_buffers;
+    uint8_t *workspace;
+};
+cudaError_t launch_pages_update(const se_params &p, const PagesUpdateCall &c, cudaStream_t stream);
+cudaError_t launch_pages_compact(const se_params &p, const PagesCompactCall &c, cudaStream_t stream);
+size_t pages_workspace_bytes(const se_params &p);
+size_t pages_workspace_zeroed_bytes(const se_params &p);
 size_t prompt_workspace_bytes(const se_params &p);
 size_t prompt_workspace_control_bytes();
 
