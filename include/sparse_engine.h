@@ -510,6 +510,14 @@ int se_kv8_decode(const se_params *p, const void *q, const void *k_cache, const 
                   float *out, float *lse, void *workspace, void *stream);
 
 /*
+ * se_chunk_attend over an 8-bit cache: same arguments and rules, codes and scales in the place of the bf16 pages.  The codes' values
+ * are exact in bf16, so out and lse are, bit for bit, what se_chunk_attend gives over a bf16 cache that holds them.
+ */
+int se_kv8_chunk_attend(const se_params *p, const void *q, int64_t q_stride, int32_t total_tokens, const int32_t *cu_seqlens,
+                        const void *k_cache, const void *v_cache, const float *scales, const int32_t *page_table,
+                        const int32_t *seq_lens, void *out, float *lse, void *workspace, void *stream);
+
+/*
  * The pool's pages: which request owns which physical page.  (Appendix A, "Logical Positions and Physical Blocks", has the
  * mapping; the paper leaves the pool to the engine.)  They work on any cache of this library, or several at once: whatever has
  * one entry per physical page is a buffer.

@@ -29,7 +29,8 @@ EXPORTS = ("se_version", "se_strerror", "se_workspace_bytes", "se_decode_num_spl
            "se_token_decode",
            "se_page_select_static", "se_decode_step", "se_decode_step_launches", "se_probe_gather",
            "se_prompt_workspace_bytes", "se_prompt_workspace_init", "se_rope_append", "se_chunk_attend",
-           "se_prompt_attend", "se_h2o_accumulate", "se_kv8_append", "se_kv8_decode", "se_pages_workspace_bytes",
+           "se_prompt_attend", "se_h2o_accumulate", "se_kv8_append", "se_kv8_decode", "se_kv8_chunk_attend",
+           "se_pages_workspace_bytes",
            "se_pages_workspace_init", "se_pages_update", "se_pages_compact")
 SE_STATIC_SCRATCH_BYTES = 4 * 1024 * 1024
 
@@ -110,6 +111,7 @@ def load(build_if_missing: bool = True):
     lib.se_pages_update.argtypes = [pp] + [i32p] * 9 + [vp, i32, vp, vp]
     lib.se_pages_compact.argtypes = [pp] + [i32p] * 7 + [vp, i32, vp, vp]
     lib.se_chunk_attend.argtypes = [pp, vp, i64, i32, i32p, vp, vp, i32p, i32p, vp, fp, vp, vp]
+    lib.se_kv8_chunk_attend.argtypes = [pp, vp, i64, i32, i32p, vp, vp, fp, i32p, i32p, vp, fp, vp, vp]
     lib.se_prompt_attend.argtypes = [pp, vp, i64, vp, i64, vp, i64, i32, i32p, vp, fp, vp, vp]
     lib.se_h2o_accumulate.argtypes = [pp, vp, i64, i32, i32p, vp, i32p, i32p, fp, fp, vp, vp]
     for name in ("se_workspace_init", "se_meta_update", "se_page_select", "se_page_select_fused",
@@ -117,7 +119,8 @@ def load(build_if_missing: bool = True):
                  "se_h2o_retain", "se_h2o_compact", "se_decode_num_splits", "se_page_select_static",
                  "se_observe_decode", "se_token_select", "se_token_decode", "se_page_select_scores",
                  "se_page_select_topk", "se_decode_step", "se_decode_step_launches", "se_prompt_workspace_init",
-                 "se_rope_append", "se_chunk_attend", "se_prompt_attend", "se_h2o_accumulate", "se_kv8_append", "se_kv8_decode", "se_pages_workspace_bytes",
+                 "se_rope_append", "se_chunk_attend", "se_prompt_attend", "se_h2o_accumulate", "se_kv8_append", "se_kv8_decode", "se_kv8_chunk_attend",
+           "se_pages_workspace_bytes",
            "se_pages_workspace_init", "se_pages_update", "se_pages_compact"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
@@ -530,6 +533,23 @@ def se_kv8_decode(p, q, k_cache, v_cache, scales, page_table, seq_lens, out, lse
           ctypes.byref(p), _ptr(q, torch.bfloat16, "q"), _ptr(k_cache, codes, "k_cache"), _ptr(v_cache, codes, "v_cache"),
           _ptr(scales, f32, "scales"), _ptr(page_table, i32, "page_table"), _ptr(seq_lens, i32, "seq_lens"), _ptr(sel_idx, i32, "sel_idx"),
           _ptr(sel_cnt, i32, "sel_cnt"), _ptr(out, f32, "out"), _ptr(lse, f32, "lse"))
+
+
+def se_kv8_chunk_attend(p, q, cu_seqlens, k_cache, v_cache, scales, page_table, seq_lens, out, workspace, lse=None) -> None:
+    """``se_chunk_attend`` over an 8-bit cache."""
+    T, H_q, D = q.shape[0], p.H_q, p.D
+    _prompt_common(p, workspace, cu_seqlens, page_table, seq_lens, k_cache, v_cache)
+    _shape(scales, (p.num_phys_pages, p.H_kv, 2), "scales")
+    _shape(out, (T, H_q, D), "out")
+    _shape(lse, (T, H_q), "lse")
+    qp, qs = _rows(q, H_q, D, "q")
+    if T == 0:           # an empty tensor has no address
+        return
+    i32, codes = torch.int32, torch.float8_e4m3fn
+    _call("se_kv8_chunk_attend", workspace, (q, cu_seqlens, k_cache, v_cache, scales, page_table, seq_lens, out, lse),
+          ctypes.byref(p), qp, qs, T, _ptr(cu_seqlens, i32, "cu_seqlens"), _ptr(k_cache, codes, "k_cache"), _ptr(v_cache, codes, "v_cache"),
+          _ptr(scales, torch.float32, "scales"), _ptr(page_table, i32, "page_table"), _ptr(seq_lens, i32, "seq_lens"),
+          _ptr(out, torch.bfloat16, "out"), _ptr(lse, torch.float32, "lse"))
 
 
 # ---- the pool's pages --------------------------------------------------------------------------------

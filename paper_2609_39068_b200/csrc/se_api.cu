@@ -494,9 +494,9 @@ int se_rope_append(const se_params *p, const void *q, int64_t q_stride, const vo
                        workspace, stream);
 }
 
-int se_chunk_attend(const se_params *p, const void *q, int64_t q_stride, int32_t total_tokens,
+static int chunk_attend(const se_params *p, const void *q, int64_t q_stride, int32_t total_tokens,
                     const int32_t *cu_seqlens, const void *k_cache, const void *v_cache,
-                    const int32_t *page_table, const int32_t *seq_lens, void *out, float *lse, void *workspace,
+                    const int32_t *page_table, const int32_t *seq_lens, void *out, float *lse, const float *scales, void *workspace,
                     void *stream) {
     int rc = validate(p);
     if (rc != SE_OK) return rc;
@@ -510,9 +510,17 @@ int se_chunk_attend(const se_params *p, const void *q, int64_t q_stride, int32_t
     AttendCall c = {};
     c.q = q, c.k = k_cache, c.v = v_cache, c.q_stride = q_stride, c.total_tokens = total_tokens;
     c.cu_seqlens = cu_seqlens, c.seq_lens = seq_lens, c.page_table = page_table;
-    c.out = out, c.lse = lse, c.workspace = static_cast<uint8_t *>(workspace);
+    c.out = out, c.lse = lse, c.workspace = static_cast<uint8_t *>(workspace), c.scales = scales;
     cudaError_t e = launch_prompt_attend(*p, c, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? SE_OK : SE_ERR_CUDA;
+}
+
+int se_chunk_attend(const se_params *p, const void *q, int64_t q_stride, int32_t total_tokens,
+                    const int32_t *cu_seqlens, const void *k_cache, const void *v_cache,
+                    const int32_t *page_table, const int32_t *seq_lens, void *out, float *lse, void *workspace,
+                    void *stream) {
+    return chunk_attend(p, q, q_stride, total_tokens, cu_seqlens, k_cache, v_cache, page_table, seq_lens, out, lse, nullptr,
+                        workspace, stream);
 }
 
 int se_prompt_attend(const se_params *p, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
@@ -588,6 +596,17 @@ int se_kv8_decode(const se_params *p, const void *q, const void *k_cache, const 
     c.sel_idx = sel_idx, c.sel_cnt = sel_cnt, c.out = out, c.lse = lse, c.workspace = static_cast<uint8_t *>(workspace);
     cudaError_t e = launch_kv8_decode(*p, c, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? SE_OK : SE_ERR_CUDA;
+}
+
+int se_kv8_chunk_attend(const se_params *p, const void *q, int64_t q_stride, int32_t total_tokens, const int32_t *cu_seqlens,
+                        const void *k_cache, const void *v_cache, const float *scales, const int32_t *page_table,
+                        const int32_t *seq_lens, void *out, float *lse, void *workspace, void *stream) {
+    int rc = validate(p);
+    if (rc != SE_OK) return rc;
+    if (!scales) return SE_ERR_NULL_POINTER;
+    if (!aligned16(scales)) return SE_ERR_MISALIGNED;
+    return chunk_attend(p, q, q_stride, total_tokens, cu_seqlens, k_cache, v_cache, page_table, seq_lens, out, lse, scales,
+                        workspace, stream);
 }
 
 // ---- the pool's pages ----

@@ -31,6 +31,7 @@
 #include <math.h>
 
 #include "se_internal.h"
+#include "se_kv8.cuh"
 #include "se_pieces.cuh"
 #include "se_tc.cuh"
 
@@ -56,12 +57,14 @@ constexpr int kMinCost = 256, kCoarse = 2048;
 // tokens is far from the end of the range).
 constexpr float kSlack = 40.f;
 
-template <int D>
+template <int D, bool KV8>
 struct Cfg {
     static constexpr int kHalves = D / 64;
     static constexpr int kTileBytes = kTile * D * 2;              // query tile
     static constexpr int kKvBytes = kKv * D * 2;                  // K or V tile
-    static constexpr int kKSlots = 2 * 128 / D, kVSlots = 3 * 128 / D;   // rings of K and V tiles, 64 and 96 KB
+    // rings of K and V tiles, 64 and 96 KB; from an 8-bit cache 64 each, and rings of its pages, 14 KB each
+    static constexpr int kKSlots = 2 * 128 / D, kVSlots = (KV8 ? 2 : 3) * 128 / D;
+    static constexpr int kRawSlots = KV8 ? 7 * 128 / D : 0, kRawBytes = kPage * D;
     static constexpr int kSlots = kKSlots + kVSlots;
     static constexpr int kMasks = 16;
     static constexpr int kSlotFloats = kTile * D + 2 * kTile;     // a partial result: O, m, l
@@ -71,6 +74,8 @@ struct Cfg {
 struct AttendArgs {
     const int32_t *cu, *seq_lens, *page_table;
     const uint16_t *v;                 // rows of the last, partly filled 16-token group are copied by hand
+    const uint8_t *k8, *v8;            // 8-bit cache: codes, and scales of K and V
+    const float2 *scales;
     long long v_stride;                // contiguous V: elements between tokens
     uint16_t *out;
     float *lse;
@@ -134,12 +139,13 @@ struct Segment {
     __device__ __forceinline__ int steps(int st) const { return st ? steps1 : steps0; }
 };
 
-template <int D>
+template <int D, bool KV8>
 struct Control {
-    uint64_t bars[kRing + 2 * Cfg<D>::kSlots];
+    uint64_t bars[kRing + 2 * Cfg<D, KV8>::kSlots];
+    uint64_t raw[KV8 ? 2 * Cfg<D, KV8>::kRawSlots : 1];            // 8-bit cache: pages of K, of V have come
     SegmentQueue<Segment> queue;
     alignas(8) uint8_t prefix[prefix_bytes(kSmemRequests)];
-    uint32_t mask[Cfg<D>::kMasks];     // present 16-token groups of the tiles in flight
+    uint32_t mask[Cfg<D, KV8>::kMasks];     // present 16-token groups of the tiles in flight
     int parts[2];                      // partial results to merge, 0: another CTA does
     uint16_t part[2][kMaxParts];
     int gave_up;
@@ -221,8 +227,8 @@ __device__ __forceinline__ void leave_ring(bool ok, uint32_t filled, uint32_t fu
 
 template <int D>
 __device__ __forceinline__ void k_role(const AttendArgs &a, const List<AttendWork> &list, const CUtensorMap *q_map, const CUtensorMap *k_map,
-                                       const CUtensorMap *k_wide, Control<D> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars, int lane) {
-    using C = Cfg<D>;
+                                       const CUtensorMap *k_wide, Control<D, false> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars, int lane) {
+    using C = Cfg<D, false>;
     volatile int *gave_up = &ctl->gave_up;
     const int tpt = kTile / a.G;
     Segment s;
@@ -286,9 +292,9 @@ __device__ __forceinline__ void k_role(const AttendArgs &a, const List<AttendWor
 }
 
 template <int D>
-__device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v_map, const CUtensorMap *v_wide, Control<D> *ctl, uint32_t ring,
+__device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v_map, const CUtensorMap *v_wide, Control<D, false> *ctl, uint32_t ring,
                                        uint32_t bars, int lane) {
-    using C = Cfg<D>;
+    using C = Cfg<D, false>;
     volatile int *gave_up = &ctl->gave_up;
     Segment s;
     Pages pages;
@@ -360,15 +366,204 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v
     leave_ring<C::kVSlots>(ok, tiles, v_full, v_empty, gave_up, a);
 }
 
+// ---- an 8-bit cache ------------------------------------------------------------------
+// The same two warps, one for K and one for V, bring pages of codes into a ring of their own (a bulk copy each, a tile ahead), turn them
+// into bf16 (exact, as the scales are powers of two) and write the tiles that the tensor copies would: everything behind them is
+// the same, and so are the results, bit for bit, as over a bf16 cache that holds the codes' values.
+//
+// Page ids and scales of 32 groups of 16 tokens at a time, a lane each, and of the next 32 ahead.
+struct CodePages {
+    int ids, next, block;
+    float scale, next_scale;
+
+    __device__ __forceinline__ void fetch(const AttendArgs &a, const Segment &s, int g, bool of_v, int &id, float &sc) const {
+        id = -1, sc = 0.f;
+        if (g * kPage >= s.t.past + s.t.n) return;
+        const int pid = a.page_table[(size_t)s.r * a.max_pages + g];
+        if (pid >= a.P_phys && !of_v) atomicOr(&a.ctl->status, SE_DEV_BAD_PAGE_ID);
+        if (pid < 0 || pid >= a.P_phys) return;
+        id = pid * a.H_kv + s.h;
+        const float2 both = a.scales[id];
+        sc = of_v ? both.y : both.x;
+    }
+    __device__ __forceinline__ void begin(const AttendArgs &a, const Segment &s, int tile, bool of_v, int lane) {
+        block = tile / (32 / kGroups);
+        fetch(a, s, block * 32 + lane, of_v, ids, scale);
+        fetch(a, s, block * 32 + 32 + lane, of_v, next, next_scale);
+    }
+    __device__ __forceinline__ void reach(const AttendArgs &a, const Segment &s, int tile, bool of_v, int lane) {
+        if (tile / (32 / kGroups) == block) return;
+        ++block;
+        ids = next, scale = next_scale;
+        fetch(a, s, block * 32 + 32 + lane, of_v, next, next_scale);
+    }
+    // group g of this block or the next
+    __device__ __forceinline__ int of(int g) const { return __shfl_sync(kFull, g / 32 == block ? ids : next, g % 32); }
+};
+
+// The tiles of one segment.  `filled`: tiles of K or V so far; `sent`, `used`: pages whose copy has been issued, that have been turned.
+template <int D, bool OF_V>
+__device__ __forceinline__ bool code_tiles(const AttendArgs &a, const Segment &s, Control<D, true> *ctl, CodePages &pages, uint32_t raw,
+                                           uint32_t tiles_at, uint32_t full, uint32_t empty, uint32_t &filled, uint32_t &sent, uint32_t &used,
+                                           bool chosen, int lane) {
+    using C = Cfg<D, true>;
+    constexpr uint32_t kSlots = OF_V ? C::kVSlots : C::kKSlots;
+    volatile int *gave_up = &ctl->gave_up;
+    const uint32_t raw_bars = smem_u32(ctl->raw) + (OF_V ? 8 * C::kRawSlots : 0);
+    const int stop = s.t.past + s.t.n;
+    int ahead = s.a * kGroups;                                             // next group whose copy is to be issued
+    pages.begin(a, s, s.a, OF_V, lane);
+    auto send = [&] {
+        while (ahead < s.b * kGroups && sent - used < (uint32_t)C::kRawSlots && ahead / 32 <= pages.block + 1) {
+            const int id = pages.of(ahead);
+            if (id >= 0) {
+                if (chosen) {
+                    const uint32_t slot = sent % C::kRawSlots;
+                    mbar_expect_tx(raw_bars + 8 * slot, C::kRawBytes + ((D == 128) == OF_V && sent == 0 ? kTestExtraTx : 0));
+                    bulk_g2s(raw + slot * C::kRawBytes, (OF_V ? a.v8 : a.k8) + (size_t)id * C::kRawBytes, C::kRawBytes, raw_bars + 8 * slot);
+                }
+                __syncwarp();
+                ++sent;
+            }
+            ++ahead;
+        }
+    };
+    send();
+    // lane -> token and 16 codes of it: eight lanes store to all banks, whatever the swizzle
+    const int row = lane >> 2, part = lane & 3;
+    for (int t = s.a; t < s.b; ++t, ++filled) {
+        const uint32_t slot = filled % kSlots, dst = tiles_at + slot * C::kKvBytes;
+        pages.reach(a, s, t, OF_V, lane);
+        send();
+        if (!warp_wait(empty + 8 * slot, (filled / kSlots & 1) ^ 1, gave_up, &a.ctl->status)) return false;
+        const unsigned mask = __ballot_sync(kFull, pages.ids >= 0) >> t % (32 / kGroups) * kGroups & 0xffu;
+        if (!OF_V && chosen) ctl->mask[filled % C::kMasks] = mask;
+#pragma unroll 1
+        for (int pg = 0; pg < kGroups; ++pg) {
+            const uint32_t page_at = dst + (OF_V ? pg * (kPage * D * 2) : pg * (kPage * 128));
+            constexpr uint32_t half_step = OF_V ? kPage * 128 : kKv * 128;
+            constexpr int N = D / 32;                                      // pieces of 16 codes per lane
+            const bool here = mask >> pg & 1;
+            if (!here && !OF_V) continue;                                  // (scores of absent groups are overwritten)
+            uint4 x[N];
+            __nv_bfloat162 f = __float2bfloat162_rn(0.f);
+            if (here) {
+                const uint32_t from = used % C::kRawSlots;
+                if (!warp_wait(raw_bars + 8 * from, used / C::kRawSlots & 1, gave_up, &a.ctl->status)) return false;
+                f = __float2bfloat162_rn(__shfl_sync(kFull, pages.scale, (t * kGroups + pg) % 32) * kv8_bf16_step());
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int token = row + 8 * (i / (D / 64)), c = part + 4 * (i % (D / 64));
+                    const uint32_t at = raw + from * C::kRawBytes + token * D + c * 16;
+                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[i].x), "=r"(x[i].y), "=r"(x[i].z), "=r"(x[i].w) : "r"(at));
+                }
+                __syncwarp();
+                ++used;
+                send();
+            }
+            // what lies behind the end of the request may be anything, and a weight of zero would not hide it
+            const int tokens = here ? min(kPage, stop - (t * kGroups + pg) * kPage) : 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int token = row + 8 * (i / (D / 64)), half = i % (D / 64);
+                if (OF_V && token >= tokens) x[i] = make_uint4(0, 0, 0, 0);
+                const uint32_t at = page_at + half * half_step + token * 128;
+                const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                uint32_t o[8];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) kv8_bf16x4(w[j], f, o[2 * j], o[2 * j + 1]);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + (((2 * part + j) ^ (token & 7)) << 4)), "r"(o[4 * j]), "r"(o[4 * j + 1]),
+                                 "r"(o[4 * j + 2]), "r"(o[4 * j + 3])
+                                 : "memory");
+            }
+        }
+        fence_async_proxy();
+        __syncwarp();
+        if (chosen) mbar_arrive(full + 8 * slot);
+        __syncwarp();
+    }
+    return true;
+}
+
+// The end of a warp that has filled `filled` slots: the products' arrivals for them, and its copies.
+template <int D, bool OF_V>
+__device__ __forceinline__ void leave_codes(bool ok, Control<D, true> *ctl, uint32_t filled, uint32_t empty, uint32_t sent, uint32_t used,
+                                            const AttendArgs &a) {
+    using C = Cfg<D, true>;
+    constexpr uint32_t kSlots = OF_V ? C::kVSlots : C::kKSlots;
+    for (uint32_t n = filled > kSlots ? filled - kSlots : 0; ok && n < filled; ++n)
+        ok = warp_wait(empty + 8 * (n % kSlots), n / kSlots & 1, &ctl->gave_up, &a.ctl->status);
+    const uint32_t raw_bars = smem_u32(ctl->raw) + (OF_V ? 8 * C::kRawSlots : 0);
+    for (; used != sent; ++used) mbar_wait(raw_bars + 8 * (used % C::kRawSlots), used / C::kRawSlots & 1);
+}
+
+template <int D>
+__device__ __forceinline__ void k8_role(const AttendArgs &a, const List<AttendWork> &list, const CUtensorMap *q_map, Control<D, true> *ctl,
+                                        uint32_t q_smem, uint32_t ring, uint32_t raw, uint32_t bars, int lane) {
+    using C = Cfg<D, true>;
+    volatile int *gave_up = &ctl->gave_up;
+    const int tpt = kTile / a.G;
+    Segment s;
+    CodePages pages;
+    uint32_t tiles = 0, queries = 0, sent = 0, used = 0;
+    const uint32_t k_full = bars + 8 * kRing, k_empty = k_full + 8 * C::kSlots;
+    const bool chosen = elect_one();
+    bool ok = true;
+    Walk<AttendWork> walk(list, a.ctl, lane);
+    while (ok && next_segment(walk, s)) {
+        ok = ctl->queue.put(queries, &s, gave_up, &a.ctl->status, lane);
+        if (!ok) break;
+        ok = warp_wait(bars + 8 * kQEmpty, (queries & 1) ^ 1, gave_up, &a.ctl->status);
+        if (!ok) break;
+        if (chosen) {
+            mbar_expect_tx(bars + 8 * kQFull, (s.alt ? 1 : 2) * tpt * a.G * D * 2);
+            for (int st = 0; st < (s.alt ? 1 : 2); ++st)
+                for (int half = 0; half < C::kHalves; ++half)
+                    tma_load_3d(q_smem + st * C::kTileBytes + half * (kTile * 128), q_map, half * 64, s.h * a.G,
+                                s.t.start + s.tok0 + st * tpt, bars + 8 * kQFull);
+        }
+        __syncwarp();
+        ++queries;
+        ok = code_tiles<D, false>(a, s, ctl, pages, raw, ring, k_full, k_empty, tiles, sent, used, chosen, lane);
+    }
+    if (ok) ok = ctl->queue.put(queries, nullptr, gave_up, &a.ctl->status, lane);
+    leave_codes<D, false>(ok, ctl, tiles, k_empty, sent, used, a);
+    if (queries) {
+        ok = ok && warp_wait(bars + 8 * kQEmpty, (queries - 1) & 1, gave_up, &a.ctl->status);
+        if (!ok) mbar_wait(bars + 8 * kQFull, (queries - 1) & 1);
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void v8_role(const AttendArgs &a, Control<D, true> *ctl, uint32_t ring, uint32_t raw, uint32_t bars, int lane) {
+    using C = Cfg<D, true>;
+    volatile int *gave_up = &ctl->gave_up;
+    CodePages pages;
+    uint32_t tiles = 0, sent = 0, used = 0, turn = 0;
+    const uint32_t v_full = bars + 8 * (kRing + C::kKSlots), v_empty = v_full + 8 * C::kSlots;
+    const bool chosen = elect_one();
+    bool ok = true;
+    while (ok) {
+        const Segment *next = ctl->queue.get(turn++, gave_up, &a.ctl->status, lane);
+        if (!next) break;
+        const Segment s = *next;
+        ok = code_tiles<D, true>(a, s, ctl, pages, raw + C::kRawSlots * C::kRawBytes, ring + C::kKSlots * C::kKvBytes, v_full, v_empty, tiles,
+                                 sent, used, chosen, lane);
+    }
+    leave_codes<D, true>(ok, ctl, tiles, v_empty, sent, used, a);
+}
+
 // ---- products ----------------------------------------------------------------------
 // One warp issues all products, in the order of the steps of both streams: it waits for every tile's barriers in order (a
 // barrier tells its phases apart by parity alone, so a warp that left one out could take the phase before for the one it
 // waits for).  The whole warp walks the list, so that addresses stay in uniform registers; one elected lane issues (a role
 // run by a single lane took 82 cycles per instruction to issue, more than the 64 that it computes).
-template <int D>
-__device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D> *ctl, uint32_t q_smem, uint32_t ring,
+template <int D, bool KV8>
+__device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D, KV8> *ctl, uint32_t q_smem, uint32_t ring,
                                          uint32_t bars, int lane) {
-    using C = Cfg<D>;
+    using C = Cfg<D, KV8>;
     volatile int *gave_up = &ctl->gave_up;
     const uint32_t tmem = ctl->tmem;
     uint32_t tiles = 0, queries = 0, p_seen = 0, o_used = 0;               // bit st: parity of the stream's next wait
@@ -471,7 +666,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(
 __device__ __forceinline__ int partial_index(int piece, int kind, int st) { return (piece * 2 + kind) * 2 + st; }
 template <int D>
 __device__ __forceinline__ float *partial_slot(const AttendArgs &a, int index) {
-    return a.partials + (size_t)index * Cfg<D>::kSlotFloats;
+    return a.partials + (size_t)index * Cfg<D, false>::kSlotFloats;
 }
 
 // 32 bytes of a thread's own row: half the instructions, each of which takes a cycle per row, of two stores of 16 bytes.
@@ -551,9 +746,9 @@ __device__ __forceinline__ void merge_rows(const AttendArgs &a, const Segment &s
     }
 }
 
-template <int D>
-__device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<AttendWork> &list, Control<D> *ctl, uint32_t bars, int st) {
-    using C = Cfg<D>;
+template <int D, bool KV8>
+__device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<AttendWork> &list, Control<D, KV8> *ctl, uint32_t bars, int st) {
+    using C = Cfg<D, KV8>;
     volatile int *gave_up = &ctl->gave_up;
     const int row = threadIdx.x & 127, lane = threadIdx.x & 31, warp = row >> 5;
     const int tpt = kTile / a.G;
@@ -779,15 +974,16 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
     }
 }
 
-template <int D>
+template <int D, bool KV8>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
               const __grid_constant__ CUtensorMap k_wide, const __grid_constant__ CUtensorMap v_map,
               const __grid_constant__ CUtensorMap v_wide, const __grid_constant__ AttendArgs a) {
-    using C = Cfg<D>;
+    using C = Cfg<D, KV8>;
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t base = smem_u32(smem);
-    Control<D> *ctl = reinterpret_cast<Control<D> *>(smem + 2 * C::kTileBytes + C::kSlots * C::kKvBytes);
+    Control<D, KV8> *ctl =
+        reinterpret_cast<Control<D, KV8> *>(smem + 2 * C::kTileBytes + C::kSlots * C::kKvBytes + 2 * C::kRawSlots * C::kRawBytes);
     const uint32_t bars = smem_u32(ctl->bars);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (base & 1023u) {                  // the swizzle pattern hangs on the address
@@ -807,11 +1003,18 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
         mbar_fence_init();
         ctl->gave_up = 0;
     }
+    if (KV8 && threadIdx.x >= 64 && threadIdx.x < 64 + 2 * C::kRawSlots) {
+        mbar_init(smem_u32(&ctl->raw[threadIdx.x - 64]), 1);
+        mbar_fence_init();
+    }
     // (read ahead: it is here when the list is)
     const uint32_t refused = threadIdx.x == 32 * kIdleWarp ? *(volatile uint32_t *)&a.ctl->needs_init : 0u;
     if (warp == kMmaWarp) tmem_alloc(smem_u32(&ctl->tmem), 512);
-    if (threadIdx.x == 32 * kKWarp) prefetch_map(&q_map), prefetch_map(&k_map);
-    if (threadIdx.x == 32 * kVWarp) prefetch_map(&v_map);
+    if (threadIdx.x == 32 * kKWarp) {
+        prefetch_map(&q_map);
+        if (!KV8) prefetch_map(&k_map);
+    }
+    if (!KV8 && threadIdx.x == 32 * kVWarp) prefetch_map(&v_map);
     const AttendWork work(a);
     List<AttendWork> made = make_list<kThreads>(work, a.B, a.H_kv, a.ctl,
                                             a.B > kSmemRequests ? a.prefixes + prefix_bytes(a.B) * blockIdx.x : ctl->prefix, smem);
@@ -835,13 +1038,20 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     if (warp >= 8) {
         regs_down<kRegsOther>();
         const uint32_t ring = base + 2 * C::kTileBytes;
-        if (warp == kKWarp) k_role<D>(a, list, &q_map, &k_map, &k_wide, ctl, base, ring, bars, lane);
-        else if (warp == kVWarp) v_role<D>(a, &v_map, &v_wide, ctl, ring, bars, lane);
-        else if (warp == kMmaWarp) mma_role<D>(a, ctl, base, ring, bars, lane);
+        if constexpr (KV8) {
+            const uint32_t raw = ring + C::kSlots * C::kKvBytes;
+            if (warp == kKWarp) k8_role<D>(a, list, &q_map, ctl, base, ring, raw, bars, lane);
+            else if (warp == kVWarp) v8_role<D>(a, ctl, ring, raw, bars, lane);
+            else if (warp == kMmaWarp) mma_role<D, KV8>(a, ctl, base, ring, bars, lane);
+        } else {
+            if (warp == kKWarp) k_role<D>(a, list, &q_map, &k_map, &k_wide, ctl, base, ring, bars, lane);
+            else if (warp == kVWarp) v_role<D>(a, &v_map, &v_wide, ctl, ring, bars, lane);
+            else if (warp == kMmaWarp) mma_role<D, KV8>(a, ctl, base, ring, bars, lane);
+        }
         __syncwarp();
     } else {
         regs_up<kRegsSoftmax>();
-        softmax_role<D>(a, list, ctl, bars, warp >> 2);
+        softmax_role<D, KV8>(a, list, ctl, bars, warp >> 2);
     }
     tc_fence_before();
     __syncthreads();
@@ -852,13 +1062,15 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
 }
 
 // ---- host side ---------------------------------------------------------------------
-template <int D>
+template <int D, bool KV8>
 cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t stream) {
-    using C = Cfg<D>;
+    using C = Cfg<D, KV8>;
     const int G = p.H_q / p.H_kv;
     CUtensorMap q_map, k_map, k_wide, v_map, v_wide;
     bool ok = make_rows_map(&q_map, c.q, D, p.H_q, c.total_tokens, c.q_stride, G, kTile / G);
-    if (c.page_table) {
+    if (KV8) {
+        k_map = k_wide = v_map = v_wide = q_map;                 // not used
+    } else if (c.page_table) {
         const long long rows = (long long)p.num_phys_pages * p.H_kv * kPage;
         ok = ok && make_rows_map(&k_map, c.k, D, 1, rows, D, 1, kPage) && make_split_map(&v_map, c.v, D, 1, rows, D, kPage);
         k_wide = k_map, v_wide = v_map;                          // not used
@@ -872,19 +1084,21 @@ cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t 
     AttendArgs a = {};
     a.cu = c.cu_seqlens, a.seq_lens = c.seq_lens, a.page_table = c.page_table;
     a.v = static_cast<const uint16_t *>(c.v), a.v_stride = c.v_stride;
+    a.k8 = static_cast<const uint8_t *>(c.k), a.v8 = static_cast<const uint8_t *>(c.v);
+    a.scales = reinterpret_cast<const float2 *>(c.scales);
     a.out = static_cast<uint16_t *>(c.out), a.lse = c.lse;
     a.ctl = reinterpret_cast<PromptControl *>(c.workspace);
     a.partials = partials_of(c.workspace);
     a.prefixes = c.workspace + prefix_workspace_offset(p.D);
     a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.G = G, a.T = c.total_tokens, a.max_pages = p.max_pages;
     a.P_phys = p.num_phys_pages, a.scale_log2 = effective_scale(p) * kLog2e;
-    auto kern = attend_kernel<D>;
+    auto kern = attend_kernel<D, KV8>;
     // the register split (setmaxnreg) draws on what the block was launched with
     cudaFuncAttributes attr;
     cudaError_t e = cudaFuncGetAttributes(&attr, kern);
     if (e != cudaSuccess) return e;
     if (attr.numRegs * kThreads < 256 * kRegsSoftmax + 128 * kRegsOther) return cudaErrorInvalidConfiguration;
-    constexpr size_t smem = 2 * C::kTileBytes + C::kSlots * C::kKvBytes + sizeof(Control<D>);
+    constexpr size_t smem = 2 * C::kTileBytes + C::kSlots * C::kKvBytes + 2 * C::kRawSlots * C::kRawBytes + sizeof(Control<D, KV8>);
     static_assert(smem <= 227 * 1024, "shared memory of a CTA");
     e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
@@ -900,7 +1114,8 @@ size_t prompt_workspace_bytes(const se_params &p) {
 }
 
 cudaError_t launch_prompt_attend(const se_params &p, const AttendCall &c, cudaStream_t stream) {
-    return p.D == 128 ? launch_attend<128>(p, c, stream) : launch_attend<64>(p, c, stream);
+    if (c.scales) return p.D == 128 ? launch_attend<128, true>(p, c, stream) : launch_attend<64, true>(p, c, stream);
+    return p.D == 128 ? launch_attend<128, false>(p, c, stream) : launch_attend<64, false>(p, c, stream);
 }
 
 }  // namespace se

@@ -105,6 +105,7 @@ struct AttendCall {
     void *out;
     float *lse;
     uint8_t *workspace;
+    const float *scales;                         // nullptr: k, v are bf16; otherwise caches of e4m3 codes with these scales
 };
 cudaError_t launch_prompt_attend(const se_params &p, const AttendCall &c, cudaStream_t stream);
 // score_accum += the queries' weights on every cached token (k, lse of `c` are read, v and out are not used)

@@ -73,4 +73,18 @@ __device__ __forceinline__ uint4 kv8_values(const uint2 &u, float scale) {
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
+// Four codes as four bf16 times `f`: exact where f = scale * kv8_bf16_step() is a power of two.  A code's exponent and mantissa, moved
+// to the place of a bf16's, are its value times 2^-120 (the difference of the biases), subnormal codes included.
+__device__ __forceinline__ constexpr float kv8_bf16_step() { return 0x1p120f; }
+__device__ __forceinline__ void kv8_bf16x4(uint32_t codes, __nv_bfloat162 f, uint32_t &lo, uint32_t &hi) {
+    uint32_t x[2] = {__byte_perm(codes, 0, 0x1404), __byte_perm(codes, 0, 0x3424)};      // a code in the upper byte of each half
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t y = (x[i] & 0x80008000u) | (x[i] >> 4 & 0x07f007f0u);
+        const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&y), f);
+        x[i] = *reinterpret_cast<const uint32_t *>(&v);
+    }
+    lo = x[0], hi = x[1];
+}
+
 }  // namespace se

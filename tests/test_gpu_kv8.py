@@ -216,3 +216,80 @@ def test_decode_reports():
     e.run()
     assert binding.se_last_device_status(e.ws) == binding.SE_DEV_BAD_LENGTH
     assert bool((e.out[1] == 0).all()) and bool(torch.isfinite(e.out[0]).all())
+
+
+# ---- chunk ----------------------------------------------------------------------------------------
+
+class Chunk:
+    """Packed new tokens over an 8-bit cache, and the bf16 cache that holds the same values."""
+
+    def __init__(self, seed, new, past, H_kv, G, D, absent=0.0, spare=0, sm_scale=0.0):
+        g = torch.Generator().manual_seed(seed)
+        self.new, self.total = new, [n + o for n, o in zip(new, past)]
+        table, P = page_tables(g, self.total, wide=1)
+        self.k8, self.v8, self.scales = ref.make_cache(g, P, H_kv, D, "cuda")
+        for c, i in ((self.k8, 0), (self.v8, 1)):
+            c.view(torch.uint8)[table[0, 0]] = torch.randint(0, 8, c.shape[1:], generator=g, dtype=torch.uint8).cuda()   # subnormal codes, largest scale
+            self.scales[table[0, 0], :, i] = 128.0
+        self.k16 = ref.values(self.k8, self.scales[..., 0]).to(torch.bfloat16)
+        self.v16 = ref.values(self.v8, self.scales[..., 1]).to(torch.bfloat16)
+        for r, t in enumerate(self.total):                          # what lies behind a request's end is never read into a result
+            if t % 16:
+                pid = int(table[r, t // 16])
+                for c in (self.k8, self.v8):
+                    c.view(torch.uint8)[pid, :, t % 16:] = 0x7f
+                for c in (self.k16, self.v16):
+                    c[pid, :, t % 16:] = float("nan")
+        if absent:
+            for r, o in enumerate(past):
+                row = table[r, :o // 16]
+                row[torch.rand(row.shape, generator=g) < absent] = -1
+        T, H_q = sum(new) + spare, H_kv * G
+        qkv = torch.randn(T, H_q + 2, D, generator=g).to(torch.bfloat16).cuda()
+        self.q = qkv[:, :H_q]                                       # a view of wider rows
+        self.table, self.seq = table.cuda(), torch.tensor(self.total, **I32)
+        self.cu = torch.tensor([0] + torch.tensor(new).cumsum(0).tolist(), **I32)
+        self.p = binding.make_params(len(new), H_q, H_kv, D, table.shape[1], P, 1, sm_scale=sm_scale)
+        self.ws = binding.alloc_prompt_workspace(self.p)
+        self.out = [torch.full((T, H_q, D), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        self.lse = [torch.full((T, H_q), float("nan"), device="cuda") for _ in range(2)]
+
+    def run(self):
+        binding.se_kv8_chunk_attend(self.p, self.q, self.cu, self.k8, self.v8, self.scales, self.table, self.seq, self.out[0], self.ws,
+                                    lse=self.lse[0])
+
+    def check(self):
+        binding.se_chunk_attend(self.p, self.q, self.cu, self.k16, self.v16, self.table, self.seq, self.out[1], self.ws, lse=self.lse[1])
+        for _ in range(2):
+            self.run()
+            assert binding.se_last_device_status(self.ws) == 0
+            assert torch.equal(self.out[0].view(torch.int16), self.out[1].view(torch.int16))
+            assert torch.equal(self.lse[0].view(torch.int32), self.lse[1].view(torch.int32))
+
+
+@pytest.mark.parametrize("new,past,H_kv,G,D,absent,spare", [
+    ([1], [0], 1, 1, 64, 0.0, 0),
+    ([1], [15], 2, 4, 128, 0.0, 2),
+    ([1], [2047], 2, 4, 64, 0.0, 0),                                # one token, many CTAs
+    ([5, 0, 1, 17], [100, 50, 16, 0], 2, 8, 128, 0.0, 5),
+    ([300, 1, 77], [1000, 5000, 0], 4, 7, 128, 0.3, 0),
+    ([129, 400], [640, 31], 1, 3, 64, 0.5, 1),
+    ([2000], [3001], 2, 4, 128, 0.0, 0),                            # neighbouring query tiles share K and V
+    ([64] * 100, [33] * 100, 1, 2, 64, 0.1, 0),                     # more requests than prefix sums in shared memory
+    ([3, 2], [160, 320], 8, 5, 128, 1.0, 0),                        # nothing but the new tokens is present
+])
+def test_chunk_is_that_of_the_values(new, past, H_kv, G, D, absent, spare):
+    """The bf16 cache of the same values gives the same bits (its own results are held to 64 bits in test_gpu_prompt.py)."""
+    Chunk(21, new, past, H_kv, G, D, absent, spare).check()
+
+
+def test_chunk_reports():
+    c = Chunk(23, [4, 9], [100, 40], 2, 4, 128)
+    c.table[0, 2] = c.p.num_phys_pages
+    c.run()
+    assert binding.se_last_device_status(c.ws) == binding.SE_DEV_BAD_PAGE_ID
+    c.table[0, 2] = -1
+    c.check()
+    c.seq[1] = 3
+    c.run()
+    assert binding.se_last_device_status(c.ws) == binding.SE_DEV_BAD_LENGTH
