@@ -510,8 +510,10 @@ int se_kv8_decode(const se_params *p, const void *q, const void *k_cache, const 
                   float *out, float *lse, void *workspace, void *stream);
 
 /*
- * se_chunk_attend over an 8-bit cache: same arguments and rules, codes and scales in the place of the bf16 pages.  The codes' values
- * are exact in bf16, so out and lse are, bit for bit, what se_chunk_attend gives over a bf16 cache that holds them.
+ * se_chunk_attend over an 8-bit cache: same arguments and rules, codes and scales in the place of the bf16 pages.
+ * Precision: as there, except that a query row enters its product with K as the sum of two rows of codes times a power of two, which
+ * is exact for elements of at least 2^-10 of the row's largest magnitude and off by at most 2^-17.8 of that magnitude for smaller ones.
+ * A row of q with a NaN or an infinity has out = lse = NaN.
  */
 int se_kv8_chunk_attend(const se_params *p, const void *q, int64_t q_stride, int32_t total_tokens, const int32_t *cu_seqlens,
                         const void *k_cache, const void *v_cache, const float *scales, const int32_t *page_table,

@@ -39,11 +39,14 @@ namespace se {
 
 namespace {
 
-constexpr int kThreads = 384;            // 2 softmax warpgroups, K warp, product warp, V warp, idle warp
+constexpr int kPlainThreads = 384;       // 2 softmax warpgroups, K warp, product warp, V warp, idle warp
+constexpr int kTurners = 4;              // 8-bit cache: a fourth warpgroup turns V's codes into bf16
 constexpr int kKWarp = 8, kMmaWarp = 9, kVWarp = 10, kIdleWarp = 11;
 // 256 * 200 + 128 * 104 = 384 * 168; nothing spills.  With 208 and 88 the copying and product warps did: packed prompts 372 us for
 // 366, mixed batch 1230 for 1200, 2048 tokens over 65536 1935 for 1890-1910.
 constexpr int kRegsSoftmax = 200, kRegsOther = 104;
+// 8-bit cache: 256 * 184 + 256 * 72 = 512 * 128.
+constexpr int kRegsSoftmax8 = 184, kRegsOther8 = 72;
 constexpr int kTile = 128;             // query rows of a tile
 constexpr int kKv = 128;               // tokens of a KV tile
 constexpr int kGroups = kKv / kPage;   // pages of a KV tile
@@ -62,9 +65,12 @@ struct Cfg {
     static constexpr int kHalves = D / 64;
     static constexpr int kTileBytes = kTile * D * 2;              // query tile
     static constexpr int kKvBytes = kKv * D * 2;                  // K or V tile
-    // rings of K and V tiles, 64 and 96 KB; from an 8-bit cache 64 each, and rings of its pages, 14 KB each
-    static constexpr int kKSlots = 2 * 128 / D, kVSlots = (KV8 ? 2 : 3) * 128 / D;
-    static constexpr int kRawSlots = KV8 ? 7 * 128 / D : 0, kRawBytes = kPage * D;
+    // rings of K and V tiles, 64 and 96 KB; from an 8-bit cache 64 each (K as codes), and each turning warp's ring of V's pages
+    static constexpr int kKSlots = (KV8 ? 4 : 2) * 128 / D, kVSlots = (KV8 ? 2 : 3) * 128 / D;
+    static constexpr int kKBytes = KV8 ? kKv * D : kKvBytes;
+    static constexpr int kRawSlots = KV8 ? 3 * 128 / D : 0, kRawBytes = kPage * D;
+    static constexpr int kThreads = kPlainThreads + (KV8 ? 32 * kTurners : 0);
+    static constexpr int kRings = kKSlots * kKBytes + kVSlots * kKvBytes + kTurners * kRawSlots * kRawBytes;
     static constexpr int kSlots = kKSlots + kVSlots;
     static constexpr int kMasks = 16;
     static constexpr int kSlotFloats = kTile * D + 2 * kTile;     // a partial result: O, m, l
@@ -74,7 +80,7 @@ struct Cfg {
 struct AttendArgs {
     const int32_t *cu, *seq_lens, *page_table;
     const uint16_t *v;                 // rows of the last, partly filled 16-token group are copied by hand
-    const uint8_t *k8, *v8;            // 8-bit cache: codes, and scales of K and V
+    const uint8_t *v8;                 // 8-bit cache: codes of V, and scales of K and V
     const float2 *scales;
     long long v_stride;                // contiguous V: elements between tokens
     uint16_t *out;
@@ -93,7 +99,7 @@ struct Int {
 
 // kRing: full barriers of the K slots and of the V slots, then the empty ones in the same order
 enum Bar { kQFull, kQEmpty, kSFull, kPReady = kSFull + 2, kOLast = kPReady + 2, kOFree = kOLast + 2, kAll = kOFree + 2,
-           kVerdict = kAll + 2, kSwap = kVerdict + 2, kDrain, kRing };
+           kVerdict = kAll + 2, kSwap = kVerdict + 2, kDrain, kQReady, kRing };
 
 // ---- the work list -----------------------------------------------------------------
 // item = two query tiles (the last one of a request may be a single tile), unit = KV tile.  Cost in tokens seen, twice
@@ -142,7 +148,10 @@ struct Segment {
 template <int D, bool KV8>
 struct Control {
     uint64_t bars[kRing + 2 * Cfg<D, KV8>::kSlots];
-    uint64_t raw[KV8 ? 2 * Cfg<D, KV8>::kRawSlots : 1];            // 8-bit cache: pages of K, of V have come
+    // 8-bit cache: V's pages have come; scales of K's pages of the tiles in flight; powers of two taken out of the query rows
+    uint64_t raw[KV8 ? kTurners * Cfg<D, KV8>::kRawSlots : 1];
+    float k_scale[KV8 ? Cfg<D, KV8>::kMasks : 1][KV8 ? kGroups : 1];
+    float q_scale[KV8 ? 2 : 1][KV8 ? 2 : 1][KV8 ? kTile : 1];              // [this segment and the next][query tile]
     SegmentQueue<Segment> queue;
     alignas(8) uint8_t prefix[prefix_bytes(kSmemRequests)];
     uint32_t mask[Cfg<D, KV8>::kMasks];     // present 16-token groups of the tiles in flight
@@ -367,17 +376,22 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v
 }
 
 // ---- an 8-bit cache ------------------------------------------------------------------
-// The same two warps, one for K and one for V, bring pages of codes into a ring of their own (a bulk copy each, a tile ahead), turn them
-// into bf16 (exact, as the scales are powers of two) and write the tiles that the tensor copies would: everything behind them is
-// the same, and so are the results, bit for bit, as over a bf16 cache that holds the codes' values.
-//
-// Page ids and scales of 32 groups of 16 tokens at a time, a lane each, and of the next 32 ahead.
+// K stays as it is: S = Q K^T runs on codes.  A query row is split into two rows of codes, q 2^-e = hi + lo, with 2^e such that its
+// largest magnitude is at most 448; a bf16's 8 significant bits fit the two 4-bit ones, so this is exact for everything above 2^-10
+// of the row's maximum and off by at most 2^-18 of it below.  Two products at twice the rate take the time of one in bf16, and
+// the scales - 2^e of the row, s_K of the page - enter the softmax in fp32.
+// V's codes become bf16 (exact, as the scales are powers of two), because weights need their range and eight bits: four warps bring
+// two pages of every tile each into a ring of their own, turn them, and write the tile that the tensor copies would.
+// (With K turned into bf16 too, by one warp and V by another, a step took 9000 to 11000 cycles instead of 3350.)
+
+// Page ids and scales of 32 groups of 16 tokens at a time, a lane each, and of the next 32 ahead.  Lane i of block b has the group
+// (32 b + i) * step + first.
 struct CodePages {
     int ids, next, block;
     float scale, next_scale;
 
     __device__ __forceinline__ void fetch(const AttendArgs &a, const Segment &s, int g, bool of_v, int &id, float &sc) const {
-        id = -1, sc = 0.f;
+        id = -1, sc = 1.f;
         if (g * kPage >= s.t.past + s.t.n) return;
         const int pid = a.page_table[(size_t)s.r * a.max_pages + g];
         if (pid >= a.P_phys && !of_v) atomicOr(&a.ctl->status, SE_DEV_BAD_PAGE_ID);
@@ -386,128 +400,35 @@ struct CodePages {
         const float2 both = a.scales[id];
         sc = of_v ? both.y : both.x;
     }
-    __device__ __forceinline__ void begin(const AttendArgs &a, const Segment &s, int tile, bool of_v, int lane) {
-        block = tile / (32 / kGroups);
-        fetch(a, s, block * 32 + lane, of_v, ids, scale);
-        fetch(a, s, block * 32 + 32 + lane, of_v, next, next_scale);
+    __device__ __forceinline__ void begin(const AttendArgs &a, const Segment &s, int j, int step, int first, bool of_v, int lane) {
+        block = j / 32;
+        fetch(a, s, (block * 32 + lane) * step + first, of_v, ids, scale);
+        fetch(a, s, (block * 32 + 32 + lane) * step + first, of_v, next, next_scale);
     }
-    __device__ __forceinline__ void reach(const AttendArgs &a, const Segment &s, int tile, bool of_v, int lane) {
-        if (tile / (32 / kGroups) == block) return;
+    __device__ __forceinline__ void reach(const AttendArgs &a, const Segment &s, int j, int step, int first, bool of_v, int lane) {
+        if (j / 32 == block) return;
         ++block;
         ids = next, scale = next_scale;
-        fetch(a, s, block * 32 + 32 + lane, of_v, next, next_scale);
+        fetch(a, s, (block * 32 + 32 + lane) * step + first, of_v, next, next_scale);
     }
-    // group g of this block or the next
-    __device__ __forceinline__ int of(int g) const { return __shfl_sync(kFull, g / 32 == block ? ids : next, g % 32); }
 };
 
-// The tiles of one segment.  `filled`: tiles of K or V so far; `sent`, `used`: pages whose copy has been issued, that have been turned.
-template <int D, bool OF_V>
-__device__ __forceinline__ bool code_tiles(const AttendArgs &a, const Segment &s, Control<D, true> *ctl, CodePages &pages, uint32_t raw,
-                                           uint32_t tiles_at, uint32_t full, uint32_t empty, uint32_t &filled, uint32_t &sent, uint32_t &used,
-                                           bool chosen, int lane) {
-    using C = Cfg<D, true>;
-    constexpr uint32_t kSlots = OF_V ? C::kVSlots : C::kKSlots;
-    volatile int *gave_up = &ctl->gave_up;
-    const uint32_t raw_bars = smem_u32(ctl->raw) + (OF_V ? 8 * C::kRawSlots : 0);
-    const int stop = s.t.past + s.t.n;
-    int ahead = s.a * kGroups;                                             // next group whose copy is to be issued
-    pages.begin(a, s, s.a, OF_V, lane);
-    auto send = [&] {
-        while (ahead < s.b * kGroups && sent - used < (uint32_t)C::kRawSlots && ahead / 32 <= pages.block + 1) {
-            const int id = pages.of(ahead);
-            if (id >= 0) {
-                if (chosen) {
-                    const uint32_t slot = sent % C::kRawSlots;
-                    mbar_expect_tx(raw_bars + 8 * slot, C::kRawBytes + ((D == 128) == OF_V && sent == 0 ? kTestExtraTx : 0));
-                    bulk_g2s(raw + slot * C::kRawBytes, (OF_V ? a.v8 : a.k8) + (size_t)id * C::kRawBytes, C::kRawBytes, raw_bars + 8 * slot);
-                }
-                __syncwarp();
-                ++sent;
-            }
-            ++ahead;
-        }
-    };
-    send();
-    // lane -> token and 16 codes of it: eight lanes store to all banks, whatever the swizzle
-    const int row = lane >> 2, part = lane & 3;
-    for (int t = s.a; t < s.b; ++t, ++filled) {
-        const uint32_t slot = filled % kSlots, dst = tiles_at + slot * C::kKvBytes;
-        pages.reach(a, s, t, OF_V, lane);
-        send();
-        if (!warp_wait(empty + 8 * slot, (filled / kSlots & 1) ^ 1, gave_up, &a.ctl->status)) return false;
-        const unsigned mask = __ballot_sync(kFull, pages.ids >= 0) >> t % (32 / kGroups) * kGroups & 0xffu;
-        if (!OF_V && chosen) ctl->mask[filled % C::kMasks] = mask;
-#pragma unroll 1
-        for (int pg = 0; pg < kGroups; ++pg) {
-            const uint32_t page_at = dst + (OF_V ? pg * (kPage * D * 2) : pg * (kPage * 128));
-            constexpr uint32_t half_step = OF_V ? kPage * 128 : kKv * 128;
-            constexpr int N = D / 32;                                      // pieces of 16 codes per lane
-            const bool here = mask >> pg & 1;
-            if (!here && !OF_V) continue;                                  // (scores of absent groups are overwritten)
-            uint4 x[N];
-            __nv_bfloat162 f = __float2bfloat162_rn(0.f);
-            if (here) {
-                const uint32_t from = used % C::kRawSlots;
-                if (!warp_wait(raw_bars + 8 * from, used / C::kRawSlots & 1, gave_up, &a.ctl->status)) return false;
-                f = __float2bfloat162_rn(__shfl_sync(kFull, pages.scale, (t * kGroups + pg) % 32) * kv8_bf16_step());
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int token = row + 8 * (i / (D / 64)), c = part + 4 * (i % (D / 64));
-                    const uint32_t at = raw + from * C::kRawBytes + token * D + c * 16;
-                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[i].x), "=r"(x[i].y), "=r"(x[i].z), "=r"(x[i].w) : "r"(at));
-                }
-                __syncwarp();
-                ++used;
-                send();
-            }
-            // what lies behind the end of the request may be anything, and a weight of zero would not hide it
-            const int tokens = here ? min(kPage, stop - (t * kGroups + pg) * kPage) : 0;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int token = row + 8 * (i / (D / 64)), half = i % (D / 64);
-                if (OF_V && token >= tokens) x[i] = make_uint4(0, 0, 0, 0);
-                const uint32_t at = page_at + half * half_step + token * 128;
-                const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-                uint32_t o[8];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) kv8_bf16x4(w[j], f, o[2 * j], o[2 * j + 1]);
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + (((2 * part + j) ^ (token & 7)) << 4)), "r"(o[4 * j]), "r"(o[4 * j + 1]),
-                                 "r"(o[4 * j + 2]), "r"(o[4 * j + 3])
-                                 : "memory");
-            }
-        }
-        fence_async_proxy();
-        __syncwarp();
-        if (chosen) mbar_arrive(full + 8 * slot);
-        __syncwarp();
-    }
-    return true;
-}
-
-// The end of a warp that has filled `filled` slots: the products' arrivals for them, and its copies.
-template <int D, bool OF_V>
-__device__ __forceinline__ void leave_codes(bool ok, Control<D, true> *ctl, uint32_t filled, uint32_t empty, uint32_t sent, uint32_t used,
-                                            const AttendArgs &a) {
-    using C = Cfg<D, true>;
-    constexpr uint32_t kSlots = OF_V ? C::kVSlots : C::kKSlots;
-    for (uint32_t n = filled > kSlots ? filled - kSlots : 0; ok && n < filled; ++n)
-        ok = warp_wait(empty + 8 * (n % kSlots), n / kSlots & 1, &ctl->gave_up, &a.ctl->status);
-    const uint32_t raw_bars = smem_u32(ctl->raw) + (OF_V ? 8 * C::kRawSlots : 0);
-    for (; used != sent; ++used) mbar_wait(raw_bars + 8 * (used % C::kRawSlots), used / C::kRawSlots & 1);
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
 }
 
 template <int D>
-__device__ __forceinline__ void k8_role(const AttendArgs &a, const List<AttendWork> &list, const CUtensorMap *q_map, Control<D, true> *ctl,
-                                        uint32_t q_smem, uint32_t ring, uint32_t raw, uint32_t bars, int lane) {
+__device__ __forceinline__ void k8_role(const AttendArgs &a, const List<AttendWork> &list, const CUtensorMap *q_map, const CUtensorMap *k_map,
+                                        Control<D, true> *ctl, uint32_t q_smem, uint32_t ring, uint32_t bars, int lane) {
     using C = Cfg<D, true>;
     volatile int *gave_up = &ctl->gave_up;
     const int tpt = kTile / a.G;
     Segment s;
     CodePages pages;
-    uint32_t tiles = 0, queries = 0, sent = 0, used = 0;
+    uint32_t tiles = 0, queries = 0;
     const uint32_t k_full = bars + 8 * kRing, k_empty = k_full + 8 * C::kSlots;
     const bool chosen = elect_one();
     bool ok = true;
@@ -515,6 +436,7 @@ __device__ __forceinline__ void k8_role(const AttendArgs &a, const List<AttendWo
     while (ok && next_segment(walk, s)) {
         ok = ctl->queue.put(queries, &s, gave_up, &a.ctl->status, lane);
         if (!ok) break;
+        pages.begin(a, s, s.a * kGroups, 1, 0, false, lane);
         ok = warp_wait(bars + 8 * kQEmpty, (queries & 1) ^ 1, gave_up, &a.ctl->status);
         if (!ok) break;
         if (chosen) {
@@ -526,33 +448,176 @@ __device__ __forceinline__ void k8_role(const AttendArgs &a, const List<AttendWo
         }
         __syncwarp();
         ++queries;
-        ok = code_tiles<D, false>(a, s, ctl, pages, raw, ring, k_full, k_empty, tiles, sent, used, chosen, lane);
+        for (int t = s.a; t < s.b; ++t, ++tiles) {
+            const uint32_t slot = tiles % C::kKSlots, bar = k_full + 8 * slot, dst = ring + slot * C::kKBytes;
+            pages.reach(a, s, t * kGroups, 1, 0, false, lane);
+            const int at = t * kGroups % 32;                               // the tile's groups are lanes at .. at + 7
+            const unsigned mask = __ballot_sync(kFull, pages.ids >= 0) >> at & 0xffu;
+            int id[kGroups];
+#pragma unroll
+            for (int pg = 0; pg < kGroups; ++pg) id[pg] = __shfl_sync(kFull, pages.ids, at + pg);
+            ok = warp_wait(k_empty + 8 * slot, (tiles / C::kKSlots & 1) ^ 1, gave_up, &a.ctl->status);
+            if (!ok) break;
+            if (lane >= at && lane < at + kGroups) ctl->k_scale[tiles % C::kMasks][lane - at] = pages.scale;
+            __syncwarp();
+            if (chosen) {
+                ctl->mask[tiles % C::kMasks] = mask;
+                mbar_expect_tx(bar, C::kKBytes + (D == 64 && tiles == 0 ? kTestExtraTx : 0));
+#pragma unroll
+                for (int pg = 0; pg < kGroups; ++pg)                       // absent: from behind the last row, zeros
+                    tma_load_2d(dst + pg * (kPage * D), k_map, 0, (id[pg] < 0 ? a.P_phys * a.H_kv : id[pg]) * kPage, bar);
+            }
+            __syncwarp();
+        }
     }
     if (ok) ok = ctl->queue.put(queries, nullptr, gave_up, &a.ctl->status, lane);
-    leave_codes<D, false>(ok, ctl, tiles, k_empty, sent, used, a);
+    leave_ring<C::kKSlots>(ok, tiles, k_full, k_empty, gave_up, a);
     if (queries) {
         ok = ok && warp_wait(bars + 8 * kQEmpty, (queries - 1) & 1, gave_up, &a.ctl->status);
         if (!ok) mbar_wait(bars + 8 * kQFull, (queries - 1) & 1);
     }
 }
 
+// Turning warp w of four: pages w and w + 4 of every tile of V.
 template <int D>
-__device__ __forceinline__ void v8_role(const AttendArgs &a, Control<D, true> *ctl, uint32_t ring, uint32_t raw, uint32_t bars, int lane) {
+__device__ __forceinline__ void v8_role(const AttendArgs &a, Control<D, true> *ctl, uint32_t tiles_at, uint32_t raw, uint32_t bars, int w, int lane) {
     using C = Cfg<D, true>;
+    constexpr int kMine = kGroups / kTurners;
+    constexpr int N = D / 32;                                              // pieces of 16 codes per lane and page
     volatile int *gave_up = &ctl->gave_up;
     CodePages pages;
-    uint32_t tiles = 0, sent = 0, used = 0, turn = 0;
+    uint32_t tiles = 0, sent = 0, used = 0, turn = 0;                      // pages whose copy has been issued, that have been turned
     const uint32_t v_full = bars + 8 * (kRing + C::kKSlots), v_empty = v_full + 8 * C::kSlots;
+    const uint32_t raw_bars = smem_u32(ctl->raw) + 8 * C::kRawSlots * w;
+    raw += C::kRawSlots * C::kRawBytes * w;
     const bool chosen = elect_one();
+    // lane -> token and 16 codes of it: eight lanes store to all banks, whatever the swizzle
+    const int row = lane >> 2, part = lane & 3;
+    const uint32_t store0 = row * 128 + (((2 * part) ^ row) << 4), store1 = row * 128 + (((2 * part + 1) ^ row) << 4);
     bool ok = true;
     while (ok) {
-        const Segment *next = ctl->queue.get(turn++, gave_up, &a.ctl->status, lane);
-        if (!next) break;
-        const Segment s = *next;
-        ok = code_tiles<D, true>(a, s, ctl, pages, raw + C::kRawSlots * C::kRawBytes, ring + C::kKSlots * C::kKvBytes, v_full, v_empty, tiles,
-                                 sent, used, chosen, lane);
+        const Segment *entry = ctl->queue.get(turn++, gave_up, &a.ctl->status, lane);
+        if (!entry) break;
+        const Segment s = *entry;
+        const int stop = s.t.past + s.t.n, end = s.b * kMine;
+        int ahead = s.a * kMine;                                           // next page whose copy is to be issued, in the warp's own count
+        pages.begin(a, s, ahead, kTurners, w, true, lane);
+        auto send = [&] {
+            while (ahead < end && sent - used < (uint32_t)C::kRawSlots && ahead / 32 <= pages.block + 1) {
+                const int id = __shfl_sync(kFull, ahead / 32 == pages.block ? pages.ids : pages.next, ahead % 32);
+                if (id >= 0) {
+                    if (chosen) {
+                        const uint32_t slot = sent % C::kRawSlots;
+                        mbar_expect_tx(raw_bars + 8 * slot, C::kRawBytes + (D == 128 && sent == 0 ? kTestExtraTx : 0));
+                        bulk_g2s(raw + slot * C::kRawBytes, a.v8 + (size_t)id * C::kRawBytes, C::kRawBytes, raw_bars + 8 * slot);
+                    }
+                    __syncwarp();
+                    ++sent;
+                }
+                ++ahead;
+            }
+        };
+        send();
+        for (int t = s.a; t < s.b; ++t, ++tiles) {
+            const uint32_t slot = tiles % C::kVSlots, dst = tiles_at + slot * C::kKvBytes;
+            pages.reach(a, s, t * kMine, kTurners, w, true, lane);
+            send();
+            ok = warp_wait(v_empty + 8 * slot, (tiles / C::kVSlots & 1) ^ 1, gave_up, &a.ctl->status);
+            if (!ok) break;
+#pragma unroll 1
+            for (int i = 0; i < kMine; ++i) {
+                const int j = t * kMine + i, group = j * kTurners + w;
+                const uint32_t at = dst + (group % kGroups) * (kPage * D * 2);
+                if (__shfl_sync(kFull, pages.ids, j % 32) < 0) {           // an absent group: zeros
+#pragma unroll
+                    for (int e = 0; e < kPage * D * 2 / 512; ++e)
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(at + lane * 16 + e * 512), "r"(0) : "memory");
+                    continue;
+                }
+                const __nv_bfloat162 f = __float2bfloat162_rn(__shfl_sync(kFull, pages.scale, j % 32) * kv8_bf16_step());
+                const uint32_t from = used % C::kRawSlots;
+                ok = warp_wait(raw_bars + 8 * from, used / C::kRawSlots & 1, gave_up, &a.ctl->status);
+                if (!ok) break;
+                uint4 x[N];
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const uint32_t src = raw + from * C::kRawBytes + row * D + part * 16 + e / (D / 64) * (8 * D) + e % (D / 64) * 64;
+                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[e].x), "=r"(x[e].y), "=r"(x[e].z), "=r"(x[e].w) : "r"(src) : "memory");
+                }
+                // what lies behind the end of the request may be anything, and a weight of zero would not hide it
+                const int tokens = stop - group * kPage;
+                if (tokens < kPage) {
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        if (row + 8 * (e / (D / 64)) >= tokens) x[e] = make_uint4(0, 0, 0, 0);
+                }
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const uint32_t c[4] = {x[e].x, x[e].y, x[e].z, x[e].w}, to = at + e / (D / 64) * 1024 + e % (D / 64) * (kPage * 128);
+                    uint32_t o[8];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) kv8_bf16x4(c[q], f, o[2 * q], o[2 * q + 1]);
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to + store0), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to + store1), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
+                }
+                __syncwarp();
+                ++used;
+                send();
+            }
+            if (!ok) break;
+            fence_async_proxy();
+            __syncwarp();
+            if (chosen) mbar_arrive(v_full + 8 * slot);
+            __syncwarp();
+        }
     }
-    leave_codes<D, true>(ok, ctl, tiles, v_empty, sent, used, a);
+    // the end of the warp: the products' arrivals for the tiles, and its copies
+    for (uint32_t n = tiles > C::kVSlots ? tiles - C::kVSlots : 0; ok && n < tiles; ++n)
+        ok = warp_wait(v_empty + 8 * (n % C::kVSlots), n / C::kVSlots & 1, gave_up, &a.ctl->status);
+    for (; used != sent; ++used) mbar_wait(raw_bars + 8 * (used % C::kRawSlots), used / C::kRawSlots & 1);
+}
+
+// A query tile of bf16 becomes codes in its place, by the threads of a warpgroup, a row each: at D = 128 two tiles, hi and lo, at
+// D = 64 one of rows that hold both (each thread's bytes stay its own, so nothing has to be waited for).
+template <int D>
+__device__ __forceinline__ void split_query(uint32_t tile, int row, bool filled, float &power) {
+    uint32_t x[D / 2];
+    uint32_t top = 0;
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c) {
+        uint4 y = make_uint4(0, 0, 0, 0);
+        if (filled) {
+            const uint32_t at = tile + c / 8 * (kTile * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4);
+            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(y.x), "=r"(y.y), "=r"(y.z), "=r"(y.w) : "r"(at) : "memory");
+        }
+        x[4 * c] = y.x, x[4 * c + 1] = y.y, x[4 * c + 2] = y.z, x[4 * c + 3] = y.w;
+        const uint32_t m = 0x7fff7fffu;                                    // (as integers: a NaN is larger than everything)
+        top = __vmaxu2(top, __vmaxu2(__vmaxu2(y.x & m, y.y & m), __vmaxu2(y.z & m, y.w & m)));
+    }
+    top = max(top & 0xffffu, top >> 16);
+    const int e = min(max((int)(top >> 7) - 135 + ((top & 127u) > 96u ? 1 : 0), -110), 110);   // smallest 2^e with the maximum at most 448 * 2^e
+    const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+    power = top >= 0x7f80u ? __uint_as_float(0x7fffffffu) : __uint_as_float((uint32_t)(127 + e) << 23);   // a row that is not finite becomes NaN
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            uint32_t h[2], l[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                float2 v = bf16x2_to_f2(x[8 * c + 2 * q + k]);
+                v.x *= down, v.y *= down;
+                h[k] = e4m3x2(v.x, v.y);
+                const float2 r = float2_of_e4m3x2(h[k]);
+                l[k] = e4m3x2(v.x - r.x, v.y - r.y);
+            }
+            hi[q] = h[0] | h[1] << 16, lo[q] = l[0] | l[1] << 16;
+        }
+        const uint32_t at = tile + row * 128, second = D == 128 ? at + kTile * 128 + ((c ^ (row & 7)) << 4) : at + (((c + 4) ^ (row & 7)) << 4);
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + ((c ^ (row & 7)) << 4)), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(second), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
+    }
 }
 
 // ---- products ----------------------------------------------------------------------
@@ -594,12 +659,20 @@ __device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D, KV8> *c
         auto scores = [&](auto stream, uint32_t tile) {
             constexpr int ST = decltype(stream)::value;
             const uint32_t slot = tile % C::kKSlots;
-            const uint64_t qd = smem_operand(q_smem + (alt ? 0 : ST * C::kTileBytes), 16, 1024);
-            const uint64_t kd = smem_operand(ring + slot * C::kKvBytes, 16, 1024);
+            if constexpr (KV8) {         // hi, then lo
+                const uint64_t qd = smem_operand(q_smem + (alt ? 0 : ST * C::kTileBytes), 16, 1024), kd = smem_codes<D>(ring + slot * C::kKBytes);
+                constexpr uint32_t lo = D == 128 ? kTile * 128 >> 4 : 64 >> 4;
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                const uint32_t off = (k / 4) * (kTile * 128 >> 4) + (k % 4) * 2;
-                mma_ss(tmem + ST * kTile, qd + off, kd + off, mma_instr(kKv, false), k > 0);
+                for (int k = 0; k < 2 * (D / 32); ++k)
+                    mma_ss_codes(tmem + ST * kTile, qd + k / (D / 32) * lo + k % (D / 32) * 2, kd + k % (D / 32) * 2, mma_instr_codes(kKv), k > 0);
+            } else {
+                const uint64_t qd = smem_operand(q_smem + (alt ? 0 : ST * C::kTileBytes), 16, 1024);
+                const uint64_t kd = smem_operand(ring + slot * C::kKvBytes, 16, 1024);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t off = (k / 4) * (kTile * 128 >> 4) + (k % 4) * 2;
+                    mma_ss(tmem + ST * kTile, qd + off, kd + off, mma_instr(kKv, false), k > 0);
+                }
             }
             mma_commit(bars + 8 * (kSFull + ST));
             if (alt || ST == 1) mma_commit(bars + 8 * (kRing + C::kSlots + slot));
@@ -620,7 +693,7 @@ __device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D, KV8> *c
             if (i >= mine) return true;
             const bool more = i + 1 < mine;
             const uint32_t tile = place(ST, i), slot = tile % C::kVSlots;
-            const uint64_t vd = smem_operand(ring + (C::kKSlots + slot) * C::kKvBytes, v_lead, 1024);
+            const uint64_t vd = smem_operand(ring + C::kKSlots * C::kKBytes + slot * C::kKvBytes, v_lead, 1024);
             // everything that can be waited for early comes before the wait for the weights
             if (!wait_v(tile) || (more && !wait_k(place(ST, i + 1)))) return false;
             if (i == 0) {                // the epilogue of the stream's last piece has read O
@@ -642,7 +715,7 @@ __device__ __forceinline__ void mma_role(const AttendArgs &a, Control<D, KV8> *c
             return true;
         };
         any = true;
-        ok = wait(kQFull, queries++) && begin(Int<0>{}) && begin(Int<1>{});
+        ok = wait(KV8 ? kQReady : kQFull, queries++) && begin(Int<0>{}) && begin(Int<1>{});
         if (ok && chosen && steps == 1) mma_commit(bars + 8 * kQEmpty);
         __syncwarp();
         for (int i = 0; i < steps && ok; ++i) {
@@ -747,7 +820,8 @@ __device__ __forceinline__ void merge_rows(const AttendArgs &a, const Segment &s
 }
 
 template <int D, bool KV8>
-__device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<AttendWork> &list, Control<D, KV8> *ctl, uint32_t bars, int st) {
+__device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<AttendWork> &list, Control<D, KV8> *ctl, uint32_t q_smem, uint32_t bars,
+                                             int st) {
     using C = Cfg<D, KV8>;
     volatile int *gave_up = &ctl->gave_up;
     const int row = threadIdx.x & 127, lane = threadIdx.x & 31, warp = row >> 5;
@@ -776,8 +850,24 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
         int left = sees - (s.a + (s.alt ? st : 0)) * kKv;                  // tokens that the row sees of this tile and the later ones
         int most = least - (s.a + (s.alt ? st : 0)) * kKv;
         uint32_t tile = tiles + (s.alt ? st : 0);
-        float m = -INFINITY;                                               // in units of the raw scores
-        float l = 0.f, lost = 0.f;     // sum of the weights over the tiles so far, and what rounding took from it (Kahan)
+        float m = -INFINITY;                                               // in units of the raw scores (8-bit cache: of powers of two)
+        [[maybe_unused]] float row_scale = 0.f;
+        if constexpr (KV8) {
+            const bool mine = !s.alt || st == 0;                           // (of a single query tile the first warpgroup's threads have a row each)
+            if (mine) {
+                if (!warp_wait(bars + 8 * kQFull, (turn - 1) & 1, gave_up, &a.ctl->status)) return;
+                float power;
+                split_query<D>(q_smem + st * C::kTileBytes, row, row < tpt * a.G, power);
+                ctl->q_scale[turn & 1][st][row] = power;
+                fence_async_proxy();
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bars + 8 * kQReady);
+            if (!warp_wait(bars + 8 * kQReady, (turn - 1) & 1, gave_up, &a.ctl->status)) return;
+            row_scale = ctl->q_scale[turn & 1][s.alt ? 0 : st][row] * sl;
+        }
+        // sum of the weights over the tiles so far, and what rounding took from it (Kahan); a row that is not finite begins with a NaN
+        float l = KV8 && row_scale != row_scale ? row_scale : 0.f, lost = 0.f;
         for (int u = 0; u < steps; ++u, ++step, left -= stride * kKv, most -= stride * kKv, tile += stride) {
             if (!warp_wait(bars + 8 * (kSFull + st), step & 1, gave_up, &a.ctl->status)) return;
             tc_fence_after();
@@ -801,14 +891,30 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
                         if (k >= left) x[k] = -INFINITY;
                 }
             }
-            float top[4] = {x[0], x[1], x[2], x[3]};
+            float mn, grown;                                               // the new maximum, by how many powers of two it is above the old one
+            const float *k_scale = ctl->k_scale[KV8 ? tile % C::kMasks : 0];
+            if constexpr (KV8) {
+                mn = m;
 #pragma unroll
-            for (int k = 4; k < kKv; k += 8)
+                for (int pg = 0; pg < kGroups; ++pg) {
+                    const float *y = x + pg * kPage;
+                    float top = max3(y[0], y[1], y[2]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) top[e] = k + 4 + e < kKv ? max3(top[e], x[k + e], x[k + 4 + e]) : fmaxf(top[e], x[k + e]);
-            const float mn = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
-            if (__any_sync(kFull, (mn - m) * sl > kSlack)) {
-                const float f = m == -INFINITY ? 0.f : ex2((m - mn) * sl);
+                    for (int k = 3; k + 1 < kPage; k += 2) top = max3(top, y[k], y[k + 1]);
+                    mn = fmaxf(mn, fmaxf(top, y[kPage - 1]) * fmaxf(k_scale[pg] * row_scale, 1e-37f));   // (0 times a masked score would be NaN)
+                }
+                grown = mn - m;
+            } else {
+                float top[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+                for (int k = 4; k < kKv; k += 8)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) top[e] = k + 4 + e < kKv ? max3(top[e], x[k + e], x[k + 4 + e]) : fmaxf(top[e], x[k + e]);
+                mn = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
+                grown = (mn - m) * sl;
+            }
+            if (__any_sync(kFull, grown > kSlack)) {
+                const float f = m == -INFINITY ? 0.f : ex2(KV8 ? m - mn : (m - mn) * sl);
                 m = mn;
                 l *= f, lost *= f;
                 if (u > 0) {             // the product before these scores is complete: they were issued behind it
@@ -824,14 +930,15 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
                     }
                 }
             }
-            const float off = m == -INFINITY ? 0.f : -m * sl;
+            const float off = m == -INFINITY ? 0.f : KV8 ? -m : -m * sl;
             float2 l2 = make_float2(0.f, 0.f);
 #pragma unroll
             for (int k = 0; k < kKv; k += 64) {
                 uint32_t p[32];
 #pragma unroll
                 for (int e = 0; e < 32; ++e) {
-                    const float2 y = ffma2(make_float2(x[k + 2 * e], x[k + 2 * e + 1]), make_float2(sl, sl), make_float2(off, off));
+                    const float by = KV8 ? fmaxf(k_scale[(k + 2 * e) / kPage] * row_scale, 1e-37f) : sl;
+                    const float2 y = ffma2(make_float2(x[k + 2 * e], x[k + 2 * e + 1]), make_float2(by, by), make_float2(off, off));
                     const float2 w = make_float2(ex2(y.x), ex2(y.y));
                     l2 = __fadd2_rn(l2, w);
                     // the weights enter the product with V as bf16 (8 significant bits), their sum keeps fp32
@@ -859,7 +966,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
 
         // ---- epilogue ----
         // -infinity says that nothing was seen, so a sum that is NaN goes with another maximum
-        const float m2 = l != l ? INFINITY : m == -INFINITY ? m : m * sl;
+        const float m2 = l != l ? INFINITY : m == -INFINITY ? m : KV8 ? m : m * sl;
         const bool live = row < ntok * a.G;
         const bool whole = s.a == 0 && s.b == s.nkv;
         const bool direct = whole && (!s.alt || s.nkv == 1);
@@ -975,7 +1082,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
 }
 
 template <int D, bool KV8>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Cfg<D, KV8>::kThreads, 1)
 attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
               const __grid_constant__ CUtensorMap k_wide, const __grid_constant__ CUtensorMap v_map,
               const __grid_constant__ CUtensorMap v_wide, const __grid_constant__ AttendArgs a) {
@@ -983,7 +1090,7 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t base = smem_u32(smem);
     Control<D, KV8> *ctl =
-        reinterpret_cast<Control<D, KV8> *>(smem + 2 * C::kTileBytes + C::kSlots * C::kKvBytes + 2 * C::kRawSlots * C::kRawBytes);
+        reinterpret_cast<Control<D, KV8> *>(smem + 2 * C::kTileBytes + C::kRings);
     const uint32_t bars = smem_u32(ctl->bars);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (base & 1023u) {                  // the swizzle pattern hangs on the address
@@ -991,19 +1098,20 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
         return;
     }
 
-    static_assert(kRing + 2 * C::kSlots <= kThreads, "a thread per barrier");
+    static_assert(kRing + 2 * C::kSlots <= kPlainThreads, "a thread per barrier");
     if (threadIdx.x < kRing + 2 * C::kSlots) {
         const int i = threadIdx.x;
         const bool by_warp = (i >= kPReady && i < kPReady + 2) || (i >= kOFree && i < kOFree + 2) || (i >= kAll && i < kAll + 2);
-        mbar_init(bars + 8 * i, i == kSwap ? 8 : by_warp ? 4 : 1);
+        const bool turned = KV8 && i >= kRing + C::kKSlots && i < kRing + C::kSlots;             // (full barriers of V)
+        mbar_init(bars + 8 * i, i == kSwap || i == kQReady ? 8 : by_warp ? 4 : turned ? kTurners : 1);
         mbar_fence_init();
     }
     if (threadIdx.x == 32) {
-        ctl->queue.init(10);
+        ctl->queue.init(KV8 ? 9 + kTurners : 10);
         mbar_fence_init();
         ctl->gave_up = 0;
     }
-    if (KV8 && threadIdx.x >= 64 && threadIdx.x < 64 + 2 * C::kRawSlots) {
+    if (KV8 && threadIdx.x >= 64 && threadIdx.x < 64 + kTurners * C::kRawSlots) {
         mbar_init(smem_u32(&ctl->raw[threadIdx.x - 64]), 1);
         mbar_fence_init();
     }
@@ -1011,15 +1119,14 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     const uint32_t refused = threadIdx.x == 32 * kIdleWarp ? *(volatile uint32_t *)&a.ctl->needs_init : 0u;
     if (warp == kMmaWarp) tmem_alloc(smem_u32(&ctl->tmem), 512);
     if (threadIdx.x == 32 * kKWarp) {
-        prefetch_map(&q_map);
-        if (!KV8) prefetch_map(&k_map);
+        prefetch_map(&q_map), prefetch_map(&k_map);
     }
     if (!KV8 && threadIdx.x == 32 * kVWarp) prefetch_map(&v_map);
     const AttendWork work(a);
-    List<AttendWork> made = make_list<kThreads>(work, a.B, a.H_kv, a.ctl,
+    List<AttendWork> made = make_list<C::kThreads>(work, a.B, a.H_kv, a.ctl,
                                             a.B > kSmemRequests ? a.prefixes + prefix_bytes(a.B) * blockIdx.x : ctl->prefix, smem);
     // query rows that no tensor copy fills (G does not divide 128) stay zero
-    for (int i = threadIdx.x; i < (work.tpt * a.G == kTile ? 0 : 2 * C::kTileBytes / 16); i += kThreads)
+    for (int i = threadIdx.x; i < (work.tpt * a.G == kTile ? 0 : 2 * C::kTileBytes / 16); i += C::kThreads)
         reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
     if (threadIdx.x == 32 * kIdleWarp) {
         if (refused) {                   // an empty list: the roles find nothing to do, and no counter moves
@@ -1036,22 +1143,24 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
 
     // (the order of the two branches moves the measured cases by 2 %, in both directions)
     if (warp >= 8) {
-        regs_down<kRegsOther>();
         const uint32_t ring = base + 2 * C::kTileBytes;
         if constexpr (KV8) {
-            const uint32_t raw = ring + C::kSlots * C::kKvBytes;
-            if (warp == kKWarp) k8_role<D>(a, list, &q_map, ctl, base, ring, raw, bars, lane);
-            else if (warp == kVWarp) v8_role<D>(a, ctl, ring, raw, bars, lane);
+            regs_down<kRegsOther8>();
+            const uint32_t v_ring = ring + C::kKSlots * C::kKBytes;
+            if (warp == kKWarp) k8_role<D>(a, list, &q_map, &k_map, ctl, base, ring, bars, lane);
             else if (warp == kMmaWarp) mma_role<D, KV8>(a, ctl, base, ring, bars, lane);
+            else if (warp >= kPlainThreads / 32)
+                v8_role<D>(a, ctl, v_ring, v_ring + C::kVSlots * C::kKvBytes, bars, warp - kPlainThreads / 32, lane);
         } else {
+            regs_down<kRegsOther>();
             if (warp == kKWarp) k_role<D>(a, list, &q_map, &k_map, &k_wide, ctl, base, ring, bars, lane);
             else if (warp == kVWarp) v_role<D>(a, &v_map, &v_wide, ctl, ring, bars, lane);
             else if (warp == kMmaWarp) mma_role<D, KV8>(a, ctl, base, ring, bars, lane);
         }
         __syncwarp();
     } else {
-        regs_up<kRegsSoftmax>();
-        softmax_role<D, KV8>(a, list, ctl, bars, warp >> 2);
+        regs_up<KV8 ? kRegsSoftmax8 : kRegsSoftmax>();
+        softmax_role<D, KV8>(a, list, ctl, base, bars, warp >> 2);
     }
     tc_fence_before();
     __syncthreads();
@@ -1069,7 +1178,8 @@ cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t 
     CUtensorMap q_map, k_map, k_wide, v_map, v_wide;
     bool ok = make_rows_map(&q_map, c.q, D, p.H_q, c.total_tokens, c.q_stride, G, kTile / G);
     if (KV8) {
-        k_map = k_wide = v_map = v_wide = q_map;                 // not used
+        ok = ok && make_codes_map(&k_map, c.k, D, (long long)p.num_phys_pages * p.H_kv * kPage, kPage);
+        k_wide = v_map = v_wide = k_map;                         // not used
     } else if (c.page_table) {
         const long long rows = (long long)p.num_phys_pages * p.H_kv * kPage;
         ok = ok && make_rows_map(&k_map, c.k, D, 1, rows, D, 1, kPage) && make_split_map(&v_map, c.v, D, 1, rows, D, kPage);
@@ -1084,7 +1194,7 @@ cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t 
     AttendArgs a = {};
     a.cu = c.cu_seqlens, a.seq_lens = c.seq_lens, a.page_table = c.page_table;
     a.v = static_cast<const uint16_t *>(c.v), a.v_stride = c.v_stride;
-    a.k8 = static_cast<const uint8_t *>(c.k), a.v8 = static_cast<const uint8_t *>(c.v);
+    a.v8 = static_cast<const uint8_t *>(c.v);
     a.scales = reinterpret_cast<const float2 *>(c.scales);
     a.out = static_cast<uint16_t *>(c.out), a.lse = c.lse;
     a.ctl = reinterpret_cast<PromptControl *>(c.workspace);
@@ -1097,12 +1207,13 @@ cudaError_t launch_attend(const se_params &p, const AttendCall &c, cudaStream_t 
     cudaFuncAttributes attr;
     cudaError_t e = cudaFuncGetAttributes(&attr, kern);
     if (e != cudaSuccess) return e;
-    if (attr.numRegs * kThreads < 256 * kRegsSoftmax + 128 * kRegsOther) return cudaErrorInvalidConfiguration;
-    constexpr size_t smem = 2 * C::kTileBytes + C::kSlots * C::kKvBytes + 2 * C::kRawSlots * C::kRawBytes + sizeof(Control<D, KV8>);
+    constexpr int kSplit = KV8 ? 256 * kRegsSoftmax8 + 256 * kRegsOther8 : 256 * kRegsSoftmax + 128 * kRegsOther;
+    if (attr.numRegs * C::kThreads < kSplit) return cudaErrorInvalidConfiguration;
+    constexpr size_t smem = 2 * C::kTileBytes + C::kRings + sizeof(Control<D, KV8>);
     static_assert(smem <= 227 * 1024, "shared memory of a CTA");
     e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    kern<<<kPromptCtas, kThreads, smem, stream>>>(q_map, k_map, k_wide, v_map, v_wide, a);
+    kern<<<kPromptCtas, C::kThreads, smem, stream>>>(q_map, k_map, k_wide, v_map, v_wide, a);
     return cudaGetLastError();
 }
 

@@ -96,6 +96,19 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(instr), "r"((uint32_t)accumulate)
         : "memory");
 }
+// The same for e4m3 operands, both K-major; one instruction = 32 along K.  smem_codes: rows of D bytes (128- or 64-byte swizzle).
+template <int D>
+__device__ __forceinline__ uint64_t smem_codes(uint32_t addr) {
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)(16 >> 4) << 16 | (uint64_t)((8 * D) >> 4) << 32 | 1ull << 46 |
+           (D == 128 ? 2ull : 4ull) << 61;
+}
+__host__ __device__ constexpr uint32_t mma_instr_codes(int N) { return 1u << 4 | (uint32_t)(N >> 3) << 17 | (uint32_t)(128 >> 4) << 24; }
+__device__ __forceinline__ void mma_ss_codes(uint32_t d, uint64_t a, uint64_t b, uint32_t instr, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr), "r"((uint32_t)accumulate)
+        : "memory");
+}
 // arrives on `bar` once every product issued so far by this thread is complete
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -197,6 +210,19 @@ inline bool make_rows_map(CUtensorMap *map, const void *base, int D, long long h
     const cuuint32_t estr[3] = {1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// e4m3 codes [rows][D], boxes of whole rows x box_rows, swizzle as wide as a row, zeros outside
+inline bool make_codes_map(CUtensorMap *map, const void *base, int D, long long rows, int box_rows) {
+    EncodeTiledFn fn = encode_tiled();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)D};
+    const cuuint32_t box[2] = {(cuuint32_t)D, (cuuint32_t)box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

@@ -7,11 +7,17 @@ codes stand for.
 Bounds of the decode kernel (out and lse fp32).  A logit is a sum of D products that are exact in fp32, kept in fp32: its error is
 at most (D + 2) * 2^-23 times the sum of the products' magnitudes.  The exponent's subtraction adds 2^-22 of its magnitude, exp2
 and the weights' sum 2^-18 relative (as in prompt_ref); a weight enters its product with V as two halves, 2^-22 relative, not
-below 2^-25 of the largest weight."""
+below 2^-25 of the largest weight.
+
+Bounds of the chunk kernel (out bf16, lse fp32): those of prompt_ref, and a query row that is split into two rows of codes.  With
+2^e the smallest power of two that brings the row's maximum to 448 or below (so the maximum is above 224 * 2^e), an element of
+at least 2^-2 * 2^e has its last bit at 2^-9 * 2^e or above, the smallest step of a code, and is exact; a smaller one is off by
+half of that step at most, 2^-10 * 2^e."""
 from __future__ import annotations
 
 import math
 
+import prompt_ref
 import torch
 
 PAGE = 16
@@ -126,4 +132,24 @@ def decode(q, k_codes, v_codes, scales, page_table, seq_lens, sel_idx, sel_cnt, 
             tol[r, rows] = 2 * werr @ vv.abs() + 2.0 ** -22 * (w @ vv.abs())
             lse[r, rows] = (top + s.log())[:, 0]
             ltol[r, rows] = (w * zerr).sum(1) + 2.0 ** -22 * lse[r, rows].abs() + 2.0 ** -22
+    return out, tol, lse, ltol
+
+
+def chunk(b, scale):
+    """prompt_ref.attend over the bf16 cache of the codes' values, with the split of the query rows in the bounds.  ``b``: a
+    prompt_ref.Batch."""
+    out, tol, lse, ltol = prompt_ref.attend(b, True, scale)
+    for r in range(b.B):
+        n, rows = b.new[r], b.rows(r)
+        if n == 0:
+            continue
+        q = b.q[rows].double().abs().view(n, b.H_kv, -1, b.D).permute(1, 2, 0, 3)
+        step = torch.exp2(torch.ceil(torch.log2(q.amax(-1, keepdim=True).clamp(min=1e-300) / 448)))
+        k, _ = prompt_ref.cached(b, r, b.k_cache)
+        v, _ = prompt_ref.cached(b, r, b.v_cache)
+        # the logits' error, and what it does to lse and (twice, for weight and sum) to the output
+        z = (((q < 0.25 * step).double() @ k[:, None].abs().transpose(-1, -2)).amax(-1, keepdim=True) * 2.0 ** -10 * step * scale)
+        put = lambda x: x.permute(2, 0, 1, 3).reshape(n, b.H_q, -1)  # noqa: E731
+        ltol[rows] += put(z)[..., 0]
+        tol[rows] += put(2.1 * z * v.abs().amax((1, 2))[:, None, None, None])
     return out, tol, lse, ltol

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import kv8_ref as ref
+import prompt_ref
 from paper_2609_39068_b200 import binding
 
 pytestmark = pytest.mark.gpu
@@ -221,7 +222,7 @@ def test_decode_reports():
 # ---- chunk ----------------------------------------------------------------------------------------
 
 class Chunk:
-    """Packed new tokens over an 8-bit cache, and the bf16 cache that holds the same values."""
+    """Packed new tokens over an 8-bit cache."""
 
     def __init__(self, seed, new, past, H_kv, G, D, absent=0.0, spare=0, sm_scale=0.0):
         g = torch.Generator().manual_seed(seed)
@@ -238,33 +239,41 @@ class Chunk:
                 pid = int(table[r, t // 16])
                 for c in (self.k8, self.v8):
                     c.view(torch.uint8)[pid, :, t % 16:] = 0x7f
-                for c in (self.k16, self.v16):
-                    c[pid, :, t % 16:] = float("nan")
         if absent:
             for r, o in enumerate(past):
                 row = table[r, :o // 16]
                 row[torch.rand(row.shape, generator=g) < absent] = -1
         T, H_q = sum(new) + spare, H_kv * G
         qkv = torch.randn(T, H_q + 2, D, generator=g).to(torch.bfloat16).cuda()
-        self.q = qkv[:, :H_q]                                       # a view of wider rows
+        self.qkv, self.q = qkv, qkv[:, :H_q]                        # a view of wider rows
+        if spare:
+            qkv[sum(new):] = float("nan")
         self.table, self.seq = table.cuda(), torch.tensor(self.total, **I32)
         self.cu = torch.tensor([0] + torch.tensor(new).cumsum(0).tolist(), **I32)
         self.p = binding.make_params(len(new), H_q, H_kv, D, table.shape[1], P, 1, sm_scale=sm_scale)
         self.ws = binding.alloc_prompt_workspace(self.p)
-        self.out = [torch.full((T, H_q, D), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
-        self.lse = [torch.full((T, H_q), float("nan"), device="cuda") for _ in range(2)]
+        self.H_q, self.H_kv, self.D, self.scale = H_q, H_kv, D, sm_scale or D ** -0.5
+        self.out = torch.full((T, H_q, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+        self.lse = torch.full((T, H_q), float("nan"), device="cuda")
 
     def run(self):
-        binding.se_kv8_chunk_attend(self.p, self.q, self.cu, self.k8, self.v8, self.scales, self.table, self.seq, self.out[0], self.ws,
-                                    lse=self.lse[0])
+        binding.se_kv8_chunk_attend(self.p, self.q, self.cu, self.k8, self.v8, self.scales, self.table, self.seq, self.out, self.ws,
+                                    lse=self.lse)
 
     def check(self):
-        binding.se_chunk_attend(self.p, self.q, self.cu, self.k16, self.v16, self.table, self.seq, self.out[1], self.ws, lse=self.lse[1])
-        for _ in range(2):
-            self.run()
-            assert binding.se_last_device_status(self.ws) == 0
-            assert torch.equal(self.out[0].view(torch.int16), self.out[1].view(torch.int16))
-            assert torch.equal(self.lse[0].view(torch.int32), self.lse[1].view(torch.int32))
+        self.run()
+        assert binding.se_last_device_status(self.ws) == 0
+        b = prompt_ref.Batch(self.H_q, self.H_kv, self.D, self.new, self.total, self.q.shape[0], self.p.max_pages, self.p.num_phys_pages,
+                             self.qkv, self.cu, self.seq, self.table, self.k16, self.v16)
+        out, tol, lse, ltol = ref.chunk(b, self.scale)
+        for got, want, t in ((self.lse.double(), lse, ltol), (self.out.double(), out, tol)):
+            live = ~want.isnan()
+            assert bool(got[~live].isnan().all())                   # spare rows are left as they were
+            bad = live & ~(torch.isinf(want) & (got == want)) & ~((got - want).abs() <= t)
+            assert not bool(bad.any()), (int(bad.sum()), float(((got - want).abs() / t)[bad].max()))
+        first = self.out.clone(), self.lse.clone()
+        self.run()                                                  # equal inputs, equal bits
+        assert torch.equal(self.out.view(torch.int16), first[0].view(torch.int16)) and torch.equal(self.lse.view(torch.int32), first[1].view(torch.int32))
 
 
 @pytest.mark.parametrize("new,past,H_kv,G,D,absent,spare", [
@@ -278,9 +287,32 @@ class Chunk:
     ([64] * 100, [33] * 100, 1, 2, 64, 0.1, 0),                     # more requests than prefix sums in shared memory
     ([3, 2], [160, 320], 8, 5, 128, 1.0, 0),                        # nothing but the new tokens is present
 ])
-def test_chunk_is_that_of_the_values(new, past, H_kv, G, D, absent, spare):
-    """The bf16 cache of the same values gives the same bits (its own results are held to 64 bits in test_gpu_prompt.py)."""
+def test_chunk(new, past, H_kv, G, D, absent, spare):
     Chunk(21, new, past, H_kv, G, D, absent, spare).check()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_chunk_of_rows_with_far_elements(D):
+    """Rows whose largest element is 2^0 .. 2^14 times the others, zero rows, tiny rows: the split of a row into codes."""
+    c = Chunk(22, [90], [700], 2, 4, D, sm_scale=0.01)
+    for i in range(15):
+        c.q[6 * i:6 * i + 6, :, 5 + i] *= 2.0 ** i
+    c.q[80:82] = 0
+    c.q[82:84] *= 2.0 ** -90
+    c.check()
+
+
+def test_chunk_rows_that_are_no_numbers_stay_alone():
+    c = Chunk(24, [200], [300], 2, 4, 128)
+    c.run()
+    want = c.out.clone()
+    c.q[7, 3, 11] = float("nan")
+    c.q[150, 6, 0] = float("inf")
+    c.run()
+    bad = torch.zeros(c.out.shape[:2], dtype=torch.bool, device="cuda")
+    bad[7, 3] = bad[150, 6] = True
+    assert bool(c.out[bad].isnan().all()) and bool(c.lse[bad].isnan().all())
+    assert torch.equal(c.out[~bad], want[~bad]) and bool(c.lse[~bad].isfinite().all())
 
 
 def test_chunk_reports():
