@@ -45,8 +45,8 @@ constexpr int kKWarp = 8, kMmaWarp = 9, kVWarp = 10, kIdleWarp = 11;
 // 256 * 200 + 128 * 104 = 384 * 168; nothing spills.  With 208 and 88 the copying and product warps did: packed prompts 372 us for
 // 366, mixed batch 1230 for 1200, 2048 tokens over 65536 1935 for 1890-1910.
 constexpr int kRegsSoftmax = 200, kRegsOther = 104;
-// 8-bit cache: 256 * 184 + 256 * 72 = 512 * 128.
-constexpr int kRegsSoftmax8 = 184, kRegsOther8 = 72;
+// 8-bit cache: 256 * 192 + 256 * 64 = 512 * 128 (2048 tokens over 63488 1.90 ms; 184 and 72: 1.95, 176 and 80: 2.05).
+constexpr int kRegsSoftmax8 = 192, kRegsOther8 = 64;
 constexpr int kTile = 128;             // query rows of a tile
 constexpr int kKv = 128;               // tokens of a KV tile
 constexpr int kGroups = kKv / kPage;   // pages of a KV tile
@@ -65,10 +65,10 @@ struct Cfg {
     static constexpr int kHalves = D / 64;
     static constexpr int kTileBytes = kTile * D * 2;              // query tile
     static constexpr int kKvBytes = kKv * D * 2;                  // K or V tile
-    // rings of K and V tiles, 64 and 96 KB; from an 8-bit cache 64 each (K as codes), and each turning warp's ring of V's pages
-    static constexpr int kKSlots = (KV8 ? 4 : 2) * 128 / D, kVSlots = (KV8 ? 2 : 3) * 128 / D;
+    // rings of K and V tiles, 64 and 96 KB; from an 8-bit cache 48 (codes) and 64, and the turning warps' rings of V's pages, 32 KB
+    static constexpr int kKSlots = (KV8 ? 3 : 2) * 128 / D, kVSlots = (KV8 ? 2 : 3) * 128 / D;
     static constexpr int kKBytes = KV8 ? kKv * D : kKvBytes;
-    static constexpr int kRawSlots = KV8 ? 3 * 128 / D : 0, kRawBytes = kPage * D;
+    static constexpr int kRawSlots = KV8 ? 2 * 128 / D : 0, kRawBytes = kGroups / kTurners * kPage * D;
     static constexpr int kThreads = kPlainThreads + (KV8 ? 32 * kTurners : 0);
     static constexpr int kRings = kKSlots * kKBytes + kVSlots * kKvBytes + kTurners * kRawSlots * kRawBytes;
     static constexpr int kSlots = kKSlots + kVSlots;
@@ -384,32 +384,42 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v
 // two pages of every tile each into a ring of their own, turn them, and write the tile that the tensor copies would.
 // (With K turned into bf16 too, by one warp and V by another, a step took 9000 to 11000 cycles instead of 3350.)
 
-// Page ids and scales of 32 groups of 16 tokens at a time, a lane each, and of the next 32 ahead.  Lane i of block b has the group
+// Page ids and scales of 32 groups of 16 tokens at a time, a lane each; scales of the next 32 and ids of the 32 behind those are on
+// their way (a scale is found through its page's id, and waiting for the id takes a round trip).  Lane i of block b has the group
 // (32 b + i) * step + first.
 struct CodePages {
-    int ids, next, block;
+    int ids, next, later, block;
     float scale, next_scale;
 
-    __device__ __forceinline__ void fetch(const AttendArgs &a, const Segment &s, int g, bool of_v, int &id, float &sc) const {
-        id = -1, sc = 1.f;
-        if (g * kPage >= s.t.past + s.t.n) return;
-        const int pid = a.page_table[(size_t)s.r * a.max_pages + g];
-        if (pid >= a.P_phys && !of_v) atomicOr(&a.ctl->status, SE_DEV_BAD_PAGE_ID);
-        if (pid < 0 || pid >= a.P_phys) return;
-        id = pid * a.H_kv + s.h;
-        const float2 both = a.scales[id];
-        sc = of_v ? both.y : both.x;
+    __device__ __forceinline__ int fetch(const AttendArgs &a, const Segment &s, int g) const {
+        return g * kPage < s.t.past + s.t.n ? a.page_table[(size_t)s.r * a.max_pages + g] : -1;
+    }
+    __device__ __forceinline__ float scale_of(const AttendArgs &a, const Segment &s, int &id, bool of_v) const {
+        if (id >= a.P_phys) {
+            if (!of_v) atomicOr(&a.ctl->status, SE_DEV_BAD_PAGE_ID);
+            id = -1;
+        }
+        return id < 0 ? 1.f : reinterpret_cast<const float *>(a.scales + ((size_t)id * a.H_kv + s.h))[of_v];
     }
     __device__ __forceinline__ void begin(const AttendArgs &a, const Segment &s, int j, int step, int first, bool of_v, int lane) {
         block = j / 32;
-        fetch(a, s, (block * 32 + lane) * step + first, of_v, ids, scale);
-        fetch(a, s, (block * 32 + 32 + lane) * step + first, of_v, next, next_scale);
+        ids = fetch(a, s, (block * 32 + lane) * step + first);
+        next = fetch(a, s, (block * 32 + 32 + lane) * step + first);
+        later = fetch(a, s, (block * 32 + 64 + lane) * step + first);
+        scale = scale_of(a, s, ids, of_v);
+        next_scale = scale_of(a, s, next, of_v);
     }
     __device__ __forceinline__ void reach(const AttendArgs &a, const Segment &s, int j, int step, int first, bool of_v, int lane) {
         if (j / 32 == block) return;
         ++block;
-        ids = next, scale = next_scale;
-        fetch(a, s, (block * 32 + 32 + lane) * step + first, of_v, next, next_scale);
+        ids = next, scale = next_scale, next = later;
+        next_scale = scale_of(a, s, next, of_v);
+        later = fetch(a, s, (block * 32 + 64 + lane) * step + first);
+    }
+    // page * H_kv + head of item j of this block or the next, -1: absent
+    __device__ __forceinline__ int of(const AttendArgs &a, const Segment &s, int j) const {
+        const int id = __shfl_sync(kFull, ids, j % 32), id1 = __shfl_sync(kFull, next, j % 32), x = j / 32 == block ? id : id1;
+        return x < 0 ? -1 : x * a.H_kv + s.h;
     }
 };
 
@@ -455,10 +465,10 @@ __device__ __forceinline__ void k8_role(const AttendArgs &a, const List<AttendWo
             const unsigned mask = __ballot_sync(kFull, pages.ids >= 0) >> at & 0xffu;
             int id[kGroups];
 #pragma unroll
-            for (int pg = 0; pg < kGroups; ++pg) id[pg] = __shfl_sync(kFull, pages.ids, at + pg);
+            for (int pg = 0; pg < kGroups; ++pg) id[pg] = pages.of(a, s, t * kGroups + pg);
             ok = warp_wait(k_empty + 8 * slot, (tiles / C::kKSlots & 1) ^ 1, gave_up, &a.ctl->status);
             if (!ok) break;
-            if (lane >= at && lane < at + kGroups) ctl->k_scale[tiles % C::kMasks][lane - at] = pages.scale;
+            if (lane >= at && lane < at + kGroups) ctl->k_scale[tiles % C::kMasks][lane - at] = fmaxf(pages.scale, 0x1p-64f);
             __syncwarp();
             if (chosen) {
                 ctl->mask[tiles % C::kMasks] = mask;
@@ -486,95 +496,79 @@ __device__ __forceinline__ void v8_role(const AttendArgs &a, Control<D, true> *c
     constexpr int N = D / 32;                                              // pieces of 16 codes per lane and page
     volatile int *gave_up = &ctl->gave_up;
     CodePages pages;
-    uint32_t tiles = 0, sent = 0, used = 0, turn = 0;                      // pages whose copy has been issued, that have been turned
+    uint32_t tiles = 0, sent = 0, turn = 0;                                // tiles that have been turned, whose copies have been issued
     const uint32_t v_full = bars + 8 * (kRing + C::kKSlots), v_empty = v_full + 8 * C::kSlots;
     const uint32_t raw_bars = smem_u32(ctl->raw) + 8 * C::kRawSlots * w;
     raw += C::kRawSlots * C::kRawBytes * w;
-    const bool chosen = elect_one();
     // lane -> token and 16 codes of it: eight lanes store to all banks, whatever the swizzle
     const int row = lane >> 2, part = lane & 3;
-    const uint32_t store0 = row * 128 + (((2 * part) ^ row) << 4), store1 = row * 128 + (((2 * part + 1) ^ row) << 4);
+    const uint32_t store0 = tiles_at + row * 128 + (((2 * part) ^ row) << 4), store1 = tiles_at + row * 128 + (((2 * part + 1) ^ row) << 4);
     bool ok = true;
     while (ok) {
         const Segment *entry = ctl->queue.get(turn++, gave_up, &a.ctl->status, lane);
         if (!entry) break;
         const Segment s = *entry;
-        const int stop = s.t.past + s.t.n, end = s.b * kMine;
-        int ahead = s.a * kMine;                                           // next page whose copy is to be issued, in the warp's own count
-        pages.begin(a, s, ahead, kTurners, w, true, lane);
-        auto send = [&] {
-            while (ahead < end && sent - used < (uint32_t)C::kRawSlots && ahead / 32 <= pages.block + 1) {
-                const int id = __shfl_sync(kFull, ahead / 32 == pages.block ? pages.ids : pages.next, ahead % 32);
-                if (id >= 0) {
-                    if (chosen) {
-                        const uint32_t slot = sent % C::kRawSlots;
-                        mbar_expect_tx(raw_bars + 8 * slot, C::kRawBytes + (D == 128 && sent == 0 ? kTestExtraTx : 0));
-                        bulk_g2s(raw + slot * C::kRawBytes, a.v8 + (size_t)id * C::kRawBytes, C::kRawBytes, raw_bars + 8 * slot);
-                    }
-                    __syncwarp();
-                    ++sent;
-                }
-                ++ahead;
-            }
+        const int stop = s.t.past + s.t.n;
+        pages.begin(a, s, s.a * kMine, kTurners, w, true, lane);
+        // the two pages of tile t, a lane each (nothing is copied for absent ones)
+        auto send = [&](int t) {
+            const int id = pages.of(a, s, t * kMine + lane % kMine);
+            const bool mine = lane < kMine && id >= 0;
+            const int present = __popc(__ballot_sync(kFull, mine));
+            const uint32_t slot = sent % C::kRawSlots, bar = raw_bars + 8 * slot;
+            if (lane == 0) mbar_expect_tx(bar, present * (kPage * D) + (D == 128 && sent == 0 ? kTestExtraTx : 0));
+            __syncwarp();
+            if (mine) bulk_g2s(raw + slot * C::kRawBytes + lane * (kPage * D), a.v8 + (size_t)id * (kPage * D), kPage * D, bar);
+            __syncwarp();
+            ++sent;
         };
-        send();
+        int ahead = s.a;
+        for (; ahead < min(s.b, s.a + C::kRawSlots); ++ahead) send(ahead);
         for (int t = s.a; t < s.b; ++t, ++tiles) {
-            const uint32_t slot = tiles % C::kVSlots, dst = tiles_at + slot * C::kKvBytes;
+            const uint32_t slot = tiles % C::kVSlots, from = tiles % C::kRawSlots;
             pages.reach(a, s, t * kMine, kTurners, w, true, lane);
-            send();
-            ok = warp_wait(v_empty + 8 * slot, (tiles / C::kVSlots & 1) ^ 1, gave_up, &a.ctl->status);
+            ok = warp_wait(v_empty + 8 * slot, (tiles / C::kVSlots & 1) ^ 1, gave_up, &a.ctl->status) &&
+                 warp_wait(raw_bars + 8 * from, tiles / C::kRawSlots & 1, gave_up, &a.ctl->status);
             if (!ok) break;
 #pragma unroll 1
             for (int i = 0; i < kMine; ++i) {
                 const int j = t * kMine + i, group = j * kTurners + w;
-                const uint32_t at = dst + (group % kGroups) * (kPage * D * 2);
-                if (__shfl_sync(kFull, pages.ids, j % 32) < 0) {           // an absent group: zeros
-#pragma unroll
-                    for (int e = 0; e < kPage * D * 2 / 512; ++e)
-                        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(at + lane * 16 + e * 512), "r"(0) : "memory");
-                    continue;
-                }
+                const bool here = __shfl_sync(kFull, pages.ids, j % 32) >= 0;
                 const __nv_bfloat162 f = __float2bfloat162_rn(__shfl_sync(kFull, pages.scale, j % 32) * kv8_bf16_step());
-                const uint32_t from = used % C::kRawSlots;
-                ok = warp_wait(raw_bars + 8 * from, used / C::kRawSlots & 1, gave_up, &a.ctl->status);
-                if (!ok) break;
                 uint4 x[N];
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    const uint32_t src = raw + from * C::kRawBytes + row * D + part * 16 + e / (D / 64) * (8 * D) + e % (D / 64) * 64;
+                    const uint32_t src = raw + from * C::kRawBytes + i * (kPage * D) + row * D + part * 16 + e / (D / 64) * (8 * D) + e % (D / 64) * 64;
                     asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[e].x), "=r"(x[e].y), "=r"(x[e].z), "=r"(x[e].w) : "r"(src) : "memory");
                 }
-                // what lies behind the end of the request may be anything, and a weight of zero would not hide it
-                const int tokens = stop - group * kPage;
+                // what lies behind the end of the request may be anything, and a weight of zero would not hide it; of an absent page too
+                const int tokens = here ? stop - group * kPage : 0;
                 if (tokens < kPage) {
 #pragma unroll
                     for (int e = 0; e < N; ++e)
                         if (row + 8 * (e / (D / 64)) >= tokens) x[e] = make_uint4(0, 0, 0, 0);
                 }
+                const uint32_t to = slot * C::kKvBytes + (group % kGroups) * (kPage * D * 2);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    const uint32_t c[4] = {x[e].x, x[e].y, x[e].z, x[e].w}, to = at + e / (D / 64) * 1024 + e % (D / 64) * (kPage * 128);
+                    const uint32_t c[4] = {x[e].x, x[e].y, x[e].z, x[e].w}, at = to + e / (D / 64) * 1024 + e % (D / 64) * (kPage * 128);
                     uint32_t o[8];
 #pragma unroll
                     for (int q = 0; q < 4; ++q) kv8_bf16x4(c[q], f, o[2 * q], o[2 * q + 1]);
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to + store0), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to + store1), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + store0), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + store1), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
                 }
-                __syncwarp();
-                ++used;
-                send();
             }
-            if (!ok) break;
             fence_async_proxy();
             __syncwarp();
-            if (chosen) mbar_arrive(v_full + 8 * slot);
-            __syncwarp();
+            if (lane == 0) mbar_arrive(v_full + 8 * slot);
+            if (ahead < s.b) send(ahead++);                                // (all lanes have their codes)
         }
     }
     // the end of the warp: the products' arrivals for the tiles, and its copies
     for (uint32_t n = tiles > C::kVSlots ? tiles - C::kVSlots : 0; ok && n < tiles; ++n)
         ok = warp_wait(v_empty + 8 * (n % C::kVSlots), n / C::kVSlots & 1, gave_up, &a.ctl->status);
-    for (; used != sent; ++used) mbar_wait(raw_bars + 8 * (used % C::kRawSlots), used / C::kRawSlots & 1);
+    for (; tiles != sent; ++tiles) mbar_wait(raw_bars + 8 * (tiles % C::kRawSlots), tiles / C::kRawSlots & 1);
 }
 
 // A query tile of bf16 becomes codes in its place, by the threads of a warpgroup, a row each: at D = 128 two tiles, hi and lo, at
@@ -868,6 +862,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
         }
         // sum of the weights over the tiles so far, and what rounding took from it (Kahan); a row that is not finite begins with a NaN
         float l = KV8 && row_scale != row_scale ? row_scale : 0.f, lost = 0.f;
+        row_scale = fmaxf(row_scale, 0x1p-60f);                            // (with the least scale of a page not 0, which times a masked score would be NaN)
         for (int u = 0; u < steps; ++u, ++step, left -= stride * kKv, most -= stride * kKv, tile += stride) {
             if (!warp_wait(bars + 8 * (kSFull + st), step & 1, gave_up, &a.ctl->status)) return;
             tc_fence_after();
@@ -901,7 +896,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
                     float top = max3(y[0], y[1], y[2]);
 #pragma unroll
                     for (int k = 3; k + 1 < kPage; k += 2) top = max3(top, y[k], y[k + 1]);
-                    mn = fmaxf(mn, fmaxf(top, y[kPage - 1]) * fmaxf(k_scale[pg] * row_scale, 1e-37f));   // (0 times a masked score would be NaN)
+                    mn = fmaxf(mn, fmaxf(top, y[kPage - 1]) * (k_scale[pg] * row_scale));
                 }
                 grown = mn - m;
             } else {
@@ -937,7 +932,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
                 uint32_t p[32];
 #pragma unroll
                 for (int e = 0; e < 32; ++e) {
-                    const float by = KV8 ? fmaxf(k_scale[(k + 2 * e) / kPage] * row_scale, 1e-37f) : sl;
+                    const float by = KV8 ? k_scale[(k + 2 * e) / kPage] * row_scale : sl;
                     const float2 y = ffma2(make_float2(x[k + 2 * e], x[k + 2 * e + 1]), make_float2(by, by), make_float2(off, off));
                     const float2 w = make_float2(ex2(y.x), ex2(y.y));
                     l2 = __fadd2_rn(l2, w);

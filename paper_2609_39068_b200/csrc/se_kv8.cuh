@@ -77,10 +77,12 @@ __device__ __forceinline__ uint4 kv8_values(const uint2 &u, float scale) {
 // to the place of a bf16's, are its value times 2^-120 (the difference of the biases), subnormal codes included.
 __device__ __forceinline__ constexpr float kv8_bf16_step() { return 0x1p120f; }
 __device__ __forceinline__ void kv8_bf16x4(uint32_t codes, __nv_bfloat162 f, uint32_t &lo, uint32_t &hi) {
-    uint32_t x[2] = {__byte_perm(codes, 0, 0x1404), __byte_perm(codes, 0, 0x3424)};      // a code in the upper byte of each half
+    uint32_t x[2];                       // halves: a code, its sign in all bits above
+    asm("prmt.b32 %0, %1, 0, 0x9180;" : "=r"(x[0]) : "r"(codes));
+    asm("prmt.b32 %0, %1, 0, 0xb3a2;" : "=r"(x[1]) : "r"(codes));
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const uint32_t y = (x[i] & 0x80008000u) | (x[i] >> 4 & 0x07f007f0u);
+        const uint32_t y = x[i] << 4 & 0x87f087f0u;
         const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&y), f);
         x[i] = *reinterpret_cast<const uint32_t *>(&v);
     }
