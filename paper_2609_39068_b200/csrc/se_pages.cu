@@ -183,7 +183,7 @@ __device__ __forceinline__ int open_page(const UpdateArgs &a, const Slot &x) {
     return is_page(a, e) ? e : -1;
 }
 
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, 2)
 pages_update_kernel(const __grid_constant__ UpdateArgs a, const __grid_constant__ Buffers buf) {
     extern __shared__ int s_asked[];                   // [B + 1] pages asked for before each slot, [B + 1] copies
     __shared__ int s_red[kWarps], s_scan[32], s_first[SE_MAX_PAGE_BUFFERS + 1];
@@ -330,7 +330,7 @@ pages_update_kernel(const __grid_constant__ UpdateArgs a, const __grid_constant_
 }
 
 // ---- compact -----------------------------------------------------------------------
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, 2)
 pages_compact_kernel(const __grid_constant__ CompactArgs a, const __grid_constant__ Buffers buf) {
     __shared__ int s_red[kWarps], s_scan[32], s_first[SE_MAX_PAGE_BUFFERS + 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
