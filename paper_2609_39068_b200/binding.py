@@ -135,13 +135,13 @@ def _check(rc: int, what: str):
 def _ptr(t: Optional[torch.Tensor], dtype, name: str):
     if t is None:
         return None
+    if t.is_cuda and t.dtype == dtype and t.is_contiguous():
+        return t.data_ptr()
     if not t.is_cuda:
         raise SparseEngineError("%s must be a CUDA tensor" % name)
     if t.dtype != dtype:
         raise SparseEngineError("%s must have dtype %s, got %s" % (name, dtype, t.dtype))
-    if not t.is_contiguous():
-        raise SparseEngineError("%s must be contiguous" % name)
-    return t.data_ptr()
+    raise SparseEngineError("%s must be contiguous" % name)
 
 
 def _stream():
@@ -359,8 +359,23 @@ def se_h2o_compact(p, k_cache, v_cache, score_accum, page_table, keep_idx, keep_
 
 # ---- prompt side: a packed batch of new tokens -------------------------------------------------------
 
+# sizes by the bytes of the se_params (they are functions of it alone; asking the library took 1.5 us of every small call)
+_prompt_bytes: dict = {}
+_pages_bytes: dict = {}
+
+
+def _size(known: dict, entry: str, p: SeParams) -> int:
+    key = bytes(p)
+    n = known.get(key)
+    if n is None:
+        if len(known) >= 4096:
+            known.clear()
+        n = known[key] = int(getattr(load(), entry)(ctypes.byref(p)))
+    return n
+
+
 def se_prompt_workspace_bytes(p: SeParams) -> int:
-    return int(load().se_prompt_workspace_bytes(ctypes.byref(p)))
+    return _size(_prompt_bytes, "se_prompt_workspace_bytes", p)
 
 
 def se_prompt_workspace_init(p: SeParams, workspace: torch.Tensor) -> None:
@@ -413,18 +428,20 @@ def _prompt_common(p: SeParams, workspace: torch.Tensor, cu_seqlens, page_table=
 
 def _call(entry: str, workspace: torch.Tensor, tensors, *args) -> None:
     """The call on the current stream of the workspace's device, where every other tensor has to be too.  (The device is
-    switched only where it has to be: torch.cuda.device and the default current_stream took 5 us of a small call.)"""
+    switched only where it has to be, and the stream's handle is asked for without an object around it: torch.cuda.device and
+    current_stream took 9 us of a small call.)"""
     ws, dev = _ptr(workspace, torch.uint8, "workspace"), workspace.get_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise SparseEngineError("all tensors must be on %s, got one on %s" % (workspace.device, t.device))
-    f = getattr(load(), entry)
-    if dev == torch.cuda.current_device():
-        rc = f(*args, ws, torch.cuda.current_stream(dev).cuda_stream)
+    f = getattr(_lib or load(), entry)
+    if dev == torch._C._cuda_getDevice():
+        rc = f(*args, ws, torch._C._cuda_getCurrentRawStream(dev))
     else:
         with torch.cuda.device(dev):
-            rc = f(*args, ws, torch.cuda.current_stream(dev).cuda_stream)
-    _check(rc, entry)
+            rc = f(*args, ws, torch._C._cuda_getCurrentRawStream(dev))
+    if rc != SE_OK:
+        _check(rc, entry)
 
 
 def _append(entry, p, q, k, v, cu_seqlens, seq_lens, page_table, positions, inv_freq, pair_axis, q_out, k_cache, v_cache,
@@ -555,7 +572,7 @@ def se_kv8_chunk_attend(p, q, cu_seqlens, k_cache, v_cache, scales, page_table, 
 # ---- the pool's pages --------------------------------------------------------------------------------
 
 def se_pages_workspace_bytes(p: SeParams) -> int:
-    return int(load().se_pages_workspace_bytes(ctypes.byref(p)))
+    return _size(_pages_bytes, "se_pages_workspace_bytes", p)
 
 
 def se_pages_workspace_init(p: SeParams, workspace: torch.Tensor) -> None:
