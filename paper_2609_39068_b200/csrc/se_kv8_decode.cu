@@ -16,8 +16,8 @@
 // bandwidth: 64 requests x 2048 tokens 63 us.)
 //
 // Split.  A tile is eight pages of a (request, kv-head) pair's list.  The tiles of all pairs are cut into 148 runs of equal
-// length, one per CTA.  One warp looks the pages up (selection, page and scale three blocks of 32 apart) and fetches them, one
-// splits q a pair ahead, one issues the products, two warpgroups take every second tile each.  At the end of a pair each puts its
+// length, one per CTA.  Four warps look the pages up (selection, page and scale a block of 32 apart) and fetch K and V, one splits q
+// a pair ahead, two issue the products, two warpgroups take every second tile each.  At the end of a pair each puts its
 // sums aside and goes on; they take turns in merging them.  A pair that several CTAs share leaves partial results in the
 // workspace, and the CTA that arrives last merges them in order: equal inputs give equal bits.
 #include <math.h>
@@ -30,8 +30,8 @@ namespace se {
 
 namespace {
 
-constexpr int kThreads = 352;          // two warpgroups, then a warp each
-constexpr int kFetchWarp = 8, kMmaWarp = 9, kQueryWarp = 10;
+constexpr int kThreads = 480;          // two warpgroups, then a warp each
+constexpr int kScoreWarp = 8, kOutWarp = 9, kQueryWarp = 10, kFetchWarp = 11, kFetchers = 2;   // (and two each for K and V)
 constexpr int kTile = 128, kGroups = kTile / kPage;
 constexpr int kChunks = 1024;          // prefix sums that a CTA keeps: of every pair, or of runs of pairs
 constexpr int kParts = 5;              // codes of a weight
@@ -41,15 +41,16 @@ constexpr int kQueries = 4;            // pairs whose q is kept
 template <int D>
 struct Cfg {
     static constexpr int kPageBytes = kPage * D, kTileBytes = kTile * D;      // of K or of V, one head
-    static constexpr int kStages = D == 128 ? 5 : 8;
+    static constexpr int kKStages = D == 128 ? 4 : 6, kVStages = D == 128 ? 6 : 10;
     static constexpr int kWeightBytes = kTile * 64;                           // a token's codes: up to 48 of 64 bytes
-    static constexpr int kQueryBytes = 2 * 16 * D;                            // hi and lo, 16 rows each
+    static constexpr int kQueryBytes = 16 * D;                                // eight rows of hi, eight of lo
     static constexpr int kPartFloats = 8 * D + 16;                            // a partial result: O, M, l
-    static constexpr int kRing = kStages * 2 * kTileBytes;
+    static constexpr int kVAt = kKStages * kTileBytes, kRing = kVAt + kVStages * kTileBytes;
     static constexpr int kQueryAt = kRing + 2 * kWeightBytes;
     static constexpr int kAsideAt = kQueryAt + kQueries * kQueryBytes;
     static constexpr int kControlAt = kAsideAt + 4 * kPartFloats * 4;         // [pair's parity][warpgroup]
 };
+static_assert(kThreads == 32 * (kFetchWarp + 2 * kFetchers), "a warp for each role");
 static_assert(Cfg<128>::kQueryAt % 1024 == 0 && Cfg<64>::kQueryAt % 1024 == 0 && Cfg<128>::kControlAt % 16 == 0 && Cfg<64>::kControlAt % 16 == 0 &&
               Cfg<128>::kQueryBytes % 1024 == 0 && Cfg<64>::kQueryBytes % 1024 == 0, "operands and 16-byte accesses");
 
@@ -60,12 +61,12 @@ struct PageInfo {
 
 template <int D>
 struct Control {
-    PageInfo info[Cfg<D>::kStages][kGroups];
+    PageInfo info[Cfg<D>::kVStages][kGroups];
     float power[kQueries][8];          // of each head: logit in powers of two = sum * power * s_K
     float top[2][2][4][8];             // largest w of a tile: [warpgroup][tile's parity][warp][head]
     float sum[2][4][8];                // sums of a pair's weights: [warpgroup][warp][head]
-    uint64_t full[Cfg<D>::kStages], empty[Cfg<D>::kStages], q_ready[kQueries], q_free[kQueries];
-    uint64_t s_full[2], p_ready[2], o_done[2], exchange[2], aside[2], merged[2], drain;
+    uint64_t k_full[Cfg<D>::kKStages], k_empty[Cfg<D>::kKStages], v_full[Cfg<D>::kVStages], v_empty[Cfg<D>::kVStages], q_ready[kQueries], q_free[kQueries];
+    uint64_t s_full[2][2], s_free[2][2], p_ready[2], o_done[2], exchange[2], aside[2], merged[2], drain[2];
     long long pre[kChunks + 1];
     long long sums[kThreads / 32];
     uint32_t tmem;
@@ -159,87 +160,116 @@ struct Walk {
 };
 
 // ---- pages ---------------------------------------------------------------------------
-// What a lane of the fetching warp knows of a page, found in three steps that lie a block of 32 pages (four tiles) apart.
+// What a lane of a fetching warp knows of a page, found in three steps that lie a block of 32 pages (four tiles) apart.
 struct Found {
-    int pair, b, len;                  // 1: pair (-1: no page), logical page, length of the request
+    int r, h, j, count, b, len;        // 1: request (-1: behind the run), head, place in the pair's list, entries of the list, logical page, length
     int row, tokens;                   // 2, 3: page * H_kv + head, -1: not present; tokens below the length
     float2 scale;                      // 3
 };
-__device__ __forceinline__ void find_page(const Args &a, const Pairs &ps, long long u0, int n, int i, Found &f) {
-    f.pair = -1;
-    if (i / kGroups >= n) return;
+// A lane's way through the pairs: tiles come in ascending order.
+struct Cursor {
+    int pair, count, r, h;
     long long first;
-    const int pair = ps.find(u0 + i / kGroups, first);
-    const int j = (int)(u0 + i / kGroups - first) * kGroups + i % kGroups;
-    if (j >= ps.pages(pair)) return;
-    f.pair = pair;
-    f.b = a.sel_idx ? a.sel_idx[(size_t)pair * a.k_max + j] : j;
-    f.len = a.seq_lens[pair / a.H_kv];
-}
+
+    __device__ __forceinline__ Cursor(const Args &a, const Pairs &ps, long long u) {
+        pair = ps.find(u, first), count = ps.count_known(pair);
+        r = pair / a.H_kv, h = pair - r * a.H_kv;
+    }
+    __device__ __forceinline__ void find_page(const Args &a, const Pairs &ps, long long u0, int n, int i, Found &f) {
+        f.r = -1;
+        if (i / kGroups >= n) return;
+        while (u0 + i / kGroups >= first + count) {
+            first += count, count = ps.count_known(++pair);
+            if (++h == a.H_kv) h = 0, ++r;
+        }
+        f.r = r, f.h = h;
+        f.j = (int)(u0 + i / kGroups - first) * kGroups + i % kGroups;
+        f.len = a.seq_lens[r];
+        // (nothing that is loaded here is used here)
+        f.count = a.sel_cnt ? a.sel_cnt[pair] : 0;
+        f.b = a.sel_idx ? a.sel_idx[(size_t)pair * a.k_max + min(f.j, a.k_max - 1)] : f.j;
+    }
+};
 __device__ __forceinline__ void find_row(const Args &a, Found &f) {
     f.row = -1, f.tokens = 0;
-    if (f.pair < 0) return;
+    if (f.r < 0 || f.j >= (a.sel_cnt ? min(f.count, a.k_max) : (f.len + kPage - 1) / kPage)) return;
     if (f.b < 0 || f.b >= a.max_pages || f.b * kPage >= f.len) {           // (only a selection can be wrong here)
         atomicOr(&a.ctl->status, SE_DEV_BAD_SELECTION);
         return;
     }
-    f.row = a.page_table[(size_t)(f.pair / a.H_kv) * a.max_pages + f.b];
+    f.row = a.page_table[(size_t)f.r * a.max_pages + f.b];
     f.tokens = min(kPage, f.len - f.b * kPage);
 }
+template <bool OF_V>
 __device__ __forceinline__ void find_scale(const Args &a, Found &f) {
     if (f.row >= a.P_phys) {
-        atomicOr(&a.ctl->status, SE_DEV_BAD_PAGE_ID);
+        if (OF_V) atomicOr(&a.ctl->status, SE_DEV_BAD_PAGE_ID);
         f.row = -1;
     }
     f.scale = make_float2(1.f, 1.f);
     if (f.row < 0) return;
-    f.row = f.row * a.H_kv + f.pair % a.H_kv;
-    f.scale = a.scales[f.row];
+    f.row = f.row * a.H_kv + f.h;
+    if (OF_V) f.scale = a.scales[f.row];
 }
 
-template <int D>
-__device__ __forceinline__ void fetch_role(const Args &a, const Pairs &ps, const CUtensorMap *k_map, const CUtensorMap *v_map, Control<D> *ctl,
-                                           uint32_t base, long long u0, int n, int lane) {
+// Two warps bring K, two V and what is to be known of the pages, each every second tile.  (One alone took 1550 cycles a tile, half of
+// them for loads that a block ahead was not far enough for.)  The rings have even numbers of slots, so a slot belongs to one warp,
+// which waits for it in every phase; a warpgroup's tiles are those of one V warp.
+template <int D, bool OF_V>
+__device__ __forceinline__ void fetch_role(const Args &a, const Pairs &ps, const CUtensorMap *map, Control<D> *ctl, uint32_t ring, long long u0, int n, int which,
+                                           int lane) {
     using C = Cfg<D>;
+    constexpr int kStages = OF_V ? C::kVStages : C::kKStages, kBlock = 32 / kGroups;
+    static_assert(kFetchers == 2 && kStages % kFetchers == 0, "slots of a warp's own");
     volatile int *gave_up = &ctl->gave_up;
-    const uint32_t full = smem_u32(ctl->full), empty = smem_u32(ctl->empty);
+    const uint32_t full = smem_u32(OF_V ? ctl->v_full : ctl->k_full), empty = smem_u32(OF_V ? ctl->v_empty : ctl->k_empty);
     const bool chosen = elect_one();
+    if (which >= n) return;
     Found now, next, later, last;
-    find_page(a, ps, u0, n, lane, now), find_page(a, ps, u0, n, 32 + lane, next), find_page(a, ps, u0, n, 64 + lane, later);
-    find_row(a, now), find_row(a, next);
-    find_scale(a, now);
+    // the lane's page of the warp's block b: place in the run's list
+    auto place = [&](int b) { return ((b * kBlock + lane / kGroups) * kFetchers + which) * kGroups + lane % kGroups; };
+    Cursor at_lane(a, ps, u0 + min(place(0) / kGroups, n - 1));
+    at_lane.find_page(a, ps, u0, n, place(0), now);
+    find_row(a, now);
+    find_scale<OF_V>(a, now);
     bool ok = true;
-    int i = 0;
-    for (; i < n; ++i) {
-        const int at = i * kGroups % 32;                                   // the tile's pages are lanes at .. at + 7
-        if (at == 0) {
-            if (i) now = next, next = later, later = last;
-            find_scale(a, next), find_row(a, later), find_page(a, ps, u0, n, i * kGroups + 96 + lane, last);
-        }
+    int i = which, m = 0;              // tile, and the warp's own count
+    for (; i < n; i += kFetchers, ++m) {
+        const int at = m % kBlock * kGroups;                               // the tile's pages are lanes at .. at + 7
+        if (at == 0 && m) now = next, next = later, later = last;
         int row[kGroups];
 #pragma unroll
         for (int pg = 0; pg < kGroups; ++pg) row[pg] = __shfl_sync(kFull, now.row, at + pg);
-        const uint32_t slot = i % C::kStages, bar = full + 8 * slot, dst = base + slot * (2 * C::kTileBytes);
-        ok = warp_wait(empty + 8 * slot, (i / C::kStages & 1) ^ 1, gave_up, &a.ctl->status);
+        const uint32_t slot = i % kStages, bar = full + 8 * slot, dst = ring + slot * C::kTileBytes;
+        ok = warp_wait(empty + 8 * slot, (i / kStages & 1) ^ 1, gave_up, &a.ctl->status);
         if (!ok) break;
-        if (lane >= at && lane < at + kGroups)
-            ctl->info[slot][lane - at] = PageInfo{now.scale.x, now.scale.y, now.row >= 0 ? now.tokens : 0, 0};
-        __syncwarp();
+        if (OF_V) {
+            if (lane >= at && lane < at + kGroups)
+                ctl->info[slot][lane - at] = PageInfo{now.scale.x, now.scale.y, now.row >= 0 ? now.tokens : 0, 0};
+            __syncwarp();
+        }
         if (chosen) {
-            mbar_expect_tx(bar, 2 * C::kTileBytes + (i == 0 ? kTestExtraTx : 0));
+            mbar_expect_tx(bar, C::kTileBytes + (OF_V && i == 0 ? kTestExtraTx : 0));
 #pragma unroll
-            for (int pg = 0; pg < kGroups; ++pg) {                         // absent: from behind the last row, zeros
-                const int y = (row[pg] < 0 ? a.P_phys * a.H_kv : row[pg]) * kPage;
-                tma_load_2d(dst + pg * C::kPageBytes, k_map, 0, y, bar);
-                tma_load_2d(dst + C::kTileBytes + pg * C::kPageBytes, v_map, 0, y, bar);
-            }
+            for (int pg = 0; pg < kGroups; ++pg)                           // absent: from behind the last row, zeros
+                tma_load_2d(dst + pg * C::kPageBytes, map, 0, (row[pg] < 0 ? a.P_phys * a.H_kv : row[pg]) * kPage, bar);
         }
         __syncwarp();
+        if (at == 0) {                 // what comes later is looked up behind the copies
+            const int b = m / kBlock;
+            if (b == 0) {
+                at_lane.find_page(a, ps, u0, n, place(1), next), at_lane.find_page(a, ps, u0, n, place(2), later);
+                find_row(a, next);
+            }
+            at_lane.find_page(a, ps, u0, n, place(b + 3), last);
+            find_row(a, later);
+            find_scale<OF_V>(a, next);
+        }
     }
     // nothing may still be on its way to the CTA's shared memory, or arrive there, when the CTA ends
-    for (int e = max(i - C::kStages, 0); e < i; ++e) {
-        ok = ok && warp_wait(empty + 8 * (e % C::kStages), e / C::kStages & 1, gave_up, &a.ctl->status);
-        if (!ok) mbar_wait(full + 8 * (e % C::kStages), e / C::kStages & 1);
+    for (int e = max(i - kStages, which); e < i; e += kFetchers) {
+        ok = ok && warp_wait(empty + 8 * (e % kStages), e / kStages & 1, gave_up, &a.ctl->status);
+        if (!ok) mbar_wait(full + 8 * (e % kStages), e / kStages & 1);
     }
 }
 
@@ -289,7 +319,7 @@ __device__ __forceinline__ void query_role(const Args &a, const Pairs &ps, Contr
             const int chunk = t + 4 * i;
             const uint32_t at = q_at + place * C::kQueryBytes + g * D + ((D == 128 ? chunk ^ g : chunk ^ (g >> 1 & 3)) << 4);
             asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
-            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + 16 * D), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + 8 * D), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
         }
         if (t == 0) ctl->power[place][g] = __uint_as_float((uint32_t)(127 + e) << 23) * a.scale_log2;
         fence_async_proxy();
@@ -302,61 +332,75 @@ __device__ __forceinline__ void query_role(const Args &a, const Pairs &ps, Contr
 }
 
 // ---- products --------------------------------------------------------------------------
-// Tile i belongs to warpgroup i % 2, whose scores and output have tensor memory of their own: S at columns 32 w, O at 64 + 64 w.
+// Tile i belongs to warpgroup i % 2, whose scores (of two tiles) and output have tensor memory of their own: S at columns 32 w and
+// 32 w + 16, O at 64 + 64 w.  Scores are made up to four tiles ahead, so that a warpgroup finds those of its next tile ready.  (A
+// barrier tells its phases apart by parity alone: each is waited for in every phase, or has one open phase at most.)
+// A warp for each of the two products: with one for both, a tile took it 1100 cycles of issuing and waiting in order.
 template <int D>
-__device__ __forceinline__ void mma_role(const Args &a, const Pairs &ps, Control<D> *ctl, uint32_t base, long long u0, int n, int lane) {
+__device__ __forceinline__ void score_role(const Args &a, const Pairs &ps, Control<D> *ctl, uint32_t base, long long u0, int n, int lane) {
     using C = Cfg<D>;
     volatile int *gave_up = &ctl->gave_up;
     const uint32_t tmem = ctl->tmem;
     const bool chosen = elect_one();
-    const int columns = a.G > 4 ? 48 : 32, width = 64;                     // codes of a token's weights (5 per head), bytes of their row
-    const uint32_t o_instr = 1u << 4 | 1u << 15 | 1u << 16 | (uint32_t)(columns >> 3) << 17 | (uint32_t)(D >> 4) << 24;   // A and B along M and N
     auto wait = [&](const uint64_t *bar, uint32_t parity) { return warp_wait(smem_u32(bar), parity & 1, gave_up, &a.ctl->status); };
-    Walk ahead(ps, u0, n), behind(ps, u0, n);                              // pairs of the scores, of the outputs
-    bool fresh = true, ok = true;                                          // the scores' pair has just begun
-    // S of tile i
-    auto scores = [&](int i) {
-        const int place = ahead.ordinal % kQueries;
-        if (fresh && !wait(&ctl->q_ready[place], ahead.ordinal / kQueries)) return false;
-        fresh = false;
-        if (!wait(&ctl->full[i % C::kStages], i / C::kStages)) return false;
+    Walk w(ps, u0, n);
+    bool fresh = true;                 // the pair has just begun
+    for (int i = 0; i < n; ++i) {
+        const int place = w.ordinal % kQueries;
+        if (fresh && !wait(&ctl->q_ready[place], w.ordinal / kQueries)) break;
+        if (!wait(&ctl->k_full[i % C::kKStages], i / C::kKStages)) break;
+        if (i >= 4 && !wait(&ctl->s_free[i & 1][i >> 1 & 1], i / 4 - 1)) break;                 // the scores that lay there have been read
         tc_fence_after();
+        const bool ends = i + 1 == w.end;
         if (chosen) {
-            const uint64_t kd = smem_codes<D>(base + i % C::kStages * (2 * C::kTileBytes));
+            const uint64_t kd = smem_codes<D>(base + i % C::kKStages * C::kTileBytes);
             const uint64_t qd = smem_codes<D>(base + C::kQueryAt + place * C::kQueryBytes);
+            const uint32_t to = tmem + (i & 1) * 32 + (i >> 1 & 1) * 16;
 #pragma unroll
-            for (int k = 0; k < 2 * (D / 32); ++k)                         // hi, then lo
-                mma_ss_codes(tmem + (i & 1) * 32, kd + k % (D / 32) * 2, qd + k / (D / 32) * (16 * D >> 4) + k % (D / 32) * 2, mma_instr_codes(16), k > 0);
-            mma_commit(smem_u32(&ctl->s_full[i & 1]));
-            if (i + 1 == ahead.end) mma_commit(smem_u32(&ctl->q_free[place]));
+            for (int k = 0; k < D / 32; ++k) mma_ss_codes(to, kd + k * 2, qd + k * 2, mma_instr_codes(16), k > 0);
+            mma_commit(smem_u32(&ctl->s_full[i & 1][i >> 1 & 1]));
+            mma_commit(smem_u32(&ctl->k_empty[i % C::kKStages]));
+            if (ends) mma_commit(smem_u32(&ctl->q_free[place]));
         }
         __syncwarp();
-        if (i + 1 == ahead.end) fresh = ahead.next();
-        return true;
-    };
-    for (int i = 0; ok && i < min(n, 2); ++i) ok = scores(i);
-    for (int i = 0; ok && i < n; ++i) {
-        ok = wait(&ctl->p_ready[i & 1], i / 2);
-        if (!ok) break;
-        tc_fence_after();
-        if (chosen) {
-            const uint64_t vd = smem_codes_mn(base + i % C::kStages * (2 * C::kTileBytes) + C::kTileBytes, D);
-            const uint64_t pd = smem_codes_mn(base + C::kRing + (i & 1) * C::kWeightBytes, width);
-            const bool first = i < behind.begin + 2;                       // the pair's first tile of this warpgroup
-#pragma unroll
-            for (int k = 0; k < kTile / 32; ++k)
-                mma_ss_codes(tmem + 64 + (i & 1) * 64, vd + k * (32 * D >> 4), pd + k * (32 * width >> 4), o_instr, !first || k > 0);
-            mma_commit(smem_u32(&ctl->o_done[i & 1]));
-            mma_commit(smem_u32(&ctl->empty[i % C::kStages]));
-        }
-        __syncwarp();
-        if (i + 1 == behind.end) behind.next();
-        if (i + 2 < n) ok = scores(i + 2);
+        fresh = ends && w.next();
     }
     // nothing may be running when tensor memory goes away
-    if (chosen) mma_commit(smem_u32(&ctl->drain));
+    if (chosen) mma_commit(smem_u32(&ctl->drain[0]));
     __syncwarp();
-    mbar_wait(smem_u32(&ctl->drain), 0);
+    mbar_wait(smem_u32(&ctl->drain[0]), 0);
+}
+
+template <int D>
+__device__ __forceinline__ void out_role(const Args &a, const Pairs &ps, Control<D> *ctl, uint32_t base, long long u0, int n, int lane) {
+    using C = Cfg<D>;
+    constexpr int kWidth = 64;         // bytes of a token's row of weights
+    volatile int *gave_up = &ctl->gave_up;
+    const uint32_t tmem = ctl->tmem;
+    const bool chosen = elect_one();
+    const int columns = a.G > 4 ? 48 : 32;
+    const uint32_t instr = 1u << 4 | 1u << 15 | 1u << 16 | (uint32_t)(columns >> 3) << 17 | (uint32_t)(D >> 4) << 24;     // A and B run along M and N
+    auto wait = [&](const uint64_t *bar, uint32_t parity) { return warp_wait(smem_u32(bar), parity & 1, gave_up, &a.ctl->status); };
+    Walk w(ps, u0, n);
+    for (int i = 0; i < n; ++i) {
+        if (!wait(&ctl->v_full[i % C::kVStages], i / C::kVStages) || !wait(&ctl->p_ready[i & 1], i / 2)) break;
+        tc_fence_after();
+        if (chosen) {
+            const uint64_t vd = smem_codes_mn(base + C::kVAt + i % C::kVStages * C::kTileBytes, D);
+            const uint64_t pd = smem_codes_mn(base + C::kRing + (i & 1) * C::kWeightBytes, kWidth);
+            const bool first = i < w.begin + 2;                            // the pair's first tile of this warpgroup
+#pragma unroll
+            for (int k = 0; k < kTile / 32; ++k)
+                mma_ss_codes(tmem + 64 + (i & 1) * 64, vd + k * (32 * D >> 4), pd + k * (32 * kWidth >> 4), instr, !first || k > 0);
+            mma_commit(smem_u32(&ctl->o_done[i & 1]));
+            mma_commit(smem_u32(&ctl->v_empty[i % C::kVStages]));
+        }
+        __syncwarp();
+        if (i + 1 == w.end) w.next();
+    }
+    if (chosen) mma_commit(smem_u32(&ctl->drain[1]));
+    __syncwarp();
+    mbar_wait(smem_u32(&ctl->drain[1]), 0);
 }
 
 // ---- softmax ------------------------------------------------------------------------------
@@ -415,11 +459,11 @@ __device__ __forceinline__ void softmax_role(const Args &a, const Pairs &ps, Con
         for (int h = 0; h < H; ++h) M[h] = -INFINITY, l[h] = 0.f;
         bool any = false;
         for (; i < w.end; i += 2) {
-            const uint32_t k = i / 2, slot = i % C::kStages;
-            if (!wait(&ctl->s_full[st], k)) return;
+            const uint32_t k = i / 2, slot = i % C::kVStages;
+            if (!wait(&ctl->v_full[slot], i / C::kVStages) || !wait(&ctl->s_full[st][k & 1], k / 2)) return;
             tc_fence_after();
             float z[16];
-            tmem_ld16(t_s, z);
+            tmem_ld16(t_s + (k & 1) * 16, z);
             const PageInfo info = ctl->info[slot][row / kPage];
             if (!any) {
 #pragma unroll
@@ -427,23 +471,23 @@ __device__ __forceinline__ void softmax_role(const Args &a, const Pairs &ps, Con
             }
             tmem_wait_ld();
             settle<16>(z);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&ctl->s_free[st][k & 1]));
             // w = logit + log2 of V's scale, in powers of two; largest of the tile
             const bool seen = row % kPage < info.tokens;
             const float shift = (float)((int)(__float_as_uint(info.v_scale) >> 23) - 127);
             // what lies behind the end of the request may be anything, and a weight of zero would not hide it
-            if (__any_sync(kFull, !seen && info.tokens > 0)) {
-                if (!wait(&ctl->full[slot], i / C::kStages)) return;
-                if (!seen && info.tokens > 0) {
+            if (!seen && info.tokens > 0) {
 #pragma unroll
-                    for (int e = 0; e < D / 16; ++e)
-                        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(base + slot * (2 * C::kTileBytes) + C::kTileBytes + row * D + e * 16), "r"(0) : "memory");
-                }
-                __syncwarp();
+                for (int e = 0; e < D / 16; ++e)
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(base + C::kVAt + slot * C::kTileBytes + row * D + e * 16), "r"(0) : "memory");
             }
+            __syncwarp();
             float tile_top[H];
 #pragma unroll
             for (int h = 0; h < H; ++h) {
-                z[h] = seen ? fmaf(z[h], f[h] * info.k_scale, shift) : -INFINITY;
+                z[h] = seen ? fmaf(z[h] + z[8 + h], f[h] * info.k_scale, shift) : -INFINITY;     // hi and lo
                 float x = z[h];
 #pragma unroll
                 for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(kFull, x, o));
@@ -608,22 +652,22 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         if (tid == 0 && blockIdx.x == 0) atomicOr(&a.ctl->status, SE_DEV_WAIT_TIMEOUT);
         return;
     }
-    if (tid < C::kStages) mbar_init(smem_u32(&ctl->full[tid]), 1), mbar_init(smem_u32(&ctl->empty[tid]), 1);
+    if (tid < C::kKStages) mbar_init(smem_u32(&ctl->k_full[tid]), 1), mbar_init(smem_u32(&ctl->k_empty[tid]), 1);
+    if (tid < C::kVStages) mbar_init(smem_u32(&ctl->v_full[tid]), 1), mbar_init(smem_u32(&ctl->v_empty[tid]), 1);
     if (tid < kQueries) mbar_init(smem_u32(&ctl->q_ready[tid]), 1), mbar_init(smem_u32(&ctl->q_free[tid]), 9);
     if (tid < 2) {
-        mbar_init(smem_u32(&ctl->s_full[tid]), 1), mbar_init(smem_u32(&ctl->o_done[tid]), 1);
+        mbar_init(smem_u32(&ctl->s_full[tid][0]), 1), mbar_init(smem_u32(&ctl->s_full[tid][1]), 1), mbar_init(smem_u32(&ctl->o_done[tid]), 1);
+        mbar_init(smem_u32(&ctl->s_free[tid][0]), 4), mbar_init(smem_u32(&ctl->s_free[tid][1]), 4);
         mbar_init(smem_u32(&ctl->p_ready[tid]), 4), mbar_init(smem_u32(&ctl->exchange[tid]), 4), mbar_init(smem_u32(&ctl->merged[tid]), 4);
         mbar_init(smem_u32(&ctl->aside[tid]), 8);
     }
     if (tid == 0) {
         ctl->gave_up = 0;
-        mbar_init(smem_u32(&ctl->drain), 1);
+        mbar_init(smem_u32(&ctl->drain[0]), 1), mbar_init(smem_u32(&ctl->drain[1]), 1);
         prefetch_map(&k_map), prefetch_map(&v_map);
     }
     mbar_fence_init();
-    // rows 8 .. 15 of every q stay zero
-    for (int i = tid; i < kQueries * C::kQueryBytes / 16; i += kThreads) reinterpret_cast<uint4 *>(smem + C::kQueryAt)[i] = make_uint4(0, 0, 0, 0);
-    if (warp == kMmaWarp) tmem_alloc(smem_u32(&ctl->tmem), 256);
+    if (warp == kScoreWarp) tmem_alloc(smem_u32(&ctl->tmem), 256);
 
     // tiles before every pair (or every run of pairs, where there are more than 1024)
     const int pairs = a.B * a.H_kv;
@@ -666,9 +710,11 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     const long long u0 = size * blockIdx.x;
     const int n = (int)min(size, max(total - u0, 0ll));
     if (n) {
-        if (warp == kFetchWarp) fetch_role<D>(a, ps, &k_map, &v_map, ctl, base, u0, n, lane);
+        if (warp >= kFetchWarp + kFetchers) fetch_role<D, true>(a, ps, &v_map, ctl, base + C::kVAt, u0, n, warp - kFetchWarp - kFetchers, lane);
+        else if (warp >= kFetchWarp) fetch_role<D, false>(a, ps, &k_map, ctl, base, u0, n, warp - kFetchWarp, lane);
         else if (warp == kQueryWarp) query_role<D>(a, ps, ctl, base + C::kQueryAt, u0, n, lane);
-        else if (warp == kMmaWarp) mma_role<D>(a, ps, ctl, base, u0, n, lane);
+        else if (warp == kScoreWarp) score_role<D>(a, ps, ctl, base, u0, n, lane);
+        else if (warp == kOutWarp) out_role<D>(a, ps, ctl, base, u0, n, lane);
         else if (a.G > 4) softmax_role<D, 8>(a, ps, ctl, smem, base, u0, n, size, warp >> 2);
         else softmax_role<D, 4>(a, ps, ctl, smem, base, u0, n, size, warp >> 2);
         __syncwarp();
@@ -686,7 +732,7 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     tc_fence_before();
     __threadfence();
     __syncthreads();
-    if (warp == kMmaWarp) {
+    if (warp == kScoreWarp) {
         tc_fence_after();
         tmem_free(ctl->tmem, 256);
     }
