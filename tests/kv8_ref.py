@@ -4,18 +4,15 @@ Nothing here calls the CUDA library.  A cache is e4m3 codes with a power-of-two 
 Codes, scales and summaries are exact, so they are compared bit for bit; attention is computed in fp64 from the values that the
 codes stand for.
 
-Bounds of both attention kernels.  A query row is split into two rows of codes: with 2^e the smallest power of two that brings the
-row's maximum to 448 or below (so the maximum is above 224 * 2^e), an element of at least 2^-2 * 2^e has its last bit at
-2^-9 * 2^e or above, the smallest step of a code, and is exact; a smaller one is off by half of that step at most, 2^-10 * 2^e.
-A logit is a sum of D products that are exact in fp32, kept in fp32: its error is at most (D + 2) * 2^-23 times the sum of the
-products' magnitudes.
+Bounds of the decode kernel (out and lse fp32).  A logit is a sum of D products that are exact in fp32, kept in fp32: its error is
+at most (D + 2) * 2^-23 times the sum of the products' magnitudes.  The exponent's subtraction adds 2^-22 of its magnitude, exp2
+and the weights' sum 2^-18 relative (as in prompt_ref); a weight enters its product with V as two halves, 2^-22 relative, not
+below 2^-25 of the largest weight.
 
-Decode (out and lse fp32): the exponent, logit plus logarithm of V's scale, adds 2^-22 of its terms' magnitudes, exp2 and the weights' sum 2^-18 relative (as
-in prompt_ref).  A weight times V's scale s enters its product with V's codes as five codes, each 16 times finer than the one
-before: what is left is at most 2^-20 of it, or 2^-10 * 16^-4 = 2^-26 of the largest weight times scale where its codes are
-subnormal.
-
-Chunk (out bf16, lse fp32): the other bounds are those of prompt_ref."""
+Bounds of the chunk kernel (out bf16, lse fp32): those of prompt_ref, and a query row that is split into two rows of codes.  With
+2^e the smallest power of two that brings the row's maximum to 448 or below (so the maximum is above 224 * 2^e), an element of
+at least 2^-2 * 2^e has its last bit at 2^-9 * 2^e or above, the smallest step of a code, and is exact; a smaller one is off by
+half of that step at most, 2^-10 * 2^e."""
 from __future__ import annotations
 
 import math
@@ -97,11 +94,6 @@ def values(codes, scale):
     return codes.double() * scale.double()[..., None, None]
 
 
-def row_step(x):
-    """Smallest 2^e with the largest magnitude of each row at most 448 * 2^e."""
-    return torch.exp2(torch.ceil(torch.log2(x.abs().amax(-1, keepdim=True).clamp(min=1e-300) / 448)))
-
-
 def decode(q, k_codes, v_codes, scales, page_table, seq_lens, sel_idx, sel_cnt, sm_scale):
     """out, its tolerance, lse, its tolerance (fp64)."""
     B, H_q, D = q.shape
@@ -114,7 +106,7 @@ def decode(q, k_codes, v_codes, scales, page_table, seq_lens, sel_idx, sel_cnt, 
         n = int(seq_lens[r])
         for h in range(H_kv):
             pages = range((n + PAGE - 1) // PAGE) if sel_idx is None else sel_idx[r, h, :int(sel_cnt[r, h])].tolist()
-            kk, vv, ss = [], [], []
+            kk, vv = [], []
             for b in pages:
                 pid = int(page_table[r, b])
                 if pid < 0:
@@ -122,24 +114,22 @@ def decode(q, k_codes, v_codes, scales, page_table, seq_lens, sel_idx, sel_cnt, 
                 m = min(PAGE, n - b * PAGE)
                 kk.append(k_codes[pid, h, :m].double() * scales[pid, h, 0].double())
                 vv.append(v_codes[pid, h, :m].double() * scales[pid, h, 1].double())
-                ss.append(scales[pid, h, 1].double().expand(m))
             if not kk:
                 continue
-            kk, vv, ss = torch.cat(kk), torch.cat(vv), torch.cat(ss)
+            kk, vv = torch.cat(kk), torch.cat(vv)
             x = q[r, h * G:(h + 1) * G].double()
             z = sm_scale * x @ kk.t()
-            step = row_step(x)
-            zerr = sm_scale * ((D + 2) * 2.0 ** -23 * (x.abs() @ kk.abs().t()) + 2.0 ** -10 * step * ((x.abs() < 0.25 * step).double() @ kk.abs().t()))
+            zerr = sm_scale * (D + 2) * 2.0 ** -23 * (x.abs() @ kk.abs().t())
             top = z.amax(1, keepdim=True)
-            zerr = zerr + 2.0 ** -22 * (z.abs() + top.abs() + ss.log().abs() + ss.log().abs().max()) + 2.0 ** -18
+            zerr = zerr + 2.0 ** -22 * (z.abs() + top.abs()) + 2.0 ** -18
             p = (z - top).exp()
             s = p.sum(1, keepdim=True)
             w = p / s
             rows = slice(h * G, (h + 1) * G)
             out[r, rows] = w @ vv
             # relative error of every weight, and of their sum
-            werr = w * (zerr + (w * zerr).sum(1, keepdim=True) + 2.0 ** -20) + 2.0 ** -26 * (w * ss).amax(1, keepdim=True) / ss
-            tol[r, rows] = 1.01 * (werr @ vv.abs()) + (D + 2 + 148) * 2.0 ** -23 * (w @ vv.abs())
+            werr = w * (zerr + (w * zerr).sum(1, keepdim=True)) + 2.0 ** -25 * w.amax(1, keepdim=True)
+            tol[r, rows] = 2 * werr @ vv.abs() + 2.0 ** -22 * (w @ vv.abs())
             lse[r, rows] = (top + s.log())[:, 0]
             ltol[r, rows] = (w * zerr).sum(1) + 2.0 ** -22 * lse[r, rows].abs() + 2.0 ** -22
     return out, tol, lse, ltol
@@ -154,7 +144,7 @@ def chunk(b, scale):
         if n == 0:
             continue
         q = b.q[rows].double().abs().view(n, b.H_kv, -1, b.D).permute(1, 2, 0, 3)
-        step = row_step(q)
+        step = torch.exp2(torch.ceil(torch.log2(q.amax(-1, keepdim=True).clamp(min=1e-300) / 448)))
         k, _ = prompt_ref.cached(b, r, b.k_cache)
         v, _ = prompt_ref.cached(b, r, b.v_cache)
         # the logits' error, and what it does to lse and (twice, for weight and sum) to the output
