@@ -2,14 +2,15 @@
 // held as e4m3 codes with a power-of-two scale per page and kv-head): over the pages of a selection, or over all present pages.
 //
 // Mathematics.  For a page with scales s_K, s_V and codes c:  z_j = sm_scale s_K (q . c_j),  out = sum_j p_j s_V c_j / sum_j p_j,
-// p_j = 2^(z_j log2 e - m).  The scales stay outside of the products, once per page: s_K multiplies 16 logits per head, s_V the
-// page's sum of p_j c_j.  The products run on mma.sync with halves, because a code is a half exactly:
+// p_j = 2^(z_j log2 e - m).  The products run on mma.sync with halves, because a code is a half exactly; s_K multiplies the page's
+// logits in fp32, s_V becomes a part of the exponent:
 //   q     is brought to a maximum of 2^13..2^14 per head by a power of two; its 8 significant bits fit a half for everything
 //         above 2^-30 of the maximum, so nothing that fp32 sums could show is lost
-//   p_j   enters as two halves, p = hi + lo (22 bits), as the output is fp32.
+//   p s_V = 2^(w - M), w = z log2 e + log2 s_V, M the running maximum of w, enters as two halves, hi + lo (22 bits), as the output
+//         is fp32: the largest are near 1 whatever the scales.  The sum of the weights takes s_V out again, in fp32.
 //
-// What bounds it: HBM, 2 * 2 * D bytes per token and kv-head and a few cycles of everything else: per page and head at D = 128
-// 64 conversions of two codes, 24 matrix instructions, 32 fp32 FMAs per warp.
+// What bounds it: HBM, 2 * 2 * D bytes per token and kv-head, and nearly as much the instructions: per page and head at D = 128 about
+// 300 for a warp, 64 of them conversions of two codes each and 24 matrix instructions.
 //
 // Split.  The list of all (request, kv-head) pairs' pages is cut into 592 runs of equal length, one per group of four warps; a
 // group's pages go round its warps, each of which keeps a ring of pages in flight (tensor copies, 128-byte swizzle) across the
@@ -334,9 +335,9 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             const float f = down * a.scale_log2;
             f0 = __shfl_sync(kFull, f, 8 * t), f1 = __shfl_sync(kFull, f, 8 * t + 4);
         }
-        float2 acc[C::kTiles][2];      // [tile][channel (D / 8) g + 2 tile, + 1]: heads 2 t, 2 t + 1
+        float acc[C::kTiles][4];       // [tile]: channel (D / 8) g + 2 tile, heads 2 t, 2 t + 1; the channel behind it
 #pragma unroll
-        for (int i = 0; i < C::kTiles; ++i) acc[i][0] = acc[i][1] = make_float2(0.f, 0.f);
+        for (int i = 0; i < C::kTiles; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
 
         for (; k < mine && k * kTeam + mate < stop; ++k) {
@@ -388,7 +389,9 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 if (tok >= tokens) z[0] = z[1] = -INFINITY;
                 if (tok + 8 >= tokens) z[2] = z[3] = -INFINITY;
             }
-            const float t0 = fmaxf(z[0], z[2]) * g0, t1 = fmaxf(z[1], z[3]) * g1;
+            // w = logit + log2 of V's scale, in powers of two: what the weights in the product with V are made of
+            const float shift = (float)((int)(__float_as_uint(sv) >> 23) - 127), inv = __uint_as_float(0x7f000000u - __float_as_uint(sv));
+            const float t0 = fmaf(fmaxf(z[0], z[2]), g0, shift), t1 = fmaf(fmaxf(z[1], z[3]), g1, shift);
             if (__any_sync(kFull, t0 > m0 + kSlack || t1 > m1 + kSlack)) {
                 float n0 = fmaxf(m0, t0), n1 = fmaxf(m1, t1);
 #pragma unroll
@@ -400,13 +403,12 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 m0 = n0, m1 = n1;
                 l0 *= r0, l1 *= r1;
 #pragma unroll
-                for (int i = 0; i < C::kTiles; ++i)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) acc[i][e].x *= r0, acc[i][e].y *= r1;
+                for (int i = 0; i < C::kTiles; ++i) acc[i][0] *= r0, acc[i][1] *= r1, acc[i][2] *= r0, acc[i][3] *= r1;
             }
-            const float p0 = ex2(fmaf(z[0], g0, -m0)), p1 = ex2(fmaf(z[1], g1, -m1));
-            const float p2 = ex2(fmaf(z[2], g0, -m0)), p3 = ex2(fmaf(z[3], g1, -m1));
-            l0 += p0 + p2, l1 += p1 + p3;
+            const float off0 = shift - m0, off1 = shift - m1;
+            const float p0 = ex2(fmaf(z[0], g0, off0)), p1 = ex2(fmaf(z[1], g1, off1));
+            const float p2 = ex2(fmaf(z[2], g0, off0)), p3 = ex2(fmaf(z[3], g1, off1));
+            l0 = fmaf(p0 + p2, inv, l0), l1 = fmaf(p1 + p3, inv, l1);
             // weights as hi + lo, two halves; transposed, they are the second operand: rows tokens, columns heads
             const uint32_t h0 = pack_half2(p0, p1), h1 = pack_half2(p2, p3);
             const float2 u = unpack_half2(h0), w = unpack_half2(h1);
@@ -444,11 +446,8 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 const uint32_t x = __byte_perm(va[i / 2], vb[i / 2], sel), y = __byte_perm(vc[i / 2], vd[i / 2], sel);
                 uint32_t a0, a1, a2, a3;
                 halves_of_e4m3x4(x, a0, a1), halves_of_e4m3x4(y, a2, a3);
-                float o[4];
-                mma_f16_first(o, a0, a1, a2, a3, e0, e1);
-                mma_f16(o, a0, a1, a2, a3, b0, b1);
-                acc[i][0] = ffma2(make_float2(o[0], o[1]), make_float2(sv, sv), acc[i][0]);
-                acc[i][1] = ffma2(make_float2(o[2], o[3]), make_float2(sv, sv), acc[i][1]);
+                mma_f16(acc[i], a0, a1, a2, a3, e0, e1);
+                mma_f16(acc[i], a0, a1, a2, a3, b0, b1);
             }
         }
 
@@ -461,8 +460,8 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 #pragma unroll
         for (int j = 0; j < C::kTiles / 2; ++j) {
             const int ch = (D / 8) * g + 4 * j;
-            *reinterpret_cast<float4 *>(own + (2 * t) * C::kPitch + ch) = make_float4(acc[2 * j][0].x, acc[2 * j][1].x, acc[2 * j + 1][0].x, acc[2 * j + 1][1].x);
-            *reinterpret_cast<float4 *>(own + (2 * t + 1) * C::kPitch + ch) = make_float4(acc[2 * j][0].y, acc[2 * j][1].y, acc[2 * j + 1][0].y, acc[2 * j + 1][1].y);
+            *reinterpret_cast<float4 *>(own + (2 * t) * C::kPitch + ch) = make_float4(acc[2 * j][0], acc[2 * j][2], acc[2 * j + 1][0], acc[2 * j + 1][2]);
+            *reinterpret_cast<float4 *>(own + (2 * t + 1) * C::kPitch + ch) = make_float4(acc[2 * j][1], acc[2 * j][3], acc[2 * j + 1][1], acc[2 * j + 1][3]);
         }
         team_sync(team);
         const int c0 = (int)(first / size), c1 = (int)((first + pages - 1) / size);      // runs that share the pair

@@ -5,9 +5,9 @@ Codes, scales and summaries are exact, so they are compared bit for bit; attenti
 codes stand for.
 
 Bounds of the decode kernel (out and lse fp32).  A logit is a sum of D products that are exact in fp32, kept in fp32: its error is
-at most (D + 2) * 2^-23 times the sum of the products' magnitudes.  The exponent's subtraction adds 2^-22 of its magnitude, exp2
-and the weights' sum 2^-18 relative (as in prompt_ref); a weight enters its product with V as two halves, 2^-22 relative, not
-below 2^-25 of the largest weight.
+at most (D + 2) * 2^-23 times the sum of the products' magnitudes.  The exponent, logit plus logarithm of V's scale, adds 2^-22 of
+its terms' magnitudes, exp2 and the weights' sum 2^-18 relative (as in prompt_ref).  A weight times V's scale enters its product
+with V's codes as two halves, 2^-22 relative, not below 2^-25 of the largest such product; the sums over tokens are fp32.
 
 Bounds of the chunk kernel (out bf16, lse fp32): those of prompt_ref, and a query row that is split into two rows of codes.  With
 2^e the smallest power of two that brings the row's maximum to 448 or below (so the maximum is above 224 * 2^e), an element of
@@ -106,7 +106,7 @@ def decode(q, k_codes, v_codes, scales, page_table, seq_lens, sel_idx, sel_cnt, 
         n = int(seq_lens[r])
         for h in range(H_kv):
             pages = range((n + PAGE - 1) // PAGE) if sel_idx is None else sel_idx[r, h, :int(sel_cnt[r, h])].tolist()
-            kk, vv = [], []
+            kk, vv, ss = [], [], []
             for b in pages:
                 pid = int(page_table[r, b])
                 if pid < 0:
@@ -114,22 +114,23 @@ def decode(q, k_codes, v_codes, scales, page_table, seq_lens, sel_idx, sel_cnt, 
                 m = min(PAGE, n - b * PAGE)
                 kk.append(k_codes[pid, h, :m].double() * scales[pid, h, 0].double())
                 vv.append(v_codes[pid, h, :m].double() * scales[pid, h, 1].double())
+                ss.append(scales[pid, h, 1].double().expand(m))
             if not kk:
                 continue
-            kk, vv = torch.cat(kk), torch.cat(vv)
+            kk, vv, ss = torch.cat(kk), torch.cat(vv), torch.cat(ss)
             x = q[r, h * G:(h + 1) * G].double()
             z = sm_scale * x @ kk.t()
             zerr = sm_scale * (D + 2) * 2.0 ** -23 * (x.abs() @ kk.abs().t())
             top = z.amax(1, keepdim=True)
-            zerr = zerr + 2.0 ** -22 * (z.abs() + top.abs()) + 2.0 ** -18
+            zerr = zerr + 2.0 ** -22 * (z.abs() + top.abs() + ss.log().abs() + ss.log().abs().max()) + 2.0 ** -18
             p = (z - top).exp()
             s = p.sum(1, keepdim=True)
             w = p / s
             rows = slice(h * G, (h + 1) * G)
             out[r, rows] = w @ vv
-            # relative error of every weight, and of their sum
-            werr = w * (zerr + (w * zerr).sum(1, keepdim=True)) + 2.0 ** -25 * w.amax(1, keepdim=True)
-            tol[r, rows] = 2 * werr @ vv.abs() + 2.0 ** -22 * (w @ vv.abs())
+            # error of every weight, and of their sum
+            werr = w * (zerr + (w * zerr).sum(1, keepdim=True) + 2.0 ** -22) + 2.0 ** -25 * (w * ss).amax(1, keepdim=True) / ss
+            tol[r, rows] = 1.01 * (werr @ vv.abs()) + 2.0 ** -18 * (w @ vv.abs())
             lse[r, rows] = (top + s.log())[:, 0]
             ltol[r, rows] = (w * zerr).sum(1) + 2.0 ** -22 * lse[r, rows].abs() + 2.0 ** -22
     return out, tol, lse, ltol
