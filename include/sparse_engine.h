@@ -71,7 +71,7 @@ extern "C" {
 #define SE_DEV_BAD_PAGE_ID          1u  /* page_table entry >= num_phys_pages              */
 #define SE_DEV_BAD_SELECTION        2u  /* sel_idx entry outside the request / sel_cnt > k_max */
 #define SE_DEV_WAIT_TIMEOUT         4u  /* a bounded wait (200 ms) on an asynchronous copy gave up */
-#define SE_DEV_BAD_LENGTH           8u  /* prompt calls: cu_seqlens / seq_lens / pair_axis entry out of range */
+#define SE_DEV_BAD_LENGTH           8u  /* prompt, 8-bit and page calls: cu_seqlens / seq_lens / pair_axis / parent entry out of range */
 #define SE_DEV_NO_PAGES            16u  /* se_pages_update: fewer free pages than asked for, nothing was changed */
 
 typedef struct se_params {
@@ -398,8 +398,8 @@ int se_h2o_compact(const se_params *p, void *k_cache, void *v_cache, float *scor
  *  - They take a workspace of their own kind: se_prompt_workspace_bytes bytes (80 MB at D = 128), initialised
  *    once by se_prompt_workspace_init, then good for any number of calls with the same se_params that are ordered
  *    on the device.  se_last_device_status reads its status word.  After a call that reported
- *    SE_DEV_WAIT_TIMEOUT it has to be initialised again: until then se_chunk_attend, se_prompt_attend and
- *    se_h2o_accumulate write nothing and report SE_DEV_WAIT_TIMEOUT each time.
+ *    SE_DEV_WAIT_TIMEOUT it has to be initialised again: until then se_chunk_attend, se_prompt_attend,
+ *    se_h2o_accumulate, se_kv8_decode and se_kv8_chunk_attend write nothing and report SE_DEV_WAIT_TIMEOUT each time.
  */
 size_t se_prompt_workspace_bytes(const se_params *p);
 int se_prompt_workspace_init(const se_params *p, void *workspace, void *stream);
@@ -499,9 +499,9 @@ int se_kv8_append(const se_params *p, const void *q, int64_t q_stride, const voi
 /*
  * Attention of one token per request over an 8-bit cache (se_sparse_decode's equations): with sel_idx / sel_cnt over the pages
  * that se_page_select left there ([B, H_kv, k_max], [B, H_kv]); with both NULL over every present page of the request (a dense
- * layer; k_max is not used).  out fp32, lse fp32; scores, statistics and sums are fp32, each weight enters its product with V
- * as two halves (22 significant bits).  No token (length 0, an empty selection, no present page): out = 0, lse = -inf.  Absent
- * pages are left out; an entry of sel_idx outside the request is skipped and reported (SE_DEV_BAD_SELECTION), as is a sel_cnt
+ * layer; k_max is not used).  out fp32, lse fp32; scores, statistics and sums are fp32; each weight, times V's scale, enters
+ * its product with V's codes as two halves (22 significant bits, steps of 2^-24 of the largest at least).  No token (length 0, an empty selection, no
+ * present page): out = 0, lse = -inf.  Absent pages are left out; an entry of sel_idx outside the request is skipped and reported (SE_DEV_BAD_SELECTION), as is a sel_cnt
  * above k_max (the first k_max entries count); a length outside 0 .. 16*max_pages is reported (SE_DEV_BAD_LENGTH).  Equal inputs
  * give equal bits.
  */

@@ -27,7 +27,8 @@
 // streams takes 3350 cycles where products and exponentials take 2048 each: a stream's chain of scores, softmax and product is
 // what bounds it.  Compared on builds that took 372 us for the packed prompts: KV tiles of 64 tokens with two score buffers per
 // stream 465-497 us, a product that begins with half of the weights 399-410 us, exponentials on the FMA units (one pair in
-// eight) 386 us.
+// eight) 386 us.  Over an 8-bit cache (KV8): 2048 tokens over 63488 1.9 ms (2.17 when calls
+// follow one another and power is the limit), the drafts 198 us (209).
 #include <math.h>
 
 #include "se_internal.h"

@@ -15,7 +15,8 @@
 //   4  the open pages' contents are copied
 // compact.  With n live pages, the i-th live page with a number from n on moves to the i-th free one below n.
 //
-// What bounds them: barriers and dependent loads for the tables (about 2 us each), HBM for the copies.
+// What bounds them: barriers and dependent loads for the tables (about 2 us each; 64 requests over a pool of 64 K pages grow by a
+// token in 11.7 us), HBM for the copies (40000 pages of four layers of codes compacted: 2.57 GB in 419 us, 6.1 TB/s).
 #include <climits>
 
 #include "se_internal.h"

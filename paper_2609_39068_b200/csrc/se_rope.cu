@@ -21,7 +21,8 @@
 // The same kernel fills a cache of e4m3 codes (KV8): a warp holds all tokens of a (page, head), so it has the page's largest
 // magnitude after five shuffles, picks the power-of-two scale, quantises, and brings older codes of the page to a scale that
 // has grown.  A power of two costs e4m3 no precision (its relative step is the same in every binade), makes the older codes'
-// second rounding exact but for subnormal codes, and makes every dequantised value a bf16 number.
+// second rounding exact but for subnormal codes, and makes every dequantised value a bf16 number.  20158 tokens of prompts,
+// 32 + 2 x 8 heads: 107 us for 459 MB (4.3 TB/s), 64 single tokens 9.9 us.
 #include <type_traits>
 
 #include "se_internal.h"
