@@ -485,7 +485,8 @@ int se_h2o_accumulate(const se_params *p, const void *q, int64_t q_stride, int32
  * and V apart,
  *     s = the smallest 2^e, -64 <= e <= 7, with max |x| <= 448 s over the page's new tokens; not below the page's scale so far,
  *         if the page held tokens of the request before (what it holds of earlier owners does not count),
- *     code = x / s rounded to the nearest code, ties to even; magnitudes above 448 s (57344 and more) become 448 s.
+ *     code = x / s rounded to the nearest code, ties to even; magnitudes above 448 s (57344 and more) become 448 s, a NaN the
+ *     code of a NaN (it does not count for s).
  * Where the scale of a page grows, the codes of its older tokens are brought to it (code * s_old / s, rounded again: exact but
  * for codes that become subnormal).  With meta != NULL the touched pages' summaries are the minimum and maximum of code * s
  * over the page's tokens below seq_lens[r].  A page that receives tokens must appear once in the page table.
@@ -500,10 +501,10 @@ int se_kv8_append(const se_params *p, const void *q, int64_t q_stride, const voi
  * Attention of one token per request over an 8-bit cache (se_sparse_decode's equations): with sel_idx / sel_cnt over the pages
  * that se_page_select left there ([B, H_kv, k_max], [B, H_kv]); with both NULL over every present page of the request (a dense
  * layer; k_max is not used).  out fp32, lse fp32; scores, statistics and sums are fp32; each weight, times V's scale, enters
- * its product with V's codes as two halves (22 significant bits, steps of 2^-24 of the largest at least).  No token (length 0, an empty selection, no
- * present page): out = 0, lse = -inf.  Absent pages are left out; an entry of sel_idx outside the request is skipped and reported (SE_DEV_BAD_SELECTION), as is a sel_cnt
- * above k_max (the first k_max entries count); a length outside 0 .. 16*max_pages is reported (SE_DEV_BAD_LENGTH).  Equal inputs
- * give equal bits.
+ * its product with V's codes as two halves (22 significant bits, steps of 2^-24 of the largest at least).  No token (length 0,
+ * an empty selection, no present page): out = 0, lse = -inf.  Absent pages are left out; an entry of sel_idx outside the request
+ * is skipped and reported (SE_DEV_BAD_SELECTION), as is a sel_cnt above k_max (the first k_max entries count); a length outside
+ * 0 .. 16*max_pages is reported (SE_DEV_BAD_LENGTH).  Equal inputs give equal bits.
  */
 int se_kv8_decode(const se_params *p, const void *q, const void *k_cache, const void *v_cache, const float *scales,
                   const int32_t *page_table, const int32_t *seq_lens, const int32_t *sel_idx, const int32_t *sel_cnt,
@@ -557,8 +558,8 @@ int se_pages_workspace_init(const se_params *p, void *workspace, void *stream);
  * first); pages that this call frees count as free.  free_pages ([1], device) receives the number of free pages left.  If more are
  * asked for than there are, nothing is changed - the outputs are the inputs, no buffer is written -, free_pages is negative (what is
  * missing) and SE_DEV_NO_PAGES is reported.
- * A slot with parent[r] outside -1 .. B-1, or a length outside 0 .. 16*max_pages, stays as it is and is reported
- * (SE_DEV_BAD_LENGTH); an entry that is no page of the pool counts as absent, is carried along and reported (SE_DEV_BAD_PAGE_ID).
+ * A slot with parent[r] outside -1 .. B-1, or with a length (its own, its new one, its parent's) outside 0 .. 16*max_pages, stays as
+ * it is, row and length bit for bit, and is reported (SE_DEV_BAD_LENGTH); an entry that is no page of the pool counts as absent, is carried along and reported (SE_DEV_BAD_PAGE_ID).
  * The outputs may be the inputs themselves: ref_count_out always, the others only without `parent` (refused with it).
  * New pages' contents are whatever they held before.
  */
@@ -574,7 +575,8 @@ int se_pages_update(const se_params *p, const int32_t *page_table, const int32_t
  *   ref_count_out    the counts at the pages' new numbers
  *   page_map         [P_phys] int32: new number of every live page, -1 for the others (for holders outside the page table)
  *   live_pages       [1] int32: n
- * page_table_out and ref_count_out may be the inputs themselves.
+ * page_table_out and ref_count_out may be the inputs themselves.  A length outside 0 .. 16*max_pages is reported
+ * (SE_DEV_BAD_LENGTH), and so is an entry that is no page of the pool (SE_DEV_BAD_PAGE_ID); such a row or entry is copied.
  */
 int se_pages_compact(const se_params *p, const int32_t *page_table, const int32_t *seq_lens, const int32_t *ref_count,
                      int32_t *page_table_out, int32_t *ref_count_out, int32_t *page_map, int32_t *live_pages,

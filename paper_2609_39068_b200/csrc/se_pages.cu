@@ -36,7 +36,8 @@ struct Control {
 
 // What becomes of a slot.
 struct Slot {
-    int parent, keep, kept, pages, len, copy, pad[2];  // parent (-1: none), tokens and pages taken over, pages and length afterwards, last page copied
+    int parent, keep, kept, pages, len, copy, asis, pad;   // parent (-1: none), tokens and pages taken over, pages and length afterwards, last
+                                                       // page copied, row left as it is
 };
 
 struct Buffers {
@@ -157,18 +158,16 @@ __device__ __forceinline__ void copy_pages(const Buffers &buf, int n, From from,
 }
 
 // ---- update ------------------------------------------------------------------------
-__device__ __forceinline__ int length_of(const UpdateArgs &a, int r) {
-    const int n = a.lens[r];
-    return n < 0 || n > a.max_pages * kPage ? 0 : n;
-}
+__device__ __forceinline__ bool in_range(const UpdateArgs &a, int n) { return n >= 0 && n <= a.max_pages * kPage; }
+__device__ __forceinline__ int length_of(const UpdateArgs &a, int r) { return in_range(a, a.lens[r]) ? a.lens[r] : 0; }
 __device__ __forceinline__ Slot plan_slot(const UpdateArgs &a, int r, bool report) {
     int s = a.parent ? a.parent[r] : r, n = a.new_lens[r];
     const int own = a.lens[r];
     Slot x = {};
     x.len = n;
-    if (s < -1 || s >= a.B || n < 0 || n > a.max_pages * kPage || own < 0 || own > a.max_pages * kPage) {
+    if (s < -1 || s >= a.B || !in_range(a, n) || !in_range(a, own) || (s >= 0 && !in_range(a, a.lens[s]))) {
         if (report) atomicOr(&a.ctl->status, SE_DEV_BAD_LENGTH);
-        s = r, n = length_of(a, r), x.len = own;                   // left as it is
+        s = r, n = length_of(a, r), x.len = own, x.asis = 1;
     }
     x.parent = s;
     x.keep = s < 0 ? 0 : min(length_of(a, s), n);
@@ -179,7 +178,7 @@ __device__ __forceinline__ Slot plan_slot(const UpdateArgs &a, int r, bool repor
 __device__ __forceinline__ bool is_page(const UpdateArgs &a, int e) { return e >= 0 && e < a.P; }
 // the page that the row ends inside of, -1: none
 __device__ __forceinline__ int open_page(const UpdateArgs &a, const Slot &x) {
-    if (x.keep % kPage == 0) return -1;
+    if (x.asis || x.keep % kPage == 0) return -1;
     const int e = a.table[(size_t)x.parent * a.max_pages + x.keep / kPage];
     return is_page(a, e) ? e : -1;
 }
@@ -316,7 +315,9 @@ pages_update_kernel(const __grid_constant__ UpdateArgs a, const __grid_constant_
         }
         const Slot x = a.slots[r];
         if (b == 0) a.lens_out[r] = x.len;
-        if (b < x.kept) {
+        if (x.asis) {
+            a.table_out[i] = a.table[i];
+        } else if (b < x.kept) {
             if (!x.copy || b != x.keep / kPage) a.table_out[i] = a.table[(size_t)x.parent * a.max_pages + b];
         } else if (b >= x.pages) {
             a.table_out[i] = -1;

@@ -167,6 +167,38 @@ def test_reports():
     assert to.tolist() == t.tolist() and co.tolist() == pool.refs
 
 
+def test_faulty_slots_stay_as_they_are():
+    """Rows and lengths bit for bit, entries behind the length included; what shares their pages goes on with copies."""
+    pool = Pool(19, 5, 40, 8, 100, alias=0, absent=0)
+    tail = [7, 99, -5]
+    pool.lens, pool.refs = [33, 33, 16 * 8 + 1, 20, -3], [2, 2, 2] + [1] * 2 + [0] * 35
+    pool.table = [[0, 1, 2, -1, -1] + tail, [0, 1, 2, -1, -1] + tail, [8, 9, 10, 11, 12] + tail, [3, 4, -1, -1, -1] + tail, [-1, 6, 6, 6, 6] + tail]
+    t, n, c = pool.on_gpu()
+    left = torch.zeros(1, **I32)
+    # slot 0 asks for too much, slots 2 and 4 have no length, slot 3 wants to go on from slot 2; slot 1 goes on from page 2, which slot 0 holds
+    new, parent = [400, 34, 8, 8, 8], [0, 1, 2, 2, 4]
+    before = [b.clone() for b in pool.buffers]
+    to, no, co = torch.full_like(t, -9), torch.full_like(n, -9), torch.full_like(c, -9)
+    binding.se_pages_update(pool.p, t, n, c, torch.tensor(new, **I32), to, no, co, left, pool.ws, parent=torch.tensor(parent, **I32),
+                            buffers=pool.buffers)
+    assert binding.se_last_device_status(pool.ws) == binding.SE_DEV_BAD_LENGTH
+    assert no.tolist() == [33, 34] + pool.lens[2:]
+    assert to.tolist() == [pool.table[0], [0, 1, 5] + [-1] * 5] + pool.table[2:]
+    assert co.tolist() == [2, 2, 1, 1, 1, 1] + [0] * 34 and left.tolist() == [34]
+    for b, x in zip(pool.buffers, before):
+        x[5] = x[2]
+        assert torch.equal(b.view(torch.uint8), x.view(torch.uint8))
+    # without parents, in place
+    binding.se_pages_update(pool.p, to, no, co, torch.tensor([-1, 34, 5, 20, 5], **I32), to, no, co, left, pool.ws, buffers=pool.buffers)
+    assert binding.se_last_device_status(pool.ws) == binding.SE_DEV_BAD_LENGTH
+    assert no.tolist() == [33, 34] + pool.lens[2:] and co.tolist() == [2, 2, 1, 1, 1, 1] + [0] * 34
+    assert to.tolist() == [pool.table[0], [0, 1, 5] + [-1] * 5] + pool.table[2:3] + [[3, 4] + [-1] * 6] + pool.table[4:]
+    # compaction leaves rows without a length alone
+    where = torch.full_like(c, -9)
+    binding.se_pages_compact(pool.p, to, no, co, torch.empty_like(t), torch.empty_like(c), where, left, pool.ws, buffers=pool.buffers)
+    assert binding.se_last_device_status(pool.ws) == binding.SE_DEV_BAD_LENGTH and left.tolist() == [6]
+
+
 def test_replayed_from_a_graph():
     pool = Pool(17, 16, 400, 12, 150)
     t, n, c = pool.on_gpu()
