@@ -501,7 +501,7 @@ int se_kv8_append(const se_params *p, const void *q, int64_t q_stride, const voi
  * Attention of one token per request over an 8-bit cache (se_sparse_decode's equations): with sel_idx / sel_cnt over the pages
  * that se_page_select left there ([B, H_kv, k_max], [B, H_kv]); with both NULL over every present page of the request (a dense
  * layer; k_max is not used).  out fp32, lse fp32; scores, statistics and sums are fp32; each weight, times V's scale, enters
- * its product with V's codes as two halves (22 significant bits, steps of 2^-24 of the largest at least).  No token (length 0,
+ * its product with V's codes as two halves (22 significant bits, steps of 2^-36 of the largest at least).  No token (length 0,
  * an empty selection, no present page): out = 0, lse = -inf.  Absent pages are left out; an entry of sel_idx outside the request
  * is skipped and reported (SE_DEV_BAD_SELECTION), as is a sel_cnt above k_max (the first k_max entries count); a length outside
  * 0 .. 16*max_pages is reported (SE_DEV_BAD_LENGTH).  Equal inputs give equal bits.

@@ -6,8 +6,8 @@
 // logits in fp32, s_V becomes a part of the exponent:
 //   q     is brought to a maximum of 2^13..2^14 per head by a power of two; its 8 significant bits fit a half for everything
 //         above 2^-30 of the maximum, so nothing that fp32 sums could show is lost
-//   p s_V = 2^(w - M), w = z log2 e + log2 s_V, M the running maximum of w, enters as two halves, hi + lo (22 bits), as the output
-//         is fp32: the largest are near 1 whatever the scales.  The sum of the weights takes s_V out again, in fp32.
+//   p s_V = 2^(w - m), w = z log2 e + log2 s_V, m 12 below the running maximum of w, enters as two halves, hi + lo (22 bits), as the
+//         output is fp32: the largest are near 2^12 whatever the scales.  The sum of the weights takes s_V out again, in fp32.
 //
 // What bounds it: HBM, 2 * 2 * D bytes per token and kv-head, and nearly as much the instructions: per page and head at D = 128 about
 // 300 for a warp, 64 of them conversions of two codes each and 24 matrix instructions.
@@ -30,7 +30,9 @@ constexpr int kWarps = 16, kThreads = 32 * kWarps;
 constexpr int kTeam = 4, kTeams = kWarps / kTeam;      // warps that share a run of pages, runs of a CTA
 constexpr int kLeast = 2 * kTeam;      // pages of a run
 constexpr int kChunks = 1024;          // prefix sums that a CTA keeps: of every pair, or of runs of pairs
-constexpr float kSlack = 8.f;          // the running maximum may lag: weights up to 2^8 stay far inside a half's range
+// The largest weight is 2^12 when the maximum moves, and 2^15 at most until it moves again: the steps of small weights are 2^-36 of the
+// largest, and 131072 of them that vanish 2^-20 of it (with the largest at 1 a row lost all tokens 17 below the first one's logit).
+constexpr float kLift = 12.f, kTop = 15.f;
 
 template <int D>
 struct Cfg {
@@ -392,8 +394,8 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             // w = logit + log2 of V's scale, in powers of two: what the weights in the product with V are made of
             const float shift = (float)((int)(__float_as_uint(sv) >> 23) - 127), inv = __uint_as_float(0x7f000000u - __float_as_uint(sv));
             const float t0 = fmaf(fmaxf(z[0], z[2]), g0, shift), t1 = fmaf(fmaxf(z[1], z[3]), g1, shift);
-            if (__any_sync(kFull, t0 > m0 + kSlack || t1 > m1 + kSlack)) {
-                float n0 = fmaxf(m0, t0), n1 = fmaxf(m1, t1);
+            if (__any_sync(kFull, t0 > m0 + kTop || t1 > m1 + kTop)) {
+                float n0 = fmaxf(m0, t0 - kLift), n1 = fmaxf(m1, t1 - kLift);
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) {
                     n0 = fmaxf(n0, __shfl_xor_sync(kFull, n0, o));

@@ -129,7 +129,7 @@ def decode(q, k_codes, v_codes, scales, page_table, seq_lens, sel_idx, sel_cnt, 
             rows = slice(h * G, (h + 1) * G)
             out[r, rows] = w @ vv
             # error of every weight, and of their sum
-            werr = w * (zerr + (w * zerr).sum(1, keepdim=True) + 2.0 ** -22) + 2.0 ** -25 * (w * ss).amax(1, keepdim=True) / ss
+            werr = w * (zerr + (w * zerr).sum(1, keepdim=True) + 2.0 ** -22) + 2.0 ** -37 * (w * ss).amax(1, keepdim=True) / ss
             tol[r, rows] = 1.01 * (werr @ vv.abs()) + 2.0 ** -18 * (w @ vv.abs())
             lse[r, rows] = (top + s.log())[:, 0]
             ltol[r, rows] = (w * zerr).sum(1) + 2.0 ** -22 * lse[r, rows].abs() + 2.0 ** -22

@@ -1,4 +1,6 @@
 """The 8-bit cache on the GPU: append and decode against the restatements of kv8_ref.py."""
+import math
+
 import pytest
 import torch
 
@@ -195,6 +197,21 @@ def test_decode_magnitudes():
     d.check()
     d.q.zero_()
     d.check()
+
+
+@pytest.mark.parametrize("length,gap", [(131000, 18.0), (131000, 22.0), (4000, 13.0)])
+def test_decode_of_one_large_weight_and_many_small_ones(length, gap):
+    """A first token that takes nearly all the weight and whose V is zero: the output is what the many others add up to."""
+    d = Decode(15, [length], 1, 2, 64)
+    codes = lambda x: torch.tensor(x).to(E4M3).view(torch.uint8).cuda()  # noqa: E731
+    d.q.fill_(1.0), d.scales.fill_(1.0)
+    d.k8.view(torch.uint8).fill_(0), d.v8.view(torch.uint8).fill_(codes(1.0))
+    first = int(d.table[0, 0])
+    d.k8.view(torch.uint8)[first, :, 0] = codes(gap / 8)            # 64 of them, over the square root of 64
+    d.v8.view(torch.uint8)[first, :, 0] = 0
+    d.check()
+    rest = (length - 1) * math.exp(-gap)
+    assert float((d.out.double() - rest / (1 + rest)).abs().max()) <= length * 2.0 ** -37 + 2.0 ** -14 * rest
 
 
 def test_decode_reports():
