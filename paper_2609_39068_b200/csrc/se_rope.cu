@@ -8,21 +8,21 @@
 // and reduced in fp64 and only the remaining fraction of a turn goes to sincospif.  One (token, pair) angle serves all
 // H_q + H_kv heads, so this costs 16 * rot/2 evaluations per page of 16 tokens.
 //
-// Work item = one touched page of one request (up to 16 new tokens, all heads), because the page's summary needs all of
-// its keys.  A CTA finds its items through a prefix sum of the requests' page counts in shared memory, fills the page's
-// table of angles, and deals (head of q, k or v) rows to its warps: a lane holds two 16-byte pieces of a token's
-// head (the two halves of eight rotation pairs), a warp reads all 16 tokens before it computes, so 8 x 16 bytes per
-// lane are in flight.  The K warps fold min and max of what they wrote, and of the page's older keys, with shuffles.
+// A warp takes a head of q, k or v of one touched page of one request (up to 16 new tokens), because the page's summary needs
+// all of its keys.  The CTAs cut the list of all (page, eight heads) into equal shares; a CTA finds its pages through a prefix sum of
+// the requests' page counts in shared memory and fills the page's table of angles.  A lane holds two 16-byte pieces of a token's
+// head (the two halves of eight rotation pairs); a warp reads all 16 tokens at once, 8 x 16 bytes per lane, while it turns those of
+// its last head.  The K warps fold min and max of what they wrote, and of the page's older keys, with shuffles.
 //
-// Bound by HBM for prompts: 24K tokens of 32 + 2 x 8 heads, D = 128, 122 us for 662 MB = 5.4 TB/s, 0.84 of a plain copy (124-125 us
-// as calls on changing inputs).  Small calls are four dependent round trips: 64 single tokens 7.7 us.  (Loading the next rows
-// while a row is turned, with the registers that takes, was slower: 8.2 us where 7.2 were taken, 128.5 us for 121.5.)
+// Bound by HBM for prompts: 20158 tokens of 32 + 2 x 8 heads, D = 128, 114 us for 662 MB = 5.8 TB/s, 0.89 of a plain copy (116 us
+// as calls on changing inputs).  Small calls are four dependent round trips: 64 single tokens 7.0 us.  (A page per CTA at a time: 5 %
+// more; angles in the order of their pairs, which the lanes then read from four banks: 23 % more over an 8-bit cache.)
 //
 // The same kernel fills a cache of e4m3 codes (KV8): a warp holds all tokens of a (page, head), so it has the page's largest
 // magnitude after five shuffles, picks the power-of-two scale, quantises, and brings older codes of the page to a scale that
 // has grown.  A power of two costs e4m3 no precision (its relative step is the same in every binade), makes the older codes'
-// second rounding exact but for subnormal codes, and makes every dequantised value a bf16 number.  20158 tokens of prompts,
-// 32 + 2 x 8 heads: 107 us for 459 MB (4.3 TB/s), 64 single tokens 9.9 us.
+// second rounding exact but for subnormal codes, and makes every dequantised value a bf16 number.  The same prompts: 83 us for
+// 459 MB (5.5 TB/s, 0.84), 64 single tokens 8.7 us.
 #include <type_traits>
 
 #include "se_internal.h"
@@ -32,7 +32,9 @@ namespace se {
 
 namespace {
 
-constexpr int kRopeThreads = 256;
+// Two CTAs per SM, whose 128 registers hold a head's rows and the next one's.  (Three of 80 registers without rows ahead took 121 us
+// for the prompts above in a 16-bit cache and 100 us in an 8-bit one, where these take 116 and 86.5.)
+constexpr int kRopeThreads = 256, kRopeCtas = 2;
 
 struct RopeArgs {
     const uint16_t *q, *k, *v;
@@ -47,6 +49,8 @@ struct RopeArgs {
     int B, H_q, H_kv, T, max_pages, P_phys, n_axes, rot;
 };
 
+// (the angle of pair i is cs[i * STEP])
+template <int STEP>
 __device__ __forceinline__ void rotate8(uint4 &lo, uint4 &hi, const float2 *cs, bool interleaved) {
     uint32_t a[4] = {lo.x, lo.y, lo.z, lo.w}, b[4] = {hi.x, hi.y, hi.z, hi.w};
     float x[8], y[8];
@@ -61,7 +65,7 @@ __device__ __forceinline__ void rotate8(uint4 &lo, uint4 &hi, const float2 *cs, 
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float2 t = cs[i];  // (cos, sin)
+        const float2 t = cs[i * STEP];   // (cos, sin)
         const float u = x[i] * t.x - y[i] * t.y;
         y[i] = y[i] * t.x + x[i] * t.y;
         x[i] = u;
@@ -89,16 +93,18 @@ __device__ __forceinline__ uint4 shfl_xor4(const uint4 &w, int m) {
                       __shfl_xor_sync(kFull, w.w, m));
 }
 
-// CTAS per SM: a CTA's latency is shorter with two (128 registers), more bytes are in flight with three (80 registers).
-template <int D, bool INTERLEAVED, int CTAS, bool KV8>
-__global__ void __launch_bounds__(kRopeThreads, CTAS)
+template <int D, bool INTERLEAVED, bool KV8>
+__global__ void __launch_bounds__(kRopeThreads, kRopeCtas)
 rope_append_kernel(const RopeArgs a) {
     constexpr int LPR = D / 16;            // lanes per token: two 16-byte pieces each
     constexpr int RP = 32 / LPR;           // tokens per warp pass
     constexpr int NP = kPage / RP;         // passes per page
     constexpr int NW = kRopeThreads / 32;
     extern __shared__ int s_first[];       // [B + 1] first item of each request
-    __shared__ float2 s_cs[kPage * (D / 2)];
+    // cos and sin of token t, pair c at t * kPitch + c % 8 * LPR + c / 8: the lanes of a warp, each with eight pairs in a row, read from all
+    // banks (in the order of the pairs they met in four of them, which took the shared memory as long as all that the kernel does)
+    constexpr int kPitch = D / 2 + LPR;
+    __shared__ float2 s_cs[kPage * kPitch];
     __shared__ int s_tot[32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
@@ -128,7 +134,16 @@ rope_append_kernel(const RopeArgs a) {
 
     const int half = a.rot / 2;
     const int HR = a.H_q + 2 * a.H_kv;
-    for (int it = blockIdx.x; it < carry; it += gridDim.x) {
+    // equal shares of the list of all (page, group of NW heads)
+    const int groups = (HR + NW - 1) / NW;
+    const long long units = (long long)carry * groups;
+    long long u = units * blockIdx.x / gridDim.x;
+    const long long end = units * (blockIdx.x + 1) / gridDim.x;
+    while (u < end) {
+        const int it = (int)(u / groups), g0 = (int)(u - (long long)it * groups);
+        const int g1 = (int)min((long long)groups, g0 + (end - u));
+        u += g1 - g0;
+        const int hr0 = g0 * NW, hr1 = min(g1 * NW, HR);
         int lo = 0, hi = a.B;              // request r with s_first[r] <= it < s_first[r + 1]
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
@@ -143,7 +158,43 @@ rope_append_kernel(const RopeArgs a) {
         const int pid = a.page_table[(size_t)r * a.max_pages + b];
         const bool cached = pid >= 0 && pid < a.P_phys;
         if (!cached && tid == 0) atomicOr(a.status, SE_DEV_BAD_PAGE_ID);
-        for (int i = tid; i < kPage * half; i += kRopeThreads) {
+        const int cp = lane % LPR, tq = lane / LPR;
+        const bool turned = cp < a.rot / 16;
+        int c_lo, c_hi;                    // the lane's two 16-byte pieces of a head's row
+        if (INTERLEAVED) c_lo = 2 * cp, c_hi = 2 * cp + 1;
+        else if (turned) c_lo = cp, c_hi = cp + a.rot / 16;
+        else c_lo = a.rot / 8 + 2 * (cp - a.rot / 16), c_hi = c_lo + 1;
+        // the rows of a head are on their way while the warp's last head is turned, the first ones while the angles are found
+        uint4 next_x[NP], next_y[NP];
+        [[maybe_unused]] float next_scale = 0.f;
+        auto fetch = [&](int hr) {
+            const bool is_q = hr < a.H_q, is_k = !is_q && hr < a.H_q + a.H_kv;
+            const int h = is_q ? hr : is_k ? hr - a.H_q : hr - a.H_q - a.H_kv;
+            const uint16_t *src = (is_q ? a.q : is_k ? a.k : a.v) + (size_t)h * D;
+            const long long stride = is_q ? a.q_stride : is_k ? a.k_stride : a.v_stride;
+            const size_t page = ((size_t)max(pid, 0) * a.H_kv + h) * (kPage * D);
+            const bool old_rows = cached && (KV8 ? !is_q : is_k && a.meta);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const int t = i * RP + tq;
+                if (t >= s0 && t < s1) {
+                    const uint4 *row = reinterpret_cast<const uint4 *>(src + (row0 + t) * stride);
+                    next_x[i] = row[c_lo], next_y[i] = row[c_hi];
+                } else if (old_rows && t < s0) {                             // older tokens of the page
+                    if constexpr (KV8) {
+                        const uint2 *row = reinterpret_cast<const uint2 *>((const uint8_t *)(is_k ? a.k_cache : a.v_cache) + page + (size_t)t * D);
+                        const uint2 u = row[c_lo], w = row[c_hi];
+                        next_x[i] = make_uint4(u.x, u.y, 0, 0), next_y[i] = make_uint4(w.x, w.y, 0, 0);
+                    } else {
+                        const uint4 *row = reinterpret_cast<const uint4 *>((const uint16_t *)a.k_cache + page + (size_t)t * D);
+                        next_x[i] = row[c_lo], next_y[i] = row[c_hi];
+                    }
+                }
+            }
+            if (KV8 && old_rows && s0 > 0) next_scale = a.scales[((size_t)pid * a.H_kv + h) * 2 + (is_k ? 0 : 1)];
+        };
+        if (hr0 + warp < hr1) fetch(hr0 + warp);
+        for (int i = tid; i < (hr0 < a.H_q + a.H_kv ? kPage * half : 0); i += kRopeThreads) {
             const int t = i / half, c = i - t * half;
             if (t < s0 || t >= s1) continue;
             int ax = a.pair_axis[c];
@@ -154,46 +205,20 @@ rope_append_kernel(const RopeArgs a) {
             const double turns = (double)a.positions[(size_t)ax * a.T + row0 + t] * a.inv_freq[c] * 0.15915494309189533577;
             float sn, cs;
             sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
-            s_cs[t * (D / 2) + c] = make_float2(cs, sn);
+            s_cs[t * kPitch + c % 8 * LPR + c / 8] = make_float2(cs, sn);
         }
         __syncthreads();
 
-        const int cp = lane % LPR, tq = lane / LPR;
-        const bool turned = cp < a.rot / 16;
-        int c_lo, c_hi;                    // the lane's two 16-byte pieces of a head's row
-        if (INTERLEAVED) c_lo = 2 * cp, c_hi = 2 * cp + 1;
-        else if (turned) c_lo = cp, c_hi = cp + a.rot / 16;
-        else c_lo = a.rot / 8 + 2 * (cp - a.rot / 16), c_hi = c_lo + 1;
-        for (int hr = warp; hr < HR; hr += NW) {
+        for (int hr = hr0 + warp; hr < hr1; hr += NW) {
             const bool is_q = hr < a.H_q, is_k = !is_q && hr < a.H_q + a.H_kv;
             const int h = is_q ? hr : is_k ? hr - a.H_q : hr - a.H_q - a.H_kv;
-            const uint16_t *src = (is_q ? a.q : is_k ? a.k : a.v) + (size_t)h * D;
-            const long long stride = is_q ? a.q_stride : is_k ? a.k_stride : a.v_stride;
             const size_t page = ((size_t)max(pid, 0) * a.H_kv + h) * (kPage * D);
             const bool want_meta = is_k && a.meta && cached;
             uint4 x[NP], y[NP];
 #pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                const int t = i * RP + tq;
-                if (t >= s0 && t < s1) {
-                    const uint4 *row = reinterpret_cast<const uint4 *>(src + (row0 + t) * stride);
-                    x[i] = row[c_lo], y[i] = row[c_hi];
-                } else if (KV8 ? !is_q && cached && t < s0 : want_meta && t < s0) {          // older tokens of the page
-                    if constexpr (KV8) {
-                        const uint2 *row = reinterpret_cast<const uint2 *>((const uint8_t *)(is_k ? a.k_cache : a.v_cache) + page + (size_t)t * D);
-                        const uint2 u = row[c_lo], w = row[c_hi];
-                        x[i] = make_uint4(u.x, u.y, 0, 0), y[i] = make_uint4(w.x, w.y, 0, 0);
-                    } else {
-                        const uint4 *row = reinterpret_cast<const uint4 *>((const uint16_t *)a.k_cache + page + (size_t)t * D);
-                        x[i] = row[c_lo], y[i] = row[c_hi];
-                    }
-                }
-            }
-            [[maybe_unused]] float *sp = nullptr, old_scale = 0.f;
-            if constexpr (KV8) {
-                sp = a.scales + ((size_t)max(pid, 0) * a.H_kv + max(h, 0)) * 2 + (is_k ? 0 : 1);
-                if (!is_q && cached && s0 > 0) old_scale = *sp;
-            }
+            for (int i = 0; i < NP; ++i) x[i] = next_x[i], y[i] = next_y[i];
+            [[maybe_unused]] const float old_scale = next_scale;
+            if (hr + NW < hr1) fetch(hr + NW);
             [[maybe_unused]] uint32_t top = 0;     // KV8: largest magnitudes so far, two bf16
             uint4 mnx = make_uint4(0x7f807f80u, 0x7f807f80u, 0x7f807f80u, 0x7f807f80u), mny = mnx;   // +inf pairs
             uint4 mxx = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u), mxy = mxx;   // -inf pairs
@@ -201,7 +226,7 @@ rope_append_kernel(const RopeArgs a) {
             for (int i = 0; i < NP; ++i) {
                 const int t = i * RP + tq;
                 if (t >= s0 && t < s1) {
-                    if ((is_q || is_k) && turned) rotate8(x[i], y[i], s_cs + t * (D / 2) + cp * 8, INTERLEAVED);
+                    if ((is_q || is_k) && turned) rotate8<LPR>(x[i], y[i], s_cs + t * kPitch + cp, INTERLEAVED);
                     if (is_q || (is_k && a.k_out)) {
                         uint4 *o = reinterpret_cast<uint4 *>(is_q ? a.q_out + ((row0 + t) * a.H_q + h) * D
                                                                   : a.k_out + ((row0 + t) * a.H_kv + h) * D);
@@ -250,7 +275,7 @@ rope_append_kernel(const RopeArgs a) {
                             fold_max(mxx, x[i]), fold_max(mxy, y[i]);
                         }
                     }
-                    if (lane == 0) *sp = scale;
+                    if (lane == 0) a.scales[((size_t)pid * a.H_kv + h) * 2 + (is_k ? 0 : 1)] = scale;
                 }
             }
             if (want_meta) {
@@ -281,24 +306,16 @@ cudaError_t launch_rope_append(const se_params &p, const RopeCall &c, cudaStream
     a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.T = c.total_tokens, a.max_pages = p.max_pages;
     a.P_phys = p.num_phys_pages, a.n_axes = c.n_axes, a.rot = c.rot_dim;
     // a request touches at most ceil((n + 15) / 16) pages
-    const long long items = (long long)c.total_tokens / kPage + 2ll * p.B;
-    const int sms = device_sm_count();
-    // Side by side, 64 single tokens: 7.2 us with two CTAs per SM, 8.4 us with three; 24K tokens of prompts: 126.8 and 121.5 us.
-    // (Until each CTA has several pages the latency of one counts.)
-    const bool many = items > 8ll * sms;
-    const long long cap = (many ? 3ll : 2ll) * sms;
-    const unsigned grid = (unsigned)(items < cap ? items : cap);
+    const int groups = (p.H_q + 2 * p.H_kv + kRopeThreads / 32 - 1) / (kRopeThreads / 32);
+    const long long units = ((long long)c.total_tokens / kPage + 2ll * p.B) * groups, cap = (long long)kRopeCtas * device_sm_count();
+    const unsigned grid = (unsigned)(units < cap ? units : cap);
     const size_t smem = ((size_t)p.B + 1) * sizeof(int);
-    auto pick = [&](auto d, auto ctas) {
-        constexpr int D = decltype(d)::value, CTAS = decltype(ctas)::value;
-        if (c.scales) return c.interleaved ? rope_append_kernel<D, true, CTAS, true> : rope_append_kernel<D, false, CTAS, true>;
-        return c.interleaved ? rope_append_kernel<D, true, CTAS, false> : rope_append_kernel<D, false, CTAS, false>;
+    auto pick = [&](auto d) {
+        constexpr int D = decltype(d)::value;
+        if (c.scales) return c.interleaved ? rope_append_kernel<D, true, true> : rope_append_kernel<D, false, true>;
+        return c.interleaved ? rope_append_kernel<D, true, false> : rope_append_kernel<D, false, false>;
     };
-    using Two = std::integral_constant<int, 2>;
-    using Three = std::integral_constant<int, 3>;
-    using D64 = std::integral_constant<int, 64>;
-    using D128 = std::integral_constant<int, 128>;
-    auto kern = p.D == 128 ? (many ? pick(D128{}, Three{}) : pick(D128{}, Two{})) : (many ? pick(D64{}, Three{}) : pick(D64{}, Two{}));
+    auto kern = p.D == 128 ? pick(std::integral_constant<int, 128>{}) : pick(std::integral_constant<int, 64>{});
     kern<<<grid, kRopeThreads, smem, stream>>>(a);
     return cudaGetLastError();
 }
