@@ -33,6 +33,8 @@ def page_tables(g, total, extra=2, wide=0):
     (7, 1, 128, [33, 2], [0, 14], 64, True, 0),                    # heads in groups of seven, part of the head, interleaved
     (4, 4, 64, [100], [60], 32, False, 0),
     (8, 8, 128, [3] * 40, list(range(40)), 128, True, 0),
+    (32, 8, 128, [700, 333], [5, 100], 128, False, 0),             # CTAs begin and end inside a page's heads
+    (2, 1, 64, [1] * 1500, [i % 40 for i in range(1500)], 64, False, 0),   # more requests than threads
 ])
 def test_append(H_q, H_kv, D, new, past, rot, interleaved, spare):
     g = torch.Generator().manual_seed(7)
@@ -172,6 +174,7 @@ class Decode:
     ([40, 33], 8, 5, 128, 1.0),                                    # every page absent
     (list(range(1, 120)), 3, 2, 64, 0.0),                          # more pairs than CTAs
     ([64] * 700, 4, 1, 128, 0.05),                                 # more pairs than prefix sums
+    ([i % 50 for i in range(8192)], 1, 1, 64, 0.0),                # the largest batch
 ])
 def test_decode_dense(lens, H_kv, G, D, absent):
     Decode(3, lens, H_kv, G, D, absent).check()

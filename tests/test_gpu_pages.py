@@ -93,7 +93,8 @@ class Pool:
 
 
 @pytest.mark.parametrize("seed,B,P,width,longest", [(1, 1, 4, 3, 40), (2, 5, 60, 9, 100), (3, 64, 1500, 30, 400), (4, 200, 3000, 20, 250),
-                                                    (5, 3, 20000, 700, 11000)])
+                                                    (5, 3, 20000, 700, 11000),
+                                                    (6, 8192, 30000, 6, 60)])
 def test_many_steps(seed, B, P, width, longest):
     """Steps after one another, each on what the last one left: forks, ends, cuts, growth, and compaction in between."""
     pool = Pool(seed, B, P, width, longest)
