@@ -173,6 +173,9 @@ class Decode:
     ([9000], 1, 8, 128, 0.5),
     ([40, 33], 8, 5, 128, 1.0),                                    # every page absent
     (list(range(1, 120)), 3, 2, 64, 0.0),                          # more pairs than CTAs
+    ([65536], 1, 3, 64, 0.1),                                      # one pair over all runs, merged in groups
+    ([3900, 4000, 90, 4090, 0, 12000], 1, 8, 128, 0.0),            # pairs of 30 to 32 runs and more, which begin and end inside groups
+    ([20000, 50000], 2, 7, 64, 0.3),
     ([64] * 700, 4, 1, 128, 0.05),                                 # more pairs than prefix sums
     ([i % 50 for i in range(8192)], 1, 1, 64, 0.0),                # the largest batch
 ])
