@@ -60,6 +60,7 @@ constexpr int kMinCost = 256, kCoarse = 2048;
 // The running maximum may lag: weights up to 2^40 lose nothing (bf16 and fp32 keep their exponents, and 2^40 * 131072
 // tokens is far from the end of the range).
 constexpr float kSlack = 40.f;
+constexpr int kNoToken = 0x7fffffff;   // later than every token
 
 template <int D, bool KV8>
 struct Cfg {
@@ -154,6 +155,8 @@ struct Control {
     float k_scale[KV8 ? Cfg<D, KV8>::kMasks : 1][KV8 ? kGroups : 1];
     float q_scale[KV8 ? 2 : 1][KV8 ? 2 : 1][KV8 ? kTile : 1];              // [this segment and the next][query tile]
     SegmentQueue<Segment> queue;
+    // 8-bit cache, for every place of the queue: whether its part of V holds NaN codes, and the first token that has one in each channel
+    int nans[KV8 ? SegmentQueue<Segment>::kDepth : 1], nan_from[KV8 ? SegmentQueue<Segment>::kDepth : 1][KV8 ? D : 1];
     alignas(8) uint8_t prefix[prefix_bytes(kSmemRequests)];
     uint32_t mask[Cfg<D, KV8>::kMasks];     // present 16-token groups of the tiles in flight
     int parts[2];                      // partial results to merge, 0: another CTA does
@@ -383,6 +386,9 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v
 // the scales - 2^e of the row, s_K of the page - enter the softmax in fp32.
 // V's codes become bf16 (exact, as the scales are powers of two), because weights need their range and eight bits: four warps bring
 // two pages of every tile each into a ring of their own, turn them, and write the tile that the tensor copies would.
+// A NaN code enters the tile as a finite value: a row that does not see its token weighs it with 0, and 0 times a NaN would reach that
+// row's sum.  The turning warps note the first token that has one in each channel, and since a row sees all tokens before a border, its
+// channels are NaN where that token lies before the row's.
 // (With K turned into bf16 too, by one warp and V by another, a step took 9000 to 11000 cycles instead of 3350.)
 
 // Page ids and scales of 32 groups of 16 tokens at a time, a lane each; scales of the next 32 and ids of the 32 behind those are on
@@ -445,7 +451,13 @@ __device__ __forceinline__ void k8_role(const AttendArgs &a, const List<AttendWo
     bool ok = true;
     Walk<AttendWork> walk(list, a.ctl, lane);
     while (ok && next_segment(walk, s)) {
-        ok = ctl->queue.put(queries, &s, gave_up, &a.ctl->status, lane);
+        ok = ctl->queue.put(queries, &s, gave_up, &a.ctl->status, lane, [&](uint32_t place) {
+            if (!*(volatile int *)&ctl->nans[place]) return;
+            for (int c = lane; c < D; c += 32) ctl->nan_from[place][c] = kNoToken;
+            __syncwarp();
+            if (lane == 0) ctl->nans[place] = 0;
+            __syncwarp();
+        });
         if (!ok) break;
         pages.begin(a, s, s.a * kGroups, 1, 0, false, lane);
         ok = warp_wait(bars + 8 * kQEmpty, (queries & 1) ^ 1, gave_up, &a.ctl->status);
@@ -548,6 +560,20 @@ __device__ __forceinline__ void v8_role(const AttendArgs &a, Control<D, true> *c
 #pragma unroll
                     for (int e = 0; e < N; ++e)
                         if (row + 8 * (e / (D / 64)) >= tokens) x[e] = make_uint4(0, 0, 0, 0);
+                }
+                uint32_t nan = 0;
+#pragma unroll
+                for (int e = 0; e < N; ++e) nan |= kv8_nan(x[e].x) | kv8_nan(x[e].y) | kv8_nan(x[e].z) | kv8_nan(x[e].w);
+                if (nan & 0x80808080u) {
+                    const uint32_t place = (turn - 1) % SegmentQueue<Segment>::kDepth;
+#pragma unroll 1
+                    for (int n = 0; n < 16 * N; ++n) {                     // (from shared memory again: registers are few)
+                        const int e = n / 16, token = row + 8 * (e / (D / 64)), ch = part * 16 + e % (D / 64) * 64 + n % 16;
+                        uint32_t code;
+                        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(code) : "r"(raw + from * C::kRawBytes + i * (kPage * D) + token * D + ch) : "memory");
+                        if (token < tokens && (code & 0x7fu) == 0x7fu) atomicMin(&ctl->nan_from[place][ch], group * kPage + token);
+                    }
+                    ctl->nans[place] = 1;
                 }
                 const uint32_t to = slot * C::kKvBytes + (group % kGroups) * (kPage * D * 2);
 #pragma unroll
@@ -961,6 +987,17 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
         }
 
         // ---- epilogue ----
+        // 32 sums of the row, from channel k on, become NaN where the row sees a NaN code of V
+        auto find_nans = [&](int k, float *o) {
+            if constexpr (KV8) {
+                const uint32_t place = (turn - 1) % SegmentQueue<Segment>::kDepth;
+                if (*(volatile int *)&ctl->nans[place]) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (*(volatile int *)&ctl->nan_from[place][k + e] < s.t.past + tok + q + 1) o[e] = __uint_as_float(0x7fffffffu);
+                }
+            }
+        };
         // -infinity says that nothing was seen, so a sum that is NaN goes with another maximum
         const float m2 = l != l ? INFINITY : m == -INFINITY ? m : KV8 ? m : m * sl;
         const bool live = row < ntok * a.G;
@@ -978,6 +1015,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
                 tmem_ld32(t_o + k, o);
                 tmem_wait_ld();
                 settle<32>(o);
+                find_nans(k, o);
                 uint32_t w[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -1013,6 +1051,7 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
                     tmem_ld32(t_o + k, o);
                     tmem_wait_ld();
                     settle<32>(o);
+                    find_nans(k, o);
                     if (live) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 8) store32(slot + (size_t)row * D + k + e, reinterpret_cast<const uint32_t *>(o + e));
@@ -1110,6 +1149,10 @@ attend_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     if (KV8 && threadIdx.x >= 64 && threadIdx.x < 64 + kTurners * C::kRawSlots) {
         mbar_init(smem_u32(&ctl->raw[threadIdx.x - 64]), 1);
         mbar_fence_init();
+    }
+    if constexpr (KV8) {
+        for (int i = threadIdx.x; i < (int)SegmentQueue<Segment>::kDepth * D; i += C::kThreads) ctl->nan_from[i / D][i % D] = kNoToken;
+        if (threadIdx.x < SegmentQueue<Segment>::kDepth) ctl->nans[threadIdx.x] = 0;
     }
     // (read ahead: it is here when the list is)
     const uint32_t refused = threadIdx.x == 32 * kIdleWarp ? *(volatile uint32_t *)&a.ctl->needs_init : 0u;

@@ -74,7 +74,8 @@ __device__ __forceinline__ uint4 kv8_values(const uint2 &u, float scale) {
 }
 
 // Four codes as four bf16 times `f`: exact where f = scale * kv8_bf16_step() is a power of two.  A code's exponent and mantissa, moved
-// to the place of a bf16's, are its value times 2^-120 (the difference of the biases), subnormal codes included.
+// to the place of a bf16's, are its value times 2^-120 (the difference of the biases), subnormal codes included.  The NaN codes (0x7f,
+// 0xff) come out as +-480 * scale: who turns codes with it has to look for them (kv8_nan).
 __device__ __forceinline__ constexpr float kv8_bf16_step() { return 0x1p120f; }
 __device__ __forceinline__ void kv8_bf16x4(uint32_t codes, __nv_bfloat162 f, uint32_t &lo, uint32_t &hi) {
     uint32_t x[2];                       // halves: a code, its sign in all bits above
@@ -88,5 +89,8 @@ __device__ __forceinline__ void kv8_bf16x4(uint32_t codes, __nv_bfloat162 f, uin
     }
     lo = x[0], hi = x[1];
 }
+
+// Not zero in the top bit of a byte: that of the four codes is a NaN's.
+__device__ __forceinline__ uint32_t kv8_nan(uint32_t codes) { return (codes & 0x7f7f7f7fu) + 0x01010101u; }
 
 }  // namespace se

@@ -199,10 +199,16 @@ struct SegmentQueue {
             mbar_init(smem_u32(&empty[k]), listeners);
         }
     }
-    // by the warp that walks, the n-th entry; false: a wait gave up
+    // by the warp that walks, the n-th entry; fresh(k), by the whole warp, makes ready what else belongs to place k; false: a wait
+    // gave up
     __device__ __forceinline__ bool put(uint32_t n, const Segment *s, volatile int *gave_up, uint32_t *status, int lane) {
+        return put(n, s, gave_up, status, lane, [](uint32_t) {});
+    }
+    template <class Fresh>
+    __device__ __forceinline__ bool put(uint32_t n, const Segment *s, volatile int *gave_up, uint32_t *status, int lane, Fresh fresh) {
         const uint32_t k = n % kDepth;
         if (!warp_wait(smem_u32(&empty[k]), (n / kDepth & 1) ^ 1, gave_up, status)) return false;
+        fresh(k);
         if (lane == 0) {
             if (s) entry[k] = *s;
             more[k] = s != nullptr;
