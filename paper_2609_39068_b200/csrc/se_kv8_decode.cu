@@ -39,6 +39,9 @@ constexpr int kChunks = 1024;          // prefix sums that a CTA keeps: of every
 // The largest weight is 2^12 when the maximum moves, and 2^15 at most until it moves again: the steps of small weights are 2^-36 of the
 // largest, and 131072 of them that vanish 2^-20 of it (with the largest at 1 a row lost all tokens 17 below the first one's logit).
 constexpr float kLift = 12.f, kTop = 15.f;
+// The tensor cores cut a sum off after each product, always towards zero: sums over 1500 pages of a warp came out 1e-4 too small.  After
+// this many pages they join those in the merge buffer, rounded to nearest: 2^-18 at most for two products a page, 5e-7 on average.
+constexpr uint32_t kFold = 16;
 
 template <int D>
 struct Cfg {
@@ -406,6 +409,32 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 #pragma unroll
         for (int i = 0; i < C::kTiles; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+        float *own = s_merge + warp * (8 * C::kPitch + 16);
+        bool folded = false;           // the merge buffer holds the sums of earlier pages, for the maxima that lie with them
+        auto fold = [&] {
+            float r0 = 0.f, r1 = 0.f;
+            if (folded) r0 = ex2(own[8 * C::kPitch + 2 * t] - m0), r1 = ex2(own[8 * C::kPitch + 2 * t + 1] - m1);
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) l0 += __shfl_xor_sync(kFull, l0, o), l1 += __shfl_xor_sync(kFull, l1, o);
+            __syncwarp();
+            if (g == 0) {
+                float *stats = own + 8 * C::kPitch + 2 * t;
+                if (folded) l0 = fmaf(stats[8], r0, l0), l1 = fmaf(stats[9], r1, l1);
+                stats[0] = m0, stats[1] = m1, stats[8] = l0, stats[9] = l1;
+            }
+#pragma unroll
+            for (int j = 0; j < C::kTiles / 2; ++j) {
+                float4 *at0 = reinterpret_cast<float4 *>(own + (2 * t) * C::kPitch + (D / 8) * g + 4 * j), *at1 = at0 + C::kPitch / 4;
+                float4 x = make_float4(acc[2 * j][0], acc[2 * j][2], acc[2 * j + 1][0], acc[2 * j + 1][2]);
+                float4 y = make_float4(acc[2 * j][1], acc[2 * j][3], acc[2 * j + 1][1], acc[2 * j + 1][3]);
+                if (folded) {
+                    const float4 u = *at0, w = *at1;
+                    x = make_float4(fmaf(u.x, r0, x.x), fmaf(u.y, r0, x.y), fmaf(u.z, r0, x.z), fmaf(u.w, r0, x.w));
+                    y = make_float4(fmaf(w.x, r1, y.x), fmaf(w.y, r1, y.y), fmaf(w.z, r1, y.z), fmaf(w.w, r1, y.w));
+                }
+                *at0 = x, *at1 = y;
+            }
+        };
 
         for (; k < mine && k * kTeam + mate < stop; ++k) {
             if (k / 32 != block) {
@@ -516,20 +545,19 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 mma_f16(acc[i], a0, a1, a2, a3, e0, e1);
                 mma_f16(acc[i], a0, a1, a2, a3, b0, b1);
             }
+            if (used % kFold == 0) {
+                fold();
+                folded = true;
+                l0 = l1 = 0.f;
+#pragma unroll
+                for (int i = 0; i < C::kTiles; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+                __syncwarp();
+            }
         }
 
         // ---- end of the pair's pages in this run ----
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) l0 += __shfl_xor_sync(kFull, l0, o), l1 += __shfl_xor_sync(kFull, l1, o);
+        fold();
         const float *team_merge = s_merge + team * kTeam * (8 * C::kPitch + 16);
-        float *own = s_merge + warp * (8 * C::kPitch + 16);
-        if (g == 0) own[8 * C::kPitch + 2 * t] = m0, own[8 * C::kPitch + 2 * t + 1] = m1, own[8 * C::kPitch + 8 + 2 * t] = l0, own[8 * C::kPitch + 9 + 2 * t] = l1;
-#pragma unroll
-        for (int j = 0; j < C::kTiles / 2; ++j) {
-            const int ch = (D / 8) * g + 4 * j;
-            *reinterpret_cast<float4 *>(own + (2 * t) * C::kPitch + ch) = make_float4(acc[2 * j][0], acc[2 * j][2], acc[2 * j + 1][0], acc[2 * j + 1][2]);
-            *reinterpret_cast<float4 *>(own + (2 * t + 1) * C::kPitch + ch) = make_float4(acc[2 * j][1], acc[2 * j][3], acc[2 * j + 1][1], acc[2 * j + 1][3]);
-        }
         team_sync(team);
         const int c0 = (int)(first / size), c1 = (int)((first + pages - 1) / size);      // runs that share the pair
         const int r = pair / a.H_kv, h = pair - r * a.H_kv;
