@@ -987,16 +987,13 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
         }
 
         // ---- epilogue ----
-        // 32 sums of the row, from channel k on, become NaN where the row sees a NaN code of V
-        auto find_nans = [&](int k, float *o) {
-            if constexpr (KV8) {
-                const uint32_t place = (turn - 1) % SegmentQueue<Segment>::kDepth;
-                if (*(volatile int *)&ctl->nans[place]) {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (*(volatile int *)&ctl->nan_from[place][k + e] < s.t.past + tok + q + 1) o[e] = __uint_as_float(0x7fffffffu);
-                }
-            }
+        // channels in which the row sees a NaN code of V, of what it has written
+        auto mark_nans = [&](auto *dst, auto nan) {
+            const uint32_t place = (turn - 1) % SegmentQueue<Segment>::kDepth;
+            if (!*(volatile int *)&ctl->nans[place]) return;
+#pragma unroll 1
+            for (int c = 0; c < D; ++c)
+                if (*(volatile int *)&ctl->nan_from[place][c] < s.t.past + tok + q + 1) dst[c] = nan;
         };
         // -infinity says that nothing was seen, so a sum that is NaN goes with another maximum
         const float m2 = l != l ? INFINITY : m == -INFINITY ? m : KV8 ? m : m * sl;
@@ -1015,7 +1012,6 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
                 tmem_ld32(t_o + k, o);
                 tmem_wait_ld();
                 settle<32>(o);
-                find_nans(k, o);
                 uint32_t w[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -1034,6 +1030,9 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
                     }
                 }
             }
+            if constexpr (KV8) {
+                if (live) mark_nans(a.out + orow * D, (uint16_t)0x7fffu);
+            }
             if (live && a.lse) a.lse[orow] = l == 0.f ? -INFINITY : (m2 + log2f(l)) * kLn2;
             tc_fence_before();
             __syncwarp();
@@ -1051,11 +1050,13 @@ __device__ __forceinline__ void softmax_role(const AttendArgs &a, const List<Att
                     tmem_ld32(t_o + k, o);
                     tmem_wait_ld();
                     settle<32>(o);
-                    find_nans(k, o);
                     if (live) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 8) store32(slot + (size_t)row * D + k + e, reinterpret_cast<const uint32_t *>(o + e));
                     }
+                }
+                if constexpr (KV8) {
+                    if (live) mark_nans(slot + (size_t)row * D, __uint_as_float(0x7fffffffu));
                 }
                 tc_fence_before();
                 __syncwarp();
