@@ -451,7 +451,7 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             const uint32_t slot = used % C::kStages, at = ring + slot * (2 * C::kPageBytes);
             if (ok && !__all_sync(kFull, mbar_wait(bars + 8 * slot, used / C::kStages & 1))) {
                 ok = false;
-                if (lane == 0) atomicOr(&a.ctl->status, SE_DEV_WAIT_TIMEOUT);
+                if (lane == 0) atomicExch(&a.ctl->needs_init, 1u), atomicOr(&a.ctl->status, SE_DEV_WAIT_TIMEOUT);
             }
             if (!ok) continue;
             // ---- logits: rows are tokens, columns are heads.  Row x of the product is token x for even x, x ^ 4 for odd x (and the
