@@ -58,7 +58,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
 
 # A second build of the same sources with -DSE_TEST_SHORT_TX: waits of the scoring kernel (se_select.cu) and of the prompt
-# kernels (se_tc.cuh) run out.  Only the tests of the bounded waits load it.
+# kernels (se_tc.cuh) run out, and the grid-wide barriers of the page kernels (se_pages.cu).  Only the tests of the bounded waits load it.
 LIB_SHORT_TX = os.path.join(HERE, "libsparse_engine_shorttx.so")
 
 

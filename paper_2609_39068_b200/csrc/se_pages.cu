@@ -63,6 +63,13 @@ struct CompactArgs {
     int B, max_pages, P;
 };
 
+// For the test of the bounded barriers (a second build of the library, never the product): they wait for a CTA that does not exist.
+#ifdef SE_TEST_SHORT_TX
+constexpr uint32_t kTestExtraCtas = 1;
+#else
+constexpr uint32_t kTestExtraCtas = 0;
+#endif
+
 // All CTAs of the launch have come here, and see what the others wrote before.  False: the wait gave up.
 __device__ __forceinline__ bool grid_sync(Control *ctl, int turn) {
     __shared__ int s_ok;
@@ -71,7 +78,7 @@ __device__ __forceinline__ bool grid_sync(Control *ctl, int turn) {
     if (threadIdx.x == 0) {
         __threadfence();
         atomicAdd(&ctl->arrived, 1u);
-        const uint32_t want = (uint32_t)turn * gridDim.x;
+        const uint32_t want = (uint32_t)turn * gridDim.x + kTestExtraCtas;
         bool ok = false;
         const unsigned long long t0 = globaltimer_ns();
         for (int it = 0; !ok; ++it) {
