@@ -9,20 +9,20 @@
 // H_q + H_kv heads, so this costs 16 * rot/2 evaluations per page of 16 tokens.
 //
 // A warp takes a head of q, k or v of one touched page of one request (up to 16 new tokens), because the page's summary needs
-// all of its keys.  The CTAs cut the list of all (page, eight heads) into equal shares; a CTA finds its pages through a prefix sum of
-// the requests' page counts in shared memory and fills the page's table of angles.  A lane holds two 16-byte pieces of a token's
-// head (the two halves of eight rotation pairs); a warp reads all 16 tokens at once, 8 x 16 bytes per lane, while it turns those of
-// its last head.  The K warps fold min and max of what they wrote, and of the page's older keys, with shuffles.
+// all of its keys.  A CTA finds its pages through a prefix sum of the requests' page counts in shared memory and fills the page's table
+// of angles.  A lane holds two 16-byte pieces of a token's head (the two halves of eight rotation pairs); a warp reads all 16 tokens at
+// once, 8 x 16 bytes per lane.  The K warps fold min and max of what they wrote, and of the page's older keys, with shuffles.  How the
+// CTAs share the pages depends on how many there are and how full (Plan, below).
 //
-// Bound by HBM for prompts: 20158 tokens of 32 + 2 x 8 heads, D = 128, 114 us for 662 MB = 5.8 TB/s, 0.89 of a plain copy (116 us
-// as calls on changing inputs).  Small calls are four dependent round trips: 64 single tokens 7.0 us.  (A page per CTA at a time: 5 %
-// more; angles in the order of their pairs, which the lanes then read from four banks: 23 % more over an 8-bit cache.)
+// Bound by HBM for prompts: 26655 tokens of 32 + 2 x 8 heads, D = 128, 114 us for 662 MB = 5.8 TB/s, 0.89 of a plain copy (116 us
+// as calls on changing inputs).  Small calls are four dependent round trips: 64 single tokens 5.5 us, 6.3 with summaries.  (Angles in the
+// order of their pairs, which the lanes then read from four banks: 23 % more over an 8-bit cache.)
 //
 // The same kernel fills a cache of e4m3 codes (KV8): a warp holds all tokens of a (page, head), so it has the page's largest
 // magnitude after five shuffles, picks the power-of-two scale, quantises, and brings older codes of the page to a scale that
 // has grown.  A power of two costs e4m3 no precision (its relative step is the same in every binade), makes the older codes'
-// second rounding exact but for subnormal codes, and makes every dequantised value a bf16 number.  The same prompts: 83 us for
-// 459 MB (5.5 TB/s, 0.84), 64 single tokens 8.7 us.
+// second rounding exact but for subnormal codes, and makes every dequantised value a bf16 number.  20158 tokens of prompts:
+// 83 us for 459 MB (5.5 TB/s, 0.84); 20000 tokens in eight equal prompts 83.4 us, into a 16-bit cache 84.5; 64 single tokens 8.4 us.
 #include <type_traits>
 
 #include "se_internal.h"
@@ -32,9 +32,23 @@ namespace se {
 
 namespace {
 
-// Two CTAs per SM, whose 128 registers hold a head's rows and the next one's.  (Three of 80 registers without rows ahead took 121 us
-// for the prompts above in a 16-bit cache and 100 us in an 8-bit one, where these take 116 and 86.5.)
-constexpr int kRopeThreads = 256, kRopeCtas = 2;
+constexpr int kRopeThreads = 256;
+
+// How the CTAs share the work, and what 32 + 2 x 8 heads at D = 128 with summaries took, 16-bit / 8-bit cache, in us:
+//   kParts   the heads of a page are cut into equal parts for as many CTAs, two per SM: up to two pages per SM
+//   kAhead   equal shares of the list of all (page, eight heads), two CTAs per SM, whose 128 registers hold a head's rows and the
+//            next one's: many well filled pages at D = 128
+//   kPages   a CTA takes whole pages, three CTAs per SM: many pages that get a few tokens each, whose time is that of a page's dependent
+//            loads, and D = 64, where a page's rows are half the bytes
+//                                   kParts         kAhead         kPages
+//   64 tokens, a page each          6.3 / 8.4      7.3 / 8.7      6.5 / 7.4
+//   256 tokens, a page each         9.9 / 11.9     13.5 / 14.9    12.5 / 14.9
+//   2048 tokens, a page each        66 / 79        80 / 89        60 / 69
+//   8 prompts of 2500 tokens        96 / 100       84.5 / 83.4    86 / 88
+//   the same, 8 + 2 x 2 heads, D 64 20.9 / 22.5    20.6 / 22.3    16.2 / 17.4
+enum Plan { kParts, kAhead, kPages };
+template <int PLAN>
+constexpr int kRopeCtas = PLAN == kPages ? 3 : 2;
 
 struct RopeArgs {
     const uint16_t *q, *k, *v;
@@ -47,6 +61,7 @@ struct RopeArgs {
     uint16_t *meta;
     uint32_t *status;
     int B, H_q, H_kv, T, max_pages, P_phys, n_axes, rot;
+    int part;                                    // kParts: groups of eight heads of a part
 };
 
 // (the angle of pair i is cs[i * STEP])
@@ -93,8 +108,8 @@ __device__ __forceinline__ uint4 shfl_xor4(const uint4 &w, int m) {
                       __shfl_xor_sync(kFull, w.w, m));
 }
 
-template <int D, bool INTERLEAVED, bool KV8>
-__global__ void __launch_bounds__(kRopeThreads, kRopeCtas)
+template <int D, bool INTERLEAVED, bool KV8, int PLAN>
+__global__ void __launch_bounds__(kRopeThreads, kRopeCtas<PLAN>)
 rope_append_kernel(const RopeArgs a) {
     constexpr int LPR = D / 16;            // lanes per token: two 16-byte pieces each
     constexpr int RP = 32 / LPR;           // tokens per warp pass
@@ -134,15 +149,18 @@ rope_append_kernel(const RopeArgs a) {
 
     const int half = a.rot / 2;
     const int HR = a.H_q + 2 * a.H_kv;
-    // equal shares of the list of all (page, group of NW heads)
-    const int groups = (HR + NW - 1) / NW;
-    const long long units = (long long)carry * groups;
-    long long u = units * blockIdx.x / gridDim.x;
-    const long long end = units * (blockIdx.x + 1) / gridDim.x;
-    while (u < end) {
-        const int it = (int)(u / groups), g0 = (int)(u - (long long)it * groups);
-        const int g1 = (int)min((long long)groups, g0 + (end - u));
-        u += g1 - g0;
+    const int groups = (HR + NW - 1) / NW;       // of NW heads
+    [[maybe_unused]] long long u = 0, end = 0;   // kAhead: the CTA's share of the list of all (page, group)
+    if constexpr (PLAN == kAhead) u = (long long)carry * groups * blockIdx.x / gridDim.x, end = (long long)carry * groups * (blockIdx.x + 1) / gridDim.x;
+    for (int page = blockIdx.x; PLAN == kAhead ? u < end : page < carry; page += gridDim.x) {
+        int it = page, g0 = 0, g1 = groups;
+        if constexpr (PLAN == kAhead) {
+            it = (int)(u / groups), g0 = (int)(u - (long long)it * groups);
+            g1 = (int)min((long long)groups, g0 + (end - u));
+            u += g1 - g0;
+        } else if constexpr (PLAN == kParts) {
+            g0 = blockIdx.y * a.part, g1 = min(g0 + a.part, groups);
+        }
         const int hr0 = g0 * NW, hr1 = min(g1 * NW, HR);
         int lo = 0, hi = a.B;              // request r with s_first[r] <= it < s_first[r + 1]
         while (hi - lo > 1) {
@@ -164,10 +182,7 @@ rope_append_kernel(const RopeArgs a) {
         if (INTERLEAVED) c_lo = 2 * cp, c_hi = 2 * cp + 1;
         else if (turned) c_lo = cp, c_hi = cp + a.rot / 16;
         else c_lo = a.rot / 8 + 2 * (cp - a.rot / 16), c_hi = c_lo + 1;
-        // the rows of a head are on their way while the warp's last head is turned, the first ones while the angles are found
-        uint4 next_x[NP], next_y[NP];
-        [[maybe_unused]] float next_scale = 0.f;
-        auto fetch = [&](int hr) {
+        auto fetch = [&](int hr, uint4 (&x)[NP], uint4 (&y)[NP], float &scale) {
             const bool is_q = hr < a.H_q, is_k = !is_q && hr < a.H_q + a.H_kv;
             const int h = is_q ? hr : is_k ? hr - a.H_q : hr - a.H_q - a.H_kv;
             const uint16_t *src = (is_q ? a.q : is_k ? a.k : a.v) + (size_t)h * D;
@@ -179,21 +194,26 @@ rope_append_kernel(const RopeArgs a) {
                 const int t = i * RP + tq;
                 if (t >= s0 && t < s1) {
                     const uint4 *row = reinterpret_cast<const uint4 *>(src + (row0 + t) * stride);
-                    next_x[i] = row[c_lo], next_y[i] = row[c_hi];
+                    x[i] = row[c_lo], y[i] = row[c_hi];
                 } else if (old_rows && t < s0) {                             // older tokens of the page
                     if constexpr (KV8) {
                         const uint2 *row = reinterpret_cast<const uint2 *>((const uint8_t *)(is_k ? a.k_cache : a.v_cache) + page + (size_t)t * D);
                         const uint2 u = row[c_lo], w = row[c_hi];
-                        next_x[i] = make_uint4(u.x, u.y, 0, 0), next_y[i] = make_uint4(w.x, w.y, 0, 0);
+                        x[i] = make_uint4(u.x, u.y, 0, 0), y[i] = make_uint4(w.x, w.y, 0, 0);
                     } else {
                         const uint4 *row = reinterpret_cast<const uint4 *>((const uint16_t *)a.k_cache + page + (size_t)t * D);
-                        next_x[i] = row[c_lo], next_y[i] = row[c_hi];
+                        x[i] = row[c_lo], y[i] = row[c_hi];
                     }
                 }
             }
-            if (KV8 && old_rows && s0 > 0) next_scale = a.scales[((size_t)pid * a.H_kv + h) * 2 + (is_k ? 0 : 1)];
+            if (KV8 && old_rows && s0 > 0) scale = a.scales[((size_t)pid * a.H_kv + h) * 2 + (is_k ? 0 : 1)];
         };
-        if (hr0 + warp < hr1) fetch(hr0 + warp);
+        // kAhead: the rows of a head are on their way while the warp's last head is turned, the first ones while the angles are found
+        [[maybe_unused]] uint4 next_x[NP], next_y[NP];
+        [[maybe_unused]] float next_scale = 0.f;
+        if constexpr (PLAN == kAhead) {
+            if (hr0 + warp < hr1) fetch(hr0 + warp, next_x, next_y, next_scale);
+        }
         for (int i = tid; i < (hr0 < a.H_q + a.H_kv ? kPage * half : 0); i += kRopeThreads) {
             const int t = i / half, c = i - t * half;
             if (t < s0 || t >= s1) continue;
@@ -215,10 +235,15 @@ rope_append_kernel(const RopeArgs a) {
             const size_t page = ((size_t)max(pid, 0) * a.H_kv + h) * (kPage * D);
             const bool want_meta = is_k && a.meta && cached;
             uint4 x[NP], y[NP];
+            float old_scale = 0.f;
+            if constexpr (PLAN == kAhead) {
 #pragma unroll
-            for (int i = 0; i < NP; ++i) x[i] = next_x[i], y[i] = next_y[i];
-            [[maybe_unused]] const float old_scale = next_scale;
-            if (hr + NW < hr1) fetch(hr + NW);
+                for (int i = 0; i < NP; ++i) x[i] = next_x[i], y[i] = next_y[i];
+                old_scale = next_scale;
+                if (hr + NW < hr1) fetch(hr + NW, next_x, next_y, next_scale);
+            } else {
+                fetch(hr, x, y, old_scale);
+            }
             [[maybe_unused]] uint32_t top = 0;     // KV8: largest magnitudes so far, two bf16
             uint4 mnx = make_uint4(0x7f807f80u, 0x7f807f80u, 0x7f807f80u, 0x7f807f80u), mny = mnx;   // +inf pairs
             uint4 mxx = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u), mxy = mxx;   // -inf pairs
@@ -305,17 +330,34 @@ cudaError_t launch_rope_append(const se_params &p, const RopeCall &c, cudaStream
     a.scales = c.scales, a.meta = (uint16_t *)c.meta, a.status = c.status;
     a.B = p.B, a.H_q = p.H_q, a.H_kv = p.H_kv, a.T = c.total_tokens, a.max_pages = p.max_pages;
     a.P_phys = p.num_phys_pages, a.n_axes = c.n_axes, a.rot = c.rot_dim;
-    // a request touches at most ceil((n + 15) / 16) pages
-    const int groups = (p.H_q + 2 * p.H_kv + kRopeThreads / 32 - 1) / (kRopeThreads / 32);
-    const long long units = ((long long)c.total_tokens / kPage + 2ll * p.B) * groups, cap = (long long)kRopeCtas * device_sm_count();
-    const unsigned grid = (unsigned)(units < cap ? units : cap);
+    // About as many pages as that are touched: a token per page, or a partly filled page per request.
+    const int sms = device_sm_count(), groups = (p.H_q + 2 * p.H_kv + kRopeThreads / 32 - 1) / (kRopeThreads / 32);
+    const long long T = c.total_tokens, pages = T < T / kPage + p.B ? T : T / kPage + p.B;
+    const bool full = p.D == 128 && 2 * T >= 11 * pages;    // (5.3 tokens a page: 13.3 us whole pages, 15.4 shares; 5.8: 36 and 32)
+    // (short pages: two rounds of two CTAs per SM where the second round of three would be nearly empty; 512 tokens 17.9 for 19.0 us)
+    const bool two = full ? pages <= sms : pages <= 2 * sms || (pages > 3 * sms && pages <= 4 * sms);
+    const int plan = two ? kParts : full ? kAhead : kPages;
     const size_t smem = ((size_t)p.B + 1) * sizeof(int);
-    auto pick = [&](auto d) {
-        constexpr int D = decltype(d)::value;
-        if (c.scales) return c.interleaved ? rope_append_kernel<D, true, true> : rope_append_kernel<D, false, true>;
-        return c.interleaved ? rope_append_kernel<D, true, false> : rope_append_kernel<D, false, false>;
+    dim3 grid(2 * sms);
+    if (plan == kParts) {
+        const int ctas = (int)(pages < 2 * sms ? pages : 2 * sms), most = 2 * sms / ctas;   // parts of a page, of equal size but for the last
+        a.part = (groups + most - 1) / most;
+        grid = dim3(ctas, (groups + a.part - 1) / a.part);
+    } else if (plan == kPages) {
+        grid = dim3(3 * sms);
+    }
+    auto pick = [&](auto d, auto n) {
+        constexpr int D = decltype(d)::value, PLAN = decltype(n)::value;
+        if (c.scales) return c.interleaved ? rope_append_kernel<D, true, true, PLAN> : rope_append_kernel<D, false, true, PLAN>;
+        return c.interleaved ? rope_append_kernel<D, true, false, PLAN> : rope_append_kernel<D, false, false, PLAN>;
     };
-    auto kern = p.D == 128 ? pick(std::integral_constant<int, 128>{}) : pick(std::integral_constant<int, 64>{});
+    using D64 = std::integral_constant<int, 64>;
+    using D128 = std::integral_constant<int, 128>;
+    using Parts = std::integral_constant<int, kParts>;
+    using Ahead = std::integral_constant<int, kAhead>;
+    using Pages = std::integral_constant<int, kPages>;
+    auto kern = p.D == 64 ? (plan == kParts ? pick(D64{}, Parts{}) : pick(D64{}, Pages{}))
+                          : plan == kParts ? pick(D128{}, Parts{}) : plan == kAhead ? pick(D128{}, Ahead{}) : pick(D128{}, Pages{});
     kern<<<grid, kRopeThreads, smem, stream>>>(a);
     return cudaGetLastError();
 }
