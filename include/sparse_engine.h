@@ -504,7 +504,8 @@ int se_kv8_append(const se_params *p, const void *q, int64_t q_stride, const voi
  * its product with V's codes as two halves (22 significant bits, steps of 2^-36 of the largest at least).  No token (length 0,
  * an empty selection, no present page): out = 0, lse = -inf.  Absent pages are left out; an entry of sel_idx outside the request
  * is skipped and reported (SE_DEV_BAD_SELECTION), as is a sel_cnt above k_max (the first k_max entries count); a length outside
- * 0 .. 16*max_pages is reported (SE_DEV_BAD_LENGTH).  Equal inputs give equal bits.
+ * 0 .. 16*max_pages is reported (SE_DEV_BAD_LENGTH).  A NaN code of V makes its channel NaN, one of K the whole row and its lse.  Equal
+ * inputs give equal bits.
  */
 int se_kv8_decode(const se_params *p, const void *q, const void *k_cache, const void *v_cache, const float *scales,
                   const int32_t *page_table, const int32_t *seq_lens, const int32_t *sel_idx, const int32_t *sel_cnt,
@@ -513,8 +514,10 @@ int se_kv8_decode(const se_params *p, const void *q, const void *k_cache, const 
 /*
  * se_chunk_attend over an 8-bit cache: same arguments and rules, codes and scales in the place of the bf16 pages.
  * Precision: as there, except that a query row enters its product with K as the sum of two rows of codes times a power of two, which
- * is exact for elements of at least 2^-10 of the row's largest magnitude and off by at most 2^-17.8 of that magnitude for smaller ones.
- * A row of q with a NaN or an infinity has out = lse = NaN.
+ * is exact for elements of at least 1/896 (2^-9.8) of the row's largest magnitude and off by at most 2^-17.8 of that magnitude for
+ * smaller ones.
+ * A row of q with a NaN or an infinity, or that sees a NaN code of K, has out = lse = NaN.  A NaN code of V makes its channel NaN in the
+ * rows that see its token, and in no others.
  */
 int se_kv8_chunk_attend(const se_params *p, const void *q, int64_t q_stride, int32_t total_tokens, const int32_t *cu_seqlens,
                         const void *k_cache, const void *v_cache, const float *scales, const int32_t *page_table,

@@ -381,9 +381,10 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v
 
 // ---- an 8-bit cache ------------------------------------------------------------------
 // K stays as it is: S = Q K^T runs on codes.  A query row is split into two rows of codes, q 2^-e = hi + lo, with 2^e such that its
-// largest magnitude is at most 448; a bf16's 8 significant bits fit the two 4-bit ones, so this is exact for everything above 2^-10
-// of the row's maximum and off by at most 2^-18 of it below.  Two products at twice the rate take the time of one in bf16, and
-// the scales - 2^e of the row, s_K of the page - enter the softmax in fp32.
+// largest magnitude is at most 448 (and above 224); a bf16's 8 significant bits fit the two 4-bit ones where its last one is not below
+// 2^-9, the smallest step of a code, so this is exact from 2^-2 on, 1/896 (2^-9.8) of the row's maximum, and off by half a step below,
+// at most 2^-17.8 of the maximum.  Two products at twice the rate take the time of one in bf16, and the scales - 2^e of the row, s_K of
+// the page - enter the softmax in fp32.
 // V's codes become bf16 (exact, as the scales are powers of two), because weights need their range and eight bits: four warps bring
 // two pages of every tile each into a ring of their own, turn them, and write the tile that the tensor copies would.
 // A NaN code enters the tile as a finite value: a row that does not see its token weighs it with 0, and 0 times a NaN would reach that
