@@ -426,6 +426,12 @@ def _prompt_common(p: SeParams, workspace: torch.Tensor, cu_seqlens, page_table=
         raise SparseEngineError("workspace is smaller than se_prompt_workspace_bytes")
 
 
+# The current device and a stream's handle: torch's own shortcuts where it has them (2.4 us less of a small call), its public calls
+# otherwise.
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_stream_handle = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
 def _call(entry: str, workspace: torch.Tensor, tensors, *args) -> None:
     """The call on the current stream of the workspace's device, where every other tensor has to be too.  (The device is
     switched only where it has to be, and the stream's handle is asked for without an object around it: torch.cuda.device and
@@ -435,11 +441,11 @@ def _call(entry: str, workspace: torch.Tensor, tensors, *args) -> None:
         if t is not None and t.get_device() != dev:
             raise SparseEngineError("all tensors must be on %s, got one on %s" % (workspace.device, t.device))
     f = getattr(_lib or load(), entry)
-    if dev == torch._C._cuda_getDevice():
-        rc = f(*args, ws, torch._C._cuda_getCurrentRawStream(dev))
+    if dev == _current_device():
+        rc = f(*args, ws, _stream_handle(dev))
     else:
         with torch.cuda.device(dev):
-            rc = f(*args, ws, torch._C._cuda_getCurrentRawStream(dev))
+            rc = f(*args, ws, _stream_handle(dev))
     if rc != SE_OK:
         _check(rc, entry)
 
