@@ -39,6 +39,9 @@ constexpr int kChunks = 1024;          // prefix sums that a CTA keeps: of every
 // The largest weight is 2^12 when the maximum moves, and 2^15 at most until it moves again: the steps of small weights are 2^-36 of the
 // largest, and 131072 of them that vanish 2^-20 of it (with the largest at 1 a row lost all tokens 17 below the first one's logit).
 constexpr float kLift = 12.f, kTop = 15.f;
+// Logits beyond this (in powers of two) are rounded like their maximum was before it is taken off: with one rounding less the largest
+// weight would be off by what the maximum was rounded by, which reaches a power of two from 2^23 on and many of them later.
+constexpr float kFar = 0x1p22f;
 // The tensor cores cut a sum off after each product, always towards zero: sums over 1500 pages of a warp came out 1e-4 too small.  After
 // this many pages they join those in the merge buffer, rounded to nearest: 2^-18 at most for two products a page, 5e-7 on average.
 constexpr uint32_t kFold = 16;
@@ -410,6 +413,7 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         for (int i = 0; i < C::kTiles; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
         float *own = s_merge + warp * (8 * C::kPitch + 16);
+        bool far = false;              // a maximum is above kFar
         bool folded = false;           // the merge buffer holds the sums of earlier pages, for the maxima that lie with them
         auto fold = [&] {
             float r0 = 0.f, r1 = 0.f;
@@ -488,8 +492,10 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             // w = logit + log2 of V's scale, in powers of two: what the weights in the product with V are made of
             const float shift = (float)((int)(__float_as_uint(sv) >> 23) - 127), inv = __uint_as_float(0x7f000000u - __float_as_uint(sv));
             const float t0 = fmaf(fmaxf(z[0], z[2]), g0, shift), t1 = fmaf(fmaxf(z[1], z[3]), g1, shift);
-            if (__any_sync(kFull, t0 > m0 + kTop || t1 > m1 + kTop)) {
+            if (__any_sync(kFull, t0 - m0 > kTop || t1 - m1 > kTop)) {
                 float n0 = fmaxf(m0, t0 - kLift), n1 = fmaxf(m1, t1 - kLift);
+                if (t0 - n0 > kTop) n0 = t0;                                             // (where the steps of fp32 are 8 and 16)
+                if (t1 - n1 > kTop) n1 = t1;
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) {
                     n0 = fmaxf(n0, __shfl_xor_sync(kFull, n0, o));
@@ -497,13 +503,15 @@ kv8_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 }
                 const float r0 = ex2(m0 - n0), r1 = ex2(m1 - n1);                        // (a page has a token, so n is a number)
                 m0 = n0, m1 = n1;
+                far = __any_sync(kFull, fabsf(m0) > kFar || fabsf(m1) > kFar);
                 l0 *= r0, l1 *= r1;
 #pragma unroll
                 for (int i = 0; i < C::kTiles; ++i) acc[i][0] *= r0, acc[i][1] *= r1, acc[i][2] *= r0, acc[i][3] *= r1;
             }
             const float off0 = shift - m0, off1 = shift - m1;
-            const float p0 = ex2(fmaf(z[0], g0, off0)), p1 = ex2(fmaf(z[1], g1, off1));
-            const float p2 = ex2(fmaf(z[2], g0, off0)), p3 = ex2(fmaf(z[3], g1, off1));
+            float w0 = fmaf(z[0], g0, off0), w1 = fmaf(z[1], g1, off1), w2 = fmaf(z[2], g0, off0), w3 = fmaf(z[3], g1, off1);
+            if (far) w0 = fmaf(z[0], g0, shift) - m0, w1 = fmaf(z[1], g1, shift) - m1, w2 = fmaf(z[2], g0, shift) - m0, w3 = fmaf(z[3], g1, shift) - m1;
+            const float p0 = ex2(w0), p1 = ex2(w1), p2 = ex2(w2), p3 = ex2(w3);
             l0 = fmaf(p0 + p2, inv, l0), l1 = fmaf(p1 + p3, inv, l1);
             // weights as hi + lo, two halves; transposed, they are the second operand: rows tokens, columns heads
             const uint32_t h0 = pack_half2(p0, p1), h1 = pack_half2(p2, p3);
