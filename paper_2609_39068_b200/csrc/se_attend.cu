@@ -27,8 +27,8 @@
 // streams takes 3350 cycles where products and exponentials take 2048 each: a stream's chain of scores, softmax and product is
 // what bounds it.  Compared on builds that took 372 us for the packed prompts: KV tiles of 64 tokens with two score buffers per
 // stream 465-497 us, a product that begins with half of the weights 399-410 us, exponentials on the FMA units (one pair in
-// eight) 386 us.  Over an 8-bit cache (KV8): 2048 tokens over 63488 1.9 ms (2.17 when calls
-// follow one another and power is the limit), the drafts 198 us (209).
+// eight) 386 us.  Over an 8-bit cache (KV8): 2048 tokens over 63488 1.92 ms (2.20 when calls
+// follow one another and power is the limit), the drafts 205 us (208-214).
 #include <math.h>
 
 #include "se_internal.h"
@@ -389,7 +389,7 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v
 // two pages of every tile each into a ring of their own, turn them, and write the tile that the tensor copies would.
 // A NaN code enters the tile as a finite value: a row that does not see its token weighs it with 0, and 0 times a NaN would reach that
 // row's sum.  The turning warps note the first token that has one in each channel, and since a row sees all tokens before a border, its
-// channels are NaN where that token lies before the row's.
+// channels are NaN where that token lies before the row's.  (Looking for the codes: drafts 204 -> 208 us, mixed batch 985 -> 1014.)
 // (With K turned into bf16 too, by one warp and V by another, a step took 9000 to 11000 cycles instead of 3350.)
 
 // Page ids and scales of 32 groups of 16 tokens at a time, a lane each; scales of the next 32 and ids of the 32 behind those are on

@@ -9,17 +9,18 @@
 //   p s_V = 2^(w - m), w = z log2 e + log2 s_V, m 12 below the running maximum of w, enters as two halves, hi + lo (22 bits), as the
 //         output is fp32: the largest are near 2^12 whatever the scales.  The sum of the weights takes s_V out again, in fp32.
 //
-// What bounds it: HBM, 2 * 2 * D bytes per token and kv-head, and nearly as much the instructions: per page and head at D = 128 about
-// 300 for a warp, 64 of them conversions of two codes each and 24 matrix instructions.
+// What bounds it: the bytes, 2 * D per token and kv-head, come at 0.70 of what a gather of the same pages without arithmetic reaches (43.1 us
+// for the first case below), so neither HBM nor the pieces of 2 KB; a page and head takes a warp about 300 instructions at D = 128, 64 of
+// them conversions of two codes each and 24 matrix instructions, and an issue slot in two is empty.
 //
 // Split.  The list of all (request, kv-head) pairs' pages is cut into 592 runs of equal length, one per group of four warps; a
 // group's pages go round its warps, each of which keeps a ring of pages in flight (tensor copies, 128-byte swizzle) across the
 // borders of pairs.  At the end of a pair's run the warps merge through shared memory; a pair that several groups share leaves
 // partial results in the workspace, and the group that arrives last merges them in order.
 //
-// Measured (device time in graphs): 64 requests x 2048 selected tokens, 8 kv-heads x 4, D = 128: 59 us for 271 MB = 4.6 TB/s, 0.70 of a
-// copy; 16 requests over 100-32767 tokens, 4 x 7: 55 us, 0.64; one request over 2048 tokens 9.6 us,
-// one head over 65536 19, eight 66 over 131000.  On the first, with caches flushed:
+// Measured (device time in graphs): 64 requests x 2048 selected tokens, 8 kv-heads x 4, D = 128: 60.5 us for 271 MB = 4.5 TB/s, 0.68 of a
+// copy; 16 requests over 100-32767 tokens, 4 x 7: 55.7 us, 0.63; one request over 2048 tokens 10.3 us,
+// one head over 65536 19.7, eight 61-66 over 131000.  On the first, with caches flushed:
 // eight warps 91 us, sixteen on their own 77, groups of four 75; one warp that fetches for fifteen 142.  Both products on tcgen05 with
 // tokens on the M side and weights as five codes: 65.0 us where this took 63.4 without flushes.
 #include <math.h>
