@@ -340,9 +340,12 @@ cudaError_t launch_rope_append(const se_params &p, const RopeCall &c, cudaStream
     const size_t smem = ((size_t)p.B + 1) * sizeof(int);
     dim3 grid(2 * sms);
     if (plan == kParts) {
-        const int ctas = (int)(pages < 2 * sms ? pages : 2 * sms), most = 2 * sms / ctas;   // parts of a page, of equal size but for the last
+        const int most = pages < 2 * sms ? 2 * sms / (int)pages : 1;      // parts of a page, of equal size but for the last
         a.part = (groups + most - 1) / most;
-        grid = dim3(ctas, (groups + a.part - 1) / a.part);
+        const int parts = (groups + a.part - 1) / a.part;
+        // (a request's tokens may begin and end inside a page, so there may be more pages)
+        const long long bound = T < T / kPage + 2ll * p.B ? T : T / kPage + 2ll * p.B, room = 2 * sms / parts;
+        grid = dim3((unsigned)(bound < room ? bound : room), parts);
     } else if (plan == kPages) {
         grid = dim3(3 * sms);
     }
