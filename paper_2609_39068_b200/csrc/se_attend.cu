@@ -564,7 +564,7 @@ __device__ __forceinline__ void v8_role(const AttendArgs &a, Control<D, true> *c
                 }
                 uint32_t nan = 0;
 #pragma unroll
-                for (int e = 0; e < N; ++e) nan |= kv8_nan(x[e].x) | kv8_nan(x[e].y) | kv8_nan(x[e].z) | kv8_nan(x[e].w);
+                for (int e = 0; e < N; ++e) nan = kv8_nan(x[e].w, kv8_nan(x[e].z, kv8_nan(x[e].y, kv8_nan(x[e].x, nan))));
                 if (nan & 0x80808080u) {
                     const uint32_t place = (turn - 1) % SegmentQueue<Segment>::kDepth;
 #pragma unroll 1

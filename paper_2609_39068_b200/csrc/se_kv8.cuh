@@ -90,7 +90,8 @@ __device__ __forceinline__ void kv8_bf16x4(uint32_t codes, __nv_bfloat162 f, uin
     lo = x[0], hi = x[1];
 }
 
-// Not zero in the top bit of a byte: that of the four codes is a NaN's.
-__device__ __forceinline__ uint32_t kv8_nan(uint32_t codes) { return (codes & 0x7f7f7f7fu) + 0x01010101u; }
+// `found`, with the top bit of some byte set if one of the four codes is a NaN's: adding one to a code changes its sign where the seven
+// bits below are all set (and a carry out of 0xff can only make more of them change).
+__device__ __forceinline__ uint32_t kv8_nan(uint32_t codes, uint32_t found) { return found | ((codes + 0x01010101u) ^ codes); }
 
 }  // namespace se
