@@ -389,7 +389,7 @@ __device__ __forceinline__ void v_role(const AttendArgs &a, const CUtensorMap *v
 // two pages of every tile each into a ring of their own, turn them, and write the tile that the tensor copies would.
 // A NaN code enters the tile as a finite value: a row that does not see its token weighs it with 0, and 0 times a NaN would reach that
 // row's sum.  The turning warps note the first token that has one in each channel, and since a row sees all tokens before a border, its
-// channels are NaN where that token lies before the row's.  (Looking for the codes: drafts 204 -> 208 us, mixed batch 985 -> 1014.)
+// channels are NaN where that token lies before the row's.  (Looking for the codes: drafts 201 -> 208 us, mixed batch 972 -> 1002.)
 // (With K turned into bf16 too, by one warp and V by another, a step took 9000 to 11000 cycles instead of 3350.)
 
 // Page ids and scales of 32 groups of 16 tokens at a time, a lane each; scales of the next 32 and ids of the 32 behind those are on
